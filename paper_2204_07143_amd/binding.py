@@ -35,6 +35,13 @@ EXPORTS_1D = (
 )
 
 
+EXPORTS_SEQ = (
+    "seq_validate_problem", "seq_attention_workspace_bytes", "seq_attention_fwd", "seq_attention_bwd", "seq_cache_validate", "seq_cache_append",
+    "seq_cache_gather", "seq_cache_attention", "seq_cache_attention_workspace_bytes",
+)
+SEQ_CACHE_APPEND, SEQ_CACHE_GATHER, SEQ_CACHE_ATTENTION = 0, 1, 2
+
+
 class Na2dError(RuntimeError):
     def __init__(self, status: int, message: str):
         super().__init__(f"na2d status {status}: {message}")
@@ -47,6 +54,21 @@ class Na2dProblem(ctypes.Structure):
 
 class Na1dProblem(ctypes.Structure):
     _fields_ = [(n, ctypes.c_int32) for n in ("B", "heads", "L", "D", "k", "dtype")]
+
+
+class SeqStrides(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int64) for n in ("batch", "head", "row")]
+
+
+class SeqProblem(ctypes.Structure):
+    _fields_ = ([(n, ctypes.c_int32) for n in ("B", "heads", "kv_heads", "Lq", "Lk", "D", "dtype", "causal", "window")]
+                + [(n, ctypes.c_float) for n in ("scale", "softcap")]
+                + [(n, SeqStrides) for n in ("q", "k", "v", "out", "dout", "dq", "dk", "dv")])
+
+
+class SeqCacheProblem(ctypes.Structure):
+    _fields_ = ([(n, ctypes.c_int32) for n in ("B", "heads", "kv_heads", "D", "page", "pages", "table_width", "dtype", "n", "window")]
+                + [(n, ctypes.c_float) for n in ("scale", "softcap")] + [(n, SeqStrides) for n in ("q", "out")])
 
 
 _lib = None
@@ -107,6 +129,24 @@ def load(path: str | None = None) -> ctypes.CDLL:
             fn = getattr(lib, name)
             fn.argtypes = argtypes
             fn.restype = ctypes.c_int
+        ps, pc, size = ctypes.POINTER(SeqProblem), ctypes.POINTER(SeqCacheProblem), ctypes.c_size_t
+        sigs_seq = {
+            "seq_validate_problem": [ps, ctypes.c_int],
+            "seq_attention_fwd": [ps] + [vp] * 9 + [size, vp],
+            "seq_attention_bwd": [ps] + [vp] * 13 + [size, vp],
+            "seq_cache_validate": [pc, ctypes.c_int],
+            "seq_cache_append": [pc] + [vp] * 10,
+            "seq_cache_gather": [pc] + [vp] * 10,
+            "seq_cache_attention": [pc] + [vp] * 10 + [size, vp],
+        }
+        for name, argtypes in sigs_seq.items():
+            fn = getattr(lib, name)
+            fn.argtypes = argtypes
+            fn.restype = ctypes.c_int
+        lib.seq_attention_workspace_bytes.argtypes = [ps, ctypes.c_int, ctypes.c_int]
+        lib.seq_attention_workspace_bytes.restype = size
+        lib.seq_cache_attention_workspace_bytes.argtypes = [pc]
+        lib.seq_cache_attention_workspace_bytes.restype = size
         lib.na1d_workspace_bytes.argtypes = [p1]
         lib.na1d_workspace_bytes.restype = ctypes.c_size_t
         lib.na1d_fused_bwd_workspace_bytes.argtypes = [p1]
@@ -448,3 +488,144 @@ def na1d_fused_bwd(q, k_, v, rpb, scale: float, lse, dout, kernel: int, dq, dk, 
                                  _ptr(d_rpb, torch.float32, _rpb1(q, kernel)) if d_rpb is not None else None,
                                  _ptr(workspace), workspace.numel() * workspace.element_size(), _stream()))
     return dq, dk, dv, d_rpb
+
+
+# ---- attention over sequences and its cache (include/seq.h) ---------------------------------------------------------------
+# q, out: [B, heads, Lq, D]; k, v: [B, kv_heads, Lk, D], with strides of their own but for the last dimension's.
+
+def _strided(t, of, shape, dtype=None):
+    """Checks of a tensor that may have strides, and its pointer."""
+    if not t.is_cuda:
+        raise ValueError("na2d takes GPU tensors only")
+    if t.device != of.device:
+        raise ValueError(f"expected a tensor on {of.device}, got one on {t.device}")
+    if t.is_neg():
+        raise ValueError("na2d does not take negated views")
+    if t.dtype != (of.dtype if dtype is None else dtype):
+        raise ValueError(f"expected dtype {of.dtype if dtype is None else dtype}, got {t.dtype}")
+    if tuple(t.shape) != tuple(shape):
+        raise ValueError(f"expected shape {tuple(shape)}, got {tuple(t.shape)}")
+    if t.stride(-1) != 1 and t.shape[-1] != 1:
+        raise ValueError("the elements of a row must be contiguous")
+    return ctypes.c_void_p(t.data_ptr())
+
+
+def _dense(t, of, shape, dtype):
+    if t is None:
+        return None
+    p = _strided(t, of, shape, dtype)
+    if not t.is_contiguous():
+        raise ValueError("na2d takes contiguous tensors only")
+    return p
+
+
+def _seq_strides(t) -> SeqStrides:
+    return SeqStrides(*(0 if n == 1 else s for n, s in zip(t.shape[:3], t.stride()[:3])))
+
+
+def _seq_stream(t):
+    return ctypes.c_void_p(torch.cuda.current_stream(t.device).cuda_stream)
+
+
+def seq_problem(q, k_, *, causal: bool, window: int, softcap: float, scale: float, **strided) -> SeqProblem:
+    """strided: the tensors by name (v, out and, backward, dout, dq, dk, dv)."""
+    if q.dim() != 4 or k_.dim() != 4:
+        raise ValueError("expected [B, heads, L, D] tensors")
+    (B, heads, Lq, D), (_, kv_heads, Lk, _) = q.shape, k_.shape
+    code = DTYPE_CODES.get(q.dtype, -1)
+    p = SeqProblem(B, heads, kv_heads, Lq, Lk, D, code, int(causal), int(window), scale, softcap)
+    for name, t in dict(q=q, k=k_, **strided).items():
+        setattr(p, name, _seq_strides(t))
+    return p
+
+
+def seq_validate_problem(p: SeqProblem, backward: bool = False) -> int:
+    return int(load().seq_validate_problem(ctypes.byref(p), int(backward)))
+
+
+def seq_attention_workspace_bytes(p: SeqProblem, marked: bool, backward: bool = False) -> int:
+    return int(load().seq_attention_workspace_bytes(ctypes.byref(p), int(marked), int(backward)))
+
+
+def _seq_inputs(q, k_, v, slopes, documents, prefix):
+    B, heads, Lq, D = q.shape
+    kv_shape = (B, k_.shape[1], k_.shape[2], D)
+    return (_strided(q, q, q.shape), _strided(k_, q, kv_shape), _strided(v, q, kv_shape), _dense(slopes, q, (heads,), torch.float32),
+            _dense(documents, q, (B, k_.shape[2]), torch.int32), _dense(prefix, q, (B, k_.shape[2]), torch.bool))
+
+
+def _bytes(workspace):
+    return (None, 0) if workspace is None else (ctypes.c_void_p(workspace.data_ptr()), workspace.numel() * workspace.element_size())
+
+
+def seq_attention_fwd(q, k_, v, slopes, documents, prefix, out, lse=None, workspace=None, *, causal=False, window=0, softcap=0.0, scale=1.0):
+    p = seq_problem(q, k_, causal=causal, window=window, softcap=softcap, scale=scale, v=v, out=out)
+    inputs = _seq_inputs(q, k_, v, slopes, documents, prefix)
+    with torch.cuda.device(q.device):
+        _check(load().seq_attention_fwd(ctypes.byref(p), *inputs, _strided(out, q, q.shape), _dense(lse, q, q.shape[:3], torch.float32), *_bytes(workspace),
+                                        _seq_stream(q)))
+    return out
+
+
+def seq_attention_bwd(q, k_, v, slopes, documents, prefix, out, lse, dout, dq, dk, dv, workspace, *, causal=False, window=0, softcap=0.0, scale=1.0):
+    p = seq_problem(q, k_, causal=causal, window=window, softcap=softcap, scale=scale, v=v, out=out, dout=dout, dq=dq, dk=dk, dv=dv)
+    inputs = _seq_inputs(q, k_, v, slopes, documents, prefix)
+    with torch.cuda.device(q.device):
+        _check(load().seq_attention_bwd(ctypes.byref(p), *inputs, _strided(out, q, q.shape), _dense(lse, q, q.shape[:3], torch.float32), _strided(dout, q, q.shape),
+                                        _strided(dq, q, q.shape), _strided(dk, q, k_.shape), _strided(dv, q, k_.shape), *_bytes(workspace), _seq_stream(q)))
+    return dq, dk, dv
+
+
+def seq_cache_problem(rows, k_pages, table, *, heads=None, window=0, softcap=0.0, scale=1.0, out=None) -> SeqCacheProblem:
+    """rows: [B, heads or kv_heads, n, D]; out: the call's other tensor of that form."""
+    if rows.dim() != 4 or k_pages.dim() != 4 or table.dim() != 2:
+        raise ValueError("expected [B, heads, n, D] rows, [pages, kv_heads, page, D] pages and a [B, width] table")
+    (B, _, n, D), (pages, kv_heads, page, _) = rows.shape, k_pages.shape
+    p = SeqCacheProblem(B, kv_heads if heads is None else heads, kv_heads, D, page, pages, table.shape[1], DTYPE_CODES.get(rows.dtype, -1), n, int(window), scale, softcap)
+    p.q, p.out = _seq_strides(rows), _seq_strides(rows if out is None else out)
+    return p
+
+
+def seq_cache_validate(p: SeqCacheProblem, call: int) -> int:
+    return int(load().seq_cache_validate(ctypes.byref(p), call))
+
+
+def _cache_inputs(rows, k_pages, v_pages, k_scales, v_scales):
+    pages, kv_heads, page, _ = k_pages.shape
+    shape = (pages, kv_heads, page, rows.shape[3])
+    return (_dense(k_pages, rows, shape, torch.int8), _dense(v_pages, rows, shape, torch.int8), _dense(k_scales, rows, shape[:2], torch.float32),
+            _dense(v_scales, rows, shape[:2], torch.float32))
+
+
+def seq_cache_append(k_, v, table, lengths, counts, k_pages, v_pages, k_scales, v_scales):
+    p = seq_cache_problem(k_, k_pages, table, out=v)
+    B, shape = k_.shape[0], (k_.shape[0], k_pages.shape[1], *k_.shape[2:])
+    cache = _cache_inputs(k_, k_pages, v_pages, k_scales, v_scales)
+    with torch.cuda.device(k_.device):
+        _check(load().seq_cache_append(ctypes.byref(p), _strided(k_, k_, shape), _strided(v, k_, shape), _dense(table, k_, (B, table.shape[1]), torch.int32),
+                                       _dense(lengths, k_, (B,), torch.int32), _dense(counts, k_, (B,), torch.int32), *cache, _seq_stream(k_)))
+
+
+def seq_cache_gather(k_pages, v_pages, k_scales, v_scales, table, lengths, first, k_, v):
+    p = seq_cache_problem(k_, k_pages, table, out=v)
+    B, shape = k_.shape[0], (k_.shape[0], k_pages.shape[1], *k_.shape[2:])
+    cache = _cache_inputs(k_, k_pages, v_pages, k_scales, v_scales)
+    with torch.cuda.device(k_.device):
+        _check(load().seq_cache_gather(ctypes.byref(p), *cache, _dense(table, k_, (B, table.shape[1]), torch.int32), _dense(lengths, k_, (B,), torch.int32),
+                                       _dense(first, k_, (B,), torch.int32), _strided(k_, k_, shape), _strided(v, k_, shape), _seq_stream(k_)))
+    return k_, v
+
+
+def seq_cache_attention_workspace_bytes(p: SeqCacheProblem) -> int:
+    return int(load().seq_cache_attention_workspace_bytes(ctypes.byref(p)))
+
+
+def seq_cache_attention(q, k_pages, v_pages, k_scales, v_scales, table, lengths, slopes, out, workspace=None, *, window=0, softcap=0.0, scale=1.0):
+    p = seq_cache_problem(q, k_pages, table, heads=q.shape[1], window=window, softcap=softcap, scale=scale, out=out)
+    B = q.shape[0]
+    cache = _cache_inputs(q, k_pages, v_pages, k_scales, v_scales)
+    with torch.cuda.device(q.device):
+        _check(load().seq_cache_attention(ctypes.byref(p), _strided(q, q, q.shape), *cache, _dense(table, q, (B, table.shape[1]), torch.int32),
+                                          _dense(lengths, q, (B,), torch.int32), _dense(slopes, q, (q.shape[1],), torch.float32), _strided(out, q, q.shape),
+                                          *_bytes(workspace), _seq_stream(q)))
+    return out

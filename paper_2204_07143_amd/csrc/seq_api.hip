@@ -1,0 +1,238 @@
+// C ABI of the attention over token sequences and of its cache: argument validation (host only, before any HIP call) and dispatch.
+#include <cmath>
+#include <initializer_list>
+
+#include "seq_cache.hpp"
+
+namespace seq {
+namespace {
+
+int elem(int dtype) { return dtype == NA2D_F32 ? 4 : 2; }
+bool misaligned(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15u) != 0; }
+int from_hip(hipError_t e) {
+    if (e == hipSuccess) return NA2D_OK;
+    (void)hipGetLastError();   // leave no stale error behind for the caller's next HIP call
+    return NA2D_ERR_LAUNCH;
+}
+// strides of a tensor [., ., rows, D]: whole multiples of 16 bytes, none negative, a plane below 2^31 bytes, an offset to any plane below 2^62 bytes
+int check_strides(const seq_strides &s, int64_t B, int64_t heads, int64_t rows, int64_t D, int e) {
+    for (int64_t x : {s.batch, s.head, s.row}) {
+        if (x < 0 || x > ((int64_t)1 << 45)) return NA2D_ERR_SHAPE;
+        if (x * e % 16) return NA2D_ERR_ALIGN;
+    }
+    if (((rows - 1) * s.row + D) * e > (int64_t)INT32_MAX || B > ((int64_t)1 << 24) || heads > ((int64_t)1 << 16)) return NA2D_ERR_SHAPE;
+    return NA2D_OK;
+}
+View view(const void *at, const seq_strides &s, int e) { return {static_cast<const char *>(at), s.batch * e, s.head * e, (int)(s.row * e)}; }
+
+int common(int B, int heads, int kv, int D, int dtype, float scale, float cap, int window) {
+    if (dtype != NA2D_F32 && dtype != NA2D_F16 && dtype != NA2D_BF16) return NA2D_ERR_DTYPE;
+    if (B <= 0 || heads <= 0 || kv <= 0 || heads % kv) return NA2D_ERR_SHAPE;
+    if (D != 32 && D != 64 && D != 128) return NA2D_ERR_HEAD_DIM;
+    if (!std::isfinite(scale) || !std::isfinite(cap) || cap < 0.f || window < 0 || window > kFar) return NA2D_ERR_SHAPE;
+    return NA2D_OK;
+}
+
+int validate(const seq_problem *p, bool backward) {
+    if (!p) return NA2D_ERR_NULL;
+    if (int e = common(p->B, p->heads, p->kv_heads, p->D, p->dtype, p->scale, p->softcap, p->window)) return e;
+    if (p->Lq <= 0 || p->Lk <= 0 || p->Lq > 1 << 24 || p->Lk > 1 << 24 || (p->causal != 0 && p->causal != 1)) return NA2D_ERR_SHAPE;
+    const int e = elem(p->dtype);
+    for (const seq_strides *s : {&p->q, &p->out})
+        if (int r = check_strides(*s, p->B, p->heads, p->Lq, p->D, e)) return r;
+    for (const seq_strides *s : {&p->k, &p->v})
+        if (int r = check_strides(*s, p->B, p->kv_heads, p->Lk, p->D, e)) return r;
+    if (backward) {
+        for (const seq_strides *s : {&p->dout, &p->dq})
+            if (int r = check_strides(*s, p->B, p->heads, p->Lq, p->D, e)) return r;
+        for (const seq_strides *s : {&p->dk, &p->dv})
+            if (int r = check_strides(*s, p->B, p->kv_heads, p->Lk, p->D, e)) return r;
+    }
+    // every launch of the passes (the smallest tiles: 64 rows) holds its workgroups
+    const int64_t q_tiles = ((int64_t)p->Lq + kTile - 1) / kTile, k_tiles = ((int64_t)p->Lk + kTile - 1) / kTile;
+    if (!launch_holds((int64_t)p->B * p->heads * q_tiles, kThreads) || !launch_holds((int64_t)p->B * p->kv_heads * k_tiles, kThreads)) return NA2D_ERR_SHAPE;
+    return NA2D_OK;
+}
+
+// The workspace: zeros, the marks of the keys' tiles, and for a backward pass the rows' statistics and the tiles' powers of two.
+struct Space {
+    int64_t marks, rows, powers, bytes;
+    Space(const seq_problem *p, bool marked, bool backward) {
+        const int64_t k_tiles = ((int64_t)p->Lk + kTile - 1) / kTile, q_tiles = ((int64_t)p->Lq + kTile - 1) / kTile;
+        marks = marked ? 64 : 0;
+        rows = (marked ? marks + (int64_t)sizeof(Marks) * p->B * k_tiles + 63 : 0) / 64 * 64;
+        powers = rows + (backward ? (int64_t)sizeof(float2) * p->B * p->heads * q_tiles * kTile : 0);
+        bytes = powers + (backward ? (int64_t)sizeof(int) * p->B * p->heads * q_tiles : 0);
+    }
+};
+
+Args args(const seq_problem *p, const float *slopes, const int32_t *documents) {
+    Args a{};
+    a.slopes = slopes, a.documents = documents;
+    a.B = p->B, a.heads = p->heads, a.kv = p->kv_heads, a.group = p->heads / p->kv_heads, a.Lq = p->Lq, a.Lk = p->Lk, a.off = p->Lk - p->Lq;
+    a.key_tiles = (p->Lk + kTile - 1) / kTile, a.query_tiles = (p->Lq + kTile - 1) / kTile;
+    a.causal = p->causal, a.window = p->window ? p->window : kFar;
+    a.dlo = p->causal ? 0 : 1 - a.window;
+    a.scale = p->scale;
+    a.c = p->softcap > 0.f ? (float)(2.0 * 1.4426950408889634 * p->scale / p->softcap) : (float)(1.4426950408889634 * p->scale);
+    a.cap = (float)(2.0 * 1.4426950408889634 * p->softcap);
+    return a;
+}
+
+#define SEQ_REQUIRE(ptr)                            \
+    do {                                            \
+        if (!(ptr)) return NA2D_ERR_NULL;           \
+        if (misaligned(ptr)) return NA2D_ERR_ALIGN; \
+    } while (0)
+
+// slopes, documents, prefix: aligned to their elements; documents need a position for every query
+int check_marks(const seq_problem *p, const float *slopes, const int32_t *documents) {
+    if (((uintptr_t)slopes | (uintptr_t)documents) & 3u) return NA2D_ERR_ALIGN;
+    return documents && p->Lq > p->Lk ? NA2D_ERR_SHAPE : NA2D_OK;
+}
+int prepare(Args &a, const seq_problem *p, const Space &s, const uint8_t *prefix, void *workspace, size_t bytes, hipStream_t st) {
+    if (s.bytes && (!workspace || misaligned(workspace) || bytes < (size_t)s.bytes)) return NA2D_ERR_WORKSPACE;
+    char *ws = static_cast<char *>(workspace);
+    if (s.marks) {
+        a.marks = reinterpret_cast<const Marks *>(ws + s.marks);
+        a.zeros = ws;
+        a.prefix = prefix != nullptr;
+        return from_hip(launch_marks(a, prefix, reinterpret_cast<Marks *>(ws + s.marks), ws, st));
+    }
+    return NA2D_OK;
+}
+
+int cache_validate(const seq_cache_problem *p, int call) {
+    if (!p) return NA2D_ERR_NULL;
+    if (call != SEQ_CACHE_APPEND && call != SEQ_CACHE_GATHER && call != SEQ_CACHE_ATTENTION) return NA2D_ERR_SHAPE;
+    if (int e = common(p->B, p->heads, p->kv_heads, p->D, p->dtype, p->scale, p->softcap, p->window)) return e;
+    if (call == SEQ_CACHE_ATTENTION && p->dtype == NA2D_F32) return NA2D_ERR_DTYPE;
+    if (p->page != 16 && p->page != 32 && p->page != 64 && p->page != 128) return NA2D_ERR_SHAPE;
+    if (p->pages <= 0 || p->table_width <= 0 || p->n <= 0 || p->n > 1 << 24 || (int64_t)p->table_width * p->page > kFar) return NA2D_ERR_SHAPE;
+    const int heads = call == SEQ_CACHE_ATTENTION ? p->heads : p->kv_heads, e = elem(p->dtype);
+    for (const seq_strides *s : {&p->q, &p->out})
+        if (int r = check_strides(*s, p->B, heads, p->n, p->D, e)) return r;
+    if (call == SEQ_CACHE_ATTENTION && (int64_t)p->heads / p->kv_heads * p->n > 1 << 24) return NA2D_ERR_SHAPE;
+    return NA2D_OK;
+}
+CacheArgs cache_args(const seq_cache_problem *p) {
+    CacheArgs a{};
+    a.B = p->B, a.heads = p->heads, a.kv = p->kv_heads, a.group = p->heads / p->kv_heads, a.pages = p->pages, a.width = p->table_width, a.n = p->n;
+    a.page_log2 = p->page == 16 ? 4 : p->page == 32 ? 5 : p->page == 64 ? 6 : 7;
+    a.window = p->window ? p->window : kFar;
+    a.c = p->softcap > 0.f ? (float)(2.0 * 1.4426950408889634 * p->scale / p->softcap) : (float)(1.4426950408889634 * p->scale);
+    a.cap = (float)(2.0 * 1.4426950408889634 * p->softcap);
+    plan_cache_attention(a, p->D, (int64_t)p->table_width * p->page);
+    return a;
+}
+bool odd4(std::initializer_list<const void *> ps) {
+    for (const void *p : ps)
+        if (reinterpret_cast<uintptr_t>(p) & 3u) return true;
+    return false;
+}
+
+}  // namespace
+}  // namespace seq
+
+using namespace seq;
+
+extern "C" {
+
+int seq_validate_problem(const seq_problem *p, int backward) { return validate(p, backward != 0); }
+
+size_t seq_attention_workspace_bytes(const seq_problem *p, int marked, int backward) {
+    return validate(p, backward != 0) == NA2D_OK ? (size_t)Space(p, marked != 0, backward != 0).bytes : 0;
+}
+
+int seq_attention_fwd(const seq_problem *p, const void *q, const void *k, const void *v, const float *slopes, const int32_t *documents, const uint8_t *prefix,
+                      void *out, float *lse, void *workspace, size_t workspace_bytes, void *stream) {
+    if (int e = validate(p, false)) return e;
+    SEQ_REQUIRE(q); SEQ_REQUIRE(k); SEQ_REQUIRE(v); SEQ_REQUIRE(out);
+    if (odd4({lse})) return NA2D_ERR_ALIGN;
+    if (int e = check_marks(p, slopes, documents)) return e;
+    if (out == q || out == k || out == v) return NA2D_ERR_ALIAS;
+    const hipStream_t st = static_cast<hipStream_t>(stream);
+    const int e = elem(p->dtype);
+    Args a = args(p, slopes, documents);
+    a.q = view(q, p->q, e), a.k = view(k, p->k, e), a.v = view(v, p->v, e), a.out = view(out, p->out, e), a.lse = lse;
+    if (int r = prepare(a, p, Space(p, documents || prefix, false), prefix, workspace, workspace_bytes, st)) return r;
+    return from_hip(launch_fwd(a, p->dtype, p->D, p->softcap > 0.f, st));
+}
+
+int seq_attention_bwd(const seq_problem *p, const void *q, const void *k, const void *v, const float *slopes, const int32_t *documents, const uint8_t *prefix,
+                      const void *out, const float *lse, const void *dout, void *dq, void *dk, void *dv, void *workspace, size_t workspace_bytes, void *stream) {
+    if (int e = validate(p, true)) return e;
+    SEQ_REQUIRE(q); SEQ_REQUIRE(k); SEQ_REQUIRE(v); SEQ_REQUIRE(out); SEQ_REQUIRE(dout); SEQ_REQUIRE(dq); SEQ_REQUIRE(dk); SEQ_REQUIRE(dv);
+    if (!lse) return NA2D_ERR_NULL;
+    if (odd4({lse})) return NA2D_ERR_ALIGN;
+    if (int e = check_marks(p, slopes, documents)) return e;
+    for (const void *o : {dq, dk, dv})
+        for (const void *i : {q, k, v, out, dout, (const void *)lse})
+            if (o == i) return NA2D_ERR_ALIAS;
+    if (dq == dk || dq == dv || dk == dv) return NA2D_ERR_ALIAS;
+    const hipStream_t st = static_cast<hipStream_t>(stream);
+    const int e = elem(p->dtype);
+    Args a = args(p, slopes, documents);
+    a.q = view(q, p->q, e), a.k = view(k, p->k, e), a.v = view(v, p->v, e), a.out = view(out, p->out, e), a.lse = const_cast<float *>(lse);
+    a.dout = view(dout, p->dout, e), a.dq = view(dq, p->dq, e), a.dk = view(dk, p->dk, e), a.dv = view(dv, p->dv, e);
+    const Space s(p, documents || prefix, true);
+    if (int r = prepare(a, p, s, prefix, workspace, workspace_bytes, st)) return r;
+    a.rows = reinterpret_cast<float2 *>(static_cast<char *>(workspace) + s.rows);
+    a.powers = reinterpret_cast<int *>(static_cast<char *>(workspace) + s.powers);
+    if (int r = from_hip(launch_rows(a, p->dtype, p->D, st))) return r;
+    if (int r = from_hip(launch_bwd_q(a, p->dtype, p->D, p->softcap > 0.f, st))) return r;
+    return from_hip(launch_bwd_kv(a, p->dtype, p->D, p->softcap > 0.f, st));
+}
+
+int seq_cache_validate(const seq_cache_problem *p, int call) { return cache_validate(p, call); }
+
+int seq_cache_append(const seq_cache_problem *p, const void *k, const void *v, const int32_t *table, const int32_t *lengths, const int32_t *counts,
+                     int8_t *k_pages, int8_t *v_pages, float *k_scales, float *v_scales, void *stream) {
+    if (int e = cache_validate(p, SEQ_CACHE_APPEND)) return e;
+    SEQ_REQUIRE(k); SEQ_REQUIRE(v); SEQ_REQUIRE(k_pages); SEQ_REQUIRE(v_pages);
+    if (!table || !lengths || !k_scales || !v_scales) return NA2D_ERR_NULL;
+    if (odd4({table, lengths, counts, k_scales, v_scales})) return NA2D_ERR_ALIGN;
+    if (k_pages == v_pages || k_scales == v_scales) return NA2D_ERR_ALIAS;
+    CacheArgs a = cache_args(p);
+    const int e = elem(p->dtype);
+    a.a = view(k, p->q, e), a.b = view(v, p->out, e), a.k = k_pages, a.v = v_pages, a.ks = k_scales, a.vs = v_scales;
+    a.table = table, a.lengths = lengths, a.extra = counts;
+    return from_hip(launch_append(a, p->dtype, p->D, static_cast<hipStream_t>(stream)));
+}
+
+int seq_cache_gather(const seq_cache_problem *p, const int8_t *k_pages, const int8_t *v_pages, const float *k_scales, const float *v_scales, const int32_t *table,
+                     const int32_t *lengths, const int32_t *first, void *k, void *v, void *stream) {
+    if (int e = cache_validate(p, SEQ_CACHE_GATHER)) return e;
+    SEQ_REQUIRE(k); SEQ_REQUIRE(v); SEQ_REQUIRE(k_pages); SEQ_REQUIRE(v_pages);
+    if (!table || !lengths || !first || !k_scales || !v_scales) return NA2D_ERR_NULL;
+    if (odd4({table, lengths, first, k_scales, v_scales})) return NA2D_ERR_ALIGN;
+    if (k == v) return NA2D_ERR_ALIAS;
+    CacheArgs a = cache_args(p);
+    const int e = elem(p->dtype);
+    a.a = view(k, p->q, e), a.b = view(v, p->out, e), a.k = const_cast<int8_t *>(k_pages), a.v = const_cast<int8_t *>(v_pages);
+    a.ks = const_cast<float *>(k_scales), a.vs = const_cast<float *>(v_scales), a.table = table, a.lengths = lengths, a.extra = first;
+    return from_hip(launch_gather(a, p->dtype, p->D, static_cast<hipStream_t>(stream)));
+}
+
+size_t seq_cache_attention_workspace_bytes(const seq_cache_problem *p) {
+    return cache_validate(p, SEQ_CACHE_ATTENTION) == NA2D_OK ? cache_attention_bytes(cache_args(p), p->D) : 0;
+}
+
+int seq_cache_attention(const seq_cache_problem *p, const void *q, const int8_t *k_pages, const int8_t *v_pages, const float *k_scales, const float *v_scales,
+                        const int32_t *table, const int32_t *lengths, const float *slopes, void *out, void *workspace, size_t workspace_bytes, void *stream) {
+    if (int e = cache_validate(p, SEQ_CACHE_ATTENTION)) return e;
+    SEQ_REQUIRE(q); SEQ_REQUIRE(out); SEQ_REQUIRE(k_pages); SEQ_REQUIRE(v_pages);
+    if (!table || !lengths || !k_scales || !v_scales) return NA2D_ERR_NULL;
+    if (odd4({table, lengths, slopes, k_scales, v_scales})) return NA2D_ERR_ALIGN;
+    if (out == q) return NA2D_ERR_ALIAS;
+    CacheArgs a = cache_args(p);
+    const size_t need = cache_attention_bytes(a, p->D);
+    if (need && (!workspace || misaligned(workspace) || workspace_bytes < need)) return NA2D_ERR_WORKSPACE;
+    const int e = elem(p->dtype);
+    a.a = view(q, p->q, e), a.b = view(out, p->out, e), a.k = const_cast<int8_t *>(k_pages), a.v = const_cast<int8_t *>(v_pages);
+    a.ks = const_cast<float *>(k_scales), a.vs = const_cast<float *>(v_scales), a.table = table, a.lengths = lengths, a.slopes = slopes;
+    a.part = static_cast<float *>(workspace);
+    return from_hip(launch_cache_attention(a, p->dtype, p->D, p->softcap > 0.f, static_cast<hipStream_t>(stream)));
+}
+
+}  // extern "C"

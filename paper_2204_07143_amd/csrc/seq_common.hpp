@@ -1,0 +1,268 @@
+// What the kernels of the attention over token sequences share: their arguments, the tiles of 64 tokens that they walk and stage, and the
+// fragments that the matrix instructions take.
+//
+// A head vector of D elements is CH = D sizeof(T) / 16 chunks of 16 bytes.  The 16 x 16 products of na2d_mfma.hpp take one chunk per lane of
+// each operand: lane (j = lane % 16, g = lane / 16) holds chunk 4 s + g of row j for step s, and of the sums column j, rows 4 g + r.  In fp32 a
+// chunk is four instructions of depth 4 (element e of the lanes' chunks).  Since a lane's four sums of a block of 16 rows are, rounded, the
+// chunk (half a chunk in 16 bit) that a product over those rows takes, the weights go from one product to the next in registers.
+#pragma once
+
+#include "na2d_mfma.hpp"
+#include "seq.h"
+
+namespace seq {
+
+using namespace na2d;
+
+constexpr int kTile = 64;        // tokens staged at a time
+constexpr int kWaves = 4, kThreads = kWaves * kWave;
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+constexpr int kFar = 1 << 30;    // a window without end
+constexpr float kLowest = -1.7e38f;   // start of a running maximum: below every finite score, and not infinite
+
+// A tile of 64 tokens as the masks see it: the range of its documents (of the tokens that are not padding; empty if there are none), and per
+// token whether it is there at all and whether it is marked as prefix.
+struct Marks {
+    int dmin, dmax;
+    uint64_t live, prefix;
+};
+
+struct View {   // one tensor: byte strides of batch and head, bytes from row to row
+    const char *at;
+    int64_t b, h;
+    int row;
+};
+
+struct Args {
+    View q, k, v, out, dout, dq, dk, dv;
+    float *lse;
+    const float *slopes;
+    const int *documents;
+    const Marks *marks;    // of every 64 keys, [B, key_tiles]; null: neither documents nor prefix
+    const char *zeros;     // 64 bytes of zeros, where marks are
+    float2 *rows;          // backward: (lse in base 2, delta) of every query, [B * heads, query_tiles * 64]
+    int *powers;           // backward, fp16: per tile of 64 queries the power of two of its largest |dout|, [B * heads, query_tiles]
+    int B, heads, kv, group, Lq, Lk, off;   // off: Lk - Lq
+    int key_tiles, query_tiles;
+    int causal, window;    // window: kFar where there is none
+    int prefix;            // marks hold prefix bits
+    int dlo;               // smallest distance that the order and the window allow; the largest is window - 1
+    float scale, c, cap;   // c: scale log2(e), or with a cap 2 scale log2(e) / cap; cap: 2 cap log2(e)
+};
+
+// ---- products --------------------------------------------------------------------------------------------------------------
+
+template <typename T> __device__ __forceinline__ f32x4 mma(u32x4 a, u32x4 b, f32x4 c) {
+    if constexpr (sizeof(T) == 2) {
+        return mfma_16x16x32<T>(a, b, c);
+    } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) c = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(a[e]), __uint_as_float(b[e]), c, 0, 0, 0);
+        return c;
+    }
+}
+template <typename T> constexpr int kRowBlocks = sizeof(T) == 2 ? 2 : 1;   // blocks of 16 rows that one chunk of weights spans
+
+// the sums of kRowBlocks blocks as a chunk, rounded to the type (nearest even)
+template <typename T> __device__ __forceinline__ u32x4 pack(const f32x4 *s) {
+    if constexpr (sizeof(T) == 4) {
+        return __builtin_bit_cast(u32x4, s[0]);
+    } else {
+        typedef T t2 __attribute__((ext_vector_type(2)));
+        typedef float f2 __attribute__((ext_vector_type(2)));
+        u32x4 r;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) r[i] = __builtin_bit_cast(uint32_t, __builtin_convertvector(f2{s[i / 2][i % 2 * 2], s[i / 2][i % 2 * 2 + 1]}, t2));
+        return r;
+    }
+}
+
+// ---- tiles in LDS ----------------------------------------------------------------------------------------------------------
+//
+// 64 rows of CH chunks, as direct loads leave them (lane l of a load writes 16 bytes at 16 l), chunk c of row r in place c ^ swizzle(r): sixteen
+// rows' chunks of one column (a row fragment), and pairs of chunks of eight rows in turn (a transposed one), then lie in different banks.
+
+template <typename T, int D> struct Tile {
+    static constexpr int CH = D * (int)sizeof(T) / 16, ROWB = CH * 16, BYTES = kTile * ROWB;
+    static constexpr int STEPS = CH / 4;                        // products over the head vector
+    static constexpr int DB = D / 16;                           // blocks of 16 channels
+    static constexpr int PER256 = CH >= 16 ? 1 : 16 / CH;       // rows in the 256 bytes of all banks
+    static constexpr int LOADS = kTile * CH / kThreads;         // of 16 bytes, per thread and image
+
+    __device__ static __forceinline__ int swizzle(int r) { return ((r / PER256 & (8 / PER256 - 1)) << 1) | (r >> 3 & 1); }
+
+    // Rows first .. first + 63 of a plane into the image at `img`; a row past the end is the last one once more, where `zeros` are given, one that is not live is zeros.
+    __device__ static __forceinline__ void stage(const char *plane, int pitch, int first, int rows, uint64_t live, const char *zeros, int img, int wave, int lane) {
+        static_assert(CH <= kWave, "a row is at most one load");
+#pragma unroll
+        for (int i = 0; i < LOADS; ++i) {
+            const int at = wave + i * kWaves, r = at * (kWave / CH) + lane / CH, c = (lane % CH) ^ swizzle(r);
+            const int row = first + r < rows ? first + r : rows - 1;
+            const unsigned off = (unsigned)(row * pitch + c * 16);
+            if (zeros) {
+                const char *g = live >> r & 1 ? plane + off : zeros;
+                global_to_lds_16(g, img + at * kWave * 16);
+            } else {
+                global_to_lds_16(plane, off, img + at * kWave * 16);
+            }
+        }
+    }
+
+    // Row fragments: lane (j, g) reads chunk 4 s + g of row 16 rb + j.
+    struct RowReader {
+        int at;
+        __device__ __forceinline__ RowReader(int lane) : at((lane & 15) * ROWB + ((lane >> 4) ^ swizzle(lane & 15)) * 16) {}
+        __device__ __forceinline__ u32x4 read(int img, int rb, int s) const { return *lds_ptr<u32x4>((at ^ (s * 64)) + img + rb * 16 * ROWB); }
+    };
+
+    // Transposed fragments: for channels 16 db .. + 15 (the product's rows) a chunk of the positions that pack() has in a lane's chunk of step t.
+    struct ColumnReader {
+        int at[sizeof(T) == 2 ? 1 : 4];
+        __device__ __forceinline__ ColumnReader(int lane) {
+            const int j = lane & 15, g = lane >> 4;
+            if constexpr (sizeof(T) == 2) {
+                const int r = 4 * g + (j >> 2);
+                at[0] = r * ROWB + (((j >> 1) & 1) ^ swizzle(r)) * 16 + (j & 1) * 8;
+            } else {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) at[e] = (4 * g + e) * ROWB + ((j >> 2) ^ swizzle(4 * g + e)) * 16 + (j & 3) * 4;
+            }
+        }
+        __device__ __forceinline__ u32x4 read(int img, int t, int db) const {
+            if constexpr (sizeof(T) == 2) {
+                const int a = (at[0] ^ (db * 32)) + img + t * 32 * ROWB;
+                const u32x2 x = lds_read_tr16(a), y = lds_read_tr16(a + 16 * ROWB);
+                return u32x4{x.x, x.y, y.x, y.y};
+            } else {
+                u32x4 r;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) r[e] = *lds_ptr<uint32_t>((at[e] ^ (db * 64)) + img + t * 16 * ROWB);
+                return r;
+            }
+        }
+    };
+
+    // This lane's chunks of row `row` straight from memory: the other operand of products with row fragments.
+    __device__ static __forceinline__ void load_row(u32x4 (&f)[STEPS], const char *plane, int pitch, int row, int lane) {
+#pragma unroll
+        for (int s = 0; s < STEPS; ++s) f[s] = *reinterpret_cast<const u32x4 *>(plane + (int64_t)row * pitch + (4 * s + (lane >> 4)) * 16);
+    }
+    // Sums with channels as rows, [DB] blocks, column `row` of a tensor: four channels of each block.
+    __device__ static __forceinline__ void store_row(const f32x4 *acc, float by, char *plane, int pitch, int row, int lane) {
+#pragma unroll
+        for (int db = 0; db < DB; ++db) {
+            char *to = plane + (int64_t)row * pitch + (16 * db + 4 * (lane >> 4)) * (int)sizeof(T);
+            const f32x4 x = acc[db] * by;
+            if constexpr (sizeof(T) == 4) {
+                *reinterpret_cast<f32x4 *>(to) = x;
+            } else {
+                typedef T t4 __attribute__((ext_vector_type(4)));
+                *reinterpret_cast<t4 *>(to) = __builtin_convertvector(x, t4);
+            }
+        }
+    }
+};
+
+// ---- masks -----------------------------------------------------------------------------------------------------------------
+
+// Queries at positions qa .. qb against keys ka .. kb: any pair, or every pair, that order and window allow.
+__device__ __forceinline__ bool near_any(const Args &p, int qa, int qb, int ka, int kb) { return qb - ka >= p.dlo && qa - kb < p.window; }
+__device__ __forceinline__ bool near_all(const Args &p, int qa, int qb, int ka, int kb) { return qa - kb >= p.dlo && qb - ka < p.window; }
+__device__ __forceinline__ bool near_one(const Args &p, int distance) { return (unsigned)(distance - p.dlo) < (unsigned)(p.window - p.dlo); }
+
+// A range of documents; every token of it being live as well.
+struct Docs {
+    int lo, hi;
+    bool all;
+    __device__ __forceinline__ bool meet(const Docs &o) const { return lo <= o.hi && o.lo <= hi; }
+    __device__ __forceinline__ bool same(const Docs &o) const { return all && o.all && lo == hi && o.lo == o.hi && lo == o.lo; }
+};
+__device__ __forceinline__ Docs no_docs() { return {0, 0, true}; }
+__device__ __forceinline__ int wave_min(int x) {
+#pragma unroll
+    for (int d = 1; d < kWave; d *= 2) x = min(x, __shfl_xor(x, d));
+    return x;
+}
+__device__ __forceinline__ int wave_max(int x) {
+#pragma unroll
+    for (int d = 1; d < kWave; d *= 2) x = max(x, __shfl_xor(x, d));
+    return x;
+}
+__device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
+// of the wave's tokens; `there` false: no token in this lane
+__device__ __forceinline__ Docs docs_of_wave(int d, bool there) {
+    const bool live = there && d >= 0;
+    Docs r{uniform(wave_min(live ? d : INT32_MAX)), uniform(wave_max(live ? d : -1)), __ballot(there && d < 0) == 0};
+    return r;
+}
+
+// Walks the tiles first .. last that `of` says something about: a lane looks at one tile, 64 at a time.  of(tile) gives bits: 1 any pair of the
+// workgroup's is seen, 2 any pair of this wave's, 4 every pair of this wave's.  The first bit must not differ between waves.
+struct Walk {
+    uint64_t todo, mine, whole;
+    int base, last;
+    __device__ __forceinline__ Walk(int first, int last_) : todo(0), mine(0), whole(0), base(first - kWave), last(last_) {}
+    template <class F> __device__ __forceinline__ int next(F of, int lane, bool &is_mine, bool &is_whole) {
+        while (!todo) {
+            base += kWave;
+            if (base > last) return -1;
+            const int bits = base + lane <= last ? of(base + lane) : 0;
+            todo = __ballot(bits & 1);
+            mine = __ballot(bits & 2);
+            whole = __ballot(bits & 4);
+        }
+        const int i = __builtin_ctzll(todo);
+        todo &= todo - 1;
+        is_mine = mine >> i & 1;
+        is_whole = whole >> i & 1;
+        return base + i;
+    }
+};
+
+// blockIdx in an order in which what follows each other runs on the same XCD (consecutive workgroups go to the eight in turn, each has an L2 of its own)
+__device__ __forceinline__ int block_in_order() {
+    const int n = gridDim.x, each = n / 8, rest = n % 8, x = blockIdx.x % 8;
+    return x * each + min(x, rest) + blockIdx.x / 8;
+}
+
+// ---- scores ----------------------------------------------------------------------------------------------------------------
+
+// A product as a score in base 2, before bias and mask.  Capped: with z = scale <q, k> / cap and r = 1 / (1 + e^2z), tanh z = 1 - 2 r, so the score is
+// cap log2(e) - (2 cap log2(e)) r, and its derivative by the product 1 - tanh^2 = 4 r (1 - r).  That form is off by 2^-24 of the cap, below what 16-bit
+// products carry; fp32 takes the library's tanh.  `slope` is what the derivative is computed from.
+template <typename T, bool CAP> __device__ __forceinline__ float score(const Args &p, float s, float &slope) {
+    if constexpr (!CAP) {
+        return s * p.c;
+    } else if constexpr (sizeof(T) == 2) {
+        const float r = __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(s * p.c));   // p.c = 2 log2(e) scale / cap
+        slope = r;
+        return __builtin_fmaf(-p.cap, r, 0.5f * p.cap);                                 // p.cap = 2 cap log2(e)
+    } else {
+        const float t = tanhf(s * (0.5f * kLn2 * p.c));
+        slope = t;
+        return 0.5f * p.cap * t;
+    }
+}
+template <typename T, bool CAP> __device__ __forceinline__ float through_cap(float ds, float slope) {
+    if constexpr (!CAP) return ds;
+    else if constexpr (sizeof(T) == 2) return ds * (4.f * slope * (1.f - slope));
+    else return ds * __builtin_fmaf(-slope, slope, 1.f);
+}
+
+// ---- host ------------------------------------------------------------------------------------------------------------------
+
+hipError_t launch_marks(const Args &a, const uint8_t *prefix, Marks *marks, char *zeros, hipStream_t st);
+hipError_t launch_fwd(const Args &a, int dtype, int D, bool capped, hipStream_t st);
+hipError_t launch_rows(const Args &a, int dtype, int D, hipStream_t st);
+hipError_t launch_bwd_q(const Args &a, int dtype, int D, bool capped, hipStream_t st);
+hipError_t launch_bwd_kv(const Args &a, int dtype, int D, bool capped, hipStream_t st);
+
+template <template <typename, int, bool> class L, typename... A> hipError_t dispatch(int dtype, int D, bool capped, const A &...a) {
+#define SEQ_D(T, N) (capped ? L<T, N, true>::go(a...) : L<T, N, false>::go(a...))
+#define SEQ_T(T) (D == 32 ? SEQ_D(T, 32) : D == 64 ? SEQ_D(T, 64) : SEQ_D(T, 128))
+    return dtype == NA2D_F32 ? SEQ_T(float) : dtype == NA2D_F16 ? SEQ_T(f16_t) : SEQ_T(bf16_t);
+#undef SEQ_T
+#undef SEQ_D
+}
+
+}  // namespace seq

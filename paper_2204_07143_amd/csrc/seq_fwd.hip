@@ -1,0 +1,241 @@
+// Attention over a sequence, forward: one pass over the keys with the running maximum and sum of a softmax.
+//
+// A wave keeps QB blocks of 16 queries as product columns, a workgroup of four waves 64 QB; per tile of 64 keys
+//   S^T = K Q^T          a lane has four scores of each block of 16 keys for its query
+//   P = exp2(S' - ref)   ref: the running maximum, followed only once it is left by more than kSlack (the sums are rescaled then)
+//   out^T += V^T P       P is the product's other operand as it lies in the registers; V through transposing LDS reads
+// Keys and values come by direct loads into two images each, the next tile on its way while one is worked on.  Tiles in which the workgroup sees
+// nothing are left out, tiles in which a wave sees all take no mask.
+#include "lds_attr.hpp"
+#include "seq_common.hpp"
+
+namespace seq {
+
+namespace {
+
+constexpr float kSlack = 8.f;   // weights reach 2^8: fp16 holds them with all digits, and their sum
+
+template <typename T, int D> constexpr int kQB = sizeof(T) == 2 ? 2 : 1;
+
+template <typename T, int D, bool CAP>
+__global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) void fwd_kernel(const Args p) {
+    using L = Tile<T, D>;
+    constexpr int QB = kQB<T, D>, RB = kRowBlocks<T>, NB = kTile / 16;
+    extern __shared__ __align__(16) char lds[];
+    __shared__ int ids[2][kTile];
+    __shared__ int range[3][kWaves];
+    const int tid = threadIdx.x, lane = tid % kWave, wave = uniform(tid / kWave), j = lane & 15, g = lane >> 4;
+    const int tiles = (p.Lq + 16 * QB * kWaves - 1) / (16 * QB * kWaves);
+    // key heads in turn, the last queries (in causal order the longest work) first, the query heads of one key head next to each other
+    int id = block_in_order();
+    const int in_group = id % p.group;
+    id /= p.group;
+    const int tile = tiles - 1 - id % tiles, plane = id / tiles, b = plane / p.kv, kh = plane % p.kv, h = kh * p.group + in_group;
+    const char *kp = p.k.at + b * p.k.b + kh * p.k.h, *vp = p.v.at + b * p.v.b + kh * p.v.h, *qp = p.q.at + b * p.q.b + h * p.q.h;
+    const int q0 = tile * 16 * QB * kWaves, qw = q0 + wave * 16 * QB;
+    const int img = lds_addr(lds);
+
+    u32x4 q[QB][L::STEPS];
+    int pos[QB], mine[QB];
+#pragma unroll
+    for (int n = 0; n < QB; ++n) {
+        const int i = min(qw + 16 * n + j, p.Lq - 1);
+        L::load_row(q[n], qp, p.q.row, i, lane);
+        pos[n] = i + p.off;
+        mine[n] = p.documents ? p.documents[(int64_t)b * p.Lk + pos[n]] : 0;
+    }
+    Docs dw = no_docs(), dg = no_docs();
+    if (p.documents) {
+        const int i = qw + lane % (16 * QB);
+        dw = docs_of_wave(p.documents[(int64_t)b * p.Lk + min(i, p.Lq - 1) + p.off], true);
+        if (lane == 0) range[0][wave] = dw.lo, range[1][wave] = dw.hi;
+        workgroup_sync();
+        dg = {range[0][0], range[1][0], false};
+#pragma unroll
+        for (int w = 1; w < kWaves; ++w) dg.lo = min(dg.lo, range[0][w]), dg.hi = max(dg.hi, range[1][w]);
+        dg.lo = uniform(dg.lo), dg.hi = uniform(dg.hi);
+    }
+    const int qa = min(q0, p.Lq - 1) + p.off, qb = min(q0 + 16 * QB * kWaves, p.Lq) - 1 + p.off;
+    const int wa = min(qw, p.Lq - 1) + p.off, wb = min(qw + 16 * QB, p.Lq) - 1 + p.off;   // (a wave past the end: the last query)
+    const Marks *marks = p.marks ? p.marks + (int64_t)b * p.key_tiles : nullptr;
+    auto of = [&](int t) {
+        const int ka = t * kTile, kb = min(ka + kTile, p.Lk) - 1;
+        bool any = near_any(p, qa, qb, ka, kb), some = near_any(p, wa, max(wa, wb), ka, kb), all = near_all(p, wa, max(wa, wb), ka, kb) && ka + kTile <= p.Lk;
+        if (marks) {
+            const Marks m = marks[t];
+            const Docs d{m.dmin, m.dmax, m.live == ~0ull};
+            any |= m.prefix != 0, some |= m.prefix != 0, all |= m.prefix == ~0ull;
+            if (p.documents) any &= d.meet(dg), some &= d.meet(dw), all &= d.same(dw);
+        }
+        return (any ? 1 : 0) | (some ? 2 : 0) | (all ? 4 : 0);
+    };
+    int first = 0, last = p.key_tiles - 1;
+    if (!p.prefix) {
+        first = max(0, qa - p.window + 1) / kTile;
+        last = min(last, max(-1, qb - p.dlo) >> 6);
+    }
+    Walk walk(first, last);
+
+    const typename L::RowReader rows(lane);
+    const typename L::ColumnReader columns(lane);
+    const float slope = p.slopes ? p.slopes[h] * kLog2e : 0.f;
+    f32x4 out[QB][L::DB];
+    float ref[QB], sum[QB];
+#pragma unroll
+    for (int n = 0; n < QB; ++n) {
+        ref[n] = kLowest, sum[n] = 0.f;
+#pragma unroll
+        for (int db = 0; db < L::DB; ++db) out[n][db] = f32x4{0.f, 0.f, 0.f, 0.f};
+    }
+
+    auto stage = [&](int t, int buf) {
+        const int to = img + buf * 2 * L::BYTES;
+        const char *zeros = p.documents ? p.zeros : nullptr;
+        const uint64_t live = zeros ? marks[t].live : 0;
+        L::stage(kp, p.k.row, t * kTile, p.Lk, live, zeros, to, wave, lane);
+        L::stage(vp, p.v.row, t * kTile, p.Lk, live, zeros, to + L::BYTES, wave, lane);
+        if (zeros && wave == 0) global_to_lds_4(reinterpret_cast<const char *>(p.documents + (int64_t)b * p.Lk), (unsigned)min(t * kTile + lane, p.Lk - 1) * 4, lds_addr(ids[buf]));
+    };
+
+    bool some, all, some_next, all_next;
+    int t = walk.next(of, lane, some, all), buf = 0;
+    if (t >= 0) stage(t, 0);
+#pragma unroll 1
+    while (t >= 0) {
+        const int after = walk.next(of, lane, some_next, all_next);
+        wait_global_loads();
+        workgroup_sync();
+        if (after >= 0) stage(after, buf ^ 1);
+        if (some) {
+            const int ki = img + buf * 2 * L::BYTES, vi = ki + L::BYTES, k0 = t * kTile;
+            f32x4 s[QB][NB];
+#pragma unroll
+            for (int n = 0; n < QB; ++n)
+#pragma unroll
+                for (int rb = 0; rb < NB; ++rb) s[n][rb] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int st = 0; st < L::STEPS; ++st)
+#pragma unroll
+                for (int rb = 0; rb < NB; ++rb) {
+                    const u32x4 a = rows.read(ki, rb, st);
+#pragma unroll
+                    for (int n = 0; n < QB; ++n) s[n][rb] = mma<T>(a, q[n][st], s[n][rb]);
+                }
+#pragma unroll
+            for (int n = 0; n < QB; ++n) {
+#pragma unroll
+                for (int rb = 0; rb < NB; ++rb)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) {
+                        float unused;
+                        s[n][rb][r] = score<T, CAP>(p, s[n][rb][r], unused);
+                    }
+                if (p.slopes) {
+                    const float from = (float)(pos[n] - k0 - 4 * g);
+#pragma unroll
+                    for (int rb = 0; rb < NB; ++rb)
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) s[n][rb][r] = __builtin_fmaf(fabsf(from - (float)(16 * rb + r)), -slope, s[n][rb][r]);
+                }
+            }
+            if (!all) {
+                const uint64_t prefix = p.prefix ? marks[t].prefix : 0;
+#pragma unroll
+                for (int rb = 0; rb < NB; ++rb)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) {
+                        const int at = 16 * rb + 4 * g + r, key = k0 + at, doc = p.documents ? ids[buf][at] : 0;
+                        const bool there = key < p.Lk && doc >= 0, always = prefix >> at & 1;
+#pragma unroll
+                        for (int n = 0; n < QB; ++n)
+                            if (!(there && doc == mine[n] && (always || near_one(p, pos[n] - key)))) s[n][rb][r] = -INFINITY;
+                    }
+            }
+            u32x4 w[QB][NB / RB];
+#pragma unroll
+            for (int n = 0; n < QB; ++n) {
+                float most = s[n][0][0];
+#pragma unroll
+                for (int rb = 0; rb < NB; ++rb)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) most = fmaxf(most, s[n][rb][r]);
+                most = column_max(most);
+                const float now = most > ref[n] + kSlack ? most : ref[n];
+                if (__any(now != ref[n])) {
+                    const float by = __builtin_amdgcn_exp2f(ref[n] - now);
+                    sum[n] *= by;
+#pragma unroll
+                    for (int db = 0; db < L::DB; ++db) out[n][db] *= by;
+                    ref[n] = now;
+                }
+#pragma unroll
+                for (int rb = 0; rb < NB; ++rb)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) {
+                        s[n][rb][r] = __builtin_amdgcn_exp2f(s[n][rb][r] - ref[n]);
+                        sum[n] += s[n][rb][r];
+                    }
+#pragma unroll
+                for (int i = 0; i < NB / RB; ++i) w[n][i] = pack<T>(&s[n][i * RB]);
+            }
+#pragma unroll
+            for (int i = 0; i < NB / RB; ++i)
+#pragma unroll
+                for (int db = 0; db < L::DB; ++db) {
+                    const u32x4 a = columns.read(vi, i, db);
+#pragma unroll
+                    for (int n = 0; n < QB; ++n) out[n][db] = mma<T>(a, w[n][i], out[n][db]);
+                }
+        }
+        t = after, some = some_next, all = all_next, buf ^= 1;
+    }
+#pragma unroll
+    for (int n = 0; n < QB; ++n) {
+        settle_products(out[n]);
+        const int i = qw + 16 * n + j;
+        const float total = column_sum(sum[n]);
+        if (i < p.Lq) {
+            L::store_row(out[n], total == 0.f ? 0.f : 1.f / total, const_cast<char *>(p.out.at) + b * p.out.b + h * p.out.h, p.out.row, i, lane);
+            if (p.lse && g == 0) p.lse[((int64_t)b * p.heads + h) * p.Lq + i] = total == 0.f ? -INFINITY : (ref[n] + __builtin_amdgcn_logf(total)) * kLn2;
+        }
+    }
+}
+
+template <typename T, int D, bool CAP> struct Fwd {
+    static hipError_t go(const Args &a, hipStream_t st) {
+        constexpr int lds = 4 * Tile<T, D>::BYTES, rows = 16 * kQB<T, D> * kWaves;
+        static LdsAllowed allowed;
+        if (hipError_t e = allow_lds(fwd_kernel<T, D, CAP>, lds, allowed); e != hipSuccess) return e;
+        const int64_t blocks = (int64_t)a.B * a.heads * ((a.Lq + rows - 1) / rows);
+        if (!launch_holds(blocks, kThreads)) return hipErrorInvalidValue;
+        fwd_kernel<T, D, CAP><<<(unsigned)blocks, kThreads, lds, st>>>(a);
+        return hipGetLastError();
+    }
+};
+
+__global__ __launch_bounds__(kThreads) void marks_kernel(const int *__restrict__ documents, const uint8_t *__restrict__ prefix, int Lk, int tiles, int total, Marks *marks, uint32_t *zeros) {
+    const int lane = threadIdx.x % kWave, n = blockIdx.x * kWaves + threadIdx.x / kWave;
+    if (blockIdx.x == 0 && threadIdx.x < 16) zeros[threadIdx.x] = 0;
+    if (n >= total) return;
+    const int b = n / tiles, t = n % tiles, at = t * kTile + lane;
+    const bool there = at < Lk;
+    const int64_t i = (int64_t)b * Lk + (there ? at : Lk - 1);
+    const int d = documents ? documents[i] : 0;
+    const bool live = there && d >= 0;
+    const Docs r = docs_of_wave(d, there);
+    const uint64_t l = __ballot(live), x = __ballot(live && prefix && prefix[i] != 0);
+    if (lane == 0) marks[n] = Marks{r.lo, r.hi, l, x};
+}
+
+}  // namespace
+
+hipError_t launch_marks(const Args &a, const uint8_t *prefix, Marks *marks, char *zeros, hipStream_t st) {
+    const int64_t total = (int64_t)a.B * a.key_tiles;
+    if (!launch_holds((total + kWaves - 1) / kWaves, kThreads)) return hipErrorInvalidValue;
+    marks_kernel<<<(unsigned)((total + kWaves - 1) / kWaves), kThreads, 0, st>>>(a.documents, prefix, a.Lk, a.key_tiles, (int)total, marks, reinterpret_cast<uint32_t *>(zeros));
+    return hipGetLastError();
+}
+
+hipError_t launch_fwd(const Args &a, int dtype, int D, bool capped, hipStream_t st) { return dispatch<Fwd>(dtype, D, capped, a, st); }
+
+}  // namespace seq

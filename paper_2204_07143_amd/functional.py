@@ -18,6 +18,7 @@ from __future__ import annotations
 import importlib.machinery
 import importlib.util
 import os
+from typing import NamedTuple
 
 import torch
 
@@ -235,3 +236,161 @@ def na2d_unfused(q, k, v, rpb=None, kernel_size: int = 7, scale: float | None = 
         return out
     logits = na2d_qk_rpb(q, k, rpb, kernel_size, scale)
     return na2d_av(na2d_softmax(logits, q, kernel_size), v, kernel_size)
+
+
+# ---- attention over sequences -----------------------------------------------------------------------------------------
+
+def _rows(t: torch.Tensor) -> torch.Tensor:
+    """``t`` as the library reads it: any strides of whole 16 bytes but for the last dimension's; a copy where it has others."""
+    t = t.resolve_neg()
+    step = 16 // t.element_size()
+    fits = (t.shape[-1] == 1 or t.stride(-1) == 1) and t.data_ptr() % 16 == 0
+    fits = fits and all(n == 1 or s % step == 0 for n, s in zip(t.shape[:-1], t.stride()[:-1]))
+    fits = fits and ((t.shape[-2] - 1) * t.stride(-2) + t.shape[-1]) * t.element_size() < 1 << 31
+    return t if fits else t.clone(memory_format=torch.contiguous_format)
+
+
+def _like(t: torch.Tensor) -> torch.Tensor:
+    """An empty tensor in ``t``'s order of dimensions, with the last one innermost."""
+    out = torch.empty_like(t)
+    return out if out.stride(-1) == 1 and _rows(out) is out else torch.empty(t.shape, dtype=t.dtype, device=t.device)
+
+
+def _scratch(size: int, like: torch.Tensor):
+    return torch.empty(size, dtype=torch.uint8, device=like.device) if size else None
+
+
+class _OnceOnly(torch.autograd.Function):
+    """Gradients as they are, tied to what they depend on by a node that raises: no second derivative, and none that is silently zero."""
+
+    @staticmethod
+    def forward(ctx, count, *tensors):
+        return tuple(t.view_as(t) for t in tensors[:count])
+
+    @staticmethod
+    def backward(ctx, *_):
+        raise RuntimeError("seq_attention has no second derivative")
+
+
+class _SeqAttention(torch.autograd.Function):
+    """Softmax attention over a sequence (include/seq.h)."""
+
+    @staticmethod
+    def forward(ctx, q, k, v, slopes, documents, prefix, settings):
+        q, k, v = _rows(q), _rows(k), _rows(v)
+        out = _like(q)
+        ctx.settings, ctx.empty = settings, 0 in q.shape or 0 in k.shape
+        train = any(ctx.needs_input_grad)
+        lse = torch.empty(q.shape[:3], dtype=torch.float32, device=q.device) if train else None
+        if ctx.empty:
+            out.zero_()
+        else:
+            marked = documents is not None or prefix is not None
+            ws = _scratch(na.seq_attention_workspace_bytes(na.seq_problem(q, k, v=v, out=out, **settings), True), q) if marked else None
+            na.seq_attention_fwd(q, k, v, slopes, documents, prefix, out, lse, ws, **settings)
+        if train:
+            ctx.save_for_backward(q, k, v, out, lse, slopes, documents, prefix)
+        return out
+
+    @staticmethod
+    def backward(ctx, dout):
+        q, k, v = ctx.saved_tensors[:3]
+        with torch.no_grad():
+            grads = _SeqAttention.gradients(ctx, dout)
+        if torch.is_grad_enabled():
+            grads = _OnceOnly.apply(3, *grads, q, k, v, dout)
+        return (*grads, None, None, None, None)
+
+    @staticmethod
+    def gradients(ctx, dout):
+        q, k, v, out, lse, slopes, documents, prefix = ctx.saved_tensors
+        dq, dk, dv = _like(q), _like(k), _like(v)
+        if ctx.empty:
+            return dq.zero_(), dk.zero_(), dv.zero_()
+        dout = _rows(dout)
+        p = na.seq_problem(q, k, v=v, out=out, dout=dout, dq=dq, dk=dk, dv=dv, **ctx.settings)
+        ws = _scratch(na.seq_attention_workspace_bytes(p, documents is not None or prefix is not None, True), q)
+        na.seq_attention_bwd(q, k, v, slopes, documents, prefix, out, lse, dout, dq, dk, dv, ws, **ctx.settings)
+        return dq, dk, dv
+
+
+def _settings(q, window, softcap, scale, slopes) -> dict:
+    if window is not None and (int(window) != window or not 1 <= window <= 1 << 30):
+        raise ValueError(f"window must be a whole number of at least 1, or None, got {window}")
+    if softcap is not None and not 0 < softcap < float("inf"):
+        raise ValueError(f"softcap must be positive and finite, or None, got {softcap}")
+    if slopes is not None and slopes.requires_grad:
+        raise ValueError("slopes are constants: they have no gradient")
+    return dict(window=0 if window is None else int(window), softcap=0.0 if softcap is None else float(softcap), scale=_scale_of(q, scale))
+
+
+def _heads_of(q, k, v):
+    if q.dim() != 4 or k.dim() != 4 or v.dim() != 4:
+        raise ValueError("expected [B, heads, L, D] tensors")
+    B, heads, _, D = q.shape
+    if k.shape != v.shape or k.shape[0] != B or k.shape[3] != D:
+        raise ValueError(f"keys {tuple(k.shape)} and values {tuple(v.shape)} do not fit queries {tuple(q.shape)}")
+    if k.shape[1] == 0 or heads % k.shape[1]:
+        raise ValueError(f"{heads} query heads cannot share {k.shape[1]} key heads")
+
+
+def seq_attention(q, k, v, *, causal: bool = False, window: int | None = None, softcap: float | None = None, slopes=None, documents=None, prefix=None,
+                  scale: float | None = None):
+    """Softmax attention of ``q`` [B, heads, Lq, D] over ``k``, ``v`` [B, kv_heads, Lk, D]; differentiable in q, k and v.
+
+    Query i stands at position i + Lk - Lq.  It sees the keys less than ``window`` away, none behind it if ``causal``, and wherever they stand those marked in
+    ``prefix`` (bool [B, Lk]); of all these only the keys of its own document (``documents``, int32 [B, Lk], Lq <= Lk; a
+    negative one marks padding, which sees and is seen by nobody).  A score is ``softcap * tanh(scale <q, k> / softcap)`` (None: ``scale <q, k>``)
+    less ``slopes[head] * |distance|`` (fp32 [heads]).  ``scale`` is D ** -0.5 unless given.  D is 32, 64 or 128; f32, f16, bf16.  The
+    tensors may be strided views ([B, L, heads, D] transposed); others than of whole 16-byte rows are copied.
+    """
+    _heads_of(q, k, v)
+    settings = dict(causal=bool(causal), **_settings(q, window, softcap, scale, slopes))
+    return _SeqAttention.apply(q, k, v, slopes, documents, prefix, settings)
+
+
+class SeqCache(NamedTuple):
+    """Keys and values in 8 bits: pages int8 [pages, kv_heads, page, D] and a scale for each page and head, fp32 [pages, kv_heads]; a value is
+    the integer times the scale.  Which page holds what is the caller's: a table, int32 [B, width], gives each sequence's pages in order."""
+    k_pages: torch.Tensor
+    v_pages: torch.Tensor
+    k_scales: torch.Tensor
+    v_scales: torch.Tensor
+
+    @classmethod
+    def empty(cls, pages: int, kv_heads: int, page: int, head_dim: int, device="cuda") -> "SeqCache":
+        cells = (torch.zeros((pages, kv_heads, page, head_dim), dtype=torch.int8, device=device) for _ in range(2))
+        return cls(*cells, *(torch.zeros((pages, kv_heads), dtype=torch.float32, device=device) for _ in range(2)))
+
+
+def seq_cache_append(cache: SeqCache, k, v, table, lengths, counts=None) -> None:
+    """Puts ``k``, ``v`` [B, kv_heads, n, D] behind the ``lengths`` (int32 [B]) tokens of each sequence, the first ``counts[b]`` of the n where ``counts``
+    (int32 [B]) is given.  A page's scale grows with its largest value; what it held is then rounded again.  ``lengths`` stays as it is.  No page may be
+    appended to by two sequences of one call; a page number that is none is passed over."""
+    if k.dim() != 4 or v.dim() != 4:
+        raise ValueError("expected [B, heads, L, D] tensors")
+    if 0 not in k.shape:
+        with torch.no_grad():
+            na.seq_cache_append(_rows(k), _rows(v), table, lengths, counts, *cache)
+
+
+def seq_cache_gather(cache: SeqCache, table, lengths, first, n: int, dtype=torch.bfloat16):
+    """The keys and values, [B, kv_heads, n, D] each, that the cache holds at positions ``first[b]`` (int32 [B]) .. + n - 1; 0 where a sequence has no token."""
+    B, (_, kv_heads, _, D) = table.shape[0], cache.k_pages.shape
+    k, v = (torch.empty((B, kv_heads, n, D), dtype=dtype, device=cache.k_pages.device) for _ in range(2))
+    return (k, v) if k.numel() == 0 else na.seq_cache_gather(*cache, table, lengths, first, k, v)
+
+
+def seq_cache_attention(q, cache: SeqCache, table, lengths, *, window: int | None = None, softcap: float | None = None, slopes=None, scale: float | None = None):
+    """Attention of each sequence's last n tokens, ``q`` [B, heads, n, D] in f16 or bf16, over its cache, which holds their keys and values already:
+    ``lengths`` counts them.  In causal order; scores as ``seq_attention`` has them.  Not differentiable."""
+    if q.dim() != 4:
+        raise ValueError("expected [B, heads, L, D] tensors")
+    settings = _settings(q, window, softcap, scale, slopes)
+    with torch.no_grad():
+        q = _rows(q)
+        out = _like(q)
+        if q.numel() == 0:
+            return out
+        p = na.seq_cache_problem(q, cache.k_pages, table, heads=q.shape[1], out=out, **settings)
+        return na.seq_cache_attention(q, *cache, table, lengths, slopes, out, _scratch(na.seq_cache_attention_workspace_bytes(p), q), **settings)
