@@ -54,18 +54,6 @@ int validate(const seq_problem *p, bool backward) {
     return NA2D_OK;
 }
 
-// The workspace: zeros, the marks of the keys' tiles, and for a backward pass the rows' statistics and the tiles' powers of two.
-struct Space {
-    int64_t marks, rows, powers, bytes;
-    Space(const seq_problem *p, bool marked, bool backward) {
-        const int64_t k_tiles = ((int64_t)p->Lk + kTile - 1) / kTile, q_tiles = ((int64_t)p->Lq + kTile - 1) / kTile;
-        marks = marked ? 64 : 0;
-        rows = (marked ? marks + (int64_t)sizeof(Marks) * p->B * k_tiles + 63 : 0) / 64 * 64;
-        powers = rows + (backward ? (int64_t)sizeof(float2) * p->B * p->heads * q_tiles * kTile : 0);
-        bytes = powers + (backward ? (int64_t)sizeof(int) * p->B * p->heads * q_tiles : 0);
-    }
-};
-
 Args args(const seq_problem *p, const float *slopes, const int32_t *documents) {
     Args a{};
     a.slopes = slopes, a.documents = documents;
@@ -76,8 +64,23 @@ Args args(const seq_problem *p, const float *slopes, const int32_t *documents) {
     a.scale = p->scale;
     a.c = p->softcap > 0.f ? (float)(2.0 * 1.4426950408889634 * p->scale / p->softcap) : (float)(1.4426950408889634 * p->scale);
     a.cap = (float)(2.0 * 1.4426950408889634 * p->softcap);
+    a.splits = kv_splits(a, p->dtype, p->D);
     return a;
 }
+
+// The workspace: zeros, the marks of the keys' tiles, and for a backward pass the rows' statistics, the tiles' powers of two and the splits' sums.
+struct Space {
+    int64_t marks, rows, powers, parts, bytes;
+    Space(const Args &a, int D, bool marked, bool backward) {
+        const int64_t queries = (int64_t)a.B * a.heads * a.query_tiles;
+        auto up = [](int64_t x) { return (x + 63) / 64 * 64; };
+        marks = marked ? 64 : 0;
+        rows = marked ? up(marks + (int64_t)sizeof(Marks) * a.B * a.key_tiles) : 0;
+        powers = up(rows + (backward ? (int64_t)sizeof(float2) * queries * kTile : 0));
+        parts = up(powers + (backward ? (int64_t)sizeof(int) * queries : 0));
+        bytes = parts + (backward && a.splits > 1 ? (int64_t)sizeof(float) * a.splits * 2 * a.B * a.kv * a.Lk * D : 0);
+    }
+};
 
 #define SEQ_REQUIRE(ptr)                            \
     do {                                            \
@@ -90,7 +93,7 @@ int check_marks(const seq_problem *p, const float *slopes, const int32_t *docume
     if (((uintptr_t)slopes | (uintptr_t)documents) & 3u) return NA2D_ERR_ALIGN;
     return documents && p->Lq > p->Lk ? NA2D_ERR_SHAPE : NA2D_OK;
 }
-int prepare(Args &a, const seq_problem *p, const Space &s, const uint8_t *prefix, void *workspace, size_t bytes, hipStream_t st) {
+int prepare(Args &a, const Space &s, const uint8_t *prefix, void *workspace, size_t bytes, hipStream_t st) {
     if (s.bytes && (!workspace || misaligned(workspace) || bytes < (size_t)s.bytes)) return NA2D_ERR_WORKSPACE;
     char *ws = static_cast<char *>(workspace);
     if (s.marks) {
@@ -141,7 +144,7 @@ extern "C" {
 int seq_validate_problem(const seq_problem *p, int backward) { return validate(p, backward != 0); }
 
 size_t seq_attention_workspace_bytes(const seq_problem *p, int marked, int backward) {
-    return validate(p, backward != 0) == NA2D_OK ? (size_t)Space(p, marked != 0, backward != 0).bytes : 0;
+    return validate(p, backward != 0) == NA2D_OK ? (size_t)Space(args(p, nullptr, nullptr), p->D, marked != 0, backward != 0).bytes : 0;
 }
 
 int seq_attention_fwd(const seq_problem *p, const void *q, const void *k, const void *v, const float *slopes, const int32_t *documents, const uint8_t *prefix,
@@ -155,7 +158,7 @@ int seq_attention_fwd(const seq_problem *p, const void *q, const void *k, const 
     const int e = elem(p->dtype);
     Args a = args(p, slopes, documents);
     a.q = view(q, p->q, e), a.k = view(k, p->k, e), a.v = view(v, p->v, e), a.out = view(out, p->out, e), a.lse = lse;
-    if (int r = prepare(a, p, Space(p, documents || prefix, false), prefix, workspace, workspace_bytes, st)) return r;
+    if (int r = prepare(a, Space(a, p->D, documents || prefix, false), prefix, workspace, workspace_bytes, st)) return r;
     return from_hip(launch_fwd(a, p->dtype, p->D, p->softcap > 0.f, st));
 }
 
@@ -175,10 +178,11 @@ int seq_attention_bwd(const seq_problem *p, const void *q, const void *k, const 
     Args a = args(p, slopes, documents);
     a.q = view(q, p->q, e), a.k = view(k, p->k, e), a.v = view(v, p->v, e), a.out = view(out, p->out, e), a.lse = const_cast<float *>(lse);
     a.dout = view(dout, p->dout, e), a.dq = view(dq, p->dq, e), a.dk = view(dk, p->dk, e), a.dv = view(dv, p->dv, e);
-    const Space s(p, documents || prefix, true);
-    if (int r = prepare(a, p, s, prefix, workspace, workspace_bytes, st)) return r;
+    const Space s(a, p->D, documents || prefix, true);
+    if (int r = prepare(a, s, prefix, workspace, workspace_bytes, st)) return r;
     a.rows = reinterpret_cast<float2 *>(static_cast<char *>(workspace) + s.rows);
     a.powers = reinterpret_cast<int *>(static_cast<char *>(workspace) + s.powers);
+    a.parts = reinterpret_cast<float *>(static_cast<char *>(workspace) + s.parts);
     if (int r = from_hip(launch_rows(a, p->dtype, p->D, st))) return r;
     if (int r = from_hip(launch_bwd_q(a, p->dtype, p->D, p->softcap > 0.f, st))) return r;
     return from_hip(launch_bwd_kv(a, p->dtype, p->D, p->softcap > 0.f, st));

@@ -8,6 +8,8 @@
 //
 // fp16 holds 2^-24 to 65504.  The weights enter dV's product times 2^8, and dS on the scale of the largest |dout| of its query (queries) or of the
 // heads that share the key (keys), so gradients far below 1 keep their digits; the powers of two come off the sums again.
+#include <algorithm>
+
 #include "lds_attr.hpp"
 #include "seq_common.hpp"
 
@@ -224,20 +226,36 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) void bwd_q_kernel
 }
 
 // ---- dK, dV ----------------------------------------------------------------------------------------------------------------
+//
+// kPair: with 128 channels in 16 bit a wave that kept both sums of 32 keys would take more than 256 registers, and run alone on its SIMD.  Two waves share
+// 32 keys instead: each forms P and dS of half of a tile's queries, the first sums dV, the second dK, and each gives the other, through LDS, the half
+// that it does not sum itself.
+//
+// The work of a workgroup, the tiles of every head that shares its keys, is split into p.splits parts of equal length where there are few workgroups; each
+// then leaves fp32 sums, which a last kernel adds in order.
+
+template <typename T, int D> constexpr bool kPair = sizeof(T) == 2 && D == 128;
+template <typename T, int D> constexpr int kKeys = 16 * kBlocks<T> * kWaves / (kPair<T, D> ? 2 : 1);   // of a workgroup
 
 template <typename T, int D, bool CAP>
-__global__ __launch_bounds__(kThreads, sizeof(T) == 2 && D < 128 ? 2 : 1) void bwd_kv_kernel(const Args p) {
+__global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) void bwd_kv_kernel(const Args p) {
     using L = Tile<T, D>;
     constexpr int KB = kBlocks<T>, RB = kRowBlocks<T>, NB = kTile / 16;
+    constexpr bool PAIR = kPair<T, D>;
     extern __shared__ __align__(16) char lds[];
     __shared__ int ids[2][kTile];
     __shared__ __align__(16) float2 stats[2][kTile];
-    __shared__ int range[6][kWaves];
+    __shared__ int range[4][kWaves];
+    __shared__ __align__(16) u32x4 given[PAIR ? kWaves : 1][KB][PAIR ? kWave : 1];
     const int tid = threadIdx.x, lane = tid % kWave, wave = uniform(tid / kWave), j = lane & 15, g = lane >> 4;
-    const int tiles = (p.Lk + 16 * KB * kWaves - 1) / (16 * KB * kWaves);
-    const int id = block_in_order(), tile = id % tiles, plane = id / tiles, b = plane / p.kv, kh = plane % p.kv;
+    const int role = PAIR ? wave & 1 : 0, group_of_keys = PAIR ? wave >> 1 : wave;
+    const int tiles = (p.Lk + kKeys<T, D> - 1) / kKeys<T, D>;
+    int id = block_in_order();
+    const int split = id % p.splits;
+    id /= p.splits;
+    const int tile = id % tiles, plane = id / tiles, b = plane / p.kv, kh = plane % p.kv;
     const char *kp = p.k.at + b * p.k.b + kh * p.k.h, *vp = p.v.at + b * p.v.b + kh * p.v.h;
-    const int k0 = tile * 16 * KB * kWaves, kw = k0 + wave * 16 * KB;
+    const int k0 = tile * kKeys<T, D>, kw = k0 + group_of_keys * 16 * KB;
     const int img = lds_addr(lds);
     const int *documents = p.documents ? p.documents + (int64_t)b * p.Lk : nullptr;
     const Marks *marks = p.marks ? p.marks + (int64_t)b * p.key_tiles : nullptr;
@@ -280,7 +298,7 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 && D < 128 ? 2 : 1) void b
         dg.lo = uniform(dg.lo), dg.hi = uniform(dg.hi);
         if (kScaled<T> && most != kNothing) power = uniform(most);
     }
-    const int ka = k0, kb = min(k0 + 16 * KB * kWaves, p.Lk) - 1;
+    const int ka = k0, kb = min(k0 + kKeys<T, D>, p.Lk) - 1;
     const int wa = min(kw, p.Lk - 1), wb = min(kw + 16 * KB, p.Lk) - 1;
     auto of = [&](int t) {
         const int qa = t * kTile + p.off, qb = min(t * kTile + kTile, p.Lq) - 1 + p.off;
@@ -299,7 +317,7 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 && D < 128 ? 2 : 1) void b
     }
     const typename L::RowReader rows(lane);
     const typename L::ColumnReader columns(lane);
-    f32x4 dk[KB][L::DB], dv[KB][L::DB];
+    f32x4 dk[KB][L::DB], dv[KB][L::DB];   // (of a pair, each wave uses dv alone: for dV the first, for dK the second)
 #pragma unroll
     for (int n = 0; n < KB; ++n)
 #pragma unroll
@@ -321,75 +339,108 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 && D < 128 ? 2 : 1) void b
         if (zeros && wave == 2) global_to_lds_4(reinterpret_cast<const char *>(documents), (unsigned)min(t * kTile + lane + p.off, p.Lk - 1) * 4, lds_addr(ids[buf]));
     };
 
-    // the heads that share these keys in turn, each one's tiles in turn
-    Walk walk(first, last);
-    int head = kh * p.group;
-    const int heads_end = head + p.group;
+    // the heads that share these keys in turn, each one's tiles in turn: from the split's first to its last
+    const int count = max(0, last - first + 1), all_tiles = p.group * count, each = (all_tiles + p.splits - 1) / p.splits;
+    const int lo = min(split * each, all_tiles), hi = min(lo + each, all_tiles);
+    const int head_lo = lo < hi ? lo / count : 0, head_hi = lo < hi ? (hi - 1) / count : -1;
+    const int tile_lo = lo < hi ? first + lo % count : 0, tile_hi = lo < hi ? first + (hi - 1) % count : -1;
+    int head = head_lo;
+    Walk walk(tile_lo, head == head_hi ? tile_hi : last);
     bool some, all, some_next = false, all_next = false;
     auto next = [&](bool &s, bool &a) {
         while (true) {
-            const int t = walk.next(of, lane, s, a);
-            if (t >= 0 || head + 1 >= heads_end) return t;
+            const int t = head <= head_hi ? walk.next(of, lane, s, a) : -1;
+            if (t >= 0 || head >= head_hi) return t;
             ++head;
-            walk = Walk(first, last);
+            walk = Walk(first, head == head_hi ? tile_hi : last);
         }
     };
-    int t = next(some, all), buf = 0, h = head;
+    int t = next(some, all), buf = 0, h = kh * p.group + head;
     if (t >= 0) stage(h, t, 0);
 #pragma unroll 1
     while (t >= 0) {
         const int after = next(some_next, all_next);
         wait_global_loads();
         workgroup_sync();
-        if (after >= 0) stage(head, after, buf ^ 1);
-        if (some) {
-            const int qi = img + buf * 2 * L::BYTES, di = qi + L::BYTES, q0 = t * kTile + p.off;
-            const float slope = p.slopes ? p.slopes[h] * kLog2e : 0.f, lower = two_to(-power - (int)kRaise<T>);
-#pragma unroll 1
-            for (int i = 0; i < NB / RB; ++i) {
-                f32x4 s[KB][RB], e[KB][RB];
+        if (after >= 0) stage(kh * p.group + head, after, buf ^ 1);
+        const int qi = img + buf * 2 * L::BYTES, di = qi + L::BYTES, q0 = t * kTile + p.off;
+        const float slope = p.slopes ? p.slopes[h] * kLog2e : 0.f, lower = two_to(-power - (int)kRaise<T>);
+        // P and dS of 16 RB queries from 16 RB i on, as chunks
+        auto weigh = [&](int i, u32x4 (&w)[KB], u32x4 (&x)[KB]) {
+            f32x4 s[KB][RB], e[KB][RB];
 #pragma unroll
-                for (int n = 0; n < KB; ++n)
+            for (int n = 0; n < KB; ++n)
 #pragma unroll
-                    for (int rb = 0; rb < RB; ++rb) s[n][rb] = e[n][rb] = f32x4{0.f, 0.f, 0.f, 0.f};
-                const int at0 = i * RB * 16 * L::ROWB;
+                for (int rb = 0; rb < RB; ++rb) s[n][rb] = e[n][rb] = f32x4{0.f, 0.f, 0.f, 0.f};
+            const int at0 = i * RB * 16 * L::ROWB;
 #pragma unroll
-                for (int st = 0; st < L::STEPS; ++st)
-#pragma unroll
-                    for (int rb = 0; rb < RB; ++rb) {
-                        const u32x4 a = rows.read(qi + at0, rb, st), c = rows.read(di + at0, rb, st);
-#pragma unroll
-                        for (int n = 0; n < KB; ++n) s[n][rb] = mma<T>(a, k[n][st], s[n][rb]), e[n][rb] = mma<T>(c, v[n][st], e[n][rb]);
-                    }
-                u32x4 w[KB], x[KB];
+            for (int st = 0; st < L::STEPS; ++st)
 #pragma unroll
                 for (int rb = 0; rb < RB; ++rb) {
-                    const int at = (i * RB + rb) * 16 + 4 * g;   // of this lane's four queries
-                    f32x4 two[2];
-                    two[0] = *reinterpret_cast<const f32x4 *>(&stats[buf][at]), two[1] = *reinterpret_cast<const f32x4 *>(&stats[buf][at + 2]);
+                    const u32x4 a = rows.read(qi + at0, rb, st), c = rows.read(di + at0, rb, st);
 #pragma unroll
-                    for (int n = 0; n < KB; ++n) {
-                        const float from = (float)(q0 + at - key[n]);
-#pragma unroll
-                        for (int r = 0; r < 4; ++r) {
-                            const float lse = two[r / 2][r % 2 * 2], delta = two[r / 2][r % 2 * 2 + 1];
-                            float by = 0.f, y = score<T, CAP>(p, s[n][rb][r], by);
-                            if (p.slopes) y = __builtin_fmaf(fabsf(from + (float)r), -slope, y);
-                            if (!all) {
-                                const int doc = documents ? ids[buf][at + r] : 0;
-                                if (!(doc >= 0 && doc == mine[n] && (always[n] || near_one(p, q0 + at + r - key[n])))) y = -INFINITY;
-                            }
-                            const float weight = __builtin_amdgcn_exp2f(y - lse);
-                            float ds = e[n][rb][r] - delta;
-                            if constexpr (kScaled<T>) ds *= lower;
-                            ds = through_cap<T, CAP>(weight * ds, by);
-                            if (!all) ds = weight == 0.f ? 0.f : ds;
-                            s[n][rb][r] = weight, e[n][rb][r] = ds;
-                        }
-                    }
+                    for (int n = 0; n < KB; ++n) s[n][rb] = mma<T>(a, k[n][st], s[n][rb]), e[n][rb] = mma<T>(c, v[n][st], e[n][rb]);
                 }
 #pragma unroll
-                for (int n = 0; n < KB; ++n) w[n] = pack<T>(s[n]), x[n] = pack<T>(e[n]);
+            for (int rb = 0; rb < RB; ++rb) {
+                const int at = (i * RB + rb) * 16 + 4 * g;   // of this lane's four queries
+                f32x4 two[2];
+                two[0] = *reinterpret_cast<const f32x4 *>(&stats[buf][at]), two[1] = *reinterpret_cast<const f32x4 *>(&stats[buf][at + 2]);
+#pragma unroll
+                for (int n = 0; n < KB; ++n) {
+                    const float from = (float)(q0 + at - key[n]);
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) {
+                        const float lse = two[r / 2][r % 2 * 2], delta = two[r / 2][r % 2 * 2 + 1];
+                        float by = 0.f, y = score<T, CAP>(p, s[n][rb][r], by);
+                        if (p.slopes) y = __builtin_fmaf(fabsf(from + (float)r), -slope, y);
+                        if (!all) {
+                            const int doc = documents ? ids[buf][at + r] : 0;
+                            if (!(doc >= 0 && doc == mine[n] && (always[n] || near_one(p, q0 + at + r - key[n])))) y = -INFINITY;
+                        }
+                        const float weight = __builtin_amdgcn_exp2f(y - lse);
+                        float ds = e[n][rb][r] - delta;
+                        if constexpr (kScaled<T>) ds *= lower;
+                        ds = through_cap<T, CAP>(weight * ds, by);
+                        if (!all) ds = weight == 0.f ? 0.f : ds;
+                        s[n][rb][r] = weight, e[n][rb][r] = ds;
+                    }
+                }
+            }
+#pragma unroll
+            for (int n = 0; n < KB; ++n) w[n] = pack<T>(s[n]), x[n] = pack<T>(e[n]);
+        };
+        if constexpr (PAIR) {
+            static_assert(!PAIR || NB / RB == 2, "a half for each");
+            u32x4 w[KB], x[KB];
+            if (some) {
+                weigh(role, w, x);
+#pragma unroll
+                for (int n = 0; n < KB; ++n) given[wave][n][lane] = role ? w[n] : x[n];
+            }
+            workgroup_sync();
+            if (some) {
+                u32x4 halves[2][KB];
+#pragma unroll
+                for (int n = 0; n < KB; ++n) {
+                    const u32x4 own = role ? x[n] : w[n], other = given[wave ^ 1][n][lane];
+                    halves[0][n] = role ? other : own, halves[1][n] = role ? own : other;
+                }
+                const int from = role ? qi : di;
+#pragma unroll
+                for (int i = 0; i < 2; ++i)
+#pragma unroll
+                    for (int db = 0; db < L::DB; ++db) {
+                        const u32x4 a = columns.read(from, i, db);
+#pragma unroll
+                        for (int n = 0; n < KB; ++n) dv[n][db] = mma<T>(a, halves[i][n], dv[n][db]);
+                    }
+            }
+        } else if (some) {
+#pragma unroll 1
+            for (int i = 0; i < NB / RB; ++i) {
+                u32x4 w[KB], x[KB];
+                weigh(i, w, x);
 #pragma unroll
                 for (int db = 0; db < L::DB; ++db) {
                     const u32x4 a = columns.read(di, i, db), c = columns.read(qi, i, db);
@@ -398,17 +449,50 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 && D < 128 ? 2 : 1) void b
                 }
             }
         }
-        t = after, h = head, some = some_next, all = all_next, buf ^= 1;
+        t = after, h = kh * p.group + head, some = some_next, all = all_next, buf ^= 1;
     }
+    // which: 0 dK, 1 dV
+    auto store = [&](int which, const f32x4 *acc, float by, int i) {
+        const View &to = which ? p.dv : p.dk;
+        if (p.splits == 1) L::store_row(acc, by, const_cast<char *>(to.at) + b * to.b + kh * to.h, to.row, i, lane);
+        else Tile<float, D>::store_row(acc, by, reinterpret_cast<char *>(p.parts + (((int64_t)split * 2 + which) * p.B * p.kv + plane) * p.Lk * D), D * 4, i, lane);
+    };
 #pragma unroll
     for (int n = 0; n < KB; ++n) {
         settle_products(dk[n]);
         settle_products(dv[n]);
         const int i = kw + 16 * n + j;
         if (i < p.Lk) {
-            L::store_row(dk[n], p.scale * two_to(power), const_cast<char *>(p.dk.at) + b * p.dk.b + kh * p.dk.h, p.dk.row, i, lane);
-            L::store_row(dv[n], two_to(-(int)kRaise<T>), const_cast<char *>(p.dv.at) + b * p.dv.b + kh * p.dv.h, p.dv.row, i, lane);
+            const float by_k = p.scale * two_to(power), by_v = two_to(-(int)kRaise<T>);
+            if constexpr (PAIR) {
+                store(role ? 0 : 1, dv[n], role ? by_k : by_v, i);
+            } else {
+                store(0, dk[n], by_k, i);
+                store(1, dv[n], by_v, i);
+            }
         }
+    }
+}
+
+// dK and dV: the splits' sums, in order; a thread per four channels.
+template <typename T, int D>
+__global__ __launch_bounds__(kThreads) void join_kv_kernel(const Args p, int64_t total) {
+    const int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x;
+    if (i >= total) return;
+    const int d = (int)(i % (D / 4)) * 4;
+    const int64_t row = i / (D / 4), each = (int64_t)p.B * p.kv * p.Lk;   // of dK, then of dV
+    f32x4 x{0.f, 0.f, 0.f, 0.f};
+    for (int s = 0; s < p.splits; ++s) x += *reinterpret_cast<const f32x4 *>(p.parts + ((int64_t)s * 2 * each + row) * D + d);
+    const bool values = row >= each;
+    const int64_t at = values ? row - each : row;
+    const View &to = values ? p.dv : p.dk;
+    const int plane = (int)(at / p.Lk);
+    char *out = const_cast<char *>(to.at) + plane / p.kv * to.b + plane % p.kv * to.h + at % p.Lk * to.row + d * (int)sizeof(T);
+    if constexpr (sizeof(T) == 4) {
+        *reinterpret_cast<f32x4 *>(out) = x;
+    } else {
+        typedef T t4 __attribute__((ext_vector_type(4)));
+        *reinterpret_cast<t4 *>(out) = __builtin_convertvector(x, t4);
     }
 }
 
@@ -433,14 +517,21 @@ template <typename T, int D, bool CAP> struct BwdQ {
 };
 template <typename T, int D, bool CAP> struct BwdKV {
     static hipError_t go(const Args &a, hipStream_t st) {
-        constexpr int lds = 4 * Tile<T, D>::BYTES, rows = 16 * kBlocks<T> * kWaves;
+        constexpr int lds = 4 * Tile<T, D>::BYTES;
         static LdsAllowed allowed;
         if (hipError_t e = allow_lds(bwd_kv_kernel<T, D, CAP>, lds, allowed); e != hipSuccess) return e;
-        const int64_t blocks = (int64_t)a.B * a.kv * ((a.Lk + rows - 1) / rows);
+        const int64_t blocks = (int64_t)a.B * a.kv * ((a.Lk + kKeys<T, D> - 1) / kKeys<T, D>) * a.splits;
         if (!launch_holds(blocks, kThreads)) return hipErrorInvalidValue;
         bwd_kv_kernel<T, D, CAP><<<(unsigned)blocks, kThreads, lds, st>>>(a);
+        if (hipError_t e = hipGetLastError(); e != hipSuccess || a.splits == 1) return e;
+        const int64_t total = (int64_t)a.B * a.kv * a.Lk * 2 * (D / 4), joins = (total + kThreads - 1) / kThreads;
+        if (!launch_holds(joins, kThreads)) return hipErrorInvalidValue;
+        join_kv_kernel<T, D><<<(unsigned)joins, kThreads, 0, st>>>(a, total);
         return hipGetLastError();
     }
+};
+template <typename T, int D, bool CAP> struct Keys {
+    static hipError_t go(int &keys) { return keys = kKeys<T, D>, hipSuccess; }
 };
 
 }  // namespace
@@ -448,5 +539,18 @@ template <typename T, int D, bool CAP> struct BwdKV {
 hipError_t launch_rows(const Args &a, int dtype, int D, hipStream_t st) { return dispatch<Rows>(dtype, D, false, a, st); }
 hipError_t launch_bwd_q(const Args &a, int dtype, int D, bool capped, hipStream_t st) { return dispatch<BwdQ>(dtype, D, capped, a, st); }
 hipError_t launch_bwd_kv(const Args &a, int dtype, int D, bool capped, hipStream_t st) { return dispatch<BwdKV>(dtype, D, capped, a, st); }
+
+
+// How many parts the work on one tile of keys is split into: until there are about kWanted workgroups, but each part is left four tiles of queries, and the parts' sums
+// stay below 256 MB.
+int kv_splits(const Args &a, int dtype, int D) {
+    int keys = 64;
+    (void)dispatch<Keys>(dtype, D, false, keys);
+    constexpr int64_t kWanted = 1024;
+    const int64_t units = (int64_t)a.B * a.kv * ((a.Lk + keys - 1) / keys), sums = (int64_t)a.B * a.kv * a.Lk * D * 8;
+    const int64_t reach = std::min<int64_t>(a.query_tiles, ((int64_t)a.window + keys) / kTile + 2);   // tiles of one head that a tile of keys can meet
+    const int64_t s = std::min({(kWanted + units - 1) / units, (int64_t)a.group * reach / 4, ((int64_t)256 << 20) / sums, (int64_t)16});
+    return (int)std::max<int64_t>(1, s);
+}
 
 }  // namespace seq

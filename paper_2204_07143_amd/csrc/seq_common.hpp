@@ -42,6 +42,8 @@ struct Args {
     const char *zeros;     // 64 bytes of zeros, where marks are
     float2 *rows;          // backward: (lse in base 2, delta) of every query, [B * heads, query_tiles * 64]
     int *powers;           // backward, fp16: per tile of 64 queries the power of two of its largest |dout|, [B * heads, query_tiles]
+    float *parts;          // backward, splits > 1: fp32 sums of dK and dV, [splits, 2, B * kv, Lk, D]
+    int splits;            // parts that the work on one tile of keys is split into
     int B, heads, kv, group, Lq, Lk, off;   // off: Lk - Lq
     int key_tiles, query_tiles;
     int causal, window;    // window: kFar where there is none
@@ -256,8 +258,9 @@ hipError_t launch_fwd(const Args &a, int dtype, int D, bool capped, hipStream_t 
 hipError_t launch_rows(const Args &a, int dtype, int D, hipStream_t st);
 hipError_t launch_bwd_q(const Args &a, int dtype, int D, bool capped, hipStream_t st);
 hipError_t launch_bwd_kv(const Args &a, int dtype, int D, bool capped, hipStream_t st);
+int kv_splits(const Args &a, int dtype, int D);
 
-template <template <typename, int, bool> class L, typename... A> hipError_t dispatch(int dtype, int D, bool capped, const A &...a) {
+template <template <typename, int, bool> class L, typename... A> hipError_t dispatch(int dtype, int D, bool capped, A &&...a) {
 #define SEQ_D(T, N) (capped ? L<T, N, true>::go(a...) : L<T, N, false>::go(a...))
 #define SEQ_T(T) (D == 32 ? SEQ_D(T, 32) : D == 64 ? SEQ_D(T, 64) : SEQ_D(T, 128))
     return dtype == NA2D_F32 ? SEQ_T(float) : dtype == NA2D_F16 ? SEQ_T(f16_t) : SEQ_T(bf16_t);
