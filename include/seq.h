@@ -56,15 +56,17 @@ int seq_validate_problem(const seq_problem *p, int backward);
 /* Bytes of workspace; 0 for an invalid problem.  `marked`: documents or prefix are given.  A forward call needs one only where this is not 0. */
 size_t seq_attention_workspace_bytes(const seq_problem *p, int marked, int backward);
 
-/* slopes: fp32 [heads] or NULL.  documents: int32 [B, Lk] or NULL, contiguous; needs Lq <= Lk.  prefix: bytes [B, Lk] or NULL, contiguous.
+/* rest (nullable, 16-bit types; strides of out): what out's rounding took from it, in the type.  A backward call that is given it takes delta = <dout, out> from
+ * their sum: where few keys carry a query's weight, out's rounding is otherwise as large a part of dS as dS's own.
+ * slopes: fp32 [heads] or NULL.  documents: int32 [B, Lk] or NULL, contiguous; needs Lq <= Lk.  prefix: bytes [B, Lk] or NULL, contiguous.
  * lse (nullable): fp32 [B, heads, Lq], contiguous; the log-sum-exp of every query's scores. */
 int seq_attention_fwd(const seq_problem *p, const void *q, const void *k, const void *v, const float *slopes, const int32_t *documents, const uint8_t *prefix,
-                      void *out, float *lse, void *workspace, size_t workspace_bytes, void *stream);
+                      void *out, float *lse, void *rest, void *workspace, size_t workspace_bytes, void *stream);
 
-/* dq, dk, dv from the forward's inputs, its out and lse, and dout.  Nothing is added in an order that varies; dk and dv are the sums over the
+/* dq, dk, dv from the forward's inputs, its out, lse and (nullable) rest, and dout.  Nothing is added in an order that varies; dk and dv are the sums over the
  * query heads that share a key head. */
 int seq_attention_bwd(const seq_problem *p, const void *q, const void *k, const void *v, const float *slopes, const int32_t *documents, const uint8_t *prefix,
-                      const void *out, const float *lse, const void *dout, void *dq, void *dk, void *dv, void *workspace, size_t workspace_bytes,
+                      const void *out, const float *lse, const void *rest, const void *dout, void *dq, void *dk, void *dv, void *workspace, size_t workspace_bytes,
                       void *stream);
 
 /*

@@ -132,8 +132,8 @@ def load(path: str | None = None) -> ctypes.CDLL:
         ps, pc, size = ctypes.POINTER(SeqProblem), ctypes.POINTER(SeqCacheProblem), ctypes.c_size_t
         sigs_seq = {
             "seq_validate_problem": [ps, ctypes.c_int],
-            "seq_attention_fwd": [ps] + [vp] * 9 + [size, vp],
-            "seq_attention_bwd": [ps] + [vp] * 13 + [size, vp],
+            "seq_attention_fwd": [ps] + [vp] * 10 + [size, vp],
+            "seq_attention_bwd": [ps] + [vp] * 14 + [size, vp],
             "seq_cache_validate": [pc, ctypes.c_int],
             "seq_cache_append": [pc] + [vp] * 10,
             "seq_cache_gather": [pc] + [vp] * 10,
@@ -558,20 +558,28 @@ def _bytes(workspace):
     return (None, 0) if workspace is None else (ctypes.c_void_p(workspace.data_ptr()), workspace.numel() * workspace.element_size())
 
 
-def seq_attention_fwd(q, k_, v, slopes, documents, prefix, out, lse=None, workspace=None, *, causal=False, window=0, softcap=0.0, scale=1.0):
+def _rest(rest, out):
+    if rest is None:
+        return None
+    if rest.stride() != out.stride():
+        raise ValueError("rest has out's strides")
+    return _strided(rest, out, out.shape)
+
+
+def seq_attention_fwd(q, k_, v, slopes, documents, prefix, out, lse=None, rest=None, workspace=None, *, causal=False, window=0, softcap=0.0, scale=1.0):
     p = seq_problem(q, k_, causal=causal, window=window, softcap=softcap, scale=scale, v=v, out=out)
     inputs = _seq_inputs(q, k_, v, slopes, documents, prefix)
     with torch.cuda.device(q.device):
-        _check(load().seq_attention_fwd(ctypes.byref(p), *inputs, _strided(out, q, q.shape), _dense(lse, q, q.shape[:3], torch.float32), *_bytes(workspace),
-                                        _seq_stream(q)))
+        _check(load().seq_attention_fwd(ctypes.byref(p), *inputs, _strided(out, q, q.shape), _dense(lse, q, q.shape[:3], torch.float32), _rest(rest, out),
+                                        *_bytes(workspace), _seq_stream(q)))
     return out
 
 
-def seq_attention_bwd(q, k_, v, slopes, documents, prefix, out, lse, dout, dq, dk, dv, workspace, *, causal=False, window=0, softcap=0.0, scale=1.0):
+def seq_attention_bwd(q, k_, v, slopes, documents, prefix, out, lse, rest, dout, dq, dk, dv, workspace, *, causal=False, window=0, softcap=0.0, scale=1.0):
     p = seq_problem(q, k_, causal=causal, window=window, softcap=softcap, scale=scale, v=v, out=out, dout=dout, dq=dq, dk=dk, dv=dv)
     inputs = _seq_inputs(q, k_, v, slopes, documents, prefix)
     with torch.cuda.device(q.device):
-        _check(load().seq_attention_bwd(ctypes.byref(p), *inputs, _strided(out, q, q.shape), _dense(lse, q, q.shape[:3], torch.float32), _strided(dout, q, q.shape),
+        _check(load().seq_attention_bwd(ctypes.byref(p), *inputs, _strided(out, q, q.shape), _dense(lse, q, q.shape[:3], torch.float32), _rest(rest, out), _strided(dout, q, q.shape),
                                         _strided(dq, q, q.shape), _strided(dk, q, k_.shape), _strided(dv, q, k_.shape), *_bytes(workspace), _seq_stream(q)))
     return dq, dk, dv
 

@@ -1,5 +1,5 @@
 // The differentiable operators of functional.py as native autograd nodes: argument checks, allocation and the calls of the C ABI
-// (na2d.h, na1d.h) without the interpreter in between.  Every gradient comes from the library's kernels, as there.
+// (na2d.h, na1d.h, seq.h) without the interpreter in between.  Every gradient comes from the library's kernels, as there.
 //
 // Each function of the module returns the operator's output, or None where something is not as the plain case has it (a tensor that is
 // not dense on one GPU or a subclass, shapes or types that do not fit, a functorch transform, forward-mode differentiation, tracing, a dispatch or
@@ -12,6 +12,8 @@
 #include <ATen/PythonTorchFunctionTLS.h>
 #include <ATen/hip/impl/HIPStreamMasqueradingAsCUDA.h>
 #include <c10/core/impl/LocalDispatchKeySet.h>
+#include <c10/core/DeviceGuard.h>
+#include <torch/csrc/Dtype.h>
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/PyInterpreter.h>
 #include <torch/csrc/autograd/custom_function.h>
@@ -27,6 +29,7 @@
 #include <optional>
 
 #include "na_typed.h"
+#include "seq.h"
 
 namespace {
 
@@ -321,6 +324,146 @@ struct Unfused : torch::autograd::Node {
     }
 };
 
+// ---- attention over sequences ------------------------------------------------------------------------------------------------
+
+// As the library reads it: strides of whole 16 bytes but for the last dimension's.
+bool whole_rows(const Tensor &t) {
+    const auto n = t.sizes(), s = t.strides();
+    const int64_t step = 16 / t.element_size();
+    for (int i = 0; i < 3; ++i)
+        if (n[i] != 1 && s[i] % step) return false;
+    return (n[3] == 1 || s[3] == 1) && (uintptr_t)t.data_ptr() % 16 == 0 && ((n[2] - 1) * s[2] + n[3]) * t.element_size() < (int64_t)1 << 31;
+}
+Tensor rows(const Tensor &t) { return whole_rows(t) ? t : t.clone(at::MemoryFormat::Contiguous); }
+Tensor rows_like(const Tensor &t) {   // empty, in t's order of dimensions, the last one innermost
+    Tensor r = at::empty_like(t);
+    return r.stride(3) == 1 && whole_rows(r) ? r : at::empty(t.sizes(), t.options());
+}
+seq_strides strides(const Tensor &t) {
+    const auto n = t.sizes(), s = t.strides();
+    return {n[0] == 1 ? 0 : s[0], n[1] == 1 ? 0 : s[1], n[2] == 1 ? 0 : s[2]};
+}
+bool small(at::IntArrayRef s) {
+    for (int64_t n : s)
+        if (n <= 0 || !fits(n)) return false;
+    return true;
+}
+
+struct SeqSettings {
+    int64_t causal, window;
+    double softcap, scale;
+};
+std::optional<seq_problem> seq_of(const Tensor &q, const Tensor &k, const Tensor &v, const Tensor &out, const SeqSettings &x) {
+    const auto code = dtype_code(q.scalar_type());
+    if (!code || q.dim() != 4 || k.dim() != 4 || !small(q.sizes()) || !small(k.sizes())) return std::nullopt;
+    seq_problem p{};
+    p.B = (int32_t)q.size(0), p.heads = (int32_t)q.size(1), p.Lq = (int32_t)q.size(2), p.D = (int32_t)q.size(3), p.kv_heads = (int32_t)k.size(1), p.Lk = (int32_t)k.size(2);
+    p.dtype = *code, p.causal = (int32_t)x.causal, p.window = (int32_t)x.window, p.softcap = (float)x.softcap, p.scale = (float)x.scale;
+    p.q = strides(q), p.k = strides(k), p.v = strides(v), p.out = strides(out);
+    return p;
+}
+// a constant of the call, or none: dense, on q's device, of this type and size
+bool constant(const Tensor &t, const Tensor &q, at::ScalarType type, at::IntArrayRef sizes) {
+    return !t.defined() || (plain(t) && t.scalar_type() == type && t.device() == q.device() && t.sizes() == sizes && t.is_contiguous());
+}
+Tensor scratch(size_t bytes, const Tensor &like) { return bytes ? workspace(bytes, like) : Tensor(); }
+size_t size_of(const Tensor &t) { return t.defined() ? (size_t)t.numel() : 0; }
+
+// Gradients as they are, tied to what they depend on by a node that raises: no second derivative, and none that is silently zero.
+struct OnceOnly : torch::autograd::Function<OnceOnly> {
+    static variable_list forward(AutogradContext *, const Tensor &dq, const Tensor &dk, const Tensor &dv, const Tensor &, const Tensor &, const Tensor &, const Tensor &) {
+        return {dq.view_as(dq), dk.view_as(dk), dv.view_as(dv)};
+    }
+    static variable_list backward(AutogradContext *, variable_list) { TORCH_CHECK(false, "seq_attention has no second derivative"); }
+};
+
+struct SeqAttention : torch::autograd::Function<SeqAttention> {
+    // lse, rest: what a backward pass takes besides out, or null
+    static Tensor run(const Tensor &q, const Tensor &k, const Tensor &v, const Tensor &slopes, const Tensor &documents, const Tensor &prefix, const SeqSettings &x, Tensor *lse,
+                      Tensor *rest) {
+        Tensor out = rows_like(q);
+        if (lse) *lse = fp32(q.sizes().slice(0, 3), q);
+        if (rest && q.element_size() == 2) *rest = at::empty_like(out);
+        const auto p = seq_of(q, k, v, out, x);
+        if (!p) throw Refused{};
+        const bool marked = documents.defined() || prefix.defined();
+        const Tensor ws = scratch(marked ? seq_attention_workspace_bytes(&*p, 1, 0) : 0, q);
+        forward_check(seq_attention_fwd(&*p, ptr(q), ptr(k), ptr(v), (const float *)ptr(slopes), (const int32_t *)ptr(documents), (const uint8_t *)ptr(prefix), ptr(out),
+                                        lse ? (float *)ptr(*lse) : nullptr, rest ? ptr(*rest) : nullptr, ptr(ws), size_of(ws), stream()));
+        return out;
+    }
+    static Tensor forward(AutogradContext *ctx, const Tensor &q_, const Tensor &k_, const Tensor &v_, const std::optional<Tensor> &slopes_, const std::optional<Tensor> &documents_,
+                          const std::optional<Tensor> &prefix_, int64_t causal, int64_t window, double softcap, double scale) {
+        const Tensor q = rows(q_), k = rows(k_), v = rows(v_), slopes = slopes_.value_or(Tensor()), documents = documents_.value_or(Tensor()), prefix = prefix_.value_or(Tensor());
+        Tensor lse, rest;
+        Tensor out = run(q, k, v, slopes, documents, prefix, {causal, window, softcap, scale}, &lse, &rest);
+        ctx->save_for_backward({q, k, v, out, lse, rest, slopes, documents, prefix});
+        ctx->saved_data["causal"] = causal;
+        ctx->saved_data["window"] = window;
+        ctx->saved_data["softcap"] = softcap;
+        ctx->saved_data["scale"] = scale;
+        return out;
+    }
+    static variable_list backward(AutogradContext *ctx, variable_list grads) {
+        const auto saved = ctx->get_saved_variables();
+        variable_list r;
+        {
+            const at::AutoGradMode off(false);
+            const Tensor &q = saved[0], &k = saved[1], &v = saved[2], &out = saved[3], &lse = saved[4], &rest = saved[5], &slopes = saved[6], &documents = saved[7], &prefix = saved[8];
+            const c10::DeviceGuard device(grads[0].device());
+            const Tensor dout = rows(grads[0].is_neg() ? grads[0].resolve_neg() : grads[0]);
+            // (a saved-tensor hook may hand back tensors of another form)
+            const auto s = dout.sizes();
+            const auto fit = [&](const Tensor &t, at::IntArrayRef sizes) {
+                TORCH_CHECK_VALUE(plain(t) && t.device() == dout.device(), "na2d takes GPU tensors only");
+                TORCH_CHECK_VALUE(t.scalar_type() == dout.scalar_type() && t.sizes() == sizes, "not a tensor of the forward pass");
+                TORCH_CHECK_VALUE(whole_rows(t), "the elements of a row must be contiguous");
+            };
+            TORCH_CHECK_VALUE(plain(dout) && k.dim() == 4, "na2d takes GPU tensors only");
+            const std::vector<int64_t> kv{s[0], k.size(1), k.size(2), s[3]};
+            fit(q, s), fit(out, s), fit(k, kv), fit(v, kv);
+            readable(lse, dout, at::kFloat, s.slice(0, 3));
+            if (rest.defined()) {
+                fit(rest, s);
+                TORCH_CHECK_VALUE(rest.strides() == out.strides(), "rest has out's strides");
+            }
+            TORCH_CHECK_VALUE(constant(slopes, dout, at::kFloat, {s[1]}) && constant(documents, dout, at::kInt, {s[0], kv[2]}) && constant(prefix, dout, at::kBool, {s[0], kv[2]}),
+                              "not a tensor of the forward pass");
+            const Tensor dq = rows_like(q), dk = rows_like(k), dv = rows_like(v);
+            auto p = valid(seq_of(q, k, v, out, {ctx->saved_data["causal"].toInt(), ctx->saved_data["window"].toInt(), ctx->saved_data["softcap"].toDouble(), ctx->saved_data["scale"].toDouble()}));
+            p.dout = strides(dout), p.dq = strides(dq), p.dk = strides(dk), p.dv = strides(dv);
+            const Tensor ws = scratch(seq_attention_workspace_bytes(&p, documents.defined() || prefix.defined(), 1), q);
+            check(seq_attention_bwd(&p, ptr(q), ptr(k), ptr(v), (const float *)ptr(slopes), (const int32_t *)ptr(documents), (const uint8_t *)ptr(prefix), ptr(out), (const float *)ptr(lse),
+                                    ptr(rest), ptr(dout), ptr(dq), ptr(dk), ptr(dv), ptr(ws), size_of(ws), stream()));
+            r = {dq, dk, dv};
+        }
+        if (at::GradMode::is_enabled()) r = OnceOnly::apply(r[0], r[1], r[2], saved[0], saved[1], saved[2], grads[0]);
+        r.resize(10);
+        return r;
+    }
+};
+
+// The cache: k_pages, v_pages, k_scales, v_scales, then table and lengths, beside a tensor [B, heads, n, D] of the call
+struct SeqCacheArgs {
+    Tensor k, v, ks, vs, table, lengths;
+    bool fit(const Tensor &of, int64_t kv_heads) const {
+        if (k.dim() != 4 || table.dim() != 2 || k.size(1) != kv_heads || !small(k.sizes()) || !small(table.sizes())) return false;
+        const auto s = k.sizes();
+        return plain(k) && plain(v) && plain(ks) && plain(vs) && plain(table) && plain(lengths) && constant(k, of, at::kChar, {s[0], s[1], s[2], of.size(3)}) && constant(v, of, at::kChar, s) &&
+               constant(ks, of, at::kFloat, {s[0], s[1]}) && constant(vs, of, at::kFloat, {s[0], s[1]}) && constant(table, of, at::kInt, {of.size(0), table.size(1)}) &&
+               constant(lengths, of, at::kInt, {of.size(0)});
+    }
+    std::optional<seq_cache_problem> problem(const Tensor &a, const Tensor &b, int64_t heads, int64_t window, double softcap, double scale) const {
+        const auto code = dtype_code(a.scalar_type());
+        if (!code || !small(a.sizes())) return std::nullopt;
+        seq_cache_problem p{};
+        p.B = (int32_t)a.size(0), p.heads = (int32_t)heads, p.kv_heads = (int32_t)k.size(1), p.D = (int32_t)a.size(3), p.page = (int32_t)k.size(2), p.pages = (int32_t)k.size(0);
+        p.table_width = (int32_t)table.size(1), p.dtype = *code, p.n = (int32_t)a.size(2), p.window = (int32_t)window, p.softcap = (float)softcap, p.scale = (float)scale;
+        p.q = strides(a), p.out = strides(b);
+        return p;
+    }
+};
+
 // ---- module ------------------------------------------------------------------------------------------------------------
 
 struct NoGil {
@@ -356,9 +499,9 @@ bool plain_modes() {
 std::optional<Tensor> maybe(const Tensor &t) { return t.defined() ? std::optional(t) : std::nullopt; }
 
 // BODY computes `out`; anything that the plain case does not have leaves it undefined
-template <typename Body> PyObject *guarded(Body body) {
+template <typename Out = Tensor, typename Body> PyObject *guarded(Body body) {
     HANDLE_TH_ERRORS
-    Tensor out;
+    Out out;
     {
         NoGil no_gil;
         try {
@@ -366,8 +509,14 @@ template <typename Body> PyObject *guarded(Body body) {
         } catch (const Refused &) {
         }
     }
-    if (!out.defined()) Py_RETURN_NONE;
-    return THPVariable_Wrap(std::move(out));
+    if constexpr (std::is_same_v<Out, Tensor>) {
+        if (out.defined()) return THPVariable_Wrap(std::move(out));
+    } else if (!out.empty()) {
+        PyObject *t = PyTuple_New((Py_ssize_t)out.size());
+        for (size_t i = 0; t && i < out.size(); ++i) PyTuple_SET_ITEM(t, (Py_ssize_t)i, THPVariable_Wrap(std::move(out[i])));
+        return t;
+    }
+    Py_RETURN_NONE;
     END_HANDLE_TH_ERRORS
 }
 
@@ -422,9 +571,127 @@ PyObject *py_na2d_unfused(PyObject *, PyObject *const *a, Py_ssize_t n) {
     });
 }
 
+// None, or a whole number of at least 1 | None, or a positive finite number | None: `otherwise`, or a number; false: something else
+bool window_arg(PyObject *o, int64_t &x) {
+    x = 0;
+    if (o == Py_None) return true;
+    x = PyLong_Check(o) ? PyLong_AsLongLong(o) : -1;
+    if (PyErr_Occurred()) PyErr_Clear();
+    return x >= 1 && x <= (int64_t)1 << 30;
+}
+bool number_arg(PyObject *o, double &x, double otherwise) {
+    x = otherwise;
+    if (o == Py_None) return true;
+    x = PyFloat_Check(o) || PyLong_Check(o) ? PyFloat_AsDouble(o) : NAN;
+    if (PyErr_Occurred()) PyErr_Clear();
+    return std::isfinite((float)x);
+}
+bool settings_args(PyObject *window, PyObject *softcap, PyObject *scale, const Tensor &q, SeqSettings &x) {
+    return window_arg(window, x.window) && number_arg(softcap, x.softcap, 0) && (softcap == Py_None || (float)x.softcap > 0) &&
+           number_arg(scale, x.scale, q.dim() == 4 && q.size(3) > 0 ? std::pow((double)q.size(3), -0.5) : 0);
+}
+
+// (q, k, v, causal, window or None, softcap or None, slopes, documents, prefix: or None, scale or None)
+PyObject *py_seq_attention(PyObject *, PyObject *const *a, Py_ssize_t n) {
+    Tensor q, k, v, slopes, documents, prefix;
+    SeqSettings x{};
+    if (n != 10 || !plain_modes() || !tensor_arg(a[0], q) || !tensor_arg(a[1], k) || !tensor_arg(a[2], v) || !PyBool_Check(a[3]) || !tensor_arg(a[6], slopes, true) ||
+        !tensor_arg(a[7], documents, true) || !tensor_arg(a[8], prefix, true) || !settings_args(a[4], a[5], a[9], q, x))
+        Py_RETURN_NONE;
+    x.causal = a[3] == Py_True;
+    return guarded([&]() -> Tensor {
+        if (!plain(q) || q.dim() != 4 || !plain(k) || k.dim() != 4 || !small(q.sizes()) || !small(k.sizes()) || q.size(1) % k.size(1)) return Tensor();
+        const auto s = q.sizes(), t = k.sizes();
+        if (!matches(k, q, {s[0], t[1], t[2], s[3]}) || !matches(v, q, t) || !constant(slopes, q, at::kFloat, {s[1]}) || !constant(documents, q, at::kInt, {s[0], t[2]}) ||
+            !constant(prefix, q, at::kBool, {s[0], t[2]}) || (slopes.defined() && slopes.requires_grad()))
+            return Tensor();
+        const c10::DeviceGuard device(q.device());
+        if (wants_grad({&q, &k, &v}))
+            return SeqAttention::apply(q, k, v, maybe(slopes), maybe(documents), maybe(prefix), x.causal, x.window, x.softcap, x.scale);
+        const at::AutoGradMode off(false);
+        return SeqAttention::run(rows(q), rows(k), rows(v), slopes, documents, prefix, x, nullptr, nullptr);
+    });
+}
+
+bool cache_args(PyObject *const *a, SeqCacheArgs &c, int table) {
+    return tensor_arg(a[0], c.k) && tensor_arg(a[1], c.v) && tensor_arg(a[2], c.ks) && tensor_arg(a[3], c.vs) && tensor_arg(a[table], c.table) && tensor_arg(a[table + 1], c.lengths);
+}
+
+// (k_pages, v_pages, k_scales, v_scales, k, v, table, lengths, counts or None): True where it was done
+PyObject *py_seq_cache_append(PyObject *, PyObject *const *a, Py_ssize_t n) {
+    SeqCacheArgs c;
+    Tensor k, v, counts;
+    if (n != 9 || !plain_modes() || !cache_args(a, c, 6) || !tensor_arg(a[4], k) || !tensor_arg(a[5], v) || !tensor_arg(a[8], counts, true)) Py_RETURN_NONE;
+    bool done = false;
+    PyObject *r = guarded([&]() -> Tensor {
+        if (!plain(k) || k.dim() != 4 || !small(k.sizes()) || !matches(v, k, k.sizes()) || !c.fit(k, k.size(1)) || !constant(counts, k, at::kInt, {k.size(0)})) return Tensor();
+        const at::AutoGradMode off(false);
+        const c10::DeviceGuard device(k.device());
+        const Tensor kr = rows(k), vr = rows(v);
+        const auto p = c.problem(kr, vr, k.size(1), 0, 0, 1);
+        if (!p) return Tensor();
+        forward_check(seq_cache_append(&*p, ptr(kr), ptr(vr), (const int32_t *)ptr(c.table), (const int32_t *)ptr(c.lengths), (const int32_t *)ptr(counts), (int8_t *)ptr(c.k), (int8_t *)ptr(c.v),
+                                       (float *)ptr(c.ks), (float *)ptr(c.vs), stream()));
+        done = true;
+        return Tensor();
+    });
+    if (r && done) {
+        Py_DECREF(r);
+        Py_RETURN_TRUE;
+    }
+    return r;
+}
+
+// (k_pages, v_pages, k_scales, v_scales, table, lengths, first, n, dtype): (k, v)
+PyObject *py_seq_cache_gather(PyObject *, PyObject *const *a, Py_ssize_t count) {
+    SeqCacheArgs c;
+    Tensor first;
+    if (count != 9 || !plain_modes() || !cache_args(a, c, 4) || !tensor_arg(a[6], first) || !PyLong_Check(a[7]) || !THPDtype_Check(a[8])) Py_RETURN_NONE;
+    const int64_t n = PyLong_AsLongLong(a[7]);
+    if (PyErr_Occurred()) PyErr_Clear();
+    const at::ScalarType type = reinterpret_cast<THPDtype *>(a[8])->scalar_type;
+    return guarded<variable_list>([&]() -> variable_list {
+        if (n <= 0 || !fits(n) || !dtype_code(type) || !plain(c.k) || c.k.dim() != 4 || c.table.dim() != 2 || !small(c.k.sizes()) || !small(c.table.sizes())) return {};
+        const at::AutoGradMode off(false);
+        const c10::DeviceGuard device(c.k.device());
+        Tensor k = at::empty({c.table.size(0), c.k.size(1), n, c.k.size(3)}, c.k.options().dtype(type)), v = at::empty_like(k);
+        if (!c.fit(k, k.size(1)) || !first.defined() || !constant(first, k, at::kInt, {k.size(0)})) return {};
+        const auto p = c.problem(k, v, k.size(1), 0, 0, 1);
+        if (!p) return {};
+        forward_check(seq_cache_gather(&*p, (const int8_t *)ptr(c.k), (const int8_t *)ptr(c.v), (const float *)ptr(c.ks), (const float *)ptr(c.vs), (const int32_t *)ptr(c.table),
+                                       (const int32_t *)ptr(c.lengths), (const int32_t *)ptr(first), ptr(k), ptr(v), stream()));
+        return {k, v};
+    });
+}
+
+// (q, k_pages, v_pages, k_scales, v_scales, table, lengths, window or None, softcap or None, slopes or None, scale or None)
+PyObject *py_seq_cache_attention(PyObject *, PyObject *const *a, Py_ssize_t n) {
+    SeqCacheArgs c;
+    Tensor q, slopes;
+    SeqSettings x{};
+    if (n != 11 || !plain_modes() || !tensor_arg(a[0], q) || !cache_args(a + 1, c, 4) || !tensor_arg(a[9], slopes, true) || !settings_args(a[7], a[8], a[10], q, x)) Py_RETURN_NONE;
+    return guarded([&]() -> Tensor {
+        if (!plain(q) || q.dim() != 4 || !small(q.sizes()) || c.k.dim() != 4 || !c.fit(q, c.k.size(1)) || !constant(slopes, q, at::kFloat, {q.size(1)}) || (slopes.defined() && slopes.requires_grad()))
+            return Tensor();
+        const at::AutoGradMode off(false);
+        const c10::DeviceGuard device(q.device());
+        const Tensor r = rows(q), out = rows_like(r);
+        const auto p = c.problem(r, out, q.size(1), x.window, x.softcap, x.scale);
+        if (!p) return Tensor();
+        const Tensor ws = scratch(seq_cache_attention_workspace_bytes(&*p), q);
+        forward_check(seq_cache_attention(&*p, ptr(r), (const int8_t *)ptr(c.k), (const int8_t *)ptr(c.v), (const float *)ptr(c.ks), (const float *)ptr(c.vs), (const int32_t *)ptr(c.table),
+                                          (const int32_t *)ptr(c.lengths), (const float *)ptr(slopes), ptr(out), ptr(ws), size_of(ws), stream()));
+        return out;
+    });
+}
+
 PyMethodDef methods[] = {{"na2d", (PyCFunction)(void (*)(void))py_na2d, METH_FASTCALL, nullptr},
                          {"na1d", (PyCFunction)(void (*)(void))py_na1d, METH_FASTCALL, nullptr},
                          {"na2d_unfused", (PyCFunction)(void (*)(void))py_na2d_unfused, METH_FASTCALL, nullptr},
+                         {"seq_attention", (PyCFunction)(void (*)(void))py_seq_attention, METH_FASTCALL, nullptr},
+                         {"seq_cache_append", (PyCFunction)(void (*)(void))py_seq_cache_append, METH_FASTCALL, nullptr},
+                         {"seq_cache_gather", (PyCFunction)(void (*)(void))py_seq_cache_gather, METH_FASTCALL, nullptr},
+                         {"seq_cache_attention", (PyCFunction)(void (*)(void))py_seq_cache_attention, METH_FASTCALL, nullptr},
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "na2d_torch", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

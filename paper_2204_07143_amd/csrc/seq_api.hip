@@ -148,35 +148,39 @@ size_t seq_attention_workspace_bytes(const seq_problem *p, int marked, int backw
 }
 
 int seq_attention_fwd(const seq_problem *p, const void *q, const void *k, const void *v, const float *slopes, const int32_t *documents, const uint8_t *prefix,
-                      void *out, float *lse, void *workspace, size_t workspace_bytes, void *stream) {
+                      void *out, float *lse, void *rest, void *workspace, size_t workspace_bytes, void *stream) {
     if (int e = validate(p, false)) return e;
     SEQ_REQUIRE(q); SEQ_REQUIRE(k); SEQ_REQUIRE(v); SEQ_REQUIRE(out);
-    if (odd4({lse})) return NA2D_ERR_ALIGN;
+    if (odd4({lse}) || misaligned(rest)) return NA2D_ERR_ALIGN;
     if (int e = check_marks(p, slopes, documents)) return e;
-    if (out == q || out == k || out == v) return NA2D_ERR_ALIAS;
+    for (const void *i : {q, k, v})
+        if (out == i || (rest && rest == i)) return NA2D_ERR_ALIAS;
+    if (rest == out) return NA2D_ERR_ALIAS;
+    if (rest && p->dtype == NA2D_F32) return NA2D_ERR_DTYPE;
     const hipStream_t st = static_cast<hipStream_t>(stream);
     const int e = elem(p->dtype);
     Args a = args(p, slopes, documents);
-    a.q = view(q, p->q, e), a.k = view(k, p->k, e), a.v = view(v, p->v, e), a.out = view(out, p->out, e), a.lse = lse;
+    a.q = view(q, p->q, e), a.k = view(k, p->k, e), a.v = view(v, p->v, e), a.out = view(out, p->out, e), a.lse = lse, a.rest = static_cast<char *>(rest);
     if (int r = prepare(a, Space(a, p->D, documents || prefix, false), prefix, workspace, workspace_bytes, st)) return r;
     return from_hip(launch_fwd(a, p->dtype, p->D, p->softcap > 0.f, st));
 }
 
 int seq_attention_bwd(const seq_problem *p, const void *q, const void *k, const void *v, const float *slopes, const int32_t *documents, const uint8_t *prefix,
-                      const void *out, const float *lse, const void *dout, void *dq, void *dk, void *dv, void *workspace, size_t workspace_bytes, void *stream) {
+                      const void *out, const float *lse, const void *rest, const void *dout, void *dq, void *dk, void *dv, void *workspace, size_t workspace_bytes, void *stream) {
     if (int e = validate(p, true)) return e;
     SEQ_REQUIRE(q); SEQ_REQUIRE(k); SEQ_REQUIRE(v); SEQ_REQUIRE(out); SEQ_REQUIRE(dout); SEQ_REQUIRE(dq); SEQ_REQUIRE(dk); SEQ_REQUIRE(dv);
     if (!lse) return NA2D_ERR_NULL;
-    if (odd4({lse})) return NA2D_ERR_ALIGN;
+    if (odd4({lse}) || misaligned(rest)) return NA2D_ERR_ALIGN;
     if (int e = check_marks(p, slopes, documents)) return e;
+    if (rest && p->dtype == NA2D_F32) return NA2D_ERR_DTYPE;
     for (const void *o : {dq, dk, dv})
-        for (const void *i : {q, k, v, out, dout, (const void *)lse})
+        for (const void *i : {q, k, v, out, dout, rest, (const void *)lse})
             if (o == i) return NA2D_ERR_ALIAS;
     if (dq == dk || dq == dv || dk == dv) return NA2D_ERR_ALIAS;
     const hipStream_t st = static_cast<hipStream_t>(stream);
     const int e = elem(p->dtype);
     Args a = args(p, slopes, documents);
-    a.q = view(q, p->q, e), a.k = view(k, p->k, e), a.v = view(v, p->v, e), a.out = view(out, p->out, e), a.lse = const_cast<float *>(lse);
+    a.q = view(q, p->q, e), a.k = view(k, p->k, e), a.v = view(v, p->v, e), a.out = view(out, p->out, e), a.lse = const_cast<float *>(lse), a.rest = const_cast<char *>(static_cast<const char *>(rest));
     a.dout = view(dout, p->dout, e), a.dq = view(dq, p->dq, e), a.dk = view(dk, p->dk, e), a.dv = view(dv, p->dv, e);
     const Space s(a, p->D, documents || prefix, true);
     if (int r = prepare(a, s, prefix, workspace, workspace_bytes, st)) return r;

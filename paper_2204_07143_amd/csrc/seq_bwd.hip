@@ -39,11 +39,12 @@ __global__ __launch_bounds__(kThreads) void rows_kernel(const Args p) {
         const int i = tile * kTile + r, at = min(i, p.Lq - 1);
         const float lse = p.lse[(int64_t)plane * p.Lq + at];
         const bool live = i < p.Lq && lse != -INFINITY;
-        const vec x = *reinterpret_cast<const vec *>(o + (int64_t)at * p.out.row + c * 16), y = *reinterpret_cast<const vec *>(d + (int64_t)at * p.dout.row + c * 16);
+        const char *xp = o + (int64_t)at * p.out.row + c * 16;
+        const vec x = *reinterpret_cast<const vec *>(xp), rest = p.rest ? *reinterpret_cast<const vec *>(xp + (p.rest - p.out.at)) : vec{}, y = *reinterpret_cast<const vec *>(d + (int64_t)at * p.dout.row + c * 16);
         float delta = 0.f;
 #pragma unroll
         for (int e = 0; e < E; ++e) {
-            delta = __builtin_fmaf((float)x[e], (float)y[e], delta);
+            delta = __builtin_fmaf((float)x[e] + (float)rest[e], (float)y[e], delta);
             if (kScaled<T> && live) most = fmaxf(most, fabsf((float)y[e]));
         }
 #pragma unroll

@@ -35,6 +35,7 @@ struct View {   // one tensor: byte strides of batch and head, bytes from row to
 
 struct Args {
     View q, k, v, out, dout, dq, dk, dv;
+    char *rest;            // strides of out
     float *lse;
     const float *slopes;
     const int *documents;
@@ -150,7 +151,8 @@ template <typename T, int D> struct Tile {
         for (int s = 0; s < STEPS; ++s) f[s] = *reinterpret_cast<const u32x4 *>(plane + (int64_t)row * pitch + (4 * s + (lane >> 4)) * 16);
     }
     // Sums with channels as rows, [DB] blocks, column `row` of a tensor: four channels of each block.
-    __device__ static __forceinline__ void store_row(const f32x4 *acc, float by, char *plane, int pitch, int row, int lane) {
+    // rest: where what the rounding took goes, as an offset from plane; 0: nowhere
+    __device__ static __forceinline__ void store_row(const f32x4 *acc, float by, char *plane, int pitch, int row, int lane, int64_t rest = 0) {
 #pragma unroll
         for (int db = 0; db < DB; ++db) {
             char *to = plane + (int64_t)row * pitch + (16 * db + 4 * (lane >> 4)) * (int)sizeof(T);
@@ -159,7 +161,9 @@ template <typename T, int D> struct Tile {
                 *reinterpret_cast<f32x4 *>(to) = x;
             } else {
                 typedef T t4 __attribute__((ext_vector_type(4)));
-                *reinterpret_cast<t4 *>(to) = __builtin_convertvector(x, t4);
+                const t4 y = __builtin_convertvector(x, t4);
+                *reinterpret_cast<t4 *>(to) = y;
+                if (rest) *reinterpret_cast<t4 *>(to + rest) = __builtin_convertvector(x - __builtin_convertvector(y, f32x4), t4);
             }
         }
     }

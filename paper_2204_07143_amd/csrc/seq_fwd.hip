@@ -195,7 +195,7 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) void fwd_kernel(c
         const int i = qw + 16 * n + j;
         const float total = column_sum(sum[n]);
         if (i < p.Lq) {
-            L::store_row(out[n], total == 0.f ? 0.f : 1.f / total, const_cast<char *>(p.out.at) + b * p.out.b + h * p.out.h, p.out.row, i, lane);
+            L::store_row(out[n], total == 0.f ? 0.f : 1.f / total, const_cast<char *>(p.out.at) + b * p.out.b + h * p.out.h, p.out.row, i, lane, p.rest ? p.rest - p.out.at : 0);
             if (p.lse && g == 0) p.lse[((int64_t)b * p.heads + h) * p.Lq + i] = total == 0.f ? -INFINITY : (ref[n] + __builtin_amdgcn_logf(total)) * kLn2;
         }
     }

@@ -6,7 +6,7 @@ between them left to the framework (arXiv 2204.07143, Appendix A, "Implementatio
 through the fused forward and the fused backward, which keep the attention tensor out of memory.
 
 Only argument marshalling and buffer allocation happen here: every gradient comes from the
-library's kernels.  ``na2d``, ``na1d`` and ``na2d_unfused`` do it in native code (``na2d_torch.so``, from
+library's kernels.  ``na2d``, ``na1d``, ``na2d_unfused`` and the attention over sequences (``seq_*``) do it in native code (``na2d_torch.so``, from
 ``csrc/host/torch_ops.cpp``): a call on small tensors takes longer in the interpreter than on the GPU.  The functions below
 serve ``na2d_qk_rpb``, ``na2d_av`` and ``na2d_softmax``, and whatever the native code hands back: invalid arguments (the
 binding's errors), functorch transforms, forward-mode differentiation, tracing, tensors that are not plain ones.  Tensors are ``[B, heads, H, W, D]`` (q, k, v, out), ``[B, heads, H, W, k*k]``
@@ -282,14 +282,15 @@ class _SeqAttention(torch.autograd.Function):
         ctx.settings, ctx.empty = settings, 0 in q.shape or 0 in k.shape
         train = any(ctx.needs_input_grad)
         lse = torch.empty(q.shape[:3], dtype=torch.float32, device=q.device) if train else None
+        rest = torch.empty_like(out) if train and q.element_size() == 2 else None
         if ctx.empty:
             out.zero_()
         else:
             marked = documents is not None or prefix is not None
             ws = _scratch(na.seq_attention_workspace_bytes(na.seq_problem(q, k, v=v, out=out, **settings), True), q) if marked else None
-            na.seq_attention_fwd(q, k, v, slopes, documents, prefix, out, lse, ws, **settings)
+            na.seq_attention_fwd(q, k, v, slopes, documents, prefix, out, lse, rest, ws, **settings)
         if train:
-            ctx.save_for_backward(q, k, v, out, lse, slopes, documents, prefix)
+            ctx.save_for_backward(q, k, v, out, lse, rest, slopes, documents, prefix)
         return out
 
     @staticmethod
@@ -303,14 +304,14 @@ class _SeqAttention(torch.autograd.Function):
 
     @staticmethod
     def gradients(ctx, dout):
-        q, k, v, out, lse, slopes, documents, prefix = ctx.saved_tensors
+        q, k, v, out, lse, rest, slopes, documents, prefix = ctx.saved_tensors
         dq, dk, dv = _like(q), _like(k), _like(v)
         if ctx.empty:
             return dq.zero_(), dk.zero_(), dv.zero_()
         dout = _rows(dout)
         p = na.seq_problem(q, k, v=v, out=out, dout=dout, dq=dq, dk=dk, dv=dv, **ctx.settings)
         ws = _scratch(na.seq_attention_workspace_bytes(p, documents is not None or prefix is not None, True), q)
-        na.seq_attention_bwd(q, k, v, slopes, documents, prefix, out, lse, dout, dq, dk, dv, ws, **ctx.settings)
+        na.seq_attention_bwd(q, k, v, slopes, documents, prefix, out, lse, rest, dout, dq, dk, dv, ws, **ctx.settings)
         return dq, dk, dv
 
 
@@ -344,6 +345,9 @@ def seq_attention(q, k, v, *, causal: bool = False, window: int | None = None, s
     less ``slopes[head] * |distance|`` (fp32 [heads]).  ``scale`` is D ** -0.5 unless given.  D is 32, 64 or 128; f32, f16, bf16.  The
     tensors may be strided views ([B, L, heads, D] transposed); others than of whole 16-byte rows are copied.
     """
+    out = _native().seq_attention(q, k, v, causal, window, softcap, slopes, documents, prefix, scale)
+    if out is not None:
+        return out
     _heads_of(q, k, v)
     settings = dict(causal=bool(causal), **_settings(q, window, softcap, scale, slopes))
     return _SeqAttention.apply(q, k, v, slopes, documents, prefix, settings)
@@ -367,6 +371,8 @@ def seq_cache_append(cache: SeqCache, k, v, table, lengths, counts=None) -> None
     """Puts ``k``, ``v`` [B, kv_heads, n, D] behind the ``lengths`` (int32 [B]) tokens of each sequence, the first ``counts[b]`` of the n where ``counts``
     (int32 [B]) is given.  A page's scale grows with its largest value; what it held is then rounded again.  ``lengths`` stays as it is.  No page may be
     appended to by two sequences of one call; a page number that is none is passed over."""
+    if _native().seq_cache_append(*cache, k, v, table, lengths, counts):
+        return
     if k.dim() != 4 or v.dim() != 4:
         raise ValueError("expected [B, heads, L, D] tensors")
     if 0 not in k.shape:
@@ -376,6 +382,9 @@ def seq_cache_append(cache: SeqCache, k, v, table, lengths, counts=None) -> None
 
 def seq_cache_gather(cache: SeqCache, table, lengths, first, n: int, dtype=torch.bfloat16):
     """The keys and values, [B, kv_heads, n, D] each, that the cache holds at positions ``first[b]`` (int32 [B]) .. + n - 1; 0 where a sequence has no token."""
+    out = _native().seq_cache_gather(*cache, table, lengths, first, n, dtype)
+    if out is not None:
+        return out
     B, (_, kv_heads, _, D) = table.shape[0], cache.k_pages.shape
     k, v = (torch.empty((B, kv_heads, n, D), dtype=dtype, device=cache.k_pages.device) for _ in range(2))
     return (k, v) if k.numel() == 0 else na.seq_cache_gather(*cache, table, lengths, first, k, v)
@@ -384,6 +393,9 @@ def seq_cache_gather(cache: SeqCache, table, lengths, first, n: int, dtype=torch
 def seq_cache_attention(q, cache: SeqCache, table, lengths, *, window: int | None = None, softcap: float | None = None, slopes=None, scale: float | None = None):
     """Attention of each sequence's last n tokens, ``q`` [B, heads, n, D] in f16 or bf16, over its cache, which holds their keys and values already:
     ``lengths`` counts them.  In causal order; scores as ``seq_attention`` has them.  Not differentiable."""
+    out = _native().seq_cache_attention(q, *cache, table, lengths, window, softcap, slopes, scale)
+    if out is not None:
+        return out
     if q.dim() != 4:
         raise ValueError("expected [B, heads, L, D] tensors")
     settings = _settings(q, window, softcap, scale, slopes)

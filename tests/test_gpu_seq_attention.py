@@ -256,3 +256,37 @@ def test_replayed_graphs(dtype, D):
         torch.cuda.synchronize()
         for _, outs in graphs:
             assert all(torch.equal(a, b) for a, b in zip(outs, eager))
+
+
+@TYPE
+def test_native_and_interpreted_host_sides(dtype):
+    """The same bits, gradients and refusals; kept for a second pass; saved-tensor hooks; what only the interpreted side takes."""
+    g = np.random.default_rng(16)
+    q, k, v = (normal(g, (2, 77, h, 64), dtype).transpose(1, 2).requires_grad_() for h in (4, 2, 2))
+    dout = normal(g, (2, 4, 77, 64), dtype)
+    documents, prefix = _marks(g, 2, 77, 2, True)
+    slopes = torch.rand(4, device="cuda")
+    settings = dict(causal=True, window=9, softcap=3.0, scale=0.2)
+    native = F.seq_attention(q, k, v, slopes=slopes, documents=documents, prefix=prefix, **settings)
+    plain = F._SeqAttention.apply(q, k, v, slopes, documents, prefix, settings)
+    assert type(native.grad_fn).__name__ != type(plain.grad_fn).__name__ and torch.equal(native, plain) and native.stride() == plain.stride()
+    for _ in range(2):
+        for a, b in zip(torch.autograd.grad(native, (q, k, v), dout, retain_graph=True), torch.autograd.grad(plain, (q, k, v), dout, retain_graph=True)):
+            assert torch.equal(a, b) and a.stride() == b.stride()
+    with torch.no_grad():
+        assert torch.equal(F.seq_attention(q, k, v, slopes=slopes, documents=documents, prefix=prefix, **settings), plain)
+    with torch.autograd.graph.saved_tensors_hooks(lambda t: t.cpu(), lambda t: t.cuda()):
+        hooked = F.seq_attention(q, k, v, slopes=slopes, documents=documents, prefix=prefix, **settings)
+    assert all(torch.equal(a, b) for a, b in zip(torch.autograd.grad(hooked, (q, k, v), dout), torch.autograd.grad(plain, (q, k, v), dout)))
+    for bad in (dict(slopes=slopes.double()), dict(slopes=slopes[:3]), dict(documents=documents.long()), dict(documents=documents[:, 1:]), dict(prefix=prefix.int()),
+                dict(prefix=prefix.cpu()), dict(documents=documents.t().contiguous().t())):
+        with pytest.raises(ValueError):
+            F.seq_attention(q, k, v, **bad)
+    with pytest.raises(ValueError):
+        F.seq_attention(q, k.float() if dtype != "f32" else k.half(), v)
+    with pytest.raises(na.Na2dError) as e:
+        F.seq_attention(q[..., :48], k[..., :48], v[..., :48])
+    assert e.value.status == -5
+    with pytest.raises(na.Na2dError) as e:
+        F.seq_attention(q, k[:, :, 1:], v[:, :, 1:], documents=documents[:, 1:].contiguous())
+    assert e.value.status == -6

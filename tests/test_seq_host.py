@@ -45,17 +45,18 @@ def test_backward_strides_count_only_there():
 def test_attention_arguments():
     lib, p = na.load(), P()
     at = lambda n: ctypes.c_void_p(4096 + 16 * n)
-    fwd = lambda p, q=at(1), k=at(2), v=at(3), slopes=None, docs=None, prefix=None, out=at(4), lse=None, ws=None, n=0: lib.seq_attention_fwd(
-        ctypes.byref(p), q, k, v, slopes, docs, prefix, out, lse, ws, n, None)
-    assert lib.seq_attention_fwd(None, *[at(1)] * 9, 0, None) == -1
+    fwd = lambda p, q=at(1), k=at(2), v=at(3), slopes=None, docs=None, prefix=None, out=at(4), lse=None, rest=None, ws=None, n=0: lib.seq_attention_fwd(
+        ctypes.byref(p), q, k, v, slopes, docs, prefix, out, lse, rest, ws, n, None)
+    assert lib.seq_attention_fwd(None, *[at(1)] * 10, 0, None) == -1
     assert fwd(p, q=None) == -1 and fwd(p, out=None) == -1
     assert fwd(p, v=ctypes.c_void_p(4100)) == -7 and fwd(p, slopes=ctypes.c_void_p(4098)) == -7 and fwd(p, lse=ctypes.c_void_p(4098)) == -7
     assert fwd(p, out=at(2)) == -10
     assert fwd(p, docs=at(9)) == -8 and fwd(p, prefix=at(9), ws=at(10), n=16) == -8 and fwd(p, docs=at(9), ws=ctypes.c_void_p(4100), n=1 << 20) == -8
     assert fwd(P(Lq=101), docs=at(9), ws=at(10), n=1 << 20) == -6   # documents need a position for every query
-    bwd = lambda p, **x: lib.seq_attention_bwd(ctypes.byref(p), *({n: at(i + 1) for i, n in enumerate(("q", "k", "v", "slopes", "docs", "prefix", "out", "lse", "dout", "dq", "dk", "dv"))}
+    bwd = lambda p, **x: lib.seq_attention_bwd(ctypes.byref(p), *({n: at(i + 1) for i, n in enumerate(("q", "k", "v", "slopes", "docs", "prefix", "out", "lse", "rest", "dout", "dq", "dk", "dv"))}
                                                                    | {"slopes": None, "docs": None, "prefix": None} | x).values(), None, 0, None)
-    assert bwd(p) == -8 and bwd(p, dout=None) == -1 and bwd(p, lse=None) == -1 and bwd(p, dq=at(1)) == -10 and bwd(p, dk=at(12)) == -10
+    assert fwd(p, rest=at(4)) == -10 and fwd(p, rest=at(1)) == -10 and fwd(P(dtype=0), rest=at(5)) == -2
+    assert bwd(p) == -8 and bwd(p, rest=at(11)) == -10 and bwd(p, dout=None) == -1 and bwd(p, lse=None) == -1 and bwd(p, dq=at(1)) == -10 and bwd(p, dk=at(13)) == -10
 
 
 def C(B=2, heads=4, kv=2, D=64, page=16, pages=8, width=4, dtype=1, n=1, window=0, scale=0.1, cap=0.0, rows=None):
