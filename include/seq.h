@@ -44,7 +44,7 @@ typedef struct {
     int32_t causal; /* 0 or 1 */
     int32_t window; /* 0: none */
     float scale;    /* finite */
-    float softcap;  /* 0: none; else finite and positive */
+    float softcap;  /* 0: none; else finite, from 2^-20 on, and in the 16-bit types at most 4096 */
     seq_strides q, k, v, out;      /* forward and backward */
     seq_strides dout, dq, dk, dv;  /* backward */
 } seq_problem;

@@ -29,6 +29,8 @@ int common(int B, int heads, int kv, int D, int dtype, float scale, float cap, i
     if (dtype != NA2D_F32 && dtype != NA2D_F16 && dtype != NA2D_BF16) return NA2D_ERR_DTYPE;
     if (B <= 0 || heads <= 0 || kv <= 0 || heads % kv) return NA2D_ERR_SHAPE;
     if (D != 32 && D != 64 && D != 128) return NA2D_ERR_HEAD_DIM;
+    // (a cap's scores are off by 2^-24 of it in 16 bit, see seq_common.hpp: up to 2^12 that is below what fp16 weights are rounded by)
+    if (cap != 0.f && (cap < 0x1p-20f || (dtype != NA2D_F32 && cap > 4096.f))) return NA2D_ERR_SHAPE;
     if (!std::isfinite(scale) || !std::isfinite(cap) || cap < 0.f || window < 0 || window > kFar) return NA2D_ERR_SHAPE;
     return NA2D_OK;
 }
@@ -62,8 +64,16 @@ Args args(const seq_problem *p, const float *slopes, const int32_t *documents) {
     a.causal = p->causal, a.window = p->window ? p->window : kFar;
     a.dlo = p->causal ? 0 : 1 - a.window;
     a.scale = p->scale;
-    a.c = p->softcap > 0.f ? (float)(2.0 * 1.4426950408889634 * p->scale / p->softcap) : (float)(1.4426950408889634 * p->scale);
-    a.cap = (float)(2.0 * 1.4426950408889634 * p->softcap);
+    constexpr double log2e = 1.4426950408889634;
+    if (p->softcap > 0.f) {
+        const bool sigmoid = p->dtype != NA2D_F32;
+        a.c = (float)(2.0 * log2e * p->scale / p->softcap);
+        a.m = (float)((sigmoid ? -2.0 : 1.0) * log2e * p->softcap), a.from = sigmoid ? (float)(log2e * p->softcap) : 0.f;
+        a.masked = sigmoid ? 1e18f : -1e18f;   // its square is finite, and its weight 0 for every cap from 2^-20 on
+    } else {
+        a.m = p->scale == 0.f ? 1e-37f : (float)(log2e * p->scale);   // (0 times what is masked would be no number)
+        a.masked = a.m > 0.f ? -INFINITY : INFINITY;
+    }
     a.splits = kv_splits(a, p->dtype, p->D);
     return a;
 }
@@ -187,7 +197,7 @@ int seq_attention_bwd(const seq_problem *p, const void *q, const void *k, const 
     a.rows = reinterpret_cast<float2 *>(static_cast<char *>(workspace) + s.rows);
     a.powers = reinterpret_cast<int *>(static_cast<char *>(workspace) + s.powers);
     a.parts = reinterpret_cast<float *>(static_cast<char *>(workspace) + s.parts);
-    if (int r = from_hip(launch_rows(a, p->dtype, p->D, st))) return r;
+    if (int r = from_hip(launch_rows(a, p->dtype, p->D, p->softcap > 0.f, st))) return r;
     if (int r = from_hip(launch_bwd_q(a, p->dtype, p->D, p->softcap > 0.f, st))) return r;
     return from_hip(launch_bwd_kv(a, p->dtype, p->D, p->softcap > 0.f, st));
 }

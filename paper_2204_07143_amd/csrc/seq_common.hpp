@@ -14,6 +14,8 @@ namespace seq {
 
 using namespace na2d;
 
+typedef int i32x4 __attribute__((ext_vector_type(4)));
+
 constexpr int kTile = 64;        // tokens staged at a time
 constexpr int kWaves = 4, kThreads = kWaves * kWave;
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
@@ -50,7 +52,10 @@ struct Args {
     int causal, window;    // window: kFar where there is none
     int prefix;            // marks hold prefix bits
     int dlo;               // smallest distance that the order and the window allow; the largest is window - 1
-    float scale, c, cap;   // c: scale log2(e), or with a cap 2 scale log2(e) / cap; cap: 2 cap log2(e)
+    float scale;
+    float c;               // capped: 2 scale log2(e) / cap
+    float m, from;         // a score in base 2 is m y + from (see Score)
+    float masked;          // the y of what is masked
 };
 
 // ---- products --------------------------------------------------------------------------------------------------------------
@@ -150,6 +155,15 @@ template <typename T, int D> struct Tile {
 #pragma unroll
         for (int s = 0; s < STEPS; ++s) f[s] = *reinterpret_cast<const u32x4 *>(plane + (int64_t)row * pitch + (4 * s + (lane >> 4)) * 16);
     }
+    __device__ static __forceinline__ void negate(u32x4 (&f)[STEPS]) {
+#pragma unroll
+        for (int s = 0; s < STEPS; ++s) f[s] ^= sizeof(T) == 2 ? 0x80008000u : 0x80000000u;
+    }
+    // zeros in place of a token that is not live
+    __device__ static __forceinline__ void clear(u32x4 (&f)[STEPS], bool live) {
+#pragma unroll
+        for (int s = 0; s < STEPS; ++s) f[s] &= live ? ~0u : 0u;
+    }
     // Sums with channels as rows, [DB] blocks, column `row` of a tensor: four channels of each block.
     // rest: where what the rounding took goes, as an offset from plane; 0: nowhere
     __device__ static __forceinline__ void store_row(const f32x4 *acc, float by, char *plane, int pitch, int row, int lane, int64_t rest = 0) {
@@ -174,7 +188,19 @@ template <typename T, int D> struct Tile {
 // Queries at positions qa .. qb against keys ka .. kb: any pair, or every pair, that order and window allow.
 __device__ __forceinline__ bool near_any(const Args &p, int qa, int qb, int ka, int kb) { return qb - ka >= p.dlo && qa - kb < p.window; }
 __device__ __forceinline__ bool near_all(const Args &p, int qa, int qb, int ka, int kb) { return qa - kb >= p.dlo && qb - ka < p.window; }
-__device__ __forceinline__ bool near_one(const Args &p, int distance) { return (unsigned)(distance - p.dlo) < (unsigned)(p.window - p.dlo); }
+
+// Bits lo .. hi - 1 of 64, whatever lo and hi.
+__device__ __forceinline__ uint64_t bits_between(int lo, int hi) {
+    lo = max(0, min(lo, 64)), hi = max(0, min(hi, 64));
+    const uint64_t from = lo < 64 ? ~0ull << lo : 0ull, to = hi < 64 ? ~(~0ull << hi) : ~0ull;
+    return from & to;
+}
+// A column's 64 rows of a tile as a mask: this lane's rows 16 rb + 4 g + r are bits 16 rb + r of mask >> 4 g.  Two instructions an element.
+__device__ __forceinline__ float keep(float y, uint64_t lane_mask, int bit, float masked) {
+    const int word = bit < 32 ? (int)(uint32_t)lane_mask : (int)(uint32_t)(lane_mask >> 32);
+    const uint32_t on = (uint32_t)(word << (31 - bit % 32) >> 31);
+    return __uint_as_float((__float_as_uint(y) & on) | (__float_as_uint(masked) & ~on));
+}
 
 // A range of documents; every token of it being live as well.
 struct Docs {
@@ -232,38 +258,39 @@ __device__ __forceinline__ int block_in_order() {
 }
 
 // ---- scores ----------------------------------------------------------------------------------------------------------------
-
-// A product as a score in base 2, before bias and mask.  Capped: with z = scale <q, k> / cap and r = 1 / (1 + e^2z), tanh z = 1 - 2 r, so the score is
-// cap log2(e) - (2 cap log2(e)) r, and its derivative by the product 1 - tanh^2 = 4 r (1 - r).  That form is off by 2^-24 of the cap, below what 16-bit
-// products carry; fp32 takes the library's tanh.  `slope` is what the derivative is computed from.
-template <typename T, bool CAP> __device__ __forceinline__ float score(const Args &p, float s, float &slope) {
-    if constexpr (!CAP) {
-        return s * p.c;
-    } else if constexpr (sizeof(T) == 2) {
-        const float r = __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(s * p.c));   // p.c = 2 log2(e) scale / cap
-        slope = r;
-        return __builtin_fmaf(-p.cap, r, 0.5f * p.cap);                                 // p.cap = 2 cap log2(e)
-    } else {
-        const float t = tanhf(s * (0.5f * kLn2 * p.c));
-        slope = t;
-        return 0.5f * p.cap * t;
+//
+// A score in base 2 is m y + from (args.m, args.from), less slope |distance|:
+//   no cap   y = <q, k>, m = scale log2(e)
+//   capped   with z = scale <q, k> / cap and y = 1 / (1 + e^2z): tanh z = 1 - 2 y, so m = -2 cap log2(e), from = cap log2(e), and the score's derivative by
+//            the product, 1 - tanh^2, is 4 y (1 - y).  That form is off by 2^-24 of the cap, below what 16-bit products carry for every cap they are given;
+//   fp32     takes the library's tanh for y, m = cap log2(e).
+// What is masked has a y that gives weights of 0 and, where 1 - tanh^2 is formed from it, something finite.
+template <typename T, bool CAP> struct Score {
+    static constexpr bool kSigmoid = CAP && sizeof(T) == 2;
+    __device__ static __forceinline__ float of(const Args &p, float s) {
+        if constexpr (!CAP) return s;
+        else if constexpr (kSigmoid) return __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(s * p.c));
+        else return tanhf(s * (0.5f * kLn2 * p.c));
     }
-}
-template <typename T, bool CAP> __device__ __forceinline__ float through_cap(float ds, float slope) {
-    if constexpr (!CAP) return ds;
-    else if constexpr (sizeof(T) == 2) return ds * (4.f * slope * (1.f - slope));
-    else return ds * __builtin_fmaf(-slope, slope, 1.f);
-}
+    // 1 - tanh^2, over 4 in 16 bit: the weights beside it are formed times 2^kQuad
+    static constexpr float kQuad = kSigmoid ? 2.f : 0.f;
+    __device__ static __forceinline__ float through(float ds, float y) {
+        if constexpr (!CAP) return ds;
+        else if constexpr (kSigmoid) return ds * __builtin_fmaf(-y, y, y);
+        else return ds * __builtin_fmaf(-y, y, 1.f);
+    }
+};
 
 // ---- host ------------------------------------------------------------------------------------------------------------------
 
 hipError_t launch_marks(const Args &a, const uint8_t *prefix, Marks *marks, char *zeros, hipStream_t st);
 hipError_t launch_fwd(const Args &a, int dtype, int D, bool capped, hipStream_t st);
-hipError_t launch_rows(const Args &a, int dtype, int D, hipStream_t st);
+hipError_t launch_rows(const Args &a, int dtype, int D, bool capped, hipStream_t st);
 hipError_t launch_bwd_q(const Args &a, int dtype, int D, bool capped, hipStream_t st);
 hipError_t launch_bwd_kv(const Args &a, int dtype, int D, bool capped, hipStream_t st);
 int kv_splits(const Args &a, int dtype, int D);
 
+// L<T, D, capped>::go(...) of a type and head dim
 template <template <typename, int, bool> class L, typename... A> hipError_t dispatch(int dtype, int D, bool capped, A &&...a) {
 #define SEQ_D(T, N) (capped ? L<T, N, true>::go(a...) : L<T, N, false>::go(a...))
 #define SEQ_T(T) (D == 32 ? SEQ_D(T, 32) : D == 64 ? SEQ_D(T, 64) : SEQ_D(T, 128))

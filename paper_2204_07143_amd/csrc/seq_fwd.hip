@@ -17,12 +17,12 @@ constexpr float kSlack = 8.f;   // weights reach 2^8: fp16 holds them with all d
 
 template <typename T, int D> constexpr int kQB = sizeof(T) == 2 ? 2 : 1;
 
-template <typename T, int D, bool CAP>
+template <typename T, int D, bool CAP, bool SLOPES>
 __global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) void fwd_kernel(const Args p) {
     using L = Tile<T, D>;
     constexpr int QB = kQB<T, D>, RB = kRowBlocks<T>, NB = kTile / 16;
     extern __shared__ __align__(16) char lds[];
-    __shared__ int ids[2][kTile];
+    __shared__ __align__(16) int ids[2][kTile];
     __shared__ int range[3][kWaves];
     const int tid = threadIdx.x, lane = tid % kWave, wave = uniform(tid / kWave), j = lane & 15, g = lane >> 4;
     const int tiles = (p.Lq + 16 * QB * kWaves - 1) / (16 * QB * kWaves);
@@ -41,6 +41,7 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) void fwd_kernel(c
     for (int n = 0; n < QB; ++n) {
         const int i = min(qw + 16 * n + j, p.Lq - 1);
         L::load_row(q[n], qp, p.q.row, i, lane);
+        if (!CAP && p.m < 0.f) L::negate(q[n]);
         pos[n] = i + p.off;
         mine[n] = p.documents ? p.documents[(int64_t)b * p.Lk + pos[n]] : 0;
     }
@@ -78,7 +79,9 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) void fwd_kernel(c
 
     const typename L::RowReader rows(lane);
     const typename L::ColumnReader columns(lane);
-    const float slope = p.slopes ? p.slopes[h] * kLog2e : 0.f;
+    const float slope = SLOPES ? p.slopes[h] * kLog2e : 0.f, m = CAP ? p.m : fabsf(p.m), from = p.from;
+    constexpr bool kLeast = Score<T, CAP>::kSigmoid && !SLOPES;   // the largest score is that of the least y
+    constexpr float masked = kLeast ? INFINITY : -INFINITY;
     f32x4 out[QB][L::DB];
     float ref[QB], sum[QB];
 #pragma unroll
@@ -121,44 +124,50 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) void fwd_kernel(c
 #pragma unroll
                     for (int n = 0; n < QB; ++n) s[n][rb] = mma<T>(a, q[n][st], s[n][rb]);
                 }
-#pragma unroll
-            for (int n = 0; n < QB; ++n) {
-#pragma unroll
-                for (int rb = 0; rb < NB; ++rb)
-#pragma unroll
-                    for (int r = 0; r < 4; ++r) {
-                        float unused;
-                        s[n][rb][r] = score<T, CAP>(p, s[n][rb][r], unused);
-                    }
-                if (p.slopes) {
-                    const float from = (float)(pos[n] - k0 - 4 * g);
-#pragma unroll
-                    for (int rb = 0; rb < NB; ++rb)
-#pragma unroll
-                        for (int r = 0; r < 4; ++r) s[n][rb][r] = __builtin_fmaf(fabsf(from - (float)(16 * rb + r)), -slope, s[n][rb][r]);
-                }
-            }
+            uint64_t seen[QB];
+            bool mixed = false;   // the tile's documents are not one
             if (!all) {
-                const uint64_t prefix = p.prefix ? marks[t].prefix : 0;
+                Marks m{0, 0, 0, 0};
+                if (marks) m = marks[t];
+                mixed = m.dmin != m.dmax;
 #pragma unroll
-                for (int rb = 0; rb < NB; ++rb)
-#pragma unroll
-                    for (int r = 0; r < 4; ++r) {
-                        const int at = 16 * rb + 4 * g + r, key = k0 + at, doc = p.documents ? ids[buf][at] : 0;
-                        const bool there = key < p.Lk && doc >= 0, always = prefix >> at & 1;
-#pragma unroll
-                        for (int n = 0; n < QB; ++n)
-                            if (!(there && doc == mine[n] && (always || near_one(p, pos[n] - key)))) s[n][rb][r] = -INFINITY;
-                    }
+                for (int n = 0; n < QB; ++n) {
+                    seen[n] = bits_between(pos[n] - p.window + 1 - k0, min(pos[n] - p.dlo + 1, p.Lk) - k0) | m.prefix;
+                    if (p.documents) seen[n] = mine[n] >= 0 && (mixed || mine[n] == m.dmin) ? seen[n] & m.live : 0;
+                    seen[n] >>= 4 * g;
+                }
             }
             u32x4 w[QB][NB / RB];
 #pragma unroll
             for (int n = 0; n < QB; ++n) {
+                const float near = SLOPES ? (float)(pos[n] - k0 - 4 * g) : 0.f;
+#pragma unroll
+                for (int rb = 0; rb < NB; ++rb)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) {
+                        s[n][rb][r] = Score<T, CAP>::of(p, s[n][rb][r]);
+                        if constexpr (SLOPES) s[n][rb][r] = __builtin_fmaf(fabsf(near - (float)(16 * rb + r)), -slope, __builtin_fmaf(m, s[n][rb][r], from));
+                    }
+                if (!all) {
+#pragma unroll
+                    for (int rb = 0; rb < NB; ++rb)
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) s[n][rb][r] = keep(s[n][rb][r], seen[n], 16 * rb + r, masked);
+                    if (mixed) {
+#pragma unroll
+                        for (int rb = 0; rb < NB; ++rb) {
+                            const i32x4 doc = *reinterpret_cast<const i32x4 *>(&ids[buf][16 * rb + 4 * g]);
+#pragma unroll
+                            for (int r = 0; r < 4; ++r) s[n][rb][r] = doc[r] == mine[n] ? s[n][rb][r] : masked;
+                        }
+                    }
+                }
                 float most = s[n][0][0];
 #pragma unroll
                 for (int rb = 0; rb < NB; ++rb)
 #pragma unroll
-                    for (int r = 0; r < 4; ++r) most = fmaxf(most, s[n][rb][r]);
+                    for (int r = 0; r < 4; ++r) most = kLeast ? fminf(most, s[n][rb][r]) : fmaxf(most, s[n][rb][r]);
+                if constexpr (!SLOPES) most = __builtin_fmaf(m, most, from);
                 most = column_max(most);
                 const float now = most > ref[n] + kSlack ? most : ref[n];
                 if (__any(now != ref[n])) {
@@ -172,7 +181,7 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) void fwd_kernel(c
                 for (int rb = 0; rb < NB; ++rb)
 #pragma unroll
                     for (int r = 0; r < 4; ++r) {
-                        s[n][rb][r] = __builtin_amdgcn_exp2f(s[n][rb][r] - ref[n]);
+                        s[n][rb][r] = __builtin_amdgcn_exp2f(SLOPES ? s[n][rb][r] - ref[n] : __builtin_fmaf(m, s[n][rb][r], from - ref[n]));
                         sum[n] += s[n][rb][r];
                     }
 #pragma unroll
@@ -202,15 +211,16 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) void fwd_kernel(c
 }
 
 template <typename T, int D, bool CAP> struct Fwd {
-    static hipError_t go(const Args &a, hipStream_t st) {
+    template <bool SLOPES> static hipError_t launch(const Args &a, hipStream_t st) {
         constexpr int lds = 4 * Tile<T, D>::BYTES, rows = 16 * kQB<T, D> * kWaves;
         static LdsAllowed allowed;
-        if (hipError_t e = allow_lds(fwd_kernel<T, D, CAP>, lds, allowed); e != hipSuccess) return e;
+        if (hipError_t e = allow_lds(fwd_kernel<T, D, CAP, SLOPES>, lds, allowed); e != hipSuccess) return e;
         const int64_t blocks = (int64_t)a.B * a.heads * ((a.Lq + rows - 1) / rows);
         if (!launch_holds(blocks, kThreads)) return hipErrorInvalidValue;
-        fwd_kernel<T, D, CAP><<<(unsigned)blocks, kThreads, lds, st>>>(a);
+        fwd_kernel<T, D, CAP, SLOPES><<<(unsigned)blocks, kThreads, lds, st>>>(a);
         return hipGetLastError();
     }
+    static hipError_t go(const Args &a, hipStream_t st) { return a.slopes ? launch<true>(a, st) : launch<false>(a, st); }
 };
 
 __global__ __launch_bounds__(kThreads) void marks_kernel(const int *__restrict__ documents, const uint8_t *__restrict__ prefix, int Lk, int tiles, int total, Marks *marks, uint32_t *zeros) {

@@ -28,7 +28,7 @@ def P(B=2, heads=4, kv=2, Lq=100, Lk=100, D=64, dtype=1, causal=1, window=0, sca
     (P(), 0), (P(Lq=1, Lk=1 << 24, kv=1, heads=1, B=1, D=32), 0), (P(window=5, cap=30.0), 0), (P(scale=-1.0), 0), (P(q=na.SeqStrides(0, 0, 64)), 0),
     (P(dtype=3), -2), (P(dtype=-1), -2), (P(D=16), -5), (P(D=96), -5),
     (P(B=0), -6), (P(heads=3), -6), (P(kv=0), -6), (P(Lq=0), -6), (P(Lk=-1), -6), (P(Lk=(1 << 24) + 1), -6), (P(causal=2), -6), (P(window=-1), -6), (P(window=(1 << 30) + 1), -6),
-    (P(scale=float("nan")), -6), (P(scale=float("inf")), -6), (P(cap=-1.0), -6), (P(cap=float("nan")), -6), (P(cap=float("inf")), -6),
+    (P(scale=float("nan")), -6), (P(scale=float("inf")), -6), (P(cap=-1.0), -6), (P(cap=float("nan")), -6), (P(cap=float("inf")), -6), (P(cap=5000.0), -6), (P(cap=5000.0, dtype=0), 0), (P(cap=1e-7), -6),
     (P(q=na.SeqStrides(6400, 6400, -64)), -6), (P(q=na.SeqStrides(6400, 6400, 1 << 26)), -6), (P(k=na.SeqStrides(6400, 6400, 68)), -7), (P(v=na.SeqStrides(6401, 6400, 64)), -7),
     (P(B=1 << 20, heads=1 << 12, kv=1, Lq=1 << 10), -6),
 ])
