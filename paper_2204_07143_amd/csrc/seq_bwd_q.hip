@@ -53,10 +53,10 @@ __global__ __launch_bounds__(kThreads) void rows_kernel(const Args p) {
 
 // ---- dQ --------------------------------------------------------------------------------------------------------------------
 
-template <typename T, int D, bool CAP, bool SLOPES>
+template <typename T, int D, bool CAP, bool SLOPES, int QB>
 __global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) void bwd_q_kernel(const Args p) {
     using L = Tile<T, D>;
-    constexpr int QB = kBlocks<T>, RB = kRowBlocks<T>, NB = kTile / 16;
+    constexpr int RB = kRowBlocks<T>, NB = kTile / 16;
     extern __shared__ __align__(16) char lds[];
     __shared__ __align__(16) int ids[2][kTile];
     __shared__ int range[2][kWaves];
@@ -247,16 +247,20 @@ template <typename T, int D, bool CAP> struct Rows {
     }
 };
 template <typename T, int D, bool CAP> struct BwdQ {
-    template <bool SLOPES> static hipError_t launch(const Args &a, hipStream_t st) {
-        constexpr int lds = 4 * Tile<T, D>::BYTES, rows = 16 * kBlocks<T> * kWaves;
+    template <bool SLOPES, int QB> static hipError_t launch(const Args &a, hipStream_t st) {
+        constexpr int lds = 4 * Tile<T, D>::BYTES, rows = 16 * QB * kWaves;
         static LdsAllowed allowed;
-        if (hipError_t e = allow_lds(bwd_q_kernel<T, D, CAP, SLOPES>, lds, allowed); e != hipSuccess) return e;
+        if (hipError_t e = allow_lds(bwd_q_kernel<T, D, CAP, SLOPES, QB>, lds, allowed); e != hipSuccess) return e;
         const int64_t blocks = (int64_t)a.B * a.heads * ((a.Lq + rows - 1) / rows);
         if (!launch_holds(blocks, kThreads)) return hipErrorInvalidValue;
-        bwd_q_kernel<T, D, CAP, SLOPES><<<(unsigned)blocks, kThreads, lds, st>>>(a);
+        bwd_q_kernel<T, D, CAP, SLOPES, QB><<<(unsigned)blocks, kThreads, lds, st>>>(a);
         return hipGetLastError();
     }
-    static hipError_t go(const Args &a, hipStream_t st) { return a.slopes ? launch<true>(a, st) : launch<false>(a, st); }
+    static hipError_t go(const Args &a, hipStream_t st) {
+        if constexpr (sizeof(T) == 2)
+            if (two_query_blocks(a)) return a.slopes ? launch<true, 2>(a, st) : launch<false, 2>(a, st);
+        return a.slopes ? launch<true, 1>(a, st) : launch<false, 1>(a, st);
+    }
 };
 
 }  // namespace

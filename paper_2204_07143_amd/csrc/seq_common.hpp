@@ -290,6 +290,9 @@ hipError_t launch_bwd_q(const Args &a, int dtype, int D, bool capped, hipStream_
 hipError_t launch_bwd_kv(const Args &a, int dtype, int D, bool capped, hipStream_t st);
 int kv_splits(const Args &a, int dtype, int D);
 
+// 16 bit: two blocks of 16 queries to a wave (a fragment of keys or values then serves two products) where that leaves two workgroups to each compute unit.
+inline bool two_query_blocks(const Args &a) { return (int64_t)a.B * a.heads * ((a.Lq + 127) / 128) >= 512; }
+
 // L<T, D, capped>::go(...) of a type and head dim
 template <template <typename, int, bool> class L, typename... A> hipError_t dispatch(int dtype, int D, bool capped, A &&...a) {
 #define SEQ_D(T, N) (capped ? L<T, N, true>::go(a...) : L<T, N, false>::go(a...))

@@ -15,12 +15,10 @@ namespace {
 
 constexpr float kSlack = 8.f;   // weights reach 2^8: fp16 holds them with all digits, and their sum
 
-template <typename T, int D> constexpr int kQB = sizeof(T) == 2 ? 2 : 1;
-
-template <typename T, int D, bool CAP, bool SLOPES>
+template <typename T, int D, bool CAP, bool SLOPES, int QB>
 __global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) void fwd_kernel(const Args p) {
     using L = Tile<T, D>;
-    constexpr int QB = kQB<T, D>, RB = kRowBlocks<T>, NB = kTile / 16;
+    constexpr int RB = kRowBlocks<T>, NB = kTile / 16;
     extern __shared__ __align__(16) char lds[];
     __shared__ __align__(16) int ids[2][kTile];
     __shared__ int range[3][kWaves];
@@ -211,16 +209,20 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) void fwd_kernel(c
 }
 
 template <typename T, int D, bool CAP> struct Fwd {
-    template <bool SLOPES> static hipError_t launch(const Args &a, hipStream_t st) {
-        constexpr int lds = 4 * Tile<T, D>::BYTES, rows = 16 * kQB<T, D> * kWaves;
+    template <bool SLOPES, int QB> static hipError_t launch(const Args &a, hipStream_t st) {
+        constexpr int lds = 4 * Tile<T, D>::BYTES, rows = 16 * QB * kWaves;
         static LdsAllowed allowed;
-        if (hipError_t e = allow_lds(fwd_kernel<T, D, CAP, SLOPES>, lds, allowed); e != hipSuccess) return e;
+        if (hipError_t e = allow_lds(fwd_kernel<T, D, CAP, SLOPES, QB>, lds, allowed); e != hipSuccess) return e;
         const int64_t blocks = (int64_t)a.B * a.heads * ((a.Lq + rows - 1) / rows);
         if (!launch_holds(blocks, kThreads)) return hipErrorInvalidValue;
-        fwd_kernel<T, D, CAP, SLOPES><<<(unsigned)blocks, kThreads, lds, st>>>(a);
+        fwd_kernel<T, D, CAP, SLOPES, QB><<<(unsigned)blocks, kThreads, lds, st>>>(a);
         return hipGetLastError();
     }
-    static hipError_t go(const Args &a, hipStream_t st) { return a.slopes ? launch<true>(a, st) : launch<false>(a, st); }
+    static hipError_t go(const Args &a, hipStream_t st) {
+        if constexpr (sizeof(T) == 2)
+            if (two_query_blocks(a)) return a.slopes ? launch<true, 2>(a, st) : launch<false, 2>(a, st);
+        return a.slopes ? launch<true, 1>(a, st) : launch<false, 1>(a, st);
+    }
 };
 
 __global__ __launch_bounds__(kThreads) void marks_kernel(const int *__restrict__ documents, const uint8_t *__restrict__ prefix, int Lk, int tiles, int total, Marks *marks, uint32_t *zeros) {
