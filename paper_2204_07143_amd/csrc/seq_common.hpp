@@ -87,17 +87,22 @@ template <typename T> __device__ __forceinline__ u32x4 pack(const f32x4 *s) {
 
 // ---- tiles in LDS ----------------------------------------------------------------------------------------------------------
 //
-// 64 rows of CH chunks, as direct loads leave them (lane l of a load writes 16 bytes at 16 l), chunk c of row r in place c ^ swizzle(r): sixteen
-// rows' chunks of one column (a row fragment), and pairs of chunks of eight rows in turn (a transposed one), then lie in different banks.
+// 64 rows of CH chunks, as direct loads leave them (lane l of a load writes 16 bytes at 16 l), chunk c of row r in place c ^ swizzle(r).
 
 template <typename T, int D> struct Tile {
     static constexpr int CH = D * (int)sizeof(T) / 16, ROWB = CH * 16, BYTES = kTile * ROWB;
     static constexpr int STEPS = CH / 4;                        // products over the head vector
     static constexpr int DB = D / 16;                           // blocks of 16 channels
-    static constexpr int PER256 = CH >= 16 ? 1 : 16 / CH;       // rows in the 256 bytes of all banks
     static constexpr int LOADS = kTile * CH / kThreads;         // of 16 bytes, per thread and image
 
-    __device__ static __forceinline__ int swizzle(int r) { return ((r / PER256 & (8 / PER256 - 1)) << 1) | (r >> 3 & 1); }
+    // Of the rows r (r0 .. r3 its low bits).  What is read at once is to lie in different banks of 256 bytes: of a row fragment the chunks g of rows 0 .. 3 and
+    // 12 .. 15 with the chunks g + 1 of rows 4 .. 11; of a transposed one, pairs of chunks of eight rows in turn.
+    __device__ static __forceinline__ int swizzle(int r) {
+        const int r0 = r & 1, r1 = r >> 1 & 1, r2 = r >> 2 & 1, r3 = r >> 3 & 1;
+        if constexpr (CH >= 16) return (r2 ^ r3) << 3 | r1 << 2 | r0 << 1 | r3;
+        else if constexpr (CH == 8) return r1 << 2 | (r2 ^ r3) << 1 | r3;
+        else return (r2 ^ r3) << 1 | r3;
+    }
 
     // Rows first .. first + 63 of a plane into the image at `img`; a row past the end is the last one once more, where `zeros` are given, one that is not live is zeros.
     __device__ static __forceinline__ void stage(const char *plane, int pitch, int first, int rows, uint64_t live, const char *zeros, int img, int wave, int lane) {
