@@ -53,7 +53,7 @@ typedef struct {
  * kv_heads; one (batch, head) plane, strides included, stays below 2^31 bytes; Lq and Lk are at most 2^24. */
 int seq_validate_problem(const seq_problem *p, int backward);
 
-/* Bytes of workspace; 0 for an invalid problem.  `marked`: documents or prefix are given.  A forward call needs one only where this is not 0. */
+/* Bytes of workspace; 0 for an invalid problem.  `marked`: documents or prefix are given.  A call needs one only where this is not 0; no initialisation. */
 size_t seq_attention_workspace_bytes(const seq_problem *p, int marked, int backward);
 
 /* rest (nullable, 16-bit types; strides of out): what out's rounding took from it, in the type.  A backward call that is given it takes delta = <dout, out> from

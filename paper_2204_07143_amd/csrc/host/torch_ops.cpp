@@ -387,7 +387,7 @@ struct SeqAttention : torch::autograd::Function<SeqAttention> {
         const auto p = seq_of(q, k, v, out, x);
         if (!p) throw Refused{};
         const bool marked = documents.defined() || prefix.defined();
-        const Tensor ws = scratch(marked ? seq_attention_workspace_bytes(&*p, 1, 0) : 0, q);
+        const Tensor ws = scratch(seq_attention_workspace_bytes(&*p, marked, 0), q);
         forward_check(seq_attention_fwd(&*p, ptr(q), ptr(k), ptr(v), (const float *)ptr(slopes), (const int32_t *)ptr(documents), (const uint8_t *)ptr(prefix), ptr(out),
                                         lse ? (float *)ptr(*lse) : nullptr, rest ? ptr(*rest) : nullptr, ptr(ws), size_of(ws), stream()));
         return out;

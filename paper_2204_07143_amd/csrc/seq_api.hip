@@ -56,7 +56,7 @@ int validate(const seq_problem *p, bool backward) {
     return NA2D_OK;
 }
 
-Args args(const seq_problem *p, const float *slopes, const int32_t *documents) {
+Args args(const seq_problem *p, const float *slopes, const int32_t *documents, bool prefix) {
     Args a{};
     a.slopes = slopes, a.documents = documents;
     a.B = p->B, a.heads = p->heads, a.kv = p->kv_heads, a.group = p->heads / p->kv_heads, a.Lq = p->Lq, a.Lk = p->Lk, a.off = p->Lk - p->Lq;
@@ -74,7 +74,8 @@ Args args(const seq_problem *p, const float *slopes, const int32_t *documents) {
         a.m = p->scale == 0.f ? 1e-37f : (float)(log2e * p->scale);   // (0 times what is masked would be no number)
         a.masked = a.m > 0.f ? -INFINITY : INFINITY;
     }
-    a.splits = kv_splits(a, p->dtype, p->D);
+    a.prefix = prefix;
+    a.q_splits = q_splits(a, p->dtype, p->D), a.k_splits = k_splits(a, p->dtype, p->D);
     return a;
 }
 
@@ -88,7 +89,9 @@ struct Space {
         rows = marked ? up(marks + (int64_t)sizeof(Marks) * a.B * a.key_tiles) : 0;
         powers = up(rows + (backward ? (int64_t)sizeof(float2) * queries * kTile : 0));
         parts = up(powers + (backward ? (int64_t)sizeof(int) * queries : 0));
-        bytes = parts + (backward && a.splits > 1 ? (int64_t)sizeof(float) * a.splits * 2 * a.B * a.kv * a.Lk * D : 0);
+        const int64_t of_q = a.q_splits > 1 ? (int64_t)sizeof(float) * a.q_splits * a.B * a.heads * a.Lq * (backward ? D : D + 2) : 0;
+        const int64_t of_k = backward && a.k_splits > 1 ? (int64_t)sizeof(float) * a.k_splits * 2 * a.B * a.kv * a.Lk * D : 0;
+        bytes = parts + (of_q > of_k ? of_q : of_k);   // (one after the other)
     }
 };
 
@@ -106,10 +109,10 @@ int check_marks(const seq_problem *p, const float *slopes, const int32_t *docume
 int prepare(Args &a, const Space &s, const uint8_t *prefix, void *workspace, size_t bytes, hipStream_t st) {
     if (s.bytes && (!workspace || misaligned(workspace) || bytes < (size_t)s.bytes)) return NA2D_ERR_WORKSPACE;
     char *ws = static_cast<char *>(workspace);
+    a.parts = reinterpret_cast<float *>(ws + s.parts);
     if (s.marks) {
         a.marks = reinterpret_cast<const Marks *>(ws + s.marks);
         a.zeros = ws;
-        a.prefix = prefix != nullptr;
         return from_hip(launch_marks(a, prefix, reinterpret_cast<Marks *>(ws + s.marks), ws, st));
     }
     return NA2D_OK;
@@ -154,7 +157,11 @@ extern "C" {
 int seq_validate_problem(const seq_problem *p, int backward) { return validate(p, backward != 0); }
 
 size_t seq_attention_workspace_bytes(const seq_problem *p, int marked, int backward) {
-    return validate(p, backward != 0) == NA2D_OK ? (size_t)Space(args(p, nullptr, nullptr), p->D, marked != 0, backward != 0).bytes : 0;
+    if (validate(p, backward != 0) != NA2D_OK) return 0;
+    // (documents alone, or with a prefix: the larger)
+    const int64_t plain = Space(args(p, nullptr, nullptr, false), p->D, marked != 0, backward != 0).bytes;
+    const int64_t prefixed = marked ? Space(args(p, nullptr, nullptr, true), p->D, true, backward != 0).bytes : 0;
+    return (size_t)(plain > prefixed ? plain : prefixed);
 }
 
 int seq_attention_fwd(const seq_problem *p, const void *q, const void *k, const void *v, const float *slopes, const int32_t *documents, const uint8_t *prefix,
@@ -169,7 +176,7 @@ int seq_attention_fwd(const seq_problem *p, const void *q, const void *k, const 
     if (rest && p->dtype == NA2D_F32) return NA2D_ERR_DTYPE;
     const hipStream_t st = static_cast<hipStream_t>(stream);
     const int e = elem(p->dtype);
-    Args a = args(p, slopes, documents);
+    Args a = args(p, slopes, documents, prefix != nullptr);
     a.q = view(q, p->q, e), a.k = view(k, p->k, e), a.v = view(v, p->v, e), a.out = view(out, p->out, e), a.lse = lse, a.rest = static_cast<char *>(rest);
     if (int r = prepare(a, Space(a, p->D, documents || prefix, false), prefix, workspace, workspace_bytes, st)) return r;
     return from_hip(launch_fwd(a, p->dtype, p->D, p->softcap > 0.f, st));
@@ -189,14 +196,13 @@ int seq_attention_bwd(const seq_problem *p, const void *q, const void *k, const 
     if (dq == dk || dq == dv || dk == dv) return NA2D_ERR_ALIAS;
     const hipStream_t st = static_cast<hipStream_t>(stream);
     const int e = elem(p->dtype);
-    Args a = args(p, slopes, documents);
+    Args a = args(p, slopes, documents, prefix != nullptr);
     a.q = view(q, p->q, e), a.k = view(k, p->k, e), a.v = view(v, p->v, e), a.out = view(out, p->out, e), a.lse = const_cast<float *>(lse), a.rest = const_cast<char *>(static_cast<const char *>(rest));
     a.dout = view(dout, p->dout, e), a.dq = view(dq, p->dq, e), a.dk = view(dk, p->dk, e), a.dv = view(dv, p->dv, e);
     const Space s(a, p->D, documents || prefix, true);
     if (int r = prepare(a, s, prefix, workspace, workspace_bytes, st)) return r;
     a.rows = reinterpret_cast<float2 *>(static_cast<char *>(workspace) + s.rows);
     a.powers = reinterpret_cast<int *>(static_cast<char *>(workspace) + s.powers);
-    a.parts = reinterpret_cast<float *>(static_cast<char *>(workspace) + s.parts);
     if (int r = from_hip(launch_rows(a, p->dtype, p->D, p->softcap > 0.f, st))) return r;
     if (int r = from_hip(launch_bwd_q(a, p->dtype, p->D, p->softcap > 0.f, st))) return r;
     return from_hip(launch_bwd_kv(a, p->dtype, p->D, p->softcap > 0.f, st));

@@ -15,4 +15,24 @@ __device__ __forceinline__ float two_to(int e) { return __builtin_amdgcn_ldexpf(
 
 template <typename T> constexpr int kBlocks = sizeof(T) == 2 ? 2 : 1;   // blocks of 16 queries, or keys, that a wave keeps
 
+// Parts' sums [parts, (a and then b), B * heads, L, D], added in order into a and b (nullable); a thread per four channels.
+template <typename T, int D>
+__global__ __launch_bounds__(kThreads) void join_kernel(const float *sums, int parts, int heads, int L, int64_t planes, View a, View b, int64_t each) {
+    const int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x;
+    if (i >= each) return;
+    const int d = (int)(i % (D / 4)) * 4;
+    const int64_t row = i / (D / 4), plane = row / L;
+    f32x4 x{0.f, 0.f, 0.f, 0.f};
+    for (int s = 0; s < parts; ++s) x += *reinterpret_cast<const f32x4 *>(sums + (int64_t)s * each * 4 + i * 4);
+    const View &to = plane < planes ? a : b;
+    const int at = (int)(plane < planes ? plane : plane - planes);
+    Tile<T, D>::store4(const_cast<char *>(to.at) + at / heads * to.b + at % heads * to.h + row % L * to.row + d * (int)sizeof(T), x);
+}
+template <typename T, int D> hipError_t join(const float *sums, int parts, int B, int heads, int L, const View &a, const View *b, hipStream_t st) {
+    const int64_t planes = (int64_t)B * heads, each = planes * L * (b ? 2 : 1) * (D / 4), blocks = (each + kThreads - 1) / kThreads;
+    if (!launch_holds(blocks, kThreads)) return hipErrorInvalidValue;
+    join_kernel<T, D><<<(unsigned)blocks, kThreads, 0, st>>>(sums, parts, heads, L, planes, a, b ? *b : a, each);
+    return hipGetLastError();
+}
+
 }  // namespace seq

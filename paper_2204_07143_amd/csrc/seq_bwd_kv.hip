@@ -1,17 +1,17 @@
 // The key side of the backward pass (see seq_bwd_q.hip).
-#include <algorithm>
-
 #include "seq_bwd.hpp"
 
 namespace seq {
 
 namespace {
 
+constexpr int64_t kWanted = 1024;   // workgroups: two rounds, for in causal order the first keys have the longest work
+
 // kPair: with 128 channels in 16 bit a wave that kept both sums of 32 keys would take more than 256 registers, and run alone on its SIMD.  Two waves share
 // 32 keys instead: each forms P and dS of half of a tile's queries, the first sums dV, the second dK, and each gives the other, through LDS, the half
 // that it does not sum itself.
 //
-// The work of a workgroup, the tiles of every head that shares its keys, is split into p.splits parts of equal length where there are few workgroups; each
+// The work of a workgroup, the tiles of every head that shares its keys, is split into p.k_splits parts of equal length where there are few workgroups; each
 // then leaves fp32 sums, which a last kernel adds in order.
 
 template <typename T, int D> constexpr bool kPair = sizeof(T) == 2 && D == 128;
@@ -31,8 +31,8 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) void bwd_kv_kerne
     const int role = PAIR ? wave & 1 : 0, group_of_keys = PAIR ? wave >> 1 : wave;
     const int tiles = (p.Lk + kKeys<T, D> - 1) / kKeys<T, D>;
     int id = block_in_order();
-    const int split = id % p.splits;
-    id /= p.splits;
+    const int split = id % p.k_splits;
+    id /= p.k_splits;
     const int tile = id % tiles, plane = id / tiles, b = plane / p.kv, kh = plane % p.kv;
     const char *kp = p.k.at + b * p.k.b + kh * p.k.h, *vp = p.v.at + b * p.v.b + kh * p.v.h;
     const int k0 = tile * kKeys<T, D>, kw = k0 + group_of_keys * 16 * KB;
@@ -121,7 +121,7 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) void bwd_kv_kerne
     };
 
     // the heads that share these keys in turn, each one's tiles in turn: from the split's first to its last
-    const int count = max(0, last - first + 1), all_tiles = p.group * count, each = (all_tiles + p.splits - 1) / p.splits;
+    const int count = max(0, last - first + 1), all_tiles = p.group * count, each = (all_tiles + p.k_splits - 1) / p.k_splits;
     const int lo = min(split * each, all_tiles), hi = min(lo + each, all_tiles);
     const int head_lo = lo < hi ? lo / count : 0, head_hi = lo < hi ? (hi - 1) / count : -1;
     const int tile_lo = lo < hi ? first + lo % count : 0, tile_hi = lo < hi ? first + (hi - 1) % count : -1;
@@ -265,7 +265,7 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) void bwd_kv_kerne
     // which: 0 dK, 1 dV
     auto store = [&](int which, const f32x4 *acc, float by, int i) {
         const View &to = which ? p.dv : p.dk;
-        if (p.splits == 1) L::store_row(acc, by, const_cast<char *>(to.at) + b * to.b + kh * to.h, to.row, i, lane);
+        if (p.k_splits == 1) L::store_row(acc, by, const_cast<char *>(to.at) + b * to.b + kh * to.h, to.row, i, lane);
         else Tile<float, D>::store_row(acc, by, reinterpret_cast<char *>(p.parts + (((int64_t)split * 2 + which) * p.B * p.kv + plane) * p.Lk * D), D * 4, i, lane);
     };
 #pragma unroll
@@ -285,42 +285,17 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) void bwd_kv_kerne
     }
 }
 
-// dK and dV: the splits' sums, in order; a thread per four channels.
-template <typename T, int D>
-__global__ __launch_bounds__(kThreads) void join_kv_kernel(const Args p, int64_t total) {
-    const int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x;
-    if (i >= total) return;
-    const int d = (int)(i % (D / 4)) * 4;
-    const int64_t row = i / (D / 4), each = (int64_t)p.B * p.kv * p.Lk;   // of dK, then of dV
-    f32x4 x{0.f, 0.f, 0.f, 0.f};
-    for (int s = 0; s < p.splits; ++s) x += *reinterpret_cast<const f32x4 *>(p.parts + ((int64_t)s * 2 * each + row) * D + d);
-    const bool values = row >= each;
-    const int64_t at = values ? row - each : row;
-    const View &to = values ? p.dv : p.dk;
-    const int plane = (int)(at / p.Lk);
-    char *out = const_cast<char *>(to.at) + plane / p.kv * to.b + plane % p.kv * to.h + at % p.Lk * to.row + d * (int)sizeof(T);
-    if constexpr (sizeof(T) == 4) {
-        *reinterpret_cast<f32x4 *>(out) = x;
-    } else {
-        typedef T t4 __attribute__((ext_vector_type(4)));
-        *reinterpret_cast<t4 *>(out) = __builtin_convertvector(x, t4);
-    }
-}
-
 template <typename T, int D, bool CAP> struct BwdKV {
     static hipError_t go(const Args &a, hipStream_t st) { return a.slopes ? launch<true>(a, st) : launch<false>(a, st); }
     template <bool SLOPES> static hipError_t launch(const Args &a, hipStream_t st) {
         constexpr int lds = 4 * Tile<T, D>::BYTES;
         static LdsAllowed allowed;
         if (hipError_t e = allow_lds(bwd_kv_kernel<T, D, CAP, SLOPES>, lds, allowed); e != hipSuccess) return e;
-        const int64_t blocks = (int64_t)a.B * a.kv * ((a.Lk + kKeys<T, D> - 1) / kKeys<T, D>) * a.splits;
+        const int64_t blocks = (int64_t)a.B * a.kv * ((a.Lk + kKeys<T, D> - 1) / kKeys<T, D>) * a.k_splits;
         if (!launch_holds(blocks, kThreads)) return hipErrorInvalidValue;
         bwd_kv_kernel<T, D, CAP, SLOPES><<<(unsigned)blocks, kThreads, lds, st>>>(a);
-        if (hipError_t e = hipGetLastError(); e != hipSuccess || a.splits == 1) return e;
-        const int64_t total = (int64_t)a.B * a.kv * a.Lk * 2 * (D / 4), joins = (total + kThreads - 1) / kThreads;
-        if (!launch_holds(joins, kThreads)) return hipErrorInvalidValue;
-        join_kv_kernel<T, D><<<(unsigned)joins, kThreads, 0, st>>>(a, total);
-        return hipGetLastError();
+        if (hipError_t e = hipGetLastError(); e != hipSuccess || a.k_splits == 1) return e;
+        return join<T, D>(a.parts, a.k_splits, a.B, a.kv, a.Lk, a.dk, &a.dv, st);
     }
 };
 template <typename T, int D, bool CAP> struct Keys {
@@ -332,16 +307,11 @@ template <typename T, int D, bool CAP> struct Keys {
 hipError_t launch_bwd_kv(const Args &a, int dtype, int D, bool capped, hipStream_t st) { return dispatch<BwdKV>(dtype, D, capped, a, st); }
 
 
-// How many parts the work on one tile of keys is split into: until there are about kWanted workgroups, but each part is left four tiles of queries, and the parts' sums
-// stay below 256 MB.
-int kv_splits(const Args &a, int dtype, int D) {
+int k_splits(const Args &a, int dtype, int D) {
     int keys = 64;
     (void)dispatch<Keys>(dtype, D, false, keys);
-    constexpr int64_t kWanted = 1024;
-    const int64_t units = (int64_t)a.B * a.kv * ((a.Lk + keys - 1) / keys), sums = (int64_t)a.B * a.kv * a.Lk * D * 8;
-    const int64_t reach = std::min<int64_t>(a.query_tiles, ((int64_t)a.window + keys) / kTile + 2);   // tiles of one head that a tile of keys can meet
-    const int64_t s = std::min({(kWanted + units - 1) / units, (int64_t)a.group * reach / 4, ((int64_t)256 << 20) / sums, (int64_t)16});
-    return (int)std::max<int64_t>(1, s);
+    const int64_t reach = (int64_t)a.window + keys;   // queries of one head that a tile of keys can meet, but for prefixes
+    return parts_of((int64_t)a.B * a.kv * ((a.Lk + keys - 1) / keys), kWanted, (a.prefix || reach > a.Lq ? a.query_tiles : reach / kTile + 2) * a.group, (int64_t)a.B * a.kv * a.Lk * D * 8);
 }
 
 }  // namespace seq

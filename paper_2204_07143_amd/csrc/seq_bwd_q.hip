@@ -63,6 +63,8 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) void bwd_q_kernel
     const int tid = threadIdx.x, lane = tid % kWave, wave = uniform(tid / kWave), j = lane & 15, g = lane >> 4;
     const int tiles = (p.Lq + 16 * QB * kWaves - 1) / (16 * QB * kWaves);
     int id = block_in_order();
+    const int split = id % p.q_splits;
+    id /= p.q_splits;
     const int in_group = id % p.group;
     id /= p.group;
     const int tile = tiles - 1 - id % tiles, plane = id / tiles, b = plane / p.kv, kh = plane % p.kv, h = kh * p.group + in_group;
@@ -126,6 +128,11 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) void bwd_q_kernel
     if (!p.prefix) {
         first = max(0, qa - p.window + 1) / kTile;
         last = min(last, max(-1, qb - p.dlo) >> 6);
+    }
+    if (p.q_splits > 1) {
+        const int each = max(0, last - first + p.q_splits) / p.q_splits;
+        first += split * each;
+        last = min(last, first + each - 1);
     }
     Walk walk(first, last);
 
@@ -234,7 +241,10 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) void bwd_q_kernel
     for (int n = 0; n < QB; ++n) {
         settle_products(dq[n]);
         const int i = qw + 16 * n + j;
-        if (i < p.Lq) L::store_row(dq[n], p.scale * two_to(power[n]), const_cast<char *>(p.dq.at) + b * p.dq.b + h * p.dq.h, p.dq.row, i, lane);
+        if (i >= p.Lq) continue;
+        const float by = p.scale * two_to(power[n]);
+        if (p.q_splits > 1) Tile<float, D>::store_row(dq[n], by, reinterpret_cast<char *>(p.parts + (((int64_t)split * p.B * p.heads + (int64_t)b * p.heads + h) * p.Lq + i) * D), 0, 0, lane);
+        else L::store_row(dq[n], by, const_cast<char *>(p.dq.at) + b * p.dq.b + h * p.dq.h, p.dq.row, i, lane);
     }
 }
 
@@ -251,10 +261,11 @@ template <typename T, int D, bool CAP> struct BwdQ {
         constexpr int lds = 4 * Tile<T, D>::BYTES, rows = 16 * QB * kWaves;
         static LdsAllowed allowed;
         if (hipError_t e = allow_lds(bwd_q_kernel<T, D, CAP, SLOPES, QB>, lds, allowed); e != hipSuccess) return e;
-        const int64_t blocks = (int64_t)a.B * a.heads * ((a.Lq + rows - 1) / rows);
+        const int64_t blocks = (int64_t)a.B * a.heads * ((a.Lq + rows - 1) / rows) * a.q_splits;
         if (!launch_holds(blocks, kThreads)) return hipErrorInvalidValue;
         bwd_q_kernel<T, D, CAP, SLOPES, QB><<<(unsigned)blocks, kThreads, lds, st>>>(a);
-        return hipGetLastError();
+        if (hipError_t e = hipGetLastError(); e != hipSuccess || a.q_splits == 1) return e;
+        return join<T, D>(a.parts, a.q_splits, a.B, a.heads, a.Lq, a.dq, nullptr, st);
     }
     static hipError_t go(const Args &a, hipStream_t st) {
         if constexpr (sizeof(T) == 2)

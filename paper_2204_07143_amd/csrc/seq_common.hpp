@@ -7,6 +7,8 @@
 // chunk (half a chunk in 16 bit) that a product over those rows takes, the weights go from one product to the next in registers.
 #pragma once
 
+#include <initializer_list>
+
 #include "na2d_mfma.hpp"
 #include "seq.h"
 
@@ -45,8 +47,9 @@ struct Args {
     const char *zeros;     // 64 bytes of zeros, where marks are
     float2 *rows;          // backward: (lse in base 2, delta) of every query, [B * heads, query_tiles * 64]
     int *powers;           // backward, fp16: per tile of 64 queries the power of two of its largest |dout|, [B * heads, query_tiles]
-    float *parts;          // backward, splits > 1: fp32 sums of dK and dV, [splits, 2, B * kv, Lk, D]
-    int splits;            // parts that the work on one tile of keys is split into
+    float *parts;          // where work is split: each part's fp32 sums.  queries: [q_splits, B * heads, Lq, D], in the forward pass with float2 (maximum, sum)
+                           // [q_splits, B * heads, Lq] behind them; keys: of dK and dV, [k_splits, 2, B * kv, Lk, D]
+    int q_splits, k_splits;   // parts that the work on one tile of queries, or of keys, is split into
     int B, heads, kv, group, Lq, Lk, off;   // off: Lk - Lq
     int key_tiles, query_tiles;
     int causal, window;    // window: kFar where there is none
@@ -169,22 +172,21 @@ template <typename T, int D> struct Tile {
 #pragma unroll
         for (int s = 0; s < STEPS; ++s) f[s] &= live ? ~0u : 0u;
     }
+    // Four channels as they are stored.  rest: where what the rounding took goes, as an offset; 0: nowhere
+    __device__ static __forceinline__ void store4(char *to, f32x4 x, int64_t rest = 0) {
+        if constexpr (sizeof(T) == 4) {
+            *reinterpret_cast<f32x4 *>(to) = x;
+        } else {
+            typedef T t4 __attribute__((ext_vector_type(4)));
+            const t4 y = __builtin_convertvector(x, t4);
+            *reinterpret_cast<t4 *>(to) = y;
+            if (rest) *reinterpret_cast<t4 *>(to + rest) = __builtin_convertvector(x - __builtin_convertvector(y, f32x4), t4);
+        }
+    }
     // Sums with channels as rows, [DB] blocks, column `row` of a tensor: four channels of each block.
-    // rest: where what the rounding took goes, as an offset from plane; 0: nowhere
     __device__ static __forceinline__ void store_row(const f32x4 *acc, float by, char *plane, int pitch, int row, int lane, int64_t rest = 0) {
 #pragma unroll
-        for (int db = 0; db < DB; ++db) {
-            char *to = plane + (int64_t)row * pitch + (16 * db + 4 * (lane >> 4)) * (int)sizeof(T);
-            const f32x4 x = acc[db] * by;
-            if constexpr (sizeof(T) == 4) {
-                *reinterpret_cast<f32x4 *>(to) = x;
-            } else {
-                typedef T t4 __attribute__((ext_vector_type(4)));
-                const t4 y = __builtin_convertvector(x, t4);
-                *reinterpret_cast<t4 *>(to) = y;
-                if (rest) *reinterpret_cast<t4 *>(to + rest) = __builtin_convertvector(x - __builtin_convertvector(y, f32x4), t4);
-            }
-        }
+        for (int db = 0; db < DB; ++db) store4(plane + (int64_t)row * pitch + (16 * db + 4 * (lane >> 4)) * (int)sizeof(T), acc[db] * by, rest);
     }
 };
 
@@ -293,7 +295,16 @@ hipError_t launch_fwd(const Args &a, int dtype, int D, bool capped, hipStream_t 
 hipError_t launch_rows(const Args &a, int dtype, int D, bool capped, hipStream_t st);
 hipError_t launch_bwd_q(const Args &a, int dtype, int D, bool capped, hipStream_t st);
 hipError_t launch_bwd_kv(const Args &a, int dtype, int D, bool capped, hipStream_t st);
-int kv_splits(const Args &a, int dtype, int D);
+int q_splits(const Args &a, int dtype, int D);
+int k_splits(const Args &a, int dtype, int D);
+
+// Parts for `units` workgroups with up to `tiles` tiles each, of which `sums` bytes are left by each part: until there are about `wanted`
+// workgroups, but each part is left four tiles, and the sums stay below 256 MB.
+inline int parts_of(int64_t units, int64_t wanted, int64_t tiles, int64_t sums) {
+    int64_t s = (wanted + units - 1) / units;
+    for (int64_t most : {tiles / 4, ((int64_t)256 << 20) / sums, (int64_t)32}) s = most < s ? most : s;
+    return (int)(s < 1 ? 1 : s);
+}
 
 // 16 bit: two blocks of 16 queries to a wave (a fragment of keys or values then serves two products) where that leaves two workgroups to each compute unit.
 inline bool two_query_blocks(const Args &a) { return (int64_t)a.B * a.heads * ((a.Lq + 127) / 128) >= 512; }

@@ -26,6 +26,8 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) void fwd_kernel(c
     const int tiles = (p.Lq + 16 * QB * kWaves - 1) / (16 * QB * kWaves);
     // key heads in turn, the last queries (in causal order the longest work) first, the query heads of one key head next to each other
     int id = block_in_order();
+    const int split = id % p.q_splits;
+    id /= p.q_splits;
     const int in_group = id % p.group;
     id /= p.group;
     const int tile = tiles - 1 - id % tiles, plane = id / tiles, b = plane / p.kv, kh = plane % p.kv, h = kh * p.group + in_group;
@@ -72,6 +74,11 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) void fwd_kernel(c
     if (!p.prefix) {
         first = max(0, qa - p.window + 1) / kTile;
         last = min(last, max(-1, qb - p.dlo) >> 6);
+    }
+    if (p.q_splits > 1) {
+        const int each = max(0, last - first + p.q_splits) / p.q_splits;
+        first += split * each;
+        last = min(last, first + each - 1);
     }
     Walk walk(first, last);
 
@@ -201,11 +208,40 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) void fwd_kernel(c
         settle_products(out[n]);
         const int i = qw + 16 * n + j;
         const float total = column_sum(sum[n]);
-        if (i < p.Lq) {
+        if (i >= p.Lq) continue;
+        const int64_t row = ((int64_t)b * p.heads + h) * p.Lq + i;
+        if (p.q_splits > 1) {
+            const int64_t all = (int64_t)p.B * p.heads * p.Lq, at = split * all + row;
+            Tile<float, D>::store_row(out[n], 1.f, reinterpret_cast<char *>(p.parts + at * D), 0, 0, lane);
+            if (g == 0) reinterpret_cast<float2 *>(p.parts + p.q_splits * all * D)[at] = float2{ref[n], total};
+        } else {
             L::store_row(out[n], total == 0.f ? 0.f : 1.f / total, const_cast<char *>(p.out.at) + b * p.out.b + h * p.out.h, p.out.row, i, lane, p.rest ? p.rest - p.out.at : 0);
-            if (p.lse && g == 0) p.lse[((int64_t)b * p.heads + h) * p.Lq + i] = total == 0.f ? -INFINITY : (ref[n] + __builtin_amdgcn_logf(total)) * kLn2;
+            if (p.lse && g == 0) p.lse[row] = total == 0.f ? -INFINITY : (ref[n] + __builtin_amdgcn_logf(total)) * kLn2;
         }
     }
+}
+
+// The splits of a row, in order; a thread per four channels.
+template <typename T, int D>
+__global__ __launch_bounds__(kThreads) void join_fwd_kernel(const Args p, int64_t total) {
+    const int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x;
+    if (i >= total) return;
+    const int d = (int)(i % (D / 4)) * 4;
+    const int64_t row = i / (D / 4), all = (int64_t)p.B * p.heads * p.Lq;
+    const float2 *stats = reinterpret_cast<const float2 *>(p.parts + p.q_splits * all * D) + row;
+    float most = kLowest, sum = 0.f;
+    for (int s = 0; s < p.q_splits; ++s) most = fmaxf(most, stats[s * all].x);
+    f32x4 x{0.f, 0.f, 0.f, 0.f};
+    for (int s = 0; s < p.q_splits; ++s) {
+        const float by = __builtin_amdgcn_exp2f(stats[s * all].x - most);
+        sum = __builtin_fmaf(stats[s * all].y, by, sum);
+        x += *reinterpret_cast<const f32x4 *>(p.parts + (s * all + row) * D + d) * by;
+    }
+    x *= sum == 0.f ? 0.f : 1.f / sum;
+    const int plane = (int)(row / p.Lq);
+    char *out = const_cast<char *>(p.out.at) + plane / p.heads * p.out.b + plane % p.heads * p.out.h + row % p.Lq * p.out.row + d * (int)sizeof(T);
+    Tile<T, D>::store4(out, x, p.rest ? p.rest - p.out.at : 0);
+    if (p.lse && d == 0) p.lse[row] = sum == 0.f ? -INFINITY : (most + __builtin_amdgcn_logf(sum)) * kLn2;
 }
 
 template <typename T, int D, bool CAP> struct Fwd {
@@ -213,9 +249,13 @@ template <typename T, int D, bool CAP> struct Fwd {
         constexpr int lds = 4 * Tile<T, D>::BYTES, rows = 16 * QB * kWaves;
         static LdsAllowed allowed;
         if (hipError_t e = allow_lds(fwd_kernel<T, D, CAP, SLOPES, QB>, lds, allowed); e != hipSuccess) return e;
-        const int64_t blocks = (int64_t)a.B * a.heads * ((a.Lq + rows - 1) / rows);
+        const int64_t blocks = (int64_t)a.B * a.heads * ((a.Lq + rows - 1) / rows) * a.q_splits;
         if (!launch_holds(blocks, kThreads)) return hipErrorInvalidValue;
         fwd_kernel<T, D, CAP, SLOPES, QB><<<(unsigned)blocks, kThreads, lds, st>>>(a);
+        if (hipError_t e = hipGetLastError(); e != hipSuccess || a.q_splits == 1) return e;
+        const int64_t total = (int64_t)a.B * a.heads * a.Lq * (D / 4), joins = (total + kThreads - 1) / kThreads;
+        if (!launch_holds(joins, kThreads)) return hipErrorInvalidValue;
+        join_fwd_kernel<T, D><<<(unsigned)joins, kThreads, 0, st>>>(a, total);
         return hipGetLastError();
     }
     static hipError_t go(const Args &a, hipStream_t st) {
@@ -246,6 +286,14 @@ hipError_t launch_marks(const Args &a, const uint8_t *prefix, Marks *marks, char
     if (!launch_holds((total + kWaves - 1) / kWaves, kThreads)) return hipErrorInvalidValue;
     marks_kernel<<<(unsigned)((total + kWaves - 1) / kWaves), kThreads, 0, st>>>(a.documents, prefix, a.Lk, a.key_tiles, (int)total, marks, reinterpret_cast<uint32_t *>(zeros));
     return hipGetLastError();
+}
+
+// Of the forward pass and of dQ.  Two rounds of workgroups are wanted where the parts' sums are small, one where they are not (us of the forward for one / two:
+// 2 x 4 x 3136 fp32, D 32, causal, 3 MB a part: 83 / 72; 16 x 2048 bf16, D 128, 17 MB: 49 / 63; not split 121 and 51).
+int q_splits(const Args &a, int dtype, int D) {
+    const int rows = dtype != NA2D_F32 && two_query_blocks(a) ? 128 : 64;
+    const int64_t reach = (int64_t)a.window + rows, sums = (int64_t)a.B * a.heads * a.Lq * (D + 2) * 4;   // keys that a tile of queries can see, but for prefixes
+    return parts_of((int64_t)a.B * a.heads * ((a.Lq + rows - 1) / rows), sums <= 4 << 20 ? 1024 : 512, a.prefix || reach > a.Lk ? a.key_tiles : reach / kTile + 2, sums);
 }
 
 hipError_t launch_fwd(const Args &a, int dtype, int D, bool capped, hipStream_t st) { return dispatch<Fwd>(dtype, D, capped, a, st); }

@@ -287,7 +287,7 @@ class _SeqAttention(torch.autograd.Function):
             out.zero_()
         else:
             marked = documents is not None or prefix is not None
-            ws = _scratch(na.seq_attention_workspace_bytes(na.seq_problem(q, k, v=v, out=out, **settings), True), q) if marked else None
+            ws = _scratch(na.seq_attention_workspace_bytes(na.seq_problem(q, k, v=v, out=out, **settings), marked), q)
             na.seq_attention_fwd(q, k, v, slopes, documents, prefix, out, lse, rest, ws, **settings)
         if train:
             ctx.save_for_backward(q, k, v, out, lse, rest, slopes, documents, prefix)

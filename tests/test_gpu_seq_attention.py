@@ -290,3 +290,18 @@ def test_native_and_interpreted_host_sides(dtype):
     with pytest.raises(na.Na2dError) as e:
         F.seq_attention(q, k[:, :, 1:], v[:, :, 1:], documents=documents[:, 1:].contiguous())
     assert e.value.status == -6
+
+
+@TYPE
+@pytest.mark.parametrize("Lq,Lk", [(5, 1500), (700, 700), (64, 2000)])
+@pytest.mark.parametrize("name", ["causal_slopes", "causal_documents", "prefix_documents", "causal_window", "documents"])
+def test_work_split_along_the_keys_and_the_queries(dtype, Lq, Lk, name):
+    """Few rows: a tile's work is split over workgroups and joined, parts without work among them."""
+    D = {5: 128, 700: 64, 64: 32}[Lq]
+    mask = dict(MASKS[name])
+    settings = dict(causal=mask.get("causal", False), window=mask.get("window", 0), softcap=mask.get("softcap", 0.0), scale=1.0)
+    q, k = (torch.empty((1, h, L, D), dtype=TYPES[dtype], device="cuda") for h, L in ((4, Lq), (2, Lk)))
+    p = na.seq_problem(q, k, v=k, out=q, **settings)
+    if name != "causal_window":
+        assert na.seq_attention_workspace_bytes(p, "docs" in mask) > 4 * q.numel()   # (it is split)
+    _check(Lq, 1, 4, 2, Lq, Lk, D, dtype, **mask)
