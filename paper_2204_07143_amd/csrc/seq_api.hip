@@ -138,7 +138,7 @@ CacheArgs cache_args(const seq_cache_problem *p) {
     a.window = p->window ? p->window : kFar;
     a.c = p->softcap > 0.f ? (float)(2.0 * 1.4426950408889634 * p->scale / p->softcap) : (float)(1.4426950408889634 * p->scale);
     a.cap = (float)(2.0 * 1.4426950408889634 * p->softcap);
-    plan_cache_attention(a, p->D, (int64_t)p->table_width * p->page);
+    plan_cache_attention(a, (int64_t)p->table_width * p->page);
     return a;
 }
 bool odd4(std::initializer_list<const void *> ps) {

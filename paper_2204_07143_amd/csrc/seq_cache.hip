@@ -8,9 +8,34 @@ namespace {
 
 constexpr float kMost = 3.402823466e38f;
 
-template <typename T> __device__ __forceinline__ float finite(T x) {   // NaN: 0; infinite: the largest finite value
-    const float f = (float)x;
-    return f != f ? 0.f : fminf(fmaxf(f, -kMost), kMost);
+__device__ __forceinline__ float finite(float x) { return x != x ? 0.f : fminf(fmaxf(x, -kMost), kMost); }
+
+// The largest magnitude of 16 bytes, as bits: at or above those of infinity if one is not finite.
+template <typename T> __device__ __forceinline__ uint32_t most_of(u32x4 x) {
+    uint32_t m = 0;
+    if constexpr (sizeof(T) == 4) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) m = max(m, x[e] & 0x7fffffffu);
+    } else {
+        typedef uint16_t h2 __attribute__((ext_vector_type(2)));
+        h2 y = __builtin_bit_cast(h2, x[0] & 0x7fff7fffu);
+#pragma unroll
+        for (int e = 1; e < 4; ++e) y = __builtin_elementwise_max(y, __builtin_bit_cast(h2, x[e] & 0x7fff7fffu));
+        m = max((uint32_t)y[0], (uint32_t)y[1]);
+    }
+    return m;
+}
+template <typename T> __device__ __forceinline__ float from_bits(uint32_t m) {
+    if constexpr (sizeof(T) == 4) return __uint_as_float(m);
+    else return (float)__builtin_bit_cast(T, (uint16_t)m);
+}
+
+// x / by to the nearest whole number, even ones from the middle, within -127 .. 127: x `over` (1 / by) is off by less than 2^-15 there, so the division is
+// needed only next to a middle.  A NaN gives 0.
+__device__ __forceinline__ int whole(float x, float by, float over) {
+    float r = x * over;
+    if (__builtin_expect(fabsf(fabsf(r - __builtin_rintf(r)) - 0.5f) < 0x1p-14f, 0)) r = x / by;
+    return max(-127, min(127, (int)__builtin_rintf(r)));
 }
 
 template <typename T, int D>
@@ -18,7 +43,7 @@ __global__ __launch_bounds__(kThreads) void append_kernel(const CacheArgs p, int
     constexpr int E = 16 / (int)sizeof(T), CH = D / E;   // elements of a chunk, chunks of a row
     typedef T vec __attribute__((ext_vector_type(E)));
     typedef int8_t bytes __attribute__((ext_vector_type(E)));
-    __shared__ float most_of[kWaves];
+    __shared__ uint32_t mosts[kWaves];
     const int tid = threadIdx.x;
     int id = blockIdx.x;
     const bool values = id & 1;
@@ -37,21 +62,33 @@ __global__ __launch_bounds__(kThreads) void append_kernel(const CacheArgs p, int
     int8_t *cells = (values ? p.v : p.k) + unit * page * D;
     float *scales = values ? p.vs : p.ks;
     const View &x = values ? p.b : p.a;
-    const char *rows = x.at + b * x.b + kh * x.h;
-    const int old = (int)(lo - start), fresh = (int)(hi - lo), skip = (int)(lo - length);
+    const int old = (int)(lo - start), fresh = (int)(hi - lo);
+    const char *rows = x.at + b * x.b + kh * x.h + (lo - length) * x.row;
 
-    float most = 0.f;
-    for (int i = tid; i < fresh * CH; i += kThreads) {
-        const vec y = *reinterpret_cast<const vec *>(rows + (int64_t)(skip + i / CH) * x.row + i % CH * 16);
-#pragma unroll
-        for (int e = 0; e < E; ++e) most = fmaxf(most, fabsf(finite(y[e])));
-    }
-#pragma unroll
-    for (int d = 1; d < kWave; d *= 2) most = fmaxf(most, __shfl_xor(most, d));
-    if (tid % kWave == 0) most_of[tid / kWave] = most;
+    uint32_t bits = 0;
+#pragma unroll 4
+    for (int i = tid; i < fresh * CH; i += kThreads) bits = max(bits, most_of<T>(*reinterpret_cast<const u32x4 *>(rows + (int64_t)(i / CH) * x.row + i % CH * 16)));
     const float before = old ? scales[unit] : 0.f;
+#pragma unroll
+    for (int d = 1; d < kWave; d *= 2) bits = max(bits, (uint32_t)__shfl_xor((int)bits, d));
+    if (tid % kWave == 0) mosts[tid / kWave] = bits;
     workgroup_sync();
-    most = fmaxf(fmaxf(most_of[0], most_of[1]), fmaxf(most_of[2], most_of[3]));
+    float most = from_bits<T>(max(max(mosts[0], mosts[1]), max(mosts[2], mosts[3])));
+    const bool ordinary = most < INFINITY;   // (the bits of a NaN are larger)
+    if (!ordinary) {   // once more, without what is no number
+        most = 0.f;
+        for (int i = tid; i < fresh * CH; i += kThreads) {
+            const vec y = *reinterpret_cast<const vec *>(rows + (int64_t)(i / CH) * x.row + i % CH * 16);
+#pragma unroll
+            for (int e = 0; e < E; ++e) most = fmaxf(most, fabsf(finite((float)y[e])));
+        }
+#pragma unroll
+        for (int d = 1; d < kWave; d *= 2) most = fmaxf(most, __shfl_xor(most, d));
+        workgroup_sync();
+        if (tid % kWave == 0) mosts[tid / kWave] = __float_as_uint(most);
+        workgroup_sync();
+        most = __uint_as_float(max(max(mosts[0], mosts[1]), max(mosts[2], mosts[3])));
+    }
     const float scale = fmaxf(before, most / 127.f), by = scale > 0.f ? scale : 1.f;
     if (tid == 0) scales[unit] = scale;
     if (old && scale != before) {
@@ -61,43 +98,70 @@ __global__ __launch_bounds__(kThreads) void append_kernel(const CacheArgs p, int
             const uint32_t w = words[i];
             uint32_t r = 0;
 #pragma unroll
-            for (int e = 0; e < 4; ++e) r |= (uint32_t)(uint8_t)(int8_t)rintf((float)(int8_t)(w >> 8 * e) * ratio) << 8 * e;
+            for (int e = 0; e < 4; ++e) r |= (uint32_t)(uint8_t)(int8_t)__builtin_rintf((float)(int8_t)(w >> 8 * e) * ratio) << 8 * e;
             words[i] = r;
         }
     }
+    // every element is divided where 1 / by may be no ordinary number either
+    const bool divide = !ordinary || !(by > 0x1p-100f && by < 0x1p100f);
+    const float over = 1.f / by;
+#pragma unroll 2
     for (int i = tid; i < fresh * CH; i += kThreads) {
-        const vec y = *reinterpret_cast<const vec *>(rows + (int64_t)(skip + i / CH) * x.row + i % CH * 16);
+        const vec y = *reinterpret_cast<const vec *>(rows + (int64_t)(i / CH) * x.row + i % CH * 16);
         bytes r;
+        if (divide) {
 #pragma unroll
-        for (int e = 0; e < E; ++e) r[e] = (int8_t)fminf(fmaxf(rintf(finite(y[e]) / by), -127.f), 127.f);
+            for (int e = 0; e < E; ++e) r[e] = (int8_t)max(-127, min(127, (int)__builtin_rintf(finite((float)y[e]) / by)));
+        } else {
+#pragma unroll
+            for (int e = 0; e < E; ++e) r[e] = (int8_t)whole((float)y[e], by, over);
+        }
         *reinterpret_cast<bytes *>(cells + (int64_t)(old + i / CH) * D + i % CH * E) = r;
     }
 }
 
+// A thread per 16 bytes of the output, of keys and of values, of kRows rows; a row's page, its scales and its cells are three reads that wait for each other,
+// the rows' are on their way together.
+constexpr int kRows = 4;
+
 template <typename T, int D>
-__global__ __launch_bounds__(kThreads) void gather_kernel(const CacheArgs p, int64_t total) {
-    constexpr int E = 16 / (int)sizeof(T), CH = D / E;
+__global__ __launch_bounds__(kThreads) void gather_kernel(const CacheArgs p, int blocks_each) {
+    constexpr int E = 16 / (int)sizeof(T), CH = D / E, STEP = kThreads / CH;   // STEP: rows of a workgroup at a time
     typedef T vec __attribute__((ext_vector_type(E)));
     typedef float fvec __attribute__((ext_vector_type(E)));
     typedef int8_t bytes __attribute__((ext_vector_type(E)));
-    const int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x;
-    if (i >= total) return;
-    const int c = (int)(i % CH);
-    const int64_t row = i / CH;
-    const int at = (int)(row % p.n), plane = (int)(row / p.n), kh = plane % p.kv, b = plane / p.kv;
-    const int64_t position = (int64_t)p.extra[b] + at;
-    int id;
-    vec k, v;
+    const int plane = blockIdx.x / blocks_each, row0 = (int)(blockIdx.x % blocks_each) * (STEP * kRows) + threadIdx.x / CH, c = threadIdx.x % CH;
+    const int b = plane / p.kv, kh = plane % p.kv;
+    const int64_t first = p.extra[b], length = p.lengths[b];
+    bool there[kRows];
+    int64_t unit[kRows];
 #pragma unroll
-    for (int e = 0; e < E; ++e) k[e] = v[e] = (T)0.f;
-    if (position >= 0 && position < p.lengths[b] && page_at(p, b, position, id)) {
-        const int64_t unit = (int64_t)id * p.kv + kh, cell = ((unit << p.page_log2) + (position & ((1 << p.page_log2) - 1))) * D + c * E;
-        const bytes x = *reinterpret_cast<const bytes *>(p.k + cell), y = *reinterpret_cast<const bytes *>(p.v + cell);
-        k = __builtin_convertvector(__builtin_convertvector(x, fvec) * p.ks[unit], vec);
-        v = __builtin_convertvector(__builtin_convertvector(y, fvec) * p.vs[unit], vec);
+    for (int i = 0; i < kRows; ++i) {
+        const int64_t position = first + row0 + i * STEP;
+        int id = 0;
+        there[i] = position >= 0 && position < length && row0 + i * STEP < p.n && page_at(p, b, position, id);
+        unit[i] = (int64_t)id * p.kv + kh;
     }
-    *reinterpret_cast<vec *>(const_cast<char *>(p.a.at) + b * p.a.b + kh * p.a.h + (int64_t)at * p.a.row + c * 16) = k;
-    *reinterpret_cast<vec *>(const_cast<char *>(p.b.at) + b * p.b.b + kh * p.b.h + (int64_t)at * p.b.row + c * 16) = v;
+    bytes x[kRows], y[kRows];
+    float ks[kRows], vs[kRows];
+#pragma unroll
+    for (int i = 0; i < kRows; ++i) {
+        x[i] = y[i] = bytes{}, ks[i] = vs[i] = 0.f;
+        if (there[i]) {
+            const int64_t cell = ((unit[i] << p.page_log2) + ((first + row0 + i * STEP) & ((1 << p.page_log2) - 1))) * D + c * E;
+            x[i] = *reinterpret_cast<const bytes *>(p.k + cell), y[i] = *reinterpret_cast<const bytes *>(p.v + cell);
+            ks[i] = p.ks[unit[i]], vs[i] = p.vs[unit[i]];
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < kRows; ++i) {
+        const int at = row0 + i * STEP;
+        if (at >= p.n) break;
+        __builtin_nontemporal_store(__builtin_convertvector(__builtin_convertvector(x[i], fvec) * ks[i], vec),
+                                    reinterpret_cast<vec *>(const_cast<char *>(p.a.at) + b * p.a.b + kh * p.a.h + (int64_t)at * p.a.row + c * 16));
+        __builtin_nontemporal_store(__builtin_convertvector(__builtin_convertvector(y[i], fvec) * vs[i], vec),
+                                    reinterpret_cast<vec *>(const_cast<char *>(p.b.at) + b * p.b.b + kh * p.b.h + (int64_t)at * p.b.row + c * 16));
+    }
 }
 
 template <typename T, int D, bool> struct Append {
@@ -111,9 +175,11 @@ template <typename T, int D, bool> struct Append {
 };
 template <typename T, int D, bool> struct Gather {
     static hipError_t go(const CacheArgs &a, hipStream_t st) {
-        const int64_t total = (int64_t)a.B * a.kv * a.n * (D * (int)sizeof(T) / 16), blocks = (total + kThreads - 1) / kThreads;
+        constexpr int rows = kThreads / (D * (int)sizeof(T) / 16) * kRows;
+        const int each = (a.n + rows - 1) / rows;
+        const int64_t blocks = (int64_t)a.B * a.kv * each;
         if (!launch_holds(blocks, kThreads)) return hipErrorInvalidValue;
-        gather_kernel<T, D><<<(unsigned)blocks, kThreads, 0, st>>>(a, total);
+        gather_kernel<T, D><<<(unsigned)blocks, kThreads, 0, st>>>(a, each);
         return hipGetLastError();
     }
 };

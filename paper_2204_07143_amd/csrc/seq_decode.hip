@@ -1,8 +1,8 @@
 // Attention of a few new tokens over a cache in 8 bits.
 //
 // The rows of a key head, its query heads times the new tokens, are columns of the products, 16 to a block; tokens come in steps of 32.  A wave
-// takes every fourth step of its workgroup's range, straight from memory into registers, the next step's bytes on their way while one is
-// worked on:
+// takes every fourth step of its workgroup's range, straight from memory into registers, the next step's keys on their way from the moment that
+// one's are used, and its values likewise:
 //   S^T = K Q^T     a byte b enters as fp16: (b ^ 0x80) behind the byte 0x64 is 1152 + b, exactly; the page's scale multiplies the sums
 //   P = exp2(S' - ref), rounded to fp16
 //   O^T += vs V^T P  a lane holds D / 16 channels of its eight tokens; product block db takes channel db of each lane, so no value changes lanes
@@ -23,64 +23,69 @@ __device__ __forceinline__ uint32_t low_pair(uint32_t x) { return minus1152(perm
 __device__ __forceinline__ uint32_t high_pair(uint32_t x) { return minus1152(perm(0x64646464u, x, 0x04030402u)); }
 
 template <int D> struct Shape {
-    static constexpr int KW = D / 32;        // words of a token's keys in a lane for each group of 8 channels per product step, two words each
     static constexpr int STEPS = D / 32;     // products over the head vector
     static constexpr int DB = D / 16;        // channels of a lane's values, blocks of 16 channels
 };
 
 // A step's bytes: two blocks of 16 keys, lane (j, g) 8 bytes of row j for each product step; of the values, channels DB j .. of the tokens 4 g + e of both blocks.
-template <int D> struct Bytes {
+// STREAM: the bytes are read once in the call, and need not stay in the caches (64 sequences of 9000 tokens, 8 x 128: 254 us / 243; where row groups read them again, 40 rows: 24.5 / 25.9)
+template <bool STREAM, typename W> __device__ __forceinline__ W read(const int8_t *at) {
+    if constexpr (STREAM) return __builtin_nontemporal_load(reinterpret_cast<const W *>(at));
+    else return *reinterpret_cast<const W *>(at);
+}
+typedef uint32_t w2 __attribute__((ext_vector_type(2)));
+
+template <int D, bool STREAM> struct Keys {
     uint32_t k[2][2 * (D / 32)];
-    uint32_t v[8][D >= 64 ? D / 64 : 1];
-    __device__ __forceinline__ void load(const int8_t *const (&kp)[2], const int8_t *const (&vp)[2], int lane) {
+    __device__ __forceinline__ void load(int i, const int8_t *at, int lane) {
         const int j = lane & 15, g = lane >> 4;
-        typedef uint32_t w2 __attribute__((ext_vector_type(2)));
+        if constexpr (D >= 64) {   // 16 bytes: two product steps
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            if constexpr (D >= 64) {   // 16 bytes: two product steps
+            for (int u = 0; u < D / 64; ++u) {
+                const u32x4 x = read<STREAM, u32x4>(at + j * D + u * 64 + g * 16);
 #pragma unroll
-                for (int u = 0; u < D / 64; ++u) {
-                    const u32x4 x = *reinterpret_cast<const u32x4 *>(kp[i] + j * D + u * 64 + g * 16);
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) k[i][4 * u + e] = x[e];
-                }
-            } else {
-                const w2 x = *reinterpret_cast<const w2 *>(kp[i] + j * D + g * 8);
-                k[i][0] = x[0], k[i][1] = x[1];
+                for (int e = 0; e < 4; ++e) k[i][4 * u + e] = x[e];
             }
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const int8_t *at = vp[i] + (4 * g + e) * D + j * (D / 16);
-                if constexpr (D == 128) {
-                    const w2 x = *reinterpret_cast<const w2 *>(at);
-                    v[4 * i + e][0] = x[0], v[4 * i + e][1] = x[1];
-                } else if constexpr (D == 64) {
-                    v[4 * i + e][0] = *reinterpret_cast<const uint32_t *>(at);
-                } else {
-                    v[4 * i + e][0] = *reinterpret_cast<const uint16_t *>(at);
-                }
-            }
+        } else {
+            const w2 x = read<STREAM, w2>(at + j * D + g * 8);
+            k[i][0] = x[0], k[i][1] = x[1];
         }
     }
-    // keys of block i for product step s
-    __device__ __forceinline__ u32x4 keys(int i, int s) const {
+    // of block i for product step s
+    __device__ __forceinline__ u32x4 get(int i, int s) const {
         const uint32_t x = k[i][2 * s] ^ 0x80808080u, y = k[i][2 * s + 1] ^ 0x80808080u;
         return u32x4{low_pair(x), high_pair(x), low_pair(y), high_pair(y)};
     }
+};
+template <int D, bool STREAM> struct Values {
+    uint32_t v[8][D >= 64 ? D / 64 : 1];
+    __device__ __forceinline__ void load(int i, const int8_t *block, int lane) {
+        const int j = lane & 15, g = lane >> 4;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const int8_t *at = block + (4 * g + e) * D + j * (D / 16);
+            if constexpr (D == 128) {
+                const w2 x = read<STREAM, w2>(at);
+                v[4 * i + e][0] = x[0], v[4 * i + e][1] = x[1];
+            } else if constexpr (D == 64) {
+                v[4 * i + e][0] = read<STREAM, uint32_t>(at);
+            } else {
+                v[4 * i + e][0] = read<STREAM, uint16_t>(at);
+            }
+        }
+    }
     // channel db of the eight tokens
-    __device__ __forceinline__ u32x4 values(int db) const {
+    __device__ __forceinline__ u32x4 get(int db) const {
         u32x4 r;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const uint32_t x = v[2 * i][db / 4] ^ 0x80808080u, y = v[2 * i + 1][db / 4] ^ 0x80808080u;
-            r[i] = minus1152(perm(y, x, 0x0c000c00u | (uint32_t)(db % 4) | (uint32_t)(db % 4 + 4) << 16) | 0x64006400u);
-        }
+        for (int i = 0; i < 4; ++i)
+            r[i] = minus1152((perm(v[2 * i + 1][db / 4], v[2 * i][db / 4], 0x0c000c00u | (uint32_t)(db % 4) | (uint32_t)(db % 4 + 4) << 16) ^ 0x00800080u) | 0x64006400u);
         return r;
     }
 };
 
-template <typename T, int D, int RT, bool CAP>
-__global__ __launch_bounds__(kThreads, (RT == 1 ? 3 : 2) - (D == 128)) void decode_kernel(const CacheArgs p) {
+template <typename T, int D, int RT, bool CAP, bool PAGE16>
+__global__ __launch_bounds__(kThreads, RT == 1 ? 3 : 2) void decode_kernel(const CacheArgs p) {
     using S = Shape<D>;
     constexpr int ROWS = 16 * RT;
     __shared__ __align__(16) float parts[kWaves][16][D + 4];
@@ -91,7 +96,7 @@ __global__ __launch_bounds__(kThreads, (RT == 1 ? 3 : 2) - (D == 128)) void deco
     id /= p.splits;
     const int rg = id % p.row_groups;
     id /= p.row_groups;
-    const int kh = id % p.kv, b = id / p.kv, page = 1 << p.page_log2;
+    const int kh = id % p.kv, b = id / p.kv, page = PAGE16 ? 16 : 1 << p.page_log2;
     const int all_rows = p.group * p.n, row0 = rg * ROWS;
     const int64_t most_tokens = (int64_t)p.width << p.page_log2;
     const int length = (int)min((int64_t)p.lengths[b], most_tokens), first_query = p.lengths[b] - p.n;
@@ -147,119 +152,137 @@ __global__ __launch_bounds__(kThreads, (RT == 1 ? 3 : 2) - (D == 128)) void deco
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
             int page_id = 0;
-            const bool there = step < to && page_at(p, b, (int64_t)step * kStep + (page == 16 ? 16 * i : 0), page_id);
+            const bool there = step < to && page_at(p, b, (int64_t)step * kStep + (PAGE16 ? 16 * i : 0), page_id);
             unit[i] = there ? page_id : -1;
             const int64_t u = (int64_t)(there ? page_id : 0) * p.kv + kh;
             ks[i] = there ? p.ks[u] : 0.f, vs[i] = there ? p.vs[u] : 0.f;
         }
     };
-    struct Step {
-        bool there[2];
-        float ks[2], vs[2];
+    auto cell_of = [&](int step, int slot, int i) {   // in bytes; of what is no page: of page 0
+        const int u = __builtin_amdgcn_readlane(unit[i], slot);
+        return (((int64_t)max(u, 0) * p.kv + kh) * page + ((step * kStep + 16 * i) & (page - 1))) * D;
     };
-    auto fetch = [&](Bytes<D> &bytes, Step &info, int step, int slot) {
-        const int8_t *kp[2], *vp[2];
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            const int u = __builtin_amdgcn_readlane(unit[i], slot);
-            info.there[i] = u >= 0;
-            info.ks[i] = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(ks[i]), slot));
-            info.vs[i] = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(vs[i]), slot));
-            const int64_t cell = (((int64_t)max(u, 0) * p.kv + kh) * page + ((step * kStep + 16 * i) & (page - 1))) * D;
-            kp[i] = p.k + cell, vp[i] = p.v + cell;
-        }
-        bytes.load(kp, vp, lane);
-    };
-    auto work = [&](const Bytes<D> &bytes, const Step &info, int step) {
-        const int t0 = step * kStep;
-        f32x4 s[RT][2];
-#pragma unroll
-        for (int n = 0; n < RT; ++n)
-#pragma unroll
-            for (int i = 0; i < 2; ++i) s[n][i] = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-        for (int st = 0; st < S::STEPS; ++st)
-#pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                const u32x4 a = bytes.keys(i, st);
-#pragma unroll
-                for (int n = 0; n < RT; ++n) s[n][i] = mma<f16_t>(a, q[n][st], s[n][i]);
-            }
-        // every row sees all of it
-        const bool all = info.there[0] && info.there[1] && t0 + kStep - 1 <= first_query && first_query + p.n - 1 - t0 < p.window;
-        u32x4 w[RT];
-#pragma unroll
-        for (int n = 0; n < RT; ++n) {
-            float most = -INFINITY;
-#pragma unroll
-            for (int i = 0; i < 2; ++i)
-#pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    const int key = t0 + 16 * i + 4 * g + r;
-                    float x = s[n][i][r] * (c[n] * info.ks[i]);
-                    if constexpr (CAP) x = __builtin_fmaf(-p.cap, __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(x)), 0.5f * p.cap);
-                    if (p.slopes) x = __builtin_fmaf((float)(pos[n] - key), -slope[n], x);
-                    if (!all && !(info.there[i] && key <= pos[n] && pos[n] - key < p.window)) x = -INFINITY;
-                    s[n][i][r] = x;
-                    most = fmaxf(most, x);
-                }
-            most = column_max(most);
-            const float now = most > ref[n] + kSlack ? most : ref[n];
-            if (__any(now != ref[n])) {
-                const float by = __builtin_amdgcn_exp2f(ref[n] - now);
-                sum[n] *= by;
-#pragma unroll
-                for (int db = 0; db < S::DB; ++db) out[n][db] *= by;
-                ref[n] = now;
-            }
-#pragma unroll
-            for (int i = 0; i < 2; ++i)
-#pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    s[n][i][r] = __builtin_amdgcn_exp2f(s[n][i][r] - ref[n]);
-                    sum[n] += s[n][i][r];
-                }
-            w[n] = pack<f16_t>(s[n]);
-        }
-        if (page == 16) {   // the two blocks have scales of their own
-#pragma unroll
-            for (int db = 0; db < S::DB; ++db) {
-                const u32x4 a = bytes.values(db);
-#pragma unroll
-                for (int n = 0; n < RT; ++n) {
-                    const f32x4 zero{0.f, 0.f, 0.f, 0.f};
-                    const f32x4 x = mma<f16_t>(a, u32x4{w[n][0], w[n][1], 0u, 0u}, zero), y = mma<f16_t>(a, u32x4{0u, 0u, w[n][2], w[n][3]}, zero);
-#pragma unroll
-                    for (int r = 0; r < 4; ++r) out[n][db][r] = __builtin_fmaf(y[r], info.vs[1], __builtin_fmaf(x[r], info.vs[0], out[n][db][r]));
-                }
-            }
-        } else {
-#pragma unroll
-            for (int db = 0; db < S::DB; ++db) {
-                const u32x4 a = bytes.values(db);
-#pragma unroll
-                for (int n = 0; n < RT; ++n) {
-                    const f32x4 x = mma<f16_t>(a, w[n], f32x4{0.f, 0.f, 0.f, 0.f});
-#pragma unroll
-                    for (int r = 0; r < 4; ++r) out[n][db][r] = __builtin_fmaf(x[r], info.vs[0], out[n][db][r]);
-                }
-            }
-        }
-    };
+    auto scale_of = [&](const float (&x)[2], int slot, int i) { return __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(x[i]), slot)); };
 
 #pragma unroll 1
     for (int base = from + wave; base < to; base += kWave * kWaves) {
         look_up(base + lane * kWaves);
         const int steps = min(kWave, (to - base + kWaves - 1) / kWaves);
-        Bytes<D> here, ahead;
-        Step info, info_ahead;
-        fetch(here, info, base, 0);
+        Keys<D, RT == 1> keys;
+        Values<D, RT == 1> values;
+#pragma unroll
+        for (int i = 0; i < 2; ++i) keys.load(i, p.k + cell_of(base, 0, i), lane);
+#pragma unroll
+        for (int i = 0; i < 2; ++i) values.load(i, p.v + cell_of(base, 0, i), lane);
 #pragma unroll 1
-        for (int i = 0; i < steps; ++i) {
-            const int next = min(i + 1, steps - 1);
-            fetch(ahead, info_ahead, base + next * kWaves, next);
-            work(here, info, base + i * kWaves);
-            here = ahead, info = info_ahead;
+        for (int at = 0; at < steps; ++at) {
+            const int step = base + at * kWaves, t0 = step * kStep;
+            f32x4 s[RT][2];
+#pragma unroll
+            for (int n = 0; n < RT; ++n)
+#pragma unroll
+                for (int i = 0; i < 2; ++i) s[n][i] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int st = 0; st < S::STEPS; ++st)
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    const u32x4 a = keys.get(i, st);
+#pragma unroll
+                    for (int n = 0; n < RT; ++n) s[n][i] = mma<f16_t>(a, q[n][st], s[n][i]);
+                }
+            const bool more = at + 1 < steps;
+            if (more) {   // the next keys, while this step's weights and values are worked on
+#pragma unroll
+                for (int i = 0; i < 2; ++i) keys.load(i, p.k + cell_of(step + kWaves, at + 1, i), lane);
+            }
+            const bool there[2] = {__builtin_amdgcn_readlane(unit[0], at) >= 0, __builtin_amdgcn_readlane(unit[1], at) >= 0};
+            // every row sees all of it
+            const bool all = there[0] && there[1] && t0 + kStep - 1 <= first_query && first_query + p.n - 1 - t0 < p.window;
+            u32x4 w[RT];
+#pragma unroll
+            for (int n = 0; n < RT; ++n) {
+                float most = -INFINITY;
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    const float by = c[n] * scale_of(ks, at, i);
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) {
+                        float x = s[n][i][r] * by;
+                        if constexpr (CAP) x = __builtin_fmaf(-p.cap, __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(x)), 0.5f * p.cap);
+                        s[n][i][r] = x;
+                    }
+                }
+                if (p.slopes) {
+                    const float near = (float)(pos[n] - t0 - 4 * g);
+#pragma unroll
+                    for (int i = 0; i < 2; ++i)
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) s[n][i][r] = __builtin_fmaf(near - (float)(16 * i + r), -slope[n], s[n][i][r]);
+                }
+                if (!all) {
+                    uint64_t seen = bits_between(pos[n] - p.window + 1 - t0, pos[n] + 1 - t0);
+                    seen &= (there[0] ? 0xffffull : 0ull) | (there[1] ? 0xffff0000ull : 0ull);
+                    seen >>= 4 * g;
+#pragma unroll
+                    for (int i = 0; i < 2; ++i)
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) s[n][i][r] = keep(s[n][i][r], seen, 16 * i + r, -INFINITY);
+                }
+#pragma unroll
+                for (int i = 0; i < 2; ++i)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) most = fmaxf(most, s[n][i][r]);
+                most = column_max(most);
+                const float now = most > ref[n] + kSlack ? most : ref[n];
+                if (__any(now != ref[n])) {
+                    const float by = __builtin_amdgcn_exp2f(ref[n] - now);
+                    sum[n] *= by;
+#pragma unroll
+                    for (int db = 0; db < S::DB; ++db) out[n][db] *= by;
+                    ref[n] = now;
+                }
+#pragma unroll
+                for (int i = 0; i < 2; ++i)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) {
+                        s[n][i][r] = __builtin_amdgcn_exp2f(s[n][i][r] - ref[n]);
+                        sum[n] += s[n][i][r];
+                    }
+                w[n] = pack<f16_t>(s[n]);
+            }
+            const float v0 = scale_of(vs, at, 0), v1 = scale_of(vs, at, 1);
+            if constexpr (PAGE16) {   // the two blocks have scales of their own
+#pragma unroll
+                for (int db = 0; db < S::DB; ++db) {
+                    u32x4 a = values.get(db);
+                    asm volatile("" : "+v"(a));
+#pragma unroll
+                    for (int n = 0; n < RT; ++n) {
+                        const f32x4 zero{0.f, 0.f, 0.f, 0.f};
+                        const f32x4 x = mfma_16x16x16<f16_t>(a[0], a[1], w[n][0], w[n][1], zero), y = mfma_16x16x16<f16_t>(a[2], a[3], w[n][2], w[n][3], zero);
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) out[n][db][r] = __builtin_fmaf(y[r], v1, __builtin_fmaf(x[r], v0, out[n][db][r]));
+                        asm volatile("" : "+v"(out[n][db]));   // (in turn: all the products' sums at once would not fit the registers)
+                    }
+                }
+            } else {
+#pragma unroll
+                for (int db = 0; db < S::DB; ++db) {
+                    u32x4 a = values.get(db);
+                    asm volatile("" : "+v"(a));
+#pragma unroll
+                    for (int n = 0; n < RT; ++n) {
+                        const f32x4 x = mma<f16_t>(a, w[n], f32x4{0.f, 0.f, 0.f, 0.f});
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) out[n][db][r] = __builtin_fmaf(x[r], v0, out[n][db][r]);
+                        asm volatile("" : "+v"(out[n][db]));
+                    }
+                }
+            }
+            if (more) {
+#pragma unroll
+                for (int i = 0; i < 2; ++i) values.load(i, p.v + cell_of(step + kWaves, at + 1, i), lane);
+            }
         }
     }
 
@@ -310,34 +333,37 @@ __global__ __launch_bounds__(kThreads, (RT == 1 ? 3 : 2) - (D == 128)) void deco
     }
 }
 
-// The splits of a row, in order; a thread per 8 channels.
+// The splits of a row: a workgroup per row, a thread per four channels of every kThreads * 4 / D-th split, then those in order.
 template <typename T, int D>
-__global__ __launch_bounds__(kThreads) void join_kernel(const CacheArgs p, int rows_each, int64_t total) {
-    const int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x;
-    if (i >= total) return;
-    const int d = (int)(i % (D / 8)) * 8, all_rows = p.group * p.n;
-    const int64_t at = i / (D / 8);
-    const int row = (int)(at % all_rows), plane = (int)(at / all_rows), b = plane / p.kv, kh = plane % p.kv;
-    const int64_t items = (int64_t)p.B * p.kv * p.row_groups * p.splits, first = ((int64_t)plane * p.row_groups + row / rows_each) * p.splits;
-    const float *stats = p.part + items * rows_each * D;
-    const int r = row % rows_each;
-    float m = kLowest;
-    for (int s = 0; s < p.splits; ++s) m = fmaxf(m, stats[((first + s) * rows_each + r) * 2]);
-    float x[8] = {}, sum = 0.f;
-    for (int s = 0; s < p.splits; ++s) {
-        const float *st = stats + ((first + s) * rows_each + r) * 2;
-        const float by = __builtin_amdgcn_exp2f(st[0] - m);
-        const f32x4 *y = reinterpret_cast<const f32x4 *>(p.part + ((first + s) * rows_each + r) * D + d);
-        const f32x4 lo = y[0], hi = y[1];
-        sum = __builtin_fmaf(st[1], by, sum);
-#pragma unroll
-        for (int e = 0; e < 4; ++e) x[e] = __builtin_fmaf(lo[e], by, x[e]), x[4 + e] = __builtin_fmaf(hi[e], by, x[4 + e]);
+__global__ __launch_bounds__(kThreads) void join_kernel(const CacheArgs p, int rows_each) {
+    constexpr int COLS = D / 4, PARTS = kThreads / COLS;
+    __shared__ __align__(16) f32x4 sums[PARTS][COLS];
+    __shared__ float2 stat[PARTS];
+    const int all_rows = p.group * p.n, col = threadIdx.x % COLS, part = threadIdx.x / COLS;
+    const int row = (int)(blockIdx.x % all_rows), plane = (int)(blockIdx.x / all_rows), b = plane / p.kv, kh = plane % p.kv;
+    const int64_t items = (int64_t)p.B * p.kv * p.row_groups * p.splits, first = (((int64_t)plane * p.row_groups + row / rows_each) * p.splits) * rows_each + row % rows_each;
+    const float2 *stats = reinterpret_cast<const float2 *>(p.part + items * rows_each * D) + first;
+    float m = kLowest, sum = 0.f;
+    f32x4 x{0.f, 0.f, 0.f, 0.f};
+    for (int s = part; s < p.splits; s += PARTS) {
+        const float2 st = stats[s * rows_each];
+        const f32x4 y = *reinterpret_cast<const f32x4 *>(p.part + (first + (int64_t)s * rows_each) * D + col * 4);
+        const float now = fmaxf(m, st.x), old = __builtin_amdgcn_exp2f(m - now), by = __builtin_amdgcn_exp2f(st.x - now);
+        m = now, sum = sum * old + st.y * by, x = x * old + y * by;
     }
-    const float by = sum == 0.f ? 0.f : 1.f / sum;
-#pragma unroll
-    for (int e = 0; e < 8; ++e) x[e] *= by;
+    sums[part][col] = x;
+    if (col == 0) stat[part] = float2{m, sum};
+    workgroup_sync();
+    if (part) return;
+    for (int s = 1; s < PARTS && s < p.splits; ++s) m = fmaxf(m, stat[s].x);
+    sum = 0.f, x = f32x4{0.f, 0.f, 0.f, 0.f};
+    for (int s = 0; s < PARTS && s < p.splits; ++s) {
+        const float by = __builtin_amdgcn_exp2f(stat[s].x - m);
+        sum += stat[s].y * by;
+        x += sums[s][col] * by;
+    }
     const int h = kh * p.group + row / p.n;
-    store_vec32<T, 8>(const_cast<char *>(p.b.at) + b * p.b.b + h * p.b.h + (int64_t)(row % p.n) * p.b.row + d * (int)sizeof(T), x);
+    Tile<T, D>::store4(const_cast<char *>(p.b.at) + b * p.b.b + h * p.b.h + (int64_t)(row % p.n) * p.b.row + col * 4 * (int)sizeof(T), x * (sum == 0.f ? 0.f : 1.f / sum));
 }
 
 int rows_each(const CacheArgs &a) { return a.group * a.n > 16 ? 32 : 16; }
@@ -346,26 +372,27 @@ template <typename T, int D, bool CAP> struct Decode {
     static hipError_t go(const CacheArgs &a, hipStream_t st) {
         const int64_t blocks = (int64_t)a.B * a.kv * a.row_groups * a.splits;
         if (!launch_holds(blocks, kThreads)) return hipErrorInvalidValue;
-        if (rows_each(a) == 16) decode_kernel<T, D, 1, CAP><<<(unsigned)blocks, kThreads, 0, st>>>(a);
-        else decode_kernel<T, D, 2, CAP><<<(unsigned)blocks, kThreads, 0, st>>>(a);
+        const bool wide = rows_each(a) > 16, page16 = a.page_log2 == 4;
+        auto *kernel = wide ? page16 ? decode_kernel<T, D, 2, CAP, true> : decode_kernel<T, D, 2, CAP, false> : page16 ? decode_kernel<T, D, 1, CAP, true> : decode_kernel<T, D, 1, CAP, false>;
+        kernel<<<(unsigned)blocks, kThreads, 0, st>>>(a);
         if (hipError_t e = hipGetLastError(); e != hipSuccess || a.splits == 1) return e;
-        const int64_t total = (int64_t)a.B * a.heads * a.n * (D / 8), joins = (total + kThreads - 1) / kThreads;
-        if (!launch_holds(joins, kThreads)) return hipErrorInvalidValue;
-        join_kernel<T, D><<<(unsigned)joins, kThreads, 0, st>>>(a, rows_each(a), total);
+        const int64_t rows = (int64_t)a.B * a.heads * a.n;
+        if (!launch_holds(rows, kThreads)) return hipErrorInvalidValue;
+        join_kernel<T, D><<<(unsigned)rows, kThreads, 0, st>>>(a, rows_each(a));
         return hipGetLastError();
     }
 };
 
 }  // namespace
 
-// Ranges are split where whole sequences would leave compute units without work: until there are about four workgroups to each of the 256, but no
-// split is given less than 256 tokens of the longest sequence that the table can hold.
-void plan_cache_attention(CacheArgs &a, int D, int64_t longest) {
-    (void)D;
+// Ranges are split until there are about sixteen workgroups to each of the 256 compute units (sequences differ in length), but no split is given less than 256
+// tokens of the longest sequence that the table can hold, or 512 where a workgroup leaves 32 rows.  us, 64 sequences of 9000 tokens, 8 x 128, for 1024, 2048 and
+// 4096 workgroups 260, 251, 243; one of 16000 tokens in 256s and 512s 23 and 22; 4 of 8000, 32 rows, 36 and 28.
+void plan_cache_attention(CacheArgs &a, int64_t longest) {
     a.row_groups = (a.group * a.n + rows_each(a) - 1) / rows_each(a);
     const int64_t reach = longest < (int64_t)a.window + a.n ? longest : (int64_t)a.window + a.n;
-    const int64_t units = (int64_t)a.B * a.kv * a.row_groups, wanted = (1024 + units - 1) / units, most = reach / 256;
-    int64_t s = wanted < most ? wanted : most;
+    const int64_t units = (int64_t)a.B * a.kv * a.row_groups, wanted = (4096 + units - 1) / units, most = reach / (rows_each(a) > 16 ? 512 : 256);
+    const int64_t s = wanted < most ? wanted : most;
     a.splits = (int)(s < 1 ? 1 : s > 128 ? 128 : s);
 }
 size_t cache_attention_bytes(const CacheArgs &a, int D) {
