@@ -11,7 +11,7 @@ constexpr int64_t kWanted = 1024;   // workgroups: two rounds, for in causal ord
 // 32 keys instead: each forms P and dS of half of a tile's queries, the first sums dV, the second dK, and each gives the other, through LDS, the half
 // that it does not sum itself.
 //
-// The work of a workgroup, the tiles of every head that shares its keys, is split into p.k_splits parts of equal length where there are few workgroups; each
+// The work of a workgroup, the tiles of every head that shares its keys, is split into p.k_splits parts of as many tiles where there are few workgroups; each
 // then leaves fp32 sums, which a last kernel adds in order.
 
 template <typename T, int D> constexpr bool kPair = sizeof(T) == 2 && D == 128;
@@ -104,15 +104,20 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) void bwd_kv_kerne
 #pragma unroll
         for (int db = 0; db < L::DB; ++db) dk[n][db] = dv[n][db] = f32x4{0.f, 0.f, 0.f, 0.f};
 
-    auto stage = [&](int h, int t, int buf) {
+    // Of a tile's queries, whose positions begin inside a tile of keys: the documents, and which are there.
+    auto marks_of = [&](int t) {
+        Marks m{0, 0, 0, 0};
+        if (documents && t >= 0) {
+            const int at = t * kTile + p.off, in = at % kTile;
+            const Marks x = uniform_marks(marks, at / kTile), y = uniform_marks(marks, min((at + kTile - 1) / kTile, p.key_tiles - 1));
+            m = Marks{min(x.dmin, y.dmin), max(x.dmax, y.dmax), x.live >> in, 0};
+            if (in) m.live |= y.live << (kTile - in);
+        }
+        return m;
+    };
+    auto stage = [&](int h, int t, int buf, uint64_t live) {
         const int to = img + buf * 2 * L::BYTES;
         const char *zeros = documents ? p.zeros : nullptr;
-        uint64_t live = 0;
-        if (zeros) {   // of the tile's queries: their positions begin inside a tile of keys
-            const int at = t * kTile + p.off, in = at % kTile;
-            live = marks[at / kTile].live >> in;
-            if (in) live |= marks[min(at / kTile + 1, p.key_tiles - 1)].live << (kTile - in);
-        }
         L::stage(p.q.at + b * p.q.b + h * p.q.h, p.q.row, t * kTile, p.Lq, live, zeros, to, wave, lane);
         L::stage(p.dout.at + b * p.dout.b + h * p.dout.h, p.dout.row, t * kTile, p.Lq, live, zeros, to + L::BYTES, wave, lane);
         if (wave < 2) global_to_lds_4(reinterpret_cast<const char *>(p.rows + (((int64_t)b * p.heads + h) * p.query_tiles + t) * kTile), (unsigned)(wave * kWave + lane) * 4,
@@ -120,44 +125,43 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) void bwd_kv_kerne
         if (zeros && wave == 2) global_to_lds_4(reinterpret_cast<const char *>(documents), (unsigned)min(t * kTile + lane + p.off, p.Lk - 1) * 4, lds_addr(ids[buf]));
     };
 
-    // the heads that share these keys in turn, each one's tiles in turn: from the split's first to its last
-    const int count = max(0, last - first + 1), all_tiles = p.group * count, each = (all_tiles + p.k_splits - 1) / p.k_splits;
-    const int lo = min(split * each, all_tiles), hi = min(lo + each, all_tiles);
-    const int head_lo = lo < hi ? lo / count : 0, head_hi = lo < hi ? (hi - 1) / count : -1;
-    const int tile_lo = lo < hi ? first + lo % count : 0, tile_hi = lo < hi ? first + (hi - 1) % count : -1;
-    int head = head_lo;
-    Walk walk(tile_lo, head == head_hi ? tile_hi : last);
+    // the heads that share these keys in turn, each one's tiles in turn: of all these, this part's
+    int head = 0, left = INT32_MAX, skip = 0;
+    if (p.k_splits > 1) {
+        const int count = Walk::count(first, last, of, lane);
+        left = (p.group * count + p.k_splits - 1) / p.k_splits;
+        if (count) head = split * left / count, skip = split * left % count;
+    }
+    Walk walk(first, last, skip);
     bool some, all, some_next = false, all_next = false;
     auto next = [&](bool &s, bool &a) {
-        while (true) {
-            const int t = head <= head_hi ? walk.next(of, lane, s, a) : -1;
-            if (t >= 0 || head >= head_hi) return t;
-            ++head;
-            walk = Walk(first, head == head_hi ? tile_hi : last);
+        while (head < p.group && left > 0) {
+            const int t = walk.next(of, lane, s, a);
+            if (t >= 0) return --left, t;
+            if (++head < p.group) walk = Walk(first, last);
         }
+        return -1;
     };
     int t = next(some, all), buf = 0, h = kh * p.group + head;
-    if (t >= 0) stage(h, t, 0);
+    Marks m = marks_of(t);
+    if (t >= 0) stage(h, t, 0, m.live);
 #pragma unroll 1
     while (t >= 0) {
         const int after = next(some_next, all_next);
+        const Marks ahead = marks_of(after);
         wait_global_loads();
         workgroup_sync();
-        if (after >= 0) stage(kh * p.group + head, after, buf ^ 1);
+        if (after >= 0) stage(kh * p.group + head, after, buf ^ 1, ahead.live);
         const int qi = img + buf * 2 * L::BYTES, di = qi + L::BYTES, q0 = t * kTile + p.off;
         const float slope = SLOPES ? p.slopes[h] * kLog2e : 0.f, lower = two_to(-power - (int)kRaise<T>);
         uint64_t seen[KB];
         bool mixed = false;   // the tile's documents are not one (what is not live has no weights anyway)
         if (some && !all) {
-            int dmin = 0;
-            if (documents) {
-                const Marks x = marks[q0 / kTile], y = marks[min((q0 + kTile - 1) / kTile, p.key_tiles - 1)];
-                dmin = min(x.dmin, y.dmin), mixed = dmin != max(x.dmax, y.dmax);
-            }
+            mixed = m.dmin != m.dmax;
 #pragma unroll
             for (int n = 0; n < KB; ++n) {
                 seen[n] = always[n] ? ~0ull : bits_between(key[n] + p.dlo - q0, min(key[n] + p.window, kFar) - q0);
-                if (documents) seen[n] = mine[n] >= 0 && (mixed || mine[n] == dmin) ? seen[n] : 0;
+                if (documents) seen[n] = mine[n] >= 0 && (mixed || mine[n] == m.dmin) ? seen[n] : 0;
                 seen[n] >>= 4 * g;
             }
         }
@@ -260,7 +264,7 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) void bwd_kv_kerne
                 }
             }
         }
-        t = after, h = kh * p.group + head, some = some_next, all = all_next, buf ^= 1;
+        t = after, h = kh * p.group + head, some = some_next, all = all_next, m = ahead, buf ^= 1;
     }
     // which: 0 dK, 1 dV
     auto store = [&](int which, const f32x4 *acc, float by, int i) {

@@ -228,6 +228,13 @@ __device__ __forceinline__ int wave_max(int x) {
     return x;
 }
 __device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
+__device__ __forceinline__ uint64_t uniform(uint64_t x) { return (uint64_t)(uint32_t)uniform((int)(uint32_t)x) | (uint64_t)(uint32_t)uniform((int)(uint32_t)(x >> 32)) << 32; }
+// A tile's marks in scalar registers.  Read before the wait for a tile's loads: behind the next tile's, which the compiler does not count, every use would wait for all of them.
+__device__ __forceinline__ Marks uniform_marks(const Marks *marks, int t) {
+    if (!marks || t < 0) return Marks{0, 0, 0, 0};
+    const Marks m = marks[t];
+    return Marks{uniform(m.dmin), uniform(m.dmax), uniform(m.live), uniform(m.prefix)};
+}
 // of the wave's tokens; `there` false: no token in this lane
 __device__ __forceinline__ Docs docs_of_wave(int d, bool there) {
     const bool live = there && d >= 0;
@@ -239,8 +246,8 @@ __device__ __forceinline__ Docs docs_of_wave(int d, bool there) {
 // workgroup's is seen, 2 any pair of this wave's, 4 every pair of this wave's.  The first bit must not differ between waves.
 struct Walk {
     uint64_t todo, mine, whole;
-    int base, last;
-    __device__ __forceinline__ Walk(int first, int last_) : todo(0), mine(0), whole(0), base(first - kWave), last(last_) {}
+    int base, last, skip;   // skip: how many of them to leave out before the first
+    __device__ __forceinline__ Walk(int first, int last_, int skip_ = 0) : todo(0), mine(0), whole(0), base(first - kWave), last(last_), skip(skip_) {}
     template <class F> __device__ __forceinline__ int next(F of, int lane, bool &is_mine, bool &is_whole) {
         while (!todo) {
             base += kWave;
@@ -249,12 +256,22 @@ struct Walk {
             todo = __ballot(bits & 1);
             mine = __ballot(bits & 2);
             whole = __ballot(bits & 4);
+            const int n = __builtin_popcountll(todo), out = min(skip, n);
+            skip -= out;
+            if (out == n) todo = 0;
+            else for (int i = 0; i < out; ++i) todo &= todo - 1;
         }
         const int i = __builtin_ctzll(todo);
         todo &= todo - 1;
         is_mine = mine >> i & 1;
         is_whole = whole >> i & 1;
         return base + i;
+    }
+    // how many there are
+    template <class F> __device__ static __forceinline__ int count(int first, int last, F of, int lane) {
+        int n = 0;
+        for (int base = first; base <= last; base += kWave) n += __builtin_popcountll(__ballot(base + lane <= last ? of(base + lane) & 1 : 0));
+        return n;
     }
 };
 

@@ -75,12 +75,13 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) void fwd_kernel(c
         first = max(0, qa - p.window + 1) / kTile;
         last = min(last, max(-1, qb - p.dlo) >> 6);
     }
+    int left = INT32_MAX, skip = 0;   // of the tiles there are, this part's
     if (p.q_splits > 1) {
-        const int each = max(0, last - first + p.q_splits) / p.q_splits;
-        first += split * each;
-        last = min(last, first + each - 1);
+        left = (Walk::count(first, last, of, lane) + p.q_splits - 1) / p.q_splits;
+        skip = split * left;
     }
-    Walk walk(first, last);
+    Walk walk(first, last, skip);
+    auto next = [&](bool &some, bool &all) { return left-- > 0 ? walk.next(of, lane, some, all) : -1; };
 
     const typename L::RowReader rows(lane);
     const typename L::ColumnReader columns(lane);
@@ -96,24 +97,25 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) void fwd_kernel(c
         for (int db = 0; db < L::DB; ++db) out[n][db] = f32x4{0.f, 0.f, 0.f, 0.f};
     }
 
-    auto stage = [&](int t, int buf) {
+    auto stage = [&](int t, int buf, uint64_t live) {
         const int to = img + buf * 2 * L::BYTES;
         const char *zeros = p.documents ? p.zeros : nullptr;
-        const uint64_t live = zeros ? marks[t].live : 0;
         L::stage(kp, p.k.row, t * kTile, p.Lk, live, zeros, to, wave, lane);
         L::stage(vp, p.v.row, t * kTile, p.Lk, live, zeros, to + L::BYTES, wave, lane);
         if (zeros && wave == 0) global_to_lds_4(reinterpret_cast<const char *>(p.documents + (int64_t)b * p.Lk), (unsigned)min(t * kTile + lane, p.Lk - 1) * 4, lds_addr(ids[buf]));
     };
 
     bool some, all, some_next, all_next;
-    int t = walk.next(of, lane, some, all), buf = 0;
-    if (t >= 0) stage(t, 0);
+    int t = next(some, all), buf = 0;
+    Marks here = uniform_marks(marks, t);
+    if (t >= 0) stage(t, 0, here.live);
 #pragma unroll 1
     while (t >= 0) {
-        const int after = walk.next(of, lane, some_next, all_next);
+        const int after = next(some_next, all_next);
+        const Marks ahead = uniform_marks(marks, after);
         wait_global_loads();
         workgroup_sync();
-        if (after >= 0) stage(after, buf ^ 1);
+        if (after >= 0) stage(after, buf ^ 1, ahead.live);
         if (some) {
             const int ki = img + buf * 2 * L::BYTES, vi = ki + L::BYTES, k0 = t * kTile;
             f32x4 s[QB][NB];
@@ -132,13 +134,11 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) void fwd_kernel(c
             uint64_t seen[QB];
             bool mixed = false;   // the tile's documents are not one
             if (!all) {
-                Marks m{0, 0, 0, 0};
-                if (marks) m = marks[t];
-                mixed = m.dmin != m.dmax;
+                mixed = here.dmin != here.dmax;
 #pragma unroll
                 for (int n = 0; n < QB; ++n) {
-                    seen[n] = bits_between(pos[n] - p.window + 1 - k0, min(pos[n] - p.dlo + 1, p.Lk) - k0) | m.prefix;
-                    if (p.documents) seen[n] = mine[n] >= 0 && (mixed || mine[n] == m.dmin) ? seen[n] & m.live : 0;
+                    seen[n] = bits_between(pos[n] - p.window + 1 - k0, min(pos[n] - p.dlo + 1, p.Lk) - k0) | here.prefix;
+                    if (p.documents) seen[n] = mine[n] >= 0 && (mixed || mine[n] == here.dmin) ? seen[n] & here.live : 0;
                     seen[n] >>= 4 * g;
                 }
             }
@@ -201,7 +201,7 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) void fwd_kernel(c
                     for (int n = 0; n < QB; ++n) out[n][db] = mma<T>(a, w[n][i], out[n][db]);
                 }
         }
-        t = after, some = some_next, all = all_next, buf ^= 1;
+        t = after, some = some_next, all = all_next, here = ahead, buf ^= 1;
     }
 #pragma unroll
     for (int n = 0; n < QB; ++n) {
