@@ -56,7 +56,7 @@ int validate(const seq_problem *p, bool backward) {
     return NA2D_OK;
 }
 
-Args args(const seq_problem *p, const float *slopes, const int32_t *documents, bool prefix) {
+Args args(const seq_problem *p, const float *slopes, const int32_t *documents, bool packed, bool prefix) {
     Args a{};
     a.slopes = slopes, a.documents = documents;
     a.B = p->B, a.heads = p->heads, a.kv = p->kv_heads, a.group = p->heads / p->kv_heads, a.Lq = p->Lq, a.Lk = p->Lk, a.off = p->Lk - p->Lq;
@@ -74,7 +74,7 @@ Args args(const seq_problem *p, const float *slopes, const int32_t *documents, b
         a.m = p->scale == 0.f ? 1e-37f : (float)(log2e * p->scale);   // (0 times what is masked would be no number)
         a.masked = a.m > 0.f ? -INFINITY : INFINITY;
     }
-    a.prefix = prefix;
+    a.packed = packed, a.prefix = prefix;
     a.q_splits = q_splits(a, p->dtype, p->D), a.k_splits = k_splits(a, p->dtype, p->D);
     return a;
 }
@@ -158,10 +158,12 @@ int seq_validate_problem(const seq_problem *p, int backward) { return validate(p
 
 size_t seq_attention_workspace_bytes(const seq_problem *p, int marked, int backward) {
     if (validate(p, backward != 0) != NA2D_OK) return 0;
-    // (documents alone, or with a prefix: the larger)
-    const int64_t plain = Space(args(p, nullptr, nullptr, false), p->D, marked != 0, backward != 0).bytes;
-    const int64_t prefixed = marked ? Space(args(p, nullptr, nullptr, true), p->D, true, backward != 0).bytes : 0;
-    return (size_t)(plain > prefixed ? plain : prefixed);
+    int64_t most = 0;
+    for (int marks = 0; marks < (marked ? 4 : 1); ++marks) {   // documents, a prefix, or both: the largest
+        const int64_t n = Space(args(p, nullptr, nullptr, marks & 1, marks & 2), p->D, marked != 0, backward != 0).bytes;
+        most = n > most ? n : most;
+    }
+    return (size_t)most;
 }
 
 int seq_attention_fwd(const seq_problem *p, const void *q, const void *k, const void *v, const float *slopes, const int32_t *documents, const uint8_t *prefix,
@@ -176,7 +178,7 @@ int seq_attention_fwd(const seq_problem *p, const void *q, const void *k, const 
     if (rest && p->dtype == NA2D_F32) return NA2D_ERR_DTYPE;
     const hipStream_t st = static_cast<hipStream_t>(stream);
     const int e = elem(p->dtype);
-    Args a = args(p, slopes, documents, prefix != nullptr);
+    Args a = args(p, slopes, documents, documents != nullptr, prefix != nullptr);
     a.q = view(q, p->q, e), a.k = view(k, p->k, e), a.v = view(v, p->v, e), a.out = view(out, p->out, e), a.lse = lse, a.rest = static_cast<char *>(rest);
     if (int r = prepare(a, Space(a, p->D, documents || prefix, false), prefix, workspace, workspace_bytes, st)) return r;
     return from_hip(launch_fwd(a, p->dtype, p->D, p->softcap > 0.f, st));
@@ -196,7 +198,7 @@ int seq_attention_bwd(const seq_problem *p, const void *q, const void *k, const 
     if (dq == dk || dq == dv || dk == dv) return NA2D_ERR_ALIAS;
     const hipStream_t st = static_cast<hipStream_t>(stream);
     const int e = elem(p->dtype);
-    Args a = args(p, slopes, documents, prefix != nullptr);
+    Args a = args(p, slopes, documents, documents != nullptr, prefix != nullptr);
     a.q = view(q, p->q, e), a.k = view(k, p->k, e), a.v = view(v, p->v, e), a.out = view(out, p->out, e), a.lse = const_cast<float *>(lse), a.rest = const_cast<char *>(static_cast<const char *>(rest));
     a.dout = view(dout, p->dout, e), a.dq = view(dq, p->dq, e), a.dk = view(dk, p->dk, e), a.dv = view(dv, p->dv, e);
     const Space s(a, p->D, documents || prefix, true);

@@ -5,7 +5,12 @@ namespace seq {
 
 namespace {
 
-constexpr int64_t kWanted = 1024;   // workgroups: two rounds, for in causal order the first keys have the longest work
+// 16 bit: two blocks of 16 keys to a wave, of a pair of waves always, else where that leaves two workgroups to each compute unit.
+bool two_key_blocks(const Args &a, int D) { return D == 128 || (int64_t)a.B * a.kv * ((a.Lk + 127) / 128) >= 512; }
+
+// Workgroups: two rounds, for in causal order the first keys have the longest work; four among documents, whose lengths differ more (8192 tokens of 9 documents,
+// 16 heads, D 128: two 219 us, four 172 and 29 for their sums).
+constexpr int64_t kWanted = 1024;
 
 // kPair: with 128 channels in 16 bit a wave that kept both sums of 32 keys would take more than 256 registers, and run alone on its SIMD.  Two waves share
 // 32 keys instead: each forms P and dS of half of a tile's queries, the first sums dV, the second dK, and each gives the other, through LDS, the half
@@ -15,12 +20,12 @@ constexpr int64_t kWanted = 1024;   // workgroups: two rounds, for in causal ord
 // then leaves fp32 sums, which a last kernel adds in order.
 
 template <typename T, int D> constexpr bool kPair = sizeof(T) == 2 && D == 128;
-template <typename T, int D> constexpr int kKeys = 16 * kBlocks<T> * kWaves / (kPair<T, D> ? 2 : 1);   // of a workgroup
+template <typename T, int D, int KB> constexpr int kKeys = 16 * KB * kWaves / (kPair<T, D> ? 2 : 1);   // of a workgroup
 
-template <typename T, int D, bool CAP, bool SLOPES>
+template <typename T, int D, bool CAP, bool SLOPES, int KB>
 __global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) void bwd_kv_kernel(const Args p) {
     using L = Tile<T, D>;
-    constexpr int KB = kBlocks<T>, RB = kRowBlocks<T>, NB = kTile / 16;
+    constexpr int RB = kRowBlocks<T>, NB = kTile / 16;
     constexpr bool PAIR = kPair<T, D>;
     extern __shared__ __align__(16) char lds[];
     __shared__ __align__(16) int ids[2][kTile];
@@ -29,13 +34,13 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) void bwd_kv_kerne
     __shared__ __align__(16) u32x4 given[PAIR ? kWaves : 1][KB][PAIR ? kWave : 1];
     const int tid = threadIdx.x, lane = tid % kWave, wave = uniform(tid / kWave), j = lane & 15, g = lane >> 4;
     const int role = PAIR ? wave & 1 : 0, group_of_keys = PAIR ? wave >> 1 : wave;
-    const int tiles = (p.Lk + kKeys<T, D> - 1) / kKeys<T, D>;
+    const int tiles = (p.Lk + kKeys<T, D, KB> - 1) / kKeys<T, D, KB>;
     int id = block_in_order();
     const int split = id % p.k_splits;
     id /= p.k_splits;
     const int tile = id % tiles, plane = id / tiles, b = plane / p.kv, kh = plane % p.kv;
     const char *kp = p.k.at + b * p.k.b + kh * p.k.h, *vp = p.v.at + b * p.v.b + kh * p.v.h;
-    const int k0 = tile * kKeys<T, D>, kw = k0 + group_of_keys * 16 * KB;
+    const int k0 = tile * kKeys<T, D, KB>, kw = k0 + group_of_keys * 16 * KB;
     const int img = lds_addr(lds);
     const int *documents = p.documents ? p.documents + (int64_t)b * p.Lk : nullptr;
     const Marks *marks = p.marks ? p.marks + (int64_t)b * p.key_tiles : nullptr;
@@ -79,14 +84,16 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) void bwd_kv_kerne
         dg.lo = uniform(dg.lo), dg.hi = uniform(dg.hi);
         if (kScaled<T> && most != kNothing) power = uniform(most);
     }
-    const int ka = k0, kb = min(k0 + kKeys<T, D>, p.Lk) - 1;
+    const int ka = k0, kb = min(k0 + kKeys<T, D, KB>, p.Lk) - 1;
     const int wa = min(kw, p.Lk - 1), wb = min(kw + 16 * KB, p.Lk) - 1;
-    auto of = [&](int t) {
+    auto of = [&](int t, Marks &m) {   // (of a tile of queries: their positions begin inside a tile of keys)
         const int qa = t * kTile + p.off, qb = min(t * kTile + kTile, p.Lq) - 1 + p.off;
         bool any = near_any(p, qa, qb, ka, kb) || prefix_any, some = near_any(p, qa, qb, wa, wb) || prefix_some, all = near_all(p, qa, qb, wa, wb) || prefix_all;
         if (documents) {
             const Marks x = marks[qa / kTile], y = marks[min((qa + kTile - 1) / kTile, p.key_tiles - 1)];
-            const Docs d{min(x.dmin, y.dmin), max(x.dmax, y.dmax), (x.live & y.live) == ~0ull};
+            const int in = qa % kTile;
+            m = Marks{min(x.dmin, y.dmin), max(x.dmax, y.dmax), in ? x.live >> in | y.live << (kTile - in) : x.live, 0};
+            const Docs d{m.dmin, m.dmax, (x.live & y.live) == ~0ull};
             any &= d.meet(dg), some &= d.meet(dw), all &= d.same(dw);
         }
         return (any ? 1 : 0) | (some ? 2 : 0) | (all ? 4 : 0);
@@ -104,17 +111,6 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) void bwd_kv_kerne
 #pragma unroll
         for (int db = 0; db < L::DB; ++db) dk[n][db] = dv[n][db] = f32x4{0.f, 0.f, 0.f, 0.f};
 
-    // Of a tile's queries, whose positions begin inside a tile of keys: the documents, and which are there.
-    auto marks_of = [&](int t) {
-        Marks m{0, 0, 0, 0};
-        if (documents && t >= 0) {
-            const int at = t * kTile + p.off, in = at % kTile;
-            const Marks x = uniform_marks(marks, at / kTile), y = uniform_marks(marks, min((at + kTile - 1) / kTile, p.key_tiles - 1));
-            m = Marks{min(x.dmin, y.dmin), max(x.dmax, y.dmax), x.live >> in, 0};
-            if (in) m.live |= y.live << (kTile - in);
-        }
-        return m;
-    };
     auto stage = [&](int h, int t, int buf, uint64_t live) {
         const int to = img + buf * 2 * L::BYTES;
         const char *zeros = documents ? p.zeros : nullptr;
@@ -134,21 +130,20 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) void bwd_kv_kerne
     }
     Walk walk(first, last, skip);
     bool some, all, some_next = false, all_next = false;
-    auto next = [&](bool &s, bool &a) {
+    auto next = [&](bool &s, bool &a, Seen &marks_of) {
         while (head < p.group && left > 0) {
-            const int t = walk.next(of, lane, s, a);
+            const int t = walk.next(of, lane, s, a, marks_of);
             if (t >= 0) return --left, t;
             if (++head < p.group) walk = Walk(first, last);
         }
         return -1;
     };
-    int t = next(some, all), buf = 0, h = kh * p.group + head;
-    Marks m = marks_of(t);
-    if (t >= 0) stage(h, t, 0, m.live);
+    Seen here{}, ahead{};
+    int t = next(some, all, here), buf = 0, h = kh * p.group + head;
+    if (t >= 0) stage(h, t, 0, here.live);
 #pragma unroll 1
     while (t >= 0) {
-        const int after = next(some_next, all_next);
-        const Marks ahead = marks_of(after);
+        const int after = next(some_next, all_next, ahead);
         wait_global_loads();
         workgroup_sync();
         if (after >= 0) stage(kh * p.group + head, after, buf ^ 1, ahead.live);
@@ -157,11 +152,11 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) void bwd_kv_kerne
         uint64_t seen[KB];
         bool mixed = false;   // the tile's documents are not one (what is not live has no weights anyway)
         if (some && !all) {
-            mixed = m.dmin != m.dmax;
+            mixed = here.mixed;
 #pragma unroll
             for (int n = 0; n < KB; ++n) {
                 seen[n] = always[n] ? ~0ull : bits_between(key[n] + p.dlo - q0, min(key[n] + p.window, kFar) - q0);
-                if (documents) seen[n] = mine[n] >= 0 && (mixed || mine[n] == m.dmin) ? seen[n] : 0;
+                if (documents) seen[n] = mine[n] >= 0 && (mixed || mine[n] == here.doc) ? seen[n] : 0;
                 seen[n] >>= 4 * g;
             }
         }
@@ -264,7 +259,7 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) void bwd_kv_kerne
                 }
             }
         }
-        t = after, h = kh * p.group + head, some = some_next, all = all_next, m = ahead, buf ^= 1;
+        t = after, h = kh * p.group + head, some = some_next, all = all_next, here = ahead, buf ^= 1;
     }
     // which: 0 dK, 1 dV
     auto store = [&](int which, const f32x4 *acc, float by, int i) {
@@ -290,20 +285,22 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) void bwd_kv_kerne
 }
 
 template <typename T, int D, bool CAP> struct BwdKV {
-    static hipError_t go(const Args &a, hipStream_t st) { return a.slopes ? launch<true>(a, st) : launch<false>(a, st); }
-    template <bool SLOPES> static hipError_t launch(const Args &a, hipStream_t st) {
+    template <bool SLOPES, int KB> static hipError_t launch(const Args &a, hipStream_t st) {
         constexpr int lds = 4 * Tile<T, D>::BYTES;
         static LdsAllowed allowed;
-        if (hipError_t e = allow_lds(bwd_kv_kernel<T, D, CAP, SLOPES>, lds, allowed); e != hipSuccess) return e;
-        const int64_t blocks = (int64_t)a.B * a.kv * ((a.Lk + kKeys<T, D> - 1) / kKeys<T, D>) * a.k_splits;
+        if (hipError_t e = allow_lds(bwd_kv_kernel<T, D, CAP, SLOPES, KB>, lds, allowed); e != hipSuccess) return e;
+        const int64_t blocks = (int64_t)a.B * a.kv * ((a.Lk + kKeys<T, D, KB> - 1) / kKeys<T, D, KB>) * a.k_splits;
         if (!launch_holds(blocks, kThreads)) return hipErrorInvalidValue;
-        bwd_kv_kernel<T, D, CAP, SLOPES><<<(unsigned)blocks, kThreads, lds, st>>>(a);
+        bwd_kv_kernel<T, D, CAP, SLOPES, KB><<<(unsigned)blocks, kThreads, lds, st>>>(a);
         if (hipError_t e = hipGetLastError(); e != hipSuccess || a.k_splits == 1) return e;
         return join<T, D>(a.parts, a.k_splits, a.B, a.kv, a.Lk, a.dk, &a.dv, st);
     }
-};
-template <typename T, int D, bool CAP> struct Keys {
-    static hipError_t go(int &keys) { return keys = kKeys<T, D>, hipSuccess; }
+    static hipError_t go(const Args &a, hipStream_t st) {
+        if constexpr (sizeof(T) == 2)
+            if (two_key_blocks(a, D)) return a.slopes ? launch<true, 2>(a, st) : launch<false, 2>(a, st);
+        if constexpr (!kPair<T, D>) return a.slopes ? launch<true, 1>(a, st) : launch<false, 1>(a, st);
+        return hipErrorInvalidValue;   // (a pair keeps two blocks)
+    }
 };
 
 }  // namespace
@@ -312,10 +309,10 @@ hipError_t launch_bwd_kv(const Args &a, int dtype, int D, bool capped, hipStream
 
 
 int k_splits(const Args &a, int dtype, int D) {
-    int keys = 64;
-    (void)dispatch<Keys>(dtype, D, false, keys);
+    const int keys = dtype != NA2D_F32 && D < 128 && two_key_blocks(a, D) ? 128 : 64;
     const int64_t reach = (int64_t)a.window + keys;   // queries of one head that a tile of keys can meet, but for prefixes
-    return parts_of((int64_t)a.B * a.kv * ((a.Lk + keys - 1) / keys), kWanted, (a.prefix || reach > a.Lq ? a.query_tiles : reach / kTile + 2) * a.group, (int64_t)a.B * a.kv * a.Lk * D * 8);
+    return parts_of((int64_t)a.B * a.kv * ((a.Lk + keys - 1) / keys), a.packed ? 2 * kWanted : kWanted, (a.prefix || reach > a.Lq ? a.query_tiles : reach / kTile + 2) * a.group,
+                    (int64_t)a.B * a.kv * a.Lk * D * 8);
 }
 
 }  // namespace seq

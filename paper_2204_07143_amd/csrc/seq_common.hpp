@@ -53,7 +53,7 @@ struct Args {
     int B, heads, kv, group, Lq, Lk, off;   // off: Lk - Lq
     int key_tiles, query_tiles;
     int causal, window;    // window: kFar where there is none
-    int prefix;            // marks hold prefix bits
+    int prefix, packed;    // marks hold prefix bits, documents
     int dlo;               // smallest distance that the order and the window allow; the largest is window - 1
     float scale;
     float c;               // capped: 2 scale log2(e) / cap
@@ -228,13 +228,6 @@ __device__ __forceinline__ int wave_max(int x) {
     return x;
 }
 __device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
-__device__ __forceinline__ uint64_t uniform(uint64_t x) { return (uint64_t)(uint32_t)uniform((int)(uint32_t)x) | (uint64_t)(uint32_t)uniform((int)(uint32_t)(x >> 32)) << 32; }
-// A tile's marks in scalar registers.  Read before the wait for a tile's loads: behind the next tile's, which the compiler does not count, every use would wait for all of them.
-__device__ __forceinline__ Marks uniform_marks(const Marks *marks, int t) {
-    if (!marks || t < 0) return Marks{0, 0, 0, 0};
-    const Marks m = marks[t];
-    return Marks{uniform(m.dmin), uniform(m.dmax), uniform(m.live), uniform(m.prefix)};
-}
 // of the wave's tokens; `there` false: no token in this lane
 __device__ __forceinline__ Docs docs_of_wave(int d, bool there) {
     const bool live = there && d >= 0;
@@ -242,20 +235,33 @@ __device__ __forceinline__ Docs docs_of_wave(int d, bool there) {
     return r;
 }
 
-// Walks the tiles first .. last that `of` says something about: a lane looks at one tile, 64 at a time.  of(tile) gives bits: 1 any pair of the
-// workgroup's is seen, 2 any pair of this wave's, 4 every pair of this wave's.  The first bit must not differ between waves.
+// What of a tile's marks the masks take.
+struct Seen {
+    int doc;               // the tile's document, if it is one
+    bool mixed;            // it is not
+    uint64_t live, prefix;
+};
+
+// Walks the tiles first .. last that `of` says something about: a lane looks at one tile, 64 at a time.  of(tile, marks) gives bits: 1 any pair of the
+// workgroup's is seen, 2 any pair of this wave's, 4 every pair of this wave's.  The first bit must not differ between waves.  The lane keeps its tile's marks:
+// read from memory when their tile's turn comes, they would be waited for behind the loads of another tile.
 struct Walk {
-    uint64_t todo, mine, whole;
+    uint64_t todo, mine, whole, mixed;
+    int doc;
+    uint64_t live, prefix;
     int base, last, skip;   // skip: how many of them to leave out before the first
-    __device__ __forceinline__ Walk(int first, int last_, int skip_ = 0) : todo(0), mine(0), whole(0), base(first - kWave), last(last_), skip(skip_) {}
-    template <class F> __device__ __forceinline__ int next(F of, int lane, bool &is_mine, bool &is_whole) {
+    __device__ __forceinline__ Walk(int first, int last_, int skip_ = 0) : todo(0), mine(0), whole(0), mixed(0), doc(0), live(0), prefix(0), base(first - kWave), last(last_), skip(skip_) {}
+    template <class F> __device__ __forceinline__ int next(F of, int lane, bool &is_mine, bool &is_whole, Seen &seen) {
         while (!todo) {
             base += kWave;
             if (base > last) return -1;
-            const int bits = base + lane <= last ? of(base + lane) : 0;
+            Marks m{0, 0, 0, 0};
+            const int bits = base + lane <= last ? of(base + lane, m) : 0;
+            doc = m.dmin, live = m.live, prefix = m.prefix;
             todo = __ballot(bits & 1);
             mine = __ballot(bits & 2);
             whole = __ballot(bits & 4);
+            mixed = __ballot(m.dmin != m.dmax);
             const int n = __builtin_popcountll(todo), out = min(skip, n);
             skip -= out;
             if (out == n) todo = 0;
@@ -265,12 +271,19 @@ struct Walk {
         todo &= todo - 1;
         is_mine = mine >> i & 1;
         is_whole = whole >> i & 1;
+        seen = {__builtin_amdgcn_readlane(doc, i), (bool)(mixed >> i & 1), lane64(live, i), lane64(prefix, i)};
         return base + i;
+    }
+    __device__ static __forceinline__ uint64_t lane64(uint64_t x, int i) {
+        return (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)x, i) | (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)(x >> 32), i) << 32;
     }
     // how many there are
     template <class F> __device__ static __forceinline__ int count(int first, int last, F of, int lane) {
         int n = 0;
-        for (int base = first; base <= last; base += kWave) n += __builtin_popcountll(__ballot(base + lane <= last ? of(base + lane) & 1 : 0));
+        for (int base = first; base <= last; base += kWave) {
+            Marks m;
+            n += __builtin_popcountll(__ballot(base + lane <= last ? of(base + lane, m) & 1 : 0));
+        }
         return n;
     }
 };

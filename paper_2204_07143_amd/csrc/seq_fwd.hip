@@ -59,11 +59,11 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) void fwd_kernel(c
     const int qa = min(q0, p.Lq - 1) + p.off, qb = min(q0 + 16 * QB * kWaves, p.Lq) - 1 + p.off;
     const int wa = min(qw, p.Lq - 1) + p.off, wb = min(qw + 16 * QB, p.Lq) - 1 + p.off;   // (a wave past the end: the last query)
     const Marks *marks = p.marks ? p.marks + (int64_t)b * p.key_tiles : nullptr;
-    auto of = [&](int t) {
+    auto of = [&](int t, Marks &m) {
         const int ka = t * kTile, kb = min(ka + kTile, p.Lk) - 1;
         bool any = near_any(p, qa, qb, ka, kb), some = near_any(p, wa, max(wa, wb), ka, kb), all = near_all(p, wa, max(wa, wb), ka, kb) && ka + kTile <= p.Lk;
         if (marks) {
-            const Marks m = marks[t];
+            m = marks[t];
             const Docs d{m.dmin, m.dmax, m.live == ~0ull};
             any |= m.prefix != 0, some |= m.prefix != 0, all |= m.prefix == ~0ull;
             if (p.documents) any &= d.meet(dg), some &= d.meet(dw), all &= d.same(dw);
@@ -81,7 +81,7 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) void fwd_kernel(c
         skip = split * left;
     }
     Walk walk(first, last, skip);
-    auto next = [&](bool &some, bool &all) { return left-- > 0 ? walk.next(of, lane, some, all) : -1; };
+    auto next = [&](bool &some, bool &all, Seen &marks_of) { return left-- > 0 ? walk.next(of, lane, some, all, marks_of) : -1; };
 
     const typename L::RowReader rows(lane);
     const typename L::ColumnReader columns(lane);
@@ -106,13 +106,12 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) void fwd_kernel(c
     };
 
     bool some, all, some_next, all_next;
-    int t = next(some, all), buf = 0;
-    Marks here = uniform_marks(marks, t);
+    Seen here{}, ahead{};
+    int t = next(some, all, here), buf = 0;
     if (t >= 0) stage(t, 0, here.live);
 #pragma unroll 1
     while (t >= 0) {
-        const int after = next(some_next, all_next);
-        const Marks ahead = uniform_marks(marks, after);
+        const int after = next(some_next, all_next, ahead);
         wait_global_loads();
         workgroup_sync();
         if (after >= 0) stage(after, buf ^ 1, ahead.live);
@@ -134,11 +133,11 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) void fwd_kernel(c
             uint64_t seen[QB];
             bool mixed = false;   // the tile's documents are not one
             if (!all) {
-                mixed = here.dmin != here.dmax;
+                mixed = here.mixed;
 #pragma unroll
                 for (int n = 0; n < QB; ++n) {
                     seen[n] = bits_between(pos[n] - p.window + 1 - k0, min(pos[n] - p.dlo + 1, p.Lk) - k0) | here.prefix;
-                    if (p.documents) seen[n] = mine[n] >= 0 && (mixed || mine[n] == here.dmin) ? seen[n] & here.live : 0;
+                    if (p.documents) seen[n] = mine[n] >= 0 && (mixed || mine[n] == here.doc) ? seen[n] & here.live : 0;
                     seen[n] >>= 4 * g;
                 }
             }
