@@ -10,7 +10,7 @@
  *    enqueue kernels (nothing else) on `stream`.  Outputs are fully overwritten.  Results are bitwise reproducible.
  *  - q, out, dout, dq: [B, heads, Lq, D]; k, v, dk, dv: [B, kv_heads, Lk, D] in the problem dtype, each with strides of its own
  *    (in elements) for batch, head and row; the D elements of a row are contiguous.  Pointers are 16-byte aligned and strides
- *    are multiples of 16 bytes.  Query head h reads key head h / (heads / kv_heads).
+ *    are multiples of 16 bytes; an input's may be 0, and no two rows of an output overlap.  Query head h reads key head h / (heads / kv_heads).
  *  - D in {32, 64, 128}; f32, f16, bf16.  Products, softmax statistics and sums are fp32; in the 16-bit types the weights, and
  *    in the backward pass their gradients, are rounded to the type where they enter a product.
  *  - Return value: NA2D_OK or a negative na2d_status; argument errors are detected on the host before any HIP call.
@@ -93,7 +93,8 @@ int seq_cache_validate(const seq_cache_problem *p, int call);
 /* Writes k, v [B, kv_heads, n, D] (strides p->q and p->out) at positions lengths[b] .. of every sequence; counts (nullable): int32 [B], how many of the n are
  * taken (at most n; 0 leaves the sequence alone).  A page's scale becomes the larger of the old one and its new tokens' largest magnitude / 127; where it grows, the
  * tokens that the page held are rounded again, to nearest even, on the new scale.  The first token of a page starts it afresh.  A NaN is
- * stored as 0, an infinity as the largest finite fp32 value.  lengths is not changed.  Two sequences must not append to the same page in one call. */
+ * stored as 0, an infinity as the largest finite fp32 value.  lengths is not changed.  A page must not be appended to twice in
+ * one call (by two sequences, or through two entries of a table): which of the values it then holds is not defined. */
 int seq_cache_append(const seq_cache_problem *p, const void *k, const void *v, const int32_t *table, const int32_t *lengths, const int32_t *counts,
                      int8_t *k_pages, int8_t *v_pages, float *k_scales, float *v_scales, void *stream);
 

@@ -1,4 +1,5 @@
 // C ABI of the attention over token sequences and of its cache: argument validation (host only, before any HIP call) and dispatch.
+#include <algorithm>
 #include <cmath>
 #include <initializer_list>
 
@@ -14,13 +15,23 @@ int from_hip(hipError_t e) {
     (void)hipGetLastError();   // leave no stale error behind for the caller's next HIP call
     return NA2D_ERR_LAUNCH;
 }
-// strides of a tensor [., ., rows, D]: whole multiples of 16 bytes, none negative, a plane below 2^31 bytes, an offset to any plane below 2^62 bytes
-int check_strides(const seq_strides &s, int64_t B, int64_t heads, int64_t rows, int64_t D, int e) {
+// strides of a tensor [B, heads, rows, D]: whole multiples of 16 bytes, none negative, a plane below 2^31 bytes, an offset to any plane below 2^60 bytes; of one
+// that is written, no two rows in the same place: in order of size, each stride reaches over all that the smaller ones span
+int check_strides(const seq_strides &s, int64_t B, int64_t heads, int64_t rows, int64_t D, int e, bool written) {
     for (int64_t x : {s.batch, s.head, s.row}) {
         if (x < 0 || x > ((int64_t)1 << 45)) return NA2D_ERR_SHAPE;
         if (x * e % 16) return NA2D_ERR_ALIGN;
     }
     if (((rows - 1) * s.row + D) * e > (int64_t)INT32_MAX || B > ((int64_t)1 << 24) || heads > ((int64_t)1 << 16)) return NA2D_ERR_SHAPE;
+    if ((double)(B - 1) * s.batch + (double)(heads - 1) * s.head > 0x1p58) return NA2D_ERR_SHAPE;
+    if (!written) return NA2D_OK;
+    struct Dim { int64_t stride, last; } dims[3] = {{s.batch, B - 1}, {s.head, heads - 1}, {s.row, rows - 1}};
+    std::sort(dims, dims + 3, [](const Dim &a, const Dim &b) { return a.stride < b.stride; });
+    int64_t span = D;
+    for (const Dim &d : dims) {
+        if (d.last && d.stride < span) return NA2D_ERR_ALIAS;
+        span += d.last * d.stride;
+    }
     return NA2D_OK;
 }
 View view(const void *at, const seq_strides &s, int e) { return {static_cast<const char *>(at), s.batch * e, s.head * e, (int)(s.row * e)}; }
@@ -40,16 +51,13 @@ int validate(const seq_problem *p, bool backward) {
     if (int e = common(p->B, p->heads, p->kv_heads, p->D, p->dtype, p->scale, p->softcap, p->window)) return e;
     if (p->Lq <= 0 || p->Lk <= 0 || p->Lq > 1 << 24 || p->Lk > 1 << 24 || (p->causal != 0 && p->causal != 1)) return NA2D_ERR_SHAPE;
     const int e = elem(p->dtype);
-    for (const seq_strides *s : {&p->q, &p->out})
-        if (int r = check_strides(*s, p->B, p->heads, p->Lq, p->D, e)) return r;
-    for (const seq_strides *s : {&p->k, &p->v})
-        if (int r = check_strides(*s, p->B, p->kv_heads, p->Lk, p->D, e)) return r;
-    if (backward) {
-        for (const seq_strides *s : {&p->dout, &p->dq})
-            if (int r = check_strides(*s, p->B, p->heads, p->Lq, p->D, e)) return r;
-        for (const seq_strides *s : {&p->dk, &p->dv})
-            if (int r = check_strides(*s, p->B, p->kv_heads, p->Lk, p->D, e)) return r;
-    }
+    const auto of_queries = [&](const seq_strides &s, bool written) { return check_strides(s, p->B, p->heads, p->Lq, p->D, e, written); };
+    const auto of_keys = [&](const seq_strides &s, bool written) { return check_strides(s, p->B, p->kv_heads, p->Lk, p->D, e, written); };
+    for (int r : {of_queries(p->q, false), of_keys(p->k, false), of_keys(p->v, false), of_queries(p->out, true)})
+        if (r) return r;
+    if (backward)
+        for (int r : {of_queries(p->dout, false), of_queries(p->dq, true), of_keys(p->dk, true), of_keys(p->dv, true)})
+            if (r) return r;
     // every launch of the passes (the smallest tiles: 64 rows) holds its workgroups
     const int64_t q_tiles = ((int64_t)p->Lq + kTile - 1) / kTile, k_tiles = ((int64_t)p->Lk + kTile - 1) / kTile;
     if (!launch_holds((int64_t)p->B * p->heads * q_tiles, kThreads) || !launch_holds((int64_t)p->B * p->kv_heads * k_tiles, kThreads)) return NA2D_ERR_SHAPE;
@@ -126,8 +134,8 @@ int cache_validate(const seq_cache_problem *p, int call) {
     if (p->page != 16 && p->page != 32 && p->page != 64 && p->page != 128) return NA2D_ERR_SHAPE;
     if (p->pages <= 0 || p->table_width <= 0 || p->n <= 0 || p->n > 1 << 24 || (int64_t)p->table_width * p->page > kFar) return NA2D_ERR_SHAPE;
     const int heads = call == SEQ_CACHE_ATTENTION ? p->heads : p->kv_heads, e = elem(p->dtype);
-    for (const seq_strides *s : {&p->q, &p->out})
-        if (int r = check_strides(*s, p->B, heads, p->n, p->D, e)) return r;
+    if (int r = check_strides(p->q, p->B, heads, p->n, p->D, e, call == SEQ_CACHE_GATHER)) return r;
+    if (int r = check_strides(p->out, p->B, heads, p->n, p->D, e, call != SEQ_CACHE_APPEND)) return r;
     if (call == SEQ_CACHE_ATTENTION && (int64_t)p->heads / p->kv_heads * p->n > 1 << 24) return NA2D_ERR_SHAPE;
     return NA2D_OK;
 }

@@ -370,7 +370,7 @@ class SeqCache(NamedTuple):
 def seq_cache_append(cache: SeqCache, k, v, table, lengths, counts=None) -> None:
     """Puts ``k``, ``v`` [B, kv_heads, n, D] behind the ``lengths`` (int32 [B]) tokens of each sequence, the first ``counts[b]`` of the n where ``counts``
     (int32 [B]) is given.  A page's scale grows with its largest value; what it held is then rounded again.  ``lengths`` stays as it is.  No page may be
-    appended to by two sequences of one call; a page number that is none is passed over."""
+    appended to twice in one call; a page number that is none is passed over."""
     if _native().seq_cache_append(*cache, k, v, table, lengths, counts):
         return
     if k.dim() != 4 or v.dim() != 4:

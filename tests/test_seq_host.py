@@ -89,6 +89,28 @@ def test_cache_arguments():
     assert lib.seq_cache_gather(ctypes.byref(p), *at[:6], None, at[8], at[9], None) == -1
 
 
+@pytest.mark.parametrize("strides,ok", [   # batch, head, row of [2, 4, 100, 64]
+    ((25600, 6400, 64), True), ((25600, 64, 256), True), ((6400, 12800, 64), True), ((64, 128, 512), True), ((51200, 6400, 64), True),
+    ((0, 6400, 64), False), ((25600, 0, 64), False), ((25600, 6400, 0), False), ((25600, 6400, 32), False), ((25600, 6392, 64), False), ((6400, 6400, 64), False), ((25600, 64, 248), False),
+    ((19200, 6400, 64), False),
+])
+def test_rows_of_outputs_do_not_overlap(strides, ok):
+    code = 0 if ok else -10
+    for name in ("q", "k", "v", "dout"):
+        assert na.seq_validate_problem(P(kv=4, **{name: na.SeqStrides(*strides)}), True) == 0
+    for name in ("out", "dq", "dk", "dv"):
+        assert na.seq_validate_problem(P(kv=4, **{name: na.SeqStrides(*strides)}), True) == code
+    rows = na.SeqStrides(*strides)
+    assert tuple(na.seq_cache_validate(C(kv=4, n=100, rows=rows), call) for call in range(3)) == (0, code, code)
+
+
+def test_strides_of_one_row_do_not_count():
+    zero = na.SeqStrides(0, 0, 0)
+    assert na.seq_validate_problem(P(B=1, heads=1, kv=1, Lq=1, Lk=1, **{n: zero for n in ("out", "dq", "dk", "dv")}), True) == 0
+    assert na.seq_validate_problem(P(out=na.SeqStrides(1 << 45, 1 << 45, 64), B=1, heads=1, kv=1)) == 0
+    assert na.seq_validate_problem(P(q=na.SeqStrides(1 << 45, 64, 64), B=1 << 20)) == -6   # no such address
+
+
 def test_python_arguments():
     x = lambda *s, **k: torch.zeros(s, **k)
     q, kv = x(2, 4, 10, 32), x(2, 2, 10, 32)
