@@ -99,7 +99,7 @@ __global__ __launch_bounds__(kThreads, RT == 1 ? 3 : 2) void decode_kernel(const
     const int kh = id % p.kv, b = id / p.kv, page = PAGE16 ? 16 : 1 << p.page_log2;
     const int all_rows = p.group * p.n, row0 = rg * ROWS;
     const int64_t most_tokens = (int64_t)p.width << p.page_log2;
-    const int length = (int)min((int64_t)p.lengths[b], most_tokens), first_query = p.lengths[b] - p.n;
+    const int tokens = max(p.lengths[b], 0), length = (int)min((int64_t)tokens, most_tokens), first_query = tokens - p.n;
 
     // rows as fp16 on a power of two of their own
     u32x4 q[RT][S::STEPS];
@@ -134,7 +134,7 @@ __global__ __launch_bounds__(kThreads, RT == 1 ? 3 : 2) void decode_kernel(const
     }
 
     // the range that any row sees, in steps, and this workgroup's part of it
-    const int begin = max(0, first_query - p.window + 1) / kStep, end = length > 0 ? (length + kStep - 1) / kStep : 0;
+    const int begin = max(0, first_query - p.window + 1) / kStep, end = (length + kStep - 1) / kStep;
     const int each = max(0, (end - begin + p.splits - 1) / p.splits), from = begin + split * each, to = min(end, from + each);
 
     f32x4 out[RT][S::DB];

@@ -305,3 +305,50 @@ def test_work_split_along_the_keys_and_the_queries(dtype, Lq, Lk, name):
     if name != "causal_window":
         assert na.seq_attention_workspace_bytes(p, "docs" in mask) > 4 * q.numel()   # (it is split)
     _check(Lq, 1, 4, 2, Lq, Lk, D, dtype, **mask)
+
+
+def test_offsets_that_pass_32_bits():
+    """Planes behind 2^32 bytes: the last tokens of the last heads see, through a window, the last keys alone."""
+    L, D, last, window = 1 << 17, 128, 10, 64
+    torch.manual_seed(17)
+    q, dout = (torch.randn((3, 44, L, D), dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    k, v = (torch.randn((3, 22, L, D), dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    assert q.numel() * 2 > 1 << 32
+    got = _run(q, k, v, dout, causal=True, window=window)
+    reach = last + window - 1
+    ends = q[2:, 42:, -last:], k[2:, 21:, -reach:], v[2:, 21:, -reach:], dout[2:, 42:, -last:]
+    want, bound = expect(*ends, "bf16", causal=True, window=window)
+    for name, x in zip(("out", "dq", "dk", "dv"), got):   # (of a key, all queries that see it stand behind it)
+        check(name, x[2:, -want[name].shape[1]:, -last:], want[name][:, :, -last:], bound[name][:, :, -last:])
+
+
+@TYPE
+def test_broadcast_gradients_and_queries(dtype):
+    """What is broadcast to a call is read where it lies, or copied: a gradient that is one number, queries that heads and sequences share."""
+    g = np.random.default_rng(18)
+    q, k, v = normal(g, (1, 1, 50, 64), dtype), *(normal(g, (2, 2, 50, 64), dtype) for _ in range(2))
+    wide = q.expand(2, 4, 50, 64)
+    one = torch.ones((), dtype=TYPES[dtype], device="cuda").expand(2, 4, 50, 64)
+    row = normal(g, (1, 1, 1, 64), dtype).expand(2, 4, 50, 64)
+    for dout in (one, row):
+        for a, b in zip(_run(wide, k, v, dout, causal=True), _run(wide.contiguous(), k, v, dout.contiguous(), causal=True)):
+            assert torch.equal(a, b)
+
+
+@TYPE
+def test_two_calls_at_once(dtype):
+    g = np.random.default_rng(19)
+    sets = [[normal(g, (1, 4, 900, 64), dtype) for _ in range(4)] for _ in range(2)]
+    masks = [dict(zip(("documents", "prefix"), _marks(g, 1, 900, 3, True))) for _ in range(2)]
+    want = [_run(*x, causal=True, **m) for x, m in zip(sets, masks)]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    got = [[], []]
+    for _ in range(3):
+        for i, stream in enumerate(streams):
+            with torch.cuda.stream(stream):
+                got[i].append(_run(*sets[i], causal=True, **masks[i]))
+    torch.cuda.synchronize()
+    for i in range(2):
+        for outs in got[i]:
+            assert all(torch.equal(a, b) for a, b in zip(outs, want[i]))

@@ -291,3 +291,49 @@ def test_rows_behind_the_counts_are_left_as_they_are():
     x = normal(g, (2, 1, 9, 32), "f32")
     F.seq_cache_append(cache, x, x, _int([[0, 1], [2, 3]]), _int([3, -1]), _int([4, 9]))
     assert np.array_equal(cache.k_pages[1:].cpu().numpy(), host[0][1:]) and np.array_equal(cache.k_pages[0, :, 7:].cpu().numpy(), host[0][0, :, 7:])
+
+
+def test_pages_behind_32_bits():
+    """Cells whose offsets pass 2^32 bytes: the same as in a small cache."""
+    g = np.random.default_rng(9)
+    kv, page, D, n = 8, 64, 128, 150
+    small_table, pages = _table(g, [400, 7 + n], page, spare=0)
+    _, small = _cache(g, pages, kv, page, D)
+    far = 70000 - 1 - 3 * np.arange(pages)   # of 64 KiB each, from 2^32 bytes on
+    assert far.min() * kv * page * D > 1 << 32
+    where = torch.from_numpy(far).cuda()
+    large = F.SeqCache(*(torch.empty((70000, *x.shape[1:]), dtype=x.dtype, device="cuda") for x in small))
+    for a, b in zip(large, small):
+        a[where] = b
+    table = np.where(small_table >= 0, far[small_table], -1)
+    tables, lengths = [_int(x.tolist()) for x in (small_table, table)], _int([400 - n, 7])
+    k, v = (normal(g, (2, kv, n, D), "bf16") for _ in range(2))
+    q = normal(g, (2, 16, 3, D), "bf16")
+    results = []
+    for cache, t in zip((small, large), tables):
+        F.seq_cache_append(cache, k, v, t, lengths)
+        results.append((*F.seq_cache_gather(cache, t, lengths + n, _int([0, -5]), 400), F.seq_cache_attention(q, cache, t, lengths + n)))
+    for a, b in zip(large, small):
+        assert torch.equal(a[where], b)
+    for a, b in zip(*results):
+        assert torch.equal(a, b)
+
+
+def test_counts_and_lengths_out_of_range():
+    """Counts above n are n; of negative counts and lengths nothing is stored or seen; what lies past the table has no page."""
+    g = np.random.default_rng(10)
+    big = 2 ** 31 - 1
+    table = np.array([[0, 1], [2, 3], [4, 5], [6, 7]], np.int32)
+    host, cache = _cache(g, 8, 2, 16, 32)
+    x = normal(g, (4, 2, 9, 32), "f16")
+    F.seq_cache_append(cache, x, x, _int(table.tolist()), _int([0, -5, big, 4]), _int([big, 9, 9, -big - 1]))
+    for i in (0, 1):
+        host[i], host[i + 2] = seq_oracle.append(host[i], host[i + 2], x.float().cpu().numpy()[:1], table[:1], [0])
+    _same(cache, host)
+    k, _ = F.seq_cache_gather(cache, _int(table.tolist()), _int([9, -5, big, 32]), _int([big - 3, -big - 1, 28, 28]), 9, dtype=torch.float32)
+    want = seq_oracle.gather(host[0], host[2], table, [9, 0, 32, 32], [40, 0, 28, 28], 9)
+    assert np.abs(k.cpu().numpy() - want).max() <= 2 * FP32 * np.abs(want).max()
+    q = normal(g, (4, 4, 2, 32), "f16")
+    got = F.seq_cache_attention(q, cache, _int(table.tolist()), _int([9, -5, -big - 1, 0]))
+    _check_attention(got[:1], q[:1], host, table[:1], [9], "f16")
+    assert (got[1:] == 0).all()
