@@ -37,17 +37,17 @@ typedef uint32_t w2 __attribute__((ext_vector_type(2)));
 
 template <int D, bool STREAM> struct Keys {
     uint32_t k[2][2 * (D / 32)];
-    __device__ __forceinline__ void load(int i, const int8_t *at, int lane) {
-        const int j = lane & 15, g = lane >> 4;
+    __device__ static __forceinline__ unsigned offset(int lane) { return (unsigned)((lane & 15) * D + (lane >> 4) * (D >= 64 ? 16 : 8)); }
+    __device__ __forceinline__ void load(int i, const int8_t *block, unsigned of) {
         if constexpr (D >= 64) {   // 16 bytes: two product steps
 #pragma unroll
             for (int u = 0; u < D / 64; ++u) {
-                const u32x4 x = read<STREAM, u32x4>(at + j * D + u * 64 + g * 16);
+                const u32x4 x = read<STREAM, u32x4>(block + of + u * 64);
 #pragma unroll
                 for (int e = 0; e < 4; ++e) k[i][4 * u + e] = x[e];
             }
         } else {
-            const w2 x = read<STREAM, w2>(at + j * D + g * 8);
+            const w2 x = read<STREAM, w2>(block + of);
             k[i][0] = x[0], k[i][1] = x[1];
         }
     }
@@ -59,11 +59,11 @@ template <int D, bool STREAM> struct Keys {
 };
 template <int D, bool STREAM> struct Values {
     uint32_t v[8][D >= 64 ? D / 64 : 1];
-    __device__ __forceinline__ void load(int i, const int8_t *block, int lane) {
-        const int j = lane & 15, g = lane >> 4;
+    __device__ static __forceinline__ unsigned offset(int lane) { return (unsigned)((lane >> 4) * 4 * D + (lane & 15) * (D / 16)); }
+    __device__ __forceinline__ void load(int i, const int8_t *block, unsigned of) {
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-            const int8_t *at = block + (4 * g + e) * D + j * (D / 16);
+            const int8_t *at = block + of + e * D;
             if constexpr (D == 128) {
                 const w2 x = read<STREAM, w2>(at);
                 v[4 * i + e][0] = x[0], v[4 * i + e][1] = x[1];
@@ -145,25 +145,33 @@ __global__ __launch_bounds__(kThreads, RT == 1 ? 3 : 2) void decode_kernel(const
 #pragma unroll
         for (int db = 0; db < S::DB; ++db) out[n][db] = f32x4{0.f, 0.f, 0.f, 0.f};
     }
-    // a lane looks up one of the wave's next 64 steps: its pages (two where they are of 16 tokens) and their scales
-    int unit[2];
-    float ks[2], vs[2];
+    // A lane looks up one of the wave's next 64 steps: its pages (two where they are of 16 tokens) and their scales.  Where there is none it reads the first
+    // entry, or the first page's scales, and takes nothing from them: without branches the reads are on their way together.
+    constexpr int PAGES = PAGE16 ? 2 : 1;
+    int unit[PAGES];
+    float ks[PAGES], vs[PAGES];
     auto look_up = [&](int step) {
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            int page_id = 0;
-            const bool there = step < to && page_at(p, b, (int64_t)step * kStep + (PAGE16 ? 16 * i : 0), page_id);
-            unit[i] = there ? page_id : -1;
-            const int64_t u = (int64_t)(there ? page_id : 0) * p.kv + kh;
-            ks[i] = there ? p.ks[u] : 0.f, vs[i] = there ? p.vs[u] : 0.f;
+        for (int i = 0; i < PAGES; ++i) {
+            const int64_t at = ((int64_t)step * kStep + 16 * i) >> (PAGE16 ? 4 : p.page_log2);
+            const bool in_table = step < to && at < p.width;
+            const int page_id = p.table[(int64_t)b * p.width + (in_table ? at : 0)];
+            unit[i] = in_table && (unsigned)page_id < (unsigned)p.pages ? page_id : -1;
+        }
+#pragma unroll
+        for (int i = 0; i < PAGES; ++i) {
+            const int64_t u = (int64_t)max(unit[i], 0) * p.kv + kh;
+            const float k = p.ks[u], v = p.vs[u];
+            ks[i] = unit[i] < 0 ? 0.f : k, vs[i] = unit[i] < 0 ? 0.f : v;
         }
     };
     auto cell_of = [&](int step, int slot, int i) {   // in bytes; of what is no page: of page 0
-        const int u = __builtin_amdgcn_readlane(unit[i], slot);
+        const int u = __builtin_amdgcn_readlane(unit[i % PAGES], slot);
         return (((int64_t)max(u, 0) * p.kv + kh) * page + ((step * kStep + 16 * i) & (page - 1))) * D;
     };
-    auto scale_of = [&](const float (&x)[2], int slot, int i) { return __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(x[i]), slot)); };
+    auto scale_of = [&](const float (&x)[PAGES], int slot, int i) { return __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(x[i % PAGES]), slot)); };
 
+    const unsigned key_at = Keys<D, RT == 1>::offset(lane), value_at = Values<D, RT == 1>::offset(lane);
 #pragma unroll 1
     for (int base = from + wave; base < to; base += kWave * kWaves) {
         look_up(base + lane * kWaves);
@@ -171,9 +179,10 @@ __global__ __launch_bounds__(kThreads, RT == 1 ? 3 : 2) void decode_kernel(const
         Keys<D, RT == 1> keys;
         Values<D, RT == 1> values;
 #pragma unroll
-        for (int i = 0; i < 2; ++i) keys.load(i, p.k + cell_of(base, 0, i), lane);
+        for (int i = 0; i < 2; ++i) keys.load(i, p.k + cell_of(base, 0, i), key_at);
+        asm volatile("" ::: "memory");   // (keys first: they are waited for first)
 #pragma unroll
-        for (int i = 0; i < 2; ++i) values.load(i, p.v + cell_of(base, 0, i), lane);
+        for (int i = 0; i < 2; ++i) values.load(i, p.v + cell_of(base, 0, i), value_at);
 #pragma unroll 1
         for (int at = 0; at < steps; ++at) {
             const int step = base + at * kWaves, t0 = step * kStep;
@@ -190,12 +199,14 @@ __global__ __launch_bounds__(kThreads, RT == 1 ? 3 : 2) void decode_kernel(const
 #pragma unroll
                     for (int n = 0; n < RT; ++n) s[n][i] = mma<f16_t>(a, q[n][st], s[n][i]);
                 }
+            // The next keys, while this step's weights and values are worked on.  Without a branch: behind one, the compiler would wait for the values, which are
+            // read last, before it takes the keys.  Behind the last step all lanes read one place of the step that they have.
             const bool more = at + 1 < steps;
-            if (more) {   // the next keys, while this step's weights and values are worked on
+            const int slot = more ? at + 1 : at, ahead = base + slot * kWaves;
+            const unsigned in_block = more ? ~0u : 0u;
 #pragma unroll
-                for (int i = 0; i < 2; ++i) keys.load(i, p.k + cell_of(step + kWaves, at + 1, i), lane);
-            }
-            const bool there[2] = {__builtin_amdgcn_readlane(unit[0], at) >= 0, __builtin_amdgcn_readlane(unit[1], at) >= 0};
+            for (int i = 0; i < 2; ++i) keys.load(i, p.k + cell_of(ahead, slot, i), key_at & in_block);
+            const bool there[2] = {__builtin_amdgcn_readlane(unit[0], at) >= 0, __builtin_amdgcn_readlane(unit[PAGES - 1], at) >= 0};
             // every row sees all of it
             const bool all = there[0] && there[1] && t0 + kStep - 1 <= first_query && first_query + p.n - 1 - t0 < p.window;
             u32x4 w[RT];
@@ -279,10 +290,8 @@ __global__ __launch_bounds__(kThreads, RT == 1 ? 3 : 2) void decode_kernel(const
                     }
                 }
             }
-            if (more) {
 #pragma unroll
-                for (int i = 0; i < 2; ++i) values.load(i, p.v + cell_of(step + kWaves, at + 1, i), lane);
-            }
+            for (int i = 0; i < 2; ++i) values.load(i, p.v + cell_of(ahead, slot, i), value_at & in_block);
         }
     }
 
