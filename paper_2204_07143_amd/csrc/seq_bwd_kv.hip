@@ -8,10 +8,6 @@ namespace {
 // 16 bit: two blocks of 16 keys to a wave, of a pair of waves always, else where that leaves two workgroups to each compute unit.
 bool two_key_blocks(const Args &a, int D) { return D == 128 || (int64_t)a.B * a.kv * ((a.Lk + 127) / 128) >= 512; }
 
-// Workgroups: two rounds, for in causal order the first keys have the longest work; four among documents, whose lengths differ more (8192 tokens of 9 documents,
-// 16 heads, D 128: two 219 us, four 172 and 29 for their sums).
-constexpr int64_t kWanted = 1024;
-
 // kPair: with 128 channels in 16 bit a wave that kept both sums of 32 keys would take more than 256 registers, and run alone on its SIMD.  Two waves share
 // 32 keys instead: each forms P and dS of half of a tile's queries, the first sums dV, the second dK, and each gives the other, through LDS, the half
 // that it does not sum itself.
@@ -307,12 +303,11 @@ template <typename T, int D, bool CAP> struct BwdKV {
 
 hipError_t launch_bwd_kv(const Args &a, int dtype, int D, bool capped, hipStream_t st) { return dispatch<BwdKV>(dtype, D, capped, a, st); }
 
-
+// A tile of 16-bit queries takes about 2.2 us.
 int k_splits(const Args &a, int dtype, int D) {
     const int keys = dtype != NA2D_F32 && D < 128 && two_key_blocks(a, D) ? 128 : 64;
-    const int64_t reach = (int64_t)a.window + keys;   // queries of one head that a tile of keys can meet, but for prefixes
-    return parts_of((int64_t)a.B * a.kv * ((a.Lk + keys - 1) / keys), a.packed ? 2 * kWanted : kWanted, (a.prefix || reach > a.Lq ? a.query_tiles : reach / kTile + 2) * a.group,
-                    (int64_t)a.B * a.kv * a.Lk * D * 8);
+    const Work w(a, keys, a.query_tiles);
+    return parts_of((int64_t)a.B * a.kv * ((a.Lk + keys - 1) / keys), w.longest * a.group, w.tiles * a.group, 2.5, (int64_t)a.B * a.kv * a.Lk * D * 8, 5.5e6);
 }
 
 }  // namespace seq

@@ -328,13 +328,33 @@ hipError_t launch_bwd_kv(const Args &a, int dtype, int D, bool capped, hipStream
 int q_splits(const Args &a, int dtype, int D);
 int k_splits(const Args &a, int dtype, int D);
 
-// Parts for `units` workgroups with up to `tiles` tiles each, of which `sums` bytes are left by each part: until there are about `wanted`
-// workgroups, but each part is left four tiles, and the sums stay below 256 MB.
-inline int parts_of(int64_t units, int64_t wanted, int64_t tiles, int64_t sums) {
-    int64_t s = (wanted + units - 1) / units;
-    for (int64_t most : {tiles / 4, ((int64_t)256 << 20) / sums, (int64_t)32}) s = most < s ? most : s;
-    return (int)(s < 1 ? 1 : s);
+// How many parts the work on a tile of queries, or of keys, is split into: the number for which an estimate in units of a tile's time is least.  `units`
+// workgroups have `longest` tiles at most, `tiles` on average, and what takes two more before them.  Two workgroups to a compute unit get all it does (four do not
+// more).  A join takes `join` tiles, and one for each `each` bytes of the `sums` that every part leaves; they stay below 256 MB.
+// Against a fixed number of workgroups (512 to 1024 in all), forward / backward in us: 4 x 12 x 512 fp16, D 64, causal 20.4 / 50 -> 12.6 / 40; 1 x 4 x 8192 fp16, D 64,
+// capped 139 / 358 -> 116 / 320; 2 x 8 over 2 x 777 bf16, D 128, 25.5 / 72 -> 19.2 / 62; 2 x 8 x 1500 of 5 documents 22.9 / 59 -> 15.4 / 40; the furthest the other way 4 x 4 x 3136 fp16,
+// D 32, not causal 79 / 197 -> 78 / 205 and 1 x 16 x 2048 bf16, D 64 37 / 112 -> 38 / 118, where a round of workgroups does not come out even.
+inline int parts_of(int64_t units, double longest, double tiles, double join, int64_t sums, double each) {
+    int best = 1;
+    double least = 0;
+    for (int s = 1; s == 1 || (s <= 32 && s * 4 <= longest && s * sums <= (int64_t)256 << 20); ++s) {
+        const double one = longest / s + 2, all = (double)units * (tiles + 2 * s) / 512, time = (one > all ? one : all) + (s > 1 ? join + (double)s * sums / each : 0);
+        if (s == 1 || time < least) best = s, least = time;
+    }
+    return best;
 }
+// The tiles that a workgroup has at most, and on average, of `all`, with tiles of `rows` of its own: what the window reaches, where no prefix reaches further; half of
+// them where there are documents (with a prefix on average only: it is for prompts, which end where the documents do); on average what lies before the middle
+// of the queries in causal order.
+struct Work {
+    double longest, tiles;
+    Work(const Args &a, int rows, int all) {
+        const int64_t reach = ((int64_t)a.window + rows) / kTile + 2;
+        longest = a.prefix || reach > all ? all : (double)reach;
+        if (a.packed && !a.prefix) longest = longest > 2 ? longest / 2 : longest;
+        tiles = longest * (a.causal && reach > all && a.Lq <= a.Lk ? 1 - 0.5 * a.Lq / a.Lk : 1.0) * (a.packed ? 0.5 : 1.0);
+    }
+};
 
 // 16 bit: two blocks of 16 queries to a wave (a fragment of keys or values then serves two products) where that leaves two workgroups to each compute unit.
 inline bool two_query_blocks(const Args &a) { return (int64_t)a.B * a.heads * ((a.Lq + 127) / 128) >= 512; }

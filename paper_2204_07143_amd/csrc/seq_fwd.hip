@@ -287,12 +287,11 @@ hipError_t launch_marks(const Args &a, const uint8_t *prefix, Marks *marks, char
     return hipGetLastError();
 }
 
-// Of the forward pass and of dQ.  Two rounds of workgroups are wanted where the parts' sums are small, one where they are not (us of the forward for one / two:
-// 2 x 4 x 3136 fp32, D 32, causal, 3 MB a part: 83 / 72; 16 x 2048 bf16, D 128, 17 MB: 49 / 63; not split 121 and 51).
+// Of the forward pass and of dQ; a tile of 16-bit keys takes about 1.2 us.
 int q_splits(const Args &a, int dtype, int D) {
     const int rows = dtype != NA2D_F32 && two_query_blocks(a) ? 128 : 64;
-    const int64_t reach = (int64_t)a.window + rows, sums = (int64_t)a.B * a.heads * a.Lq * (D + 2) * 4;   // keys that a tile of queries can see, but for prefixes
-    return parts_of((int64_t)a.B * a.heads * ((a.Lq + rows - 1) / rows), sums <= 4 << 20 ? 1024 : 512, a.prefix || reach > a.Lk ? a.key_tiles : reach / kTile + 2, sums);
+    const Work w(a, rows, a.key_tiles);
+    return parts_of((int64_t)a.B * a.heads * ((a.Lq + rows - 1) / rows), w.longest, w.tiles, 4, (int64_t)a.B * a.heads * a.Lq * (D + 2) * 4, 2.5e6);
 }
 
 hipError_t launch_fwd(const Args &a, int dtype, int D, bool capped, hipStream_t st) { return dispatch<Fwd>(dtype, D, capped, a, st); }
