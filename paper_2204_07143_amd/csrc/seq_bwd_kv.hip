@@ -5,8 +5,7 @@ namespace seq {
 
 namespace {
 
-// 16 bit: two blocks of 16 keys to a wave, of a pair of waves always, else where that leaves two workgroups to each compute unit.
-bool two_key_blocks(const Args &a, int D) { return D == 128 || (int64_t)a.B * a.kv * ((a.Lk + 127) / 128) >= 512; }
+bool two_key_blocks(const Args &a, int D) { return D == 128 || two_blocks(a, D, (int64_t)a.B * a.kv, a.Lk); }   // (a pair keeps two)
 
 // kPair: with 128 channels in 16 bit a wave that kept both sums of 32 keys would take more than 256 registers, and run alone on its SIMD.  Two waves share
 // 32 keys instead: each forms P and dS of half of a tile's queries, the first sums dV, the second dK, and each gives the other, through LDS, the half

@@ -268,7 +268,7 @@ template <typename T, int D, bool CAP> struct BwdQ {
     }
     static hipError_t go(const Args &a, hipStream_t st) {
         if constexpr (sizeof(T) == 2)
-            if (two_query_blocks(a)) return a.slopes ? launch<true, 2>(a, st) : launch<false, 2>(a, st);
+            if (two_query_blocks(a, D)) return a.slopes ? launch<true, 2>(a, st) : launch<false, 2>(a, st);
         return a.slopes ? launch<true, 1>(a, st) : launch<false, 1>(a, st);
     }
 };

@@ -265,7 +265,7 @@ template <typename T, int D, bool CAP> struct Fwd {
     }
     static hipError_t go(const Args &a, hipStream_t st) {
         if constexpr (sizeof(T) == 2)
-            if (two_query_blocks(a)) return a.slopes ? launch<true, 2>(a, st) : launch<false, 2>(a, st);
+            if (two_query_blocks(a, D)) return a.slopes ? launch<true, 2>(a, st) : launch<false, 2>(a, st);
         return a.slopes ? launch<true, 1>(a, st) : launch<false, 1>(a, st);
     }
 };
@@ -295,7 +295,7 @@ hipError_t launch_marks(const Args &a, const uint8_t *prefix, Marks *marks, char
 
 // Of the forward pass and of dQ; a tile of 16-bit keys takes about 1.2 us.
 int q_splits(const Args &a, int dtype, int D) {
-    const int rows = dtype != NA2D_F32 && two_query_blocks(a) ? 128 : 64;
+    const int rows = dtype != NA2D_F32 && two_query_blocks(a, D) ? 128 : 64;
     const Work w(a, rows, a.key_tiles);
     return parts_of((int64_t)a.B * a.heads * ((a.Lq + rows - 1) / rows), w.longest, w.tiles, 4, (int64_t)a.B * a.heads * a.Lq * (D + 2) * 4, 2.5e6);
 }

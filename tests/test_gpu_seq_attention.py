@@ -359,3 +359,12 @@ def test_two_calls_at_once(dtype):
 @pytest.mark.parametrize("std", [0.01, 30.0])
 def test_caps_that_are_reached(dtype, cap, std):
     _check(20, 1, 2, 1, 150, 150, 64, dtype, q_std=std, causal=True, softcap=cap, docs=2)
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("D", [32, 64, 128])
+@pytest.mark.parametrize("name", ["plain", "causal_cap", "window_prefix_documents_slopes"])
+def test_many_heads(dtype, D, name):
+    """Enough rows for two blocks of them to a wave, where the order of the work allows it."""
+    mask = {"plain": dict(), "causal_cap": dict(causal=True, softcap=20.0), "window_prefix_documents_slopes": dict(window=90, prefix=True, docs=3, slopes=True)}[name]
+    _check(21, 2, 128, 128, 190, 190, D, dtype, **mask)
