@@ -7,6 +7,10 @@
 //   P = exp2(S' - ref), rounded to fp16
 //   O^T += vs V^T P  a lane holds D / 16 channels of its eight tokens; product block db takes channel db of each lane, so no value changes lanes
 // The four waves' parts are joined through LDS.  Few sequences: their ranges are split over workgroups, and a second kernel joins the splits in order.
+//
+// Bound by memory where there is much to read: 64 sequences of up to 16000 tokens, 32 heads over 8, D 128, capped, 1.2 GB in 222 us, 5.6 of the 5.7 TB/s that a
+// large read reaches.  Short ranges are bound by what follows on each other: about 4 us to the first step and behind the last, 0.85 us a step of a wave (1.25 with 32 rows), two launches.
+// 16 sequences with a window of 2048 and 5 tokens each, 16 heads over 2: 15 + 4 us (reads two steps ahead 16, 48 rows to a workgroup 18, 256 tokens a split 15).
 #include "seq_cache.hpp"
 
 namespace seq {
