@@ -73,7 +73,6 @@ Args args(const seq_problem *p, const float *slopes, const int32_t *documents, b
     a.dlo = p->causal ? 0 : 1 - a.window;
     a.scale = p->scale;
     constexpr double log2e = 1.4426950408889634;
-    a.bounded = p->softcap > 0.f && p->softcap * log2e <= 80.0;
     if (p->softcap > 0.f) {
         const bool sigmoid = p->dtype != NA2D_F32;
         a.c = (float)(2.0 * log2e * p->scale / p->softcap);

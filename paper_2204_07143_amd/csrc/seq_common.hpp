@@ -59,7 +59,6 @@ struct Args {
     float c;               // capped: 2 scale log2(e) / cap
     float m, from;         // a score in base 2 is m y + from (see Score)
     float masked;          // the y of what is masked
-    int bounded;           // a cap of at most 80 / log2(e)
 };
 
 // ---- products --------------------------------------------------------------------------------------------------------------

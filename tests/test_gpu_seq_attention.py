@@ -355,7 +355,7 @@ def test_two_calls_at_once(dtype):
 
 
 @TYPE
-@pytest.mark.parametrize("cap", [0.5, 50.0, 55.45, 55.46, 300.0])   # weights from e^-cap to e^cap; from 80 / log2(e) = 55.452 on they are taken off a running maximum
+@pytest.mark.parametrize("cap", [0.5, 50.0, 55.45, 55.46, 300.0])   # weights from e^-cap to e^cap
 @pytest.mark.parametrize("std", [0.01, 30.0])
 def test_caps_that_are_reached(dtype, cap, std):
     _check(20, 1, 2, 1, 150, 150, 64, dtype, q_std=std, causal=True, softcap=cap, docs=2)
