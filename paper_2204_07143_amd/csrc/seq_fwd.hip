@@ -9,7 +9,7 @@
 //
 // What bounds it: the SIMDs, which issue about 35 vector instructions to every 16 products of a tile.  Two images of 64 keys each take 64 KB at 128 channels in
 // 16 bit, so two workgroups are on a compute unit, and a wave keeps 32 queries so that a fragment from LDS serves two products (no bank conflicts are left).
-// bf16, D 128: 2 x 16 over 4 x 8192, not causal, 1.08 ms or 1.02 PFLOP/s, 90 % of a library product of 8192 x 8192; 4 x 16 over 4 x 2048, causal, capped, 118 us, where the cap's
+// bf16, D 128: 2 x 16 over 4 x 8192, not causal, 1.08 to 1.13 ms or about 1 PFLOP/s, 88 % of a library product of 8192 x 8192; 4 x 16 over 4 x 2048, causal, capped, 124 us, where the cap's
 // exponential and reciprocal (a quarter of the rate each) make vector instructions 52 % of the cycles and matrix instructions 24 %.  fp32, D 32, 2 x 4 x 3136, causal,
 // slopes: 71 us, matrix instructions 46 % of the cycles and vector ones 30 %, which an fp32 matrix instruction does not let pass beside it.
 #include "lds_attr.hpp"
