@@ -85,8 +85,9 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) void bwd_kv_kerne
         const int qa = t * kTile + p.off, qb = min(t * kTile + kTile, p.Lq) - 1 + p.off;
         bool any = near_any(p, qa, qb, ka, kb) || prefix_any, some = near_any(p, qa, qb, wa, wb) || prefix_some, all = near_all(p, qa, qb, wa, wb) || prefix_all;
         if (documents) {
-            const Marks x = marks[qa / kTile], y = marks[min((qa + kTile - 1) / kTile, p.key_tiles - 1)];
-            const int in = qa % kTile;
+            // (a last tile may begin inside the last keys: nothing follows them, so what is staged behind the last query, which may be padding, is zeros)
+            const int at = qa / kTile, in = qa % kTile;
+            const Marks x = marks[at], y = !in ? x : at + 1 < p.key_tiles ? marks[at + 1] : Marks{INT32_MAX, -1, 0, 0};
             m = Marks{min(x.dmin, y.dmin), max(x.dmax, y.dmax), in ? x.live >> in | y.live << (kTile - in) : x.live, 0};
             const Docs d{m.dmin, m.dmax, (x.live & y.live) == ~0ull};
             any &= d.meet(dg), some &= d.meet(dw), all &= d.same(dw);

@@ -368,3 +368,26 @@ def test_many_heads(dtype, D, name):
     """Enough rows for two blocks of them to a wave, where the order of the work allows it."""
     mask = {"plain": dict(), "causal_cap": dict(causal=True, softcap=20.0), "window_prefix_documents_slopes": dict(window=90, prefix=True, docs=3, slopes=True)}[name]
     _check(21, 2, 128, 128, 190, 190, D, dtype, **mask)
+
+
+@TYPE
+@pytest.mark.parametrize("Lq,Lk", [(3, 10), (65, 130), (37, 301), (100, 164), (64, 100), (1, 65)])
+def test_padding_behind_fewer_queries_than_keys_may_hold_anything(dtype, Lq, Lk):
+    """The last queries' tile begins inside the last keys' tile: what is staged behind the last query, which is padding, enters no product."""
+    g = np.random.default_rng(22)
+    q, dout = (normal(g, (2, 4, Lq, 64), dtype) for _ in range(2))
+    k, v = (normal(g, (2, 2, Lk, 64), dtype) for _ in range(2))
+    documents = torch.zeros((2, Lk), dtype=torch.int32, device="cuda")
+    documents[:, -1] = -1
+    documents[1, :Lk // 3] = -1
+    dead = (documents < 0)[:, None, :, None]
+    mine = dead[:, :, Lk - Lq:]
+    mask = dict(documents=documents, causal=True)
+    clean = _run(q, k, v, dout, **mask)
+    for value in (float("nan"), float("inf")):
+        fouled = _run(q.masked_fill(mine, value), k.masked_fill(dead, value), v.masked_fill(dead, value), dout.masked_fill(mine, value), **mask)
+        for a, b in zip(clean, fouled):
+            assert torch.isfinite(b).all() and torch.equal(a, b)
+    want, bound = expect(q, k, v, dout, dtype, **mask)
+    for name, x in zip(("out", "dq", "dk", "dv"), clean):
+        check(name, x, want[name], bound[name])
