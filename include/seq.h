@@ -72,8 +72,8 @@ int seq_attention_bwd(const seq_problem *p, const void *q, const void *k, const 
 /*
  * The cache: pages of `page` consecutive tokens of one sequence, k_pages and v_pages int8 [pages, kv_heads, page, D], contiguous, with one fp32 scale
  * for each page and head, k_scales and v_scales [pages, kv_heads]; a value is the integer times the scale.  table: int32 [B, table_width]; position t of
- * sequence b lies in page table[b, t / page] at t % page.  lengths: int32 [B], tokens of each sequence.  Entries of the table that a sequence
- * does not reach may be anything.  A page number outside [0, pages) is no page: nothing is written there, and nothing there is seen or
+ * sequence b lies in page table[b, t / page] at t % page.  lengths: int32 [B], tokens of each sequence.  Entries of the table whose positions a call
+ * does not reach (behind the sequence, or before every query's window) may be anything, pages that nothing was ever written to included.  A page number outside [0, pages) is no page: nothing is written there, and nothing there is seen or
  * read; positions beyond table_width pages likewise.
  */
 typedef struct {

@@ -138,7 +138,7 @@ __global__ __launch_bounds__(kThreads, RT == 1 ? 3 : 2) void decode_kernel(const
     }
 
     // the range that any row sees, in steps, and this workgroup's part of it
-    const int begin = max(0, first_query - p.window + 1) / kStep, end = (length + kStep - 1) / kStep;
+    const int least = max(0, first_query - p.window + 1), begin = least / kStep, end = (length + kStep - 1) / kStep;   // least: the first position that is seen
     const int each = max(0, (end - begin + p.splits - 1) / p.splits), from = begin + split * each, to = min(end, from + each);
 
     f32x4 out[RT][S::DB];
@@ -150,17 +150,18 @@ __global__ __launch_bounds__(kThreads, RT == 1 ? 3 : 2) void decode_kernel(const
         for (int db = 0; db < S::DB; ++db) out[n][db] = f32x4{0.f, 0.f, 0.f, 0.f};
     }
     // A lane looks up one of the wave's next 64 steps: its pages (two where they are of 16 tokens) and their scales.  Where there is none it reads the first
-    // entry, or the first page's scales, and takes nothing from them: without branches the reads are on their way together.
+    // entry, or the first page's scales, and takes nothing from them: without branches the reads are on their way together.  Of a step's two pages one may hold
+    // no token that is seen: its entry and its scale may be anything (a weight of 0 times a scale that is NaN would be NaN), and it is none.
     constexpr int PAGES = PAGE16 ? 2 : 1;
     int unit[PAGES];
     float ks[PAGES], vs[PAGES];
     auto look_up = [&](int step) {
 #pragma unroll
         for (int i = 0; i < PAGES; ++i) {
-            const int64_t at = ((int64_t)step * kStep + 16 * i) >> (PAGE16 ? 4 : p.page_log2);
-            const bool in_table = step < to && at < p.width;
-            const int page_id = p.table[(int64_t)b * p.width + (in_table ? at : 0)];
-            unit[i] = in_table && (unsigned)page_id < (unsigned)p.pages ? page_id : -1;
+            const int64_t token = (int64_t)step * kStep + 16 * i;
+            const bool seen = step < to && token < length && (!PAGE16 || token + 16 > least);   // (what is seen is in the table: length is)
+            const int page_id = p.table[(int64_t)b * p.width + (seen ? token >> (PAGE16 ? 4 : p.page_log2) : 0)];
+            unit[i] = seen && (unsigned)page_id < (unsigned)p.pages ? page_id : -1;
         }
 #pragma unroll
         for (int i = 0; i < PAGES; ++i) {

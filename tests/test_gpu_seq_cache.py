@@ -337,3 +337,26 @@ def test_counts_and_lengths_out_of_range():
     got = F.seq_cache_attention(q, cache, _int(table.tolist()), _int([9, -5, -big - 1, 0]))
     _check_attention(got[:1], q[:1], host, table[:1], [9], "f16")
     assert (got[1:] == 0).all()
+
+
+@pytest.mark.parametrize("page", [16, 32, 128])
+@pytest.mark.parametrize("n,window", [(1, None), (5, None), (1, 5), (3, 20)])   # four heads share a key head: one block of rows, and two
+def test_entries_that_no_query_reaches_may_name_pages_never_written(page, n, window):
+    g = np.random.default_rng(11)
+    lengths = [10, 33, 48, 7, 100, 5 * page + 1, 1000]
+    table, pages = _table(g, lengths, page, spare=1, width=-(-1000 // page) + 3)
+    never, = set(range(pages)) - set(table.ravel().tolist())
+    host, _ = _cache(g, pages, 2, page, 64)
+    q = normal(g, (len(lengths), 8, n, 64), "f16")
+    dead = np.ones_like(table, dtype=bool)   # entries all of whose positions lie behind the sequence, or before every query's window
+    for b, L in enumerate(lengths):
+        first = max(0, L - n - (window or L + n) + 1)
+        dead[b, first // page:(L - 1) // page + 1] = False
+    results = []
+    for entry, scale in ((-1, 0.02), (never, float("nan")), (never, float("inf"))):
+        host[2][never] = host[3][never] = scale
+        cache = F.SeqCache(*(torch.from_numpy(x).cuda() for x in host))
+        results.append(F.seq_cache_attention(q, cache, _int(np.where(dead, entry, table).tolist()), _int(lengths), window=window))
+    assert torch.isfinite(results[0]).all()
+    for x in results[1:]:
+        assert torch.equal(x, results[0])
