@@ -127,7 +127,7 @@ __global__ __launch_bounds__(kThreads, RT == 1 ? 3 : 2) void decode_kernel(const
         }
         most = column_max(most);
         const int power = most > 0.f && most < INFINITY ? __builtin_amdgcn_frexp_expf(most) : 0;
-        c[n] = p.c * __builtin_amdgcn_ldexpf(1.f, power);
+        c[n] = __builtin_amdgcn_ldexpf(p.c, power);   // (bfloat16's power may be 128: 2^128 alone is infinite)
 #pragma unroll
         for (int s = 0; s < S::STEPS; ++s) {
             f16x8 y;

@@ -360,3 +360,15 @@ def test_entries_that_no_query_reaches_may_name_pages_never_written(page, n, win
     assert torch.isfinite(results[0]).all()
     for x in results[1:]:
         assert torch.equal(x, results[0])
+
+
+def test_queries_up_to_the_types_largest():
+    g = np.random.default_rng(12)
+    table, pages = _table(g, [90, 90], 32)
+    host, _ = _cache(g, pages, 1, 32, 32)
+    host[2] /= 8   # (scores of a few units)
+    cache = F.SeqCache(*(torch.from_numpy(x).cuda() for x in host))
+    q = torch.from_numpy(g.uniform(-3.3e38, 3.3e38, (2, 4, 1, 32)).astype(np.float32)).to(torch.bfloat16).cuda()
+    assert (q.abs().amax(-1) >= 2.0 ** 127).all()
+    got = F.seq_cache_attention(q, cache, _int(table.tolist()), _int([90, 90]), scale=2e-38)
+    _check_attention(got, q, host, table, [90, 90], "bf16", scale=float(np.float32(2e-38)))
