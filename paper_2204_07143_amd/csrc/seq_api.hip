@@ -22,6 +22,7 @@ int check_strides(const seq_strides &s, int64_t B, int64_t heads, int64_t rows, 
         if (x < 0 || x > ((int64_t)1 << 45)) return NA2D_ERR_SHAPE;
         if (x * e % 16) return NA2D_ERR_ALIGN;
     }
+    if (rows > 1 && s.row > (int64_t)INT32_MAX / e / (rows - 1)) return NA2D_ERR_SHAPE;   // (first: the product below would pass 64 bits)
     if (((rows - 1) * s.row + D) * e > (int64_t)INT32_MAX || B > ((int64_t)1 << 24) || heads > ((int64_t)1 << 16)) return NA2D_ERR_SHAPE;
     if ((double)(B - 1) * s.batch + (double)(heads - 1) * s.head > 0x1p58) return NA2D_ERR_SHAPE;
     if (!written) return NA2D_OK;

@@ -128,3 +128,18 @@ def test_python_arguments():
                  lambda: F.seq_cache_attention(q.half(), cache, table, lengths)):
         with pytest.raises(ValueError, match="GPU tensors only"):
             call()
+
+
+def test_planes_whose_size_passes_64_bits():
+    """2^22 rows 2^42 elements apart are 2^64 elements: refused, not taken for none."""
+    rows, far = (1 << 22) + 1, na.SeqStrides(0, 0, 1 << 42)
+    for name in ("q", "out", "dout", "dq"):
+        assert na.seq_validate_problem(P(B=1, heads=1, kv=1, Lq=rows, Lk=rows, **{name: far}), True) == -6
+    for name in ("k", "v", "dk", "dv"):
+        assert na.seq_validate_problem(P(B=1, heads=1, kv=1, Lk=rows, **{name: far}), True) == -6
+    for last in (1 << 24, (1 << 24) - 1):
+        assert na.seq_validate_problem(P(B=1, heads=1, kv=1, Lq=last, q=na.SeqStrides(0, 0, 1 << 45))) == -6
+    assert tuple(na.seq_cache_validate(C(B=1, heads=1, kv=1, n=rows, rows=far), call) for call in range(3)) == (-6, -6, -6)
+    # the largest plane there is
+    assert na.seq_validate_problem(P(B=1, heads=1, kv=1, Lq=(1 << 24) - 1, Lk=64, D=64, q=na.SeqStrides(0, 0, 64), out=na.SeqStrides(0, 0, 64))) == 0
+    assert na.seq_validate_problem(P(B=1, heads=1, kv=1, Lq=1 << 24, Lk=64, D=64, q=na.SeqStrides(0, 0, 64), out=na.SeqStrides(0, 0, 64))) == -6
