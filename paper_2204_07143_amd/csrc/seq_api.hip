@@ -61,7 +61,8 @@ int validate(const seq_problem *p, bool backward) {
             if (r) return r;
     // every launch of the passes (the smallest tiles: 64 rows) holds its workgroups
     const int64_t q_tiles = ((int64_t)p->Lq + kTile - 1) / kTile, k_tiles = ((int64_t)p->Lk + kTile - 1) / kTile;
-    if (!launch_holds((int64_t)p->B * p->heads * q_tiles, kThreads) || !launch_holds((int64_t)p->B * p->kv_heads * k_tiles, kThreads)) return NA2D_ERR_SHAPE;
+    const int64_t of_q = (int64_t)p->B * p->heads * q_tiles, of_k = (int64_t)p->B * p->kv_heads * k_tiles;
+    if (!launch_holds(of_q, kThreads) || !launch_holds(of_k, kThreads) || (backward && !launch_holds(of_q + of_k, kThreads))) return NA2D_ERR_SHAPE;
     return NA2D_OK;
 }
 
@@ -90,14 +91,15 @@ Args args(const seq_problem *p, const float *slopes, const int32_t *documents, b
 
 // The workspace: zeros, the marks of the keys' tiles, and for a backward pass the rows' statistics, the tiles' powers of two and the splits' sums.
 struct Space {
-    int64_t marks, rows, powers, parts, bytes;
+    int64_t marks, rows, powers, value_powers, parts, bytes;
     Space(const Args &a, int D, bool marked, bool backward) {
         const int64_t queries = (int64_t)a.B * a.heads * a.query_tiles;
         auto up = [](int64_t x) { return (x + 63) / 64 * 64; };
         marks = marked ? 64 : 0;
         rows = marked ? up(marks + (int64_t)sizeof(Marks) * a.B * a.key_tiles) : 0;
         powers = up(rows + (backward ? (int64_t)sizeof(float2) * queries * kTile : 0));
-        parts = up(powers + (backward ? (int64_t)sizeof(int) * queries : 0));
+        value_powers = up(powers + (backward ? (int64_t)sizeof(int) * queries : 0));
+        parts = up(value_powers + (backward ? (int64_t)sizeof(int) * a.B * a.kv * a.key_tiles : 0));
         const int64_t of_q = a.q_splits > 1 ? (int64_t)sizeof(float) * a.q_splits * a.B * a.heads * a.Lq * (backward ? D : D + 2) : 0;
         const int64_t of_k = backward && a.k_splits > 1 ? (int64_t)sizeof(float) * a.k_splits * 2 * a.B * a.kv * a.Lk * D : 0;
         bytes = parts + (of_q > of_k ? of_q : of_k);   // (one after the other)
@@ -214,6 +216,7 @@ int seq_attention_bwd(const seq_problem *p, const void *q, const void *k, const 
     if (int r = prepare(a, s, prefix, workspace, workspace_bytes, st)) return r;
     a.rows = reinterpret_cast<float2 *>(static_cast<char *>(workspace) + s.rows);
     a.powers = reinterpret_cast<int *>(static_cast<char *>(workspace) + s.powers);
+    a.value_powers = reinterpret_cast<int *>(static_cast<char *>(workspace) + s.value_powers);
     if (int r = from_hip(launch_rows(a, p->dtype, p->D, p->softcap > 0.f, st))) return r;
     if (int r = from_hip(launch_bwd_q(a, p->dtype, p->D, p->softcap > 0.f, st))) return r;
     return from_hip(launch_bwd_kv(a, p->dtype, p->D, p->softcap > 0.f, st));

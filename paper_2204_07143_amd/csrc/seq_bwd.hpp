@@ -7,10 +7,15 @@
 namespace seq {
 
 template <typename T> constexpr bool kScaled = __is_same(T, f16_t);
-template <typename T> constexpr float kRaise = kScaled<T> ? 8.f : 0.f;   // weights are formed times 2^kRaise
+template <typename T> constexpr float kRaise = kScaled<T> ? 10.f : 0.f;   // weights are formed times 2^kRaise
 constexpr int kNothing = -1000;   // power of two of a tile of zeros
 
-__device__ __forceinline__ int power_of(float most) { return most > 0.f ? min(16, __builtin_amdgcn_frexp_expf(most)) : kNothing; }   // (infinite: 16)
+__device__ __forceinline__ int power_of(float most, int highest) { return most > 0.f ? min(highest, __builtin_amdgcn_frexp_expf(most)) : kNothing; }   // (infinite: highest)
+constexpr int kMostDout = 16, kMostValues = 23;   // fp16, and 128 of them
+// The power of two that dS is raised by on the scale of |dout|, 2^power: with 2^e above every sum |v_j| that its rows see, |dP| and |delta| are below 2^(power + e); delta is the
+// weights' mean of dP, so |P (dP - delta)| <= 2 P (1 - P) max |dP| is below half of that, and raised below 2^14.  Flat rows over n keys, dS of 1 / n of it, keep
+// fp16's eleven digits to n of about 2^20, and one of them less for each power of two beyond.
+__device__ __forceinline__ int raise_of(int e) { return 15 - (e == kNothing ? 0 : e); }
 __device__ __forceinline__ float two_to(int e) { return __builtin_amdgcn_ldexpf(1.f, e); }
 
 template <typename T> constexpr int kBlocks = sizeof(T) == 2 ? 2 : 1;   // blocks of 16 queries, or keys, that a wave keeps

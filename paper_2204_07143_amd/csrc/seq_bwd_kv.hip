@@ -25,7 +25,7 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) void bwd_kv_kerne
     extern __shared__ __align__(16) char lds[];
     __shared__ __align__(16) int ids[2][kTile];
     __shared__ __align__(16) float2 stats[2][kTile];
-    __shared__ int range[4][kWaves];
+    __shared__ int range[5][kWaves];
     __shared__ __align__(16) u32x4 given[PAIR ? kWaves : 1][KB][PAIR ? kWave : 1];
     const int tid = threadIdx.x, lane = tid % kWave, wave = uniform(tid / kWave), j = lane & 15, g = lane >> 4;
     const int role = PAIR ? wave & 1 : 0, group_of_keys = PAIR ? wave >> 1 : wave;
@@ -55,7 +55,7 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) void bwd_kv_kerne
     }
     Docs dw = no_docs(), dg = no_docs();
     bool prefix_any = false, prefix_some = false, prefix_all = false;
-    int power = 0;
+    int power = 0, raise = 0;   // dS is held times 2^(raise - power)
     if (marks || kScaled<T>) {
         const int i = min(kw + lane % (16 * KB), p.Lk - 1);
         if (documents) dw = docs_of_wave(documents[i], true);
@@ -63,21 +63,23 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) void bwd_kv_kerne
             const uint64_t x = __ballot(marks[i / kTile].prefix >> (i % kTile) & 1);
             prefix_some = x != 0, prefix_all = x == ~0ull;
         }
-        int most = kNothing;
-        if constexpr (kScaled<T>) {   // over the tiles of every head that shares these keys
-            const int *of = p.powers + ((int64_t)b * p.heads + kh * p.group) * p.query_tiles;
+        int most = kNothing, values = kNothing;
+        if constexpr (kScaled<T>) {   // over the tiles of every head that shares these keys, and of all keys that their queries may see
+            const int *of = p.powers + ((int64_t)b * p.heads + kh * p.group) * p.query_tiles, *of_v = p.value_powers + (int64_t)plane * p.key_tiles;
             for (int n = tid; n < p.group * p.query_tiles; n += kThreads) most = max(most, of[n]);
-            most = wave_max(most);
+            for (int n = tid; n < p.key_tiles; n += kThreads) values = max(values, of_v[n]);
+            most = wave_max(most), values = wave_max(values);
         }
-        if (lane == 0) range[0][wave] = dw.lo, range[1][wave] = dw.hi, range[2][wave] = prefix_some, range[3][wave] = most;
+        if (lane == 0) range[0][wave] = dw.lo, range[1][wave] = dw.hi, range[2][wave] = prefix_some, range[3][wave] = most, range[4][wave] = values;
         workgroup_sync();
         dg = {range[0][0], range[1][0], false};
-        most = range[3][0];
+        most = range[3][0], values = range[4][0];
         prefix_any = range[2][0] | range[2][1] | range[2][2] | range[2][3];
 #pragma unroll
-        for (int w = 1; w < kWaves; ++w) dg.lo = min(dg.lo, range[0][w]), dg.hi = max(dg.hi, range[1][w]), most = max(most, range[3][w]);
+        for (int w = 1; w < kWaves; ++w) dg.lo = min(dg.lo, range[0][w]), dg.hi = max(dg.hi, range[1][w]), most = max(most, range[3][w]), values = max(values, range[4][w]);
         dg.lo = uniform(dg.lo), dg.hi = uniform(dg.hi);
         if (kScaled<T> && most != kNothing) power = uniform(most);
+        if (kScaled<T>) raise = raise_of(uniform(values));
     }
     const int ka = k0, kb = min(k0 + kKeys<T, D, KB>, p.Lk) - 1;
     const int wa = min(kw, p.Lk - 1), wb = min(kw + 16 * KB, p.Lk) - 1;
@@ -144,7 +146,7 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) void bwd_kv_kerne
         workgroup_sync();
         if (after >= 0) stage(kh * p.group + head, after, buf ^ 1, ahead.live);
         const int qi = img + buf * 2 * L::BYTES, di = qi + L::BYTES, q0 = t * kTile + p.off;
-        const float slope = SLOPES ? p.slopes[h] * kLog2e : 0.f, lower = two_to(-power - (int)kRaise<T>);
+        const float slope = SLOPES ? p.slopes[h] * kLog2e : 0.f, lower = two_to(raise - power - (int)kRaise<T>);
         uint64_t seen[KB];
         bool mixed = false;   // the tile's documents are not one (what is not live has no weights anyway)
         if (some && !all) {
@@ -269,7 +271,7 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) void bwd_kv_kerne
         settle_products(dv[n]);
         const int i = kw + 16 * n + j;
         if (i < p.Lk) {
-            const float by_k = p.scale * two_to(power), by_v = two_to(-(int)(kRaise<T> + Score<T, CAP>::kQuad));
+            const float by_k = p.scale * two_to(power - raise), by_v = two_to(-(int)(kRaise<T> + Score<T, CAP>::kQuad));
             if constexpr (PAIR) {
                 store(role ? 0 : 1, dv[n], role ? by_k : by_v, i);
             } else {

@@ -1,6 +1,6 @@
 // Attention over a sequence, backward, from the forward's log-sum-exp: the weights are formed again per tile, nothing of their size reaches memory.
 //
-//   rows      delta_i = <dout_i, out_i>, lse in base 2; fp16: the power of two of a tile's largest |dout|
+//   rows      delta_i = <dout_i, out_i>, lse in base 2; fp16: the powers of two of a tile's largest |dout|, and of its keys' largest sum |v|
 //   queries   S^T = K Q^T, dP^T = V dO^T, dS = P (dP - delta) (1 - tanh^2), dQ^T += K^T dS       a wave keeps 16 QB queries, walks the keys
 //   keys      S = Q K^T, dP = dO V^T, dV^T += dO^T P, dK^T += Q^T dS                             a wave keeps 16 KB keys, walks the queries of
 //                                                                                               every head that shares them
@@ -9,8 +9,9 @@
 // 15 for the key side's join (vector instructions 49 and 42 % of the cycles, matrix ones 30 and 25 %).  The rows are read at the rate of memory: 100 MB in 16 us.
 // fp32, D 32, 2 x 4 x 3136, causal, slopes: 5 + 96 + 5 + 125 + 6 us, matrix instructions 52 % of the cycles.
 //
-// fp16 holds 2^-24 to 65504.  The weights enter dV's product times 2^8, and dS on the scale of the largest |dout| of its query (queries) or of the
-// heads that share the key (keys), so gradients far below 1 keep their digits; the powers of two come off the sums again.
+// fp16 holds 2^-24 to 65504.  The weights enter dV's product times 2^10, and dS on a scale that the largest |dout| of its query (queries) or of the heads that share
+// the key (keys) and the largest sum |v| of the keys make: as high as it can be without passing 65504 (raise_of()), so gradients far below 1, weights of 2^-20 of a
+// million keys and values of thousands keep their digits; the powers of two come off the sums again.
 #include "seq_bwd.hpp"
 
 namespace seq {
@@ -23,10 +24,38 @@ __global__ __launch_bounds__(kThreads) void rows_kernel(const Args p) {
     constexpr int E = 16 / (int)sizeof(T);
     typedef T vec __attribute__((ext_vector_type(E)));
     __shared__ float most_of[kWaves];
-    const int tid = threadIdx.x, plane = blockIdx.x / p.query_tiles, tile = blockIdx.x % p.query_tiles, b = plane / p.heads, h = plane % p.heads;
-    const char *o = p.out.at + b * p.out.b + h * p.out.h, *d = p.dout.at + b * p.dout.b + h * p.dout.h;
-    const int c = tid % L::CH;
+    const int tid = threadIdx.x, c = tid % L::CH;
     float most = 0.f;
+    auto power = [&](int highest) {   // of the workgroup's largest
+#pragma unroll
+        for (int n = 1; n < kWave; n *= 2) most = fmaxf(most, __shfl_xor(most, n));
+        if (tid % kWave == 0) most_of[tid / kWave] = most;
+        workgroup_sync();
+        return power_of(fmaxf(fmaxf(most_of[0], most_of[1]), fmaxf(most_of[2], most_of[3])), highest);
+    };
+    if constexpr (kScaled<T>) {
+        const int unit = (int)blockIdx.x - p.B * p.heads * p.query_tiles;
+        if (unit >= 0) {   // a tile of keys
+            const int plane = unit / p.key_tiles, tile = unit % p.key_tiles, b = plane / p.kv;
+            const char *v = p.v.at + b * p.v.b + plane % p.kv * p.v.h;
+#pragma unroll
+            for (int r = tid / L::CH; r < kTile; r += kThreads / L::CH) {
+                const int i = tile * kTile + r, at = min(i, p.Lk - 1);
+                const vec x = *reinterpret_cast<const vec *>(v + (int64_t)at * p.v.row + c * 16);
+                float sum = 0.f;
+#pragma unroll
+                for (int e = 0; e < E; ++e) sum += fabsf((float)x[e]);
+#pragma unroll
+                for (int n = 1; n < L::CH; n *= 2) sum += __shfl_xor(sum, n);
+                if (!p.documents || p.documents[(int64_t)b * p.Lk + at] >= 0) most = fmaxf(most, sum);
+            }
+            const int e = power(kMostValues);
+            if (tid == 0) p.value_powers[unit] = e;
+            return;
+        }
+    }
+    const int plane = blockIdx.x / p.query_tiles, tile = blockIdx.x % p.query_tiles, b = plane / p.heads, h = plane % p.heads;
+    const char *o = p.out.at + b * p.out.b + h * p.out.h, *d = p.dout.at + b * p.dout.b + h * p.dout.h;
 #pragma unroll
     for (int r = tid / L::CH; r < kTile; r += kThreads / L::CH) {
         const int i = tile * kTile + r, at = min(i, p.Lq - 1);
@@ -46,11 +75,8 @@ __global__ __launch_bounds__(kThreads) void rows_kernel(const Args p) {
         if (c == 0) p.rows[((int64_t)plane * p.query_tiles + tile) * kTile + r] = live ? float2{p.from - lse * kLog2e + kRaise<T> + Score<T, CAP>::kQuad, delta} : float2{-INFINITY, 0.f};
     }
     if constexpr (kScaled<T>) {
-#pragma unroll
-        for (int n = 1; n < kWave; n *= 2) most = fmaxf(most, __shfl_xor(most, n));
-        if (tid % kWave == 0) most_of[tid / kWave] = most;
-        workgroup_sync();
-        if (tid == 0) p.powers[blockIdx.x] = power_of(fmaxf(fmaxf(most_of[0], most_of[1]), fmaxf(most_of[2], most_of[3])));
+        const int e = power(kMostDout);
+        if (tid == 0) p.powers[blockIdx.x] = e;
     }
 }
 
@@ -97,9 +123,8 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) void bwd_q_kernel
             for (int s = 0; s < L::STEPS; ++s)
 #pragma unroll
                 for (int e = 0; e < 8; ++e) most = fmaxf(most, fabsf((float)__builtin_bit_cast(vec, d[n][s])[e]));
-            power[n] = power_of(column_max(most));
+            power[n] = power_of(column_max(most), kMostDout);
             if (power[n] == kNothing) power[n] = 0;
-            lse[n] -= kRaise<T> + (float)power[n];
         }
     }
     Docs dw = no_docs(), dg = no_docs();
@@ -131,6 +156,13 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) void bwd_q_kernel
     if (!p.prefix) {
         first = max(0, qa - p.window + 1) / kTile;
         last = min(last, max(-1, qb - p.dlo) >> 6);
+    }
+    if constexpr (kScaled<T>) {
+        int e = kNothing;
+        for (int t = first + lane; t <= last; t += kWave) e = max(e, p.value_powers[((int64_t)b * p.kv + kh) * p.key_tiles + t]);
+        const int raise = raise_of(uniform(wave_max(e)));
+#pragma unroll
+        for (int n = 0; n < QB; ++n) power[n] -= raise, lse[n] -= kRaise<T> + (float)power[n];
     }
     int left = INT32_MAX, skip = 0;   // of the tiles there are, this part's
     if (p.q_splits > 1) {
@@ -252,7 +284,7 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) void bwd_q_kernel
 
 template <typename T, int D, bool CAP> struct Rows {
     static hipError_t go(const Args &a, hipStream_t st) {
-        const int64_t blocks = (int64_t)a.B * a.heads * a.query_tiles;
+        const int64_t blocks = (int64_t)a.B * a.heads * a.query_tiles + (kScaled<T> ? (int64_t)a.B * a.kv * a.key_tiles : 0);
         if (!launch_holds(blocks, kThreads)) return hipErrorInvalidValue;
         rows_kernel<T, D, CAP><<<(unsigned)blocks, kThreads, 0, st>>>(a);
         return hipGetLastError();

@@ -46,7 +46,8 @@ struct Args {
     const Marks *marks;    // of every 64 keys, [B, key_tiles]; null: neither documents nor prefix
     const char *zeros;     // 64 bytes of zeros, where marks are
     float2 *rows;          // backward: (lse in base 2, delta) of every query, [B * heads, query_tiles * 64]
-    int *powers;           // backward, fp16: per tile of 64 queries the power of two of its largest |dout|, [B * heads, query_tiles]
+    int *powers;           // backward, fp16: per tile of 64 queries the power of two of its largest |dout|, [B * heads, query_tiles], and
+    int *value_powers;     // per tile of 64 keys that of its values' largest sum of magnitudes, [B * kv, key_tiles]
     float *parts;          // where work is split: each part's fp32 sums.  queries: [q_splits, B * heads, Lq, D], in the forward pass with float2 (maximum, sum)
                            // [q_splits, B * heads, Lq] behind them; keys: of dK and dV, [k_splits, 2, B * kv, Lk, D]
     int q_splits, k_splits;   // parts that the work on one tile of queries, or of keys, is split into

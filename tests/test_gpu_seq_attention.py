@@ -3,10 +3,11 @@ import numpy as np
 import pytest
 import torch
 
+from oracle import seq_oracle
 from paper_2204_07143_amd import binding as na
 from paper_2204_07143_amd import functional as F
 
-from seq_util import HALF, TYPES, check, expect, f64, normal
+from seq_util import FP32, HALF, TYPES, check, expect, f64, normal
 
 pytestmark = pytest.mark.gpu
 
@@ -390,4 +391,52 @@ def test_padding_behind_fewer_queries_than_keys_may_hold_anything(dtype, Lq, Lk)
             assert torch.isfinite(b).all() and torch.equal(a, b)
     want, bound = expect(q, k, v, dout, dtype, **mask)
     for name, x in zip(("out", "dq", "dk", "dv"), clean):
+        check(name, x, want[name], bound[name])
+
+
+def test_flat_rows_over_a_million_keys_in_fp16():
+    """Weights of 2^-20 each, and dS with them: both keep fp16's digits.
+
+    A rounding is taken as independent of the others, of mean zero and within half a step, so a sum of n of them stays (Hoeffding) within 6 times the root of the sum of their
+    squares but in 2 of 10^8 cases.  Of dS: u |dS|, or half of 2^-24 on the scale it is held on, 2^15 of |dout| |v| for the largest there are, each taken to its power of two.
+    """
+    Lq, Lk, D, u = 2, 1 << 20, 32, HALF["f16"]
+    torch.manual_seed(23)
+    q, dout = (torch.randn((1, 1, Lq, D), device="cuda").mul_(s).half() for s in (1.0, 1000.0))   # (dk is of 2^-9 or so then, and none of fp16's smallest)
+    k, v = (torch.randn((1, 1, Lk, D), device="cuda").half() for _ in range(2))
+    got = _run(q, k, v, dout)
+    size = float(v.double().abs().sum(-1).max())
+    want, bound = expect(q, k, v, dout, "f16")
+    check("out", got[0], want["out"], bound["out"])
+    step = 2.0 ** -40 * 2 * size * 4   # of |dout|'s largest element in a row; 4: the other row's may be larger, and its power of two
+    bounds = seq_oracle.attention(*(f64(x) for x in (q, k, v, dout)), u=u, e=FP32, tiny=step)[1]
+    check("dk", got[2], want["dk"], bounds["dk"] + 2.0 ** -25)
+    # P: half of 2^-24 on a scale of 2^10
+    bounds = seq_oracle.attention(*(f64(x) for x in (q, k, v, dout)), u=u, e=FP32, tiny=2.0 ** -35)[1]
+    check("dv", got[3], want["dv"], bounds["dv"] + 2.0 ** -25)
+    q, k, v, dout = (x[0, 0].double() for x in (q, k, v, dout))
+    p = torch.softmax(q @ k.T * D ** -0.5, 1)
+    out = p @ v
+    ds = p * (dout @ v.T - (dout * out).sum(1, keepdim=True)) * D ** -0.5
+    off = u * ds.abs() + step * D ** -0.5 * dout.abs().amax(1, keepdim=True)
+    # the sum: a rounding to fp32 for every four keys at most, each within 2^-24 of the largest partial sum
+    partial = torch.stack([(row[:, None] * k).cumsum(0).abs().amax(0) for row in ds])
+    of_delta = (u + FP32) * (dout * out).abs().sum(1, keepdim=True) * (p @ k).abs() * D ** -0.5
+    tol = 6 * torch.sqrt(off.square() @ k.square()) + 6 * (Lk / 4) ** 0.5 * 2.0 ** -24 * partial + of_delta + (u + FP32) * (ds @ k).abs() + 2.0 ** -25
+    check("dq", got[1][0, 0], (ds @ k).cpu().numpy(), tol.cpu().numpy())
+
+
+@pytest.mark.parametrize("D", [32, 64, 128])
+@pytest.mark.parametrize("cap", [None, 50.0])
+def test_products_of_dout_and_values_beyond_fp16(D, cap):
+    """|dP| reaches D * 4000, dS half of that: held on a scale that takes in the values' size, as gradients that fp16 holds."""
+    g = np.random.default_rng(24)
+    q, k = normal(g, (1, 2, 40, D), "f16", 0.3), normal(g, (1, 1, 40, D), "f16", 0.05)
+    signs = torch.from_numpy(g.choice([-1.0, 1.0], (1, 1, 40, 1)).astype(np.float32)).cuda()
+    v = (4000 * signs.expand(1, 1, 40, D)).half().contiguous()
+    dout = (1 + normal(g, (1, 2, 40, D), "f32", 0.01)).half()
+    mask = dict(causal=True, softcap=cap)
+    got = _run(q, k, v, dout, **mask)
+    want, bound = expect(q, k, v, dout, "f16", **mask)
+    for name, x in zip(("out", "dq", "dk", "dv"), got):
         check(name, x, want[name], bound[name])
