@@ -41,7 +41,7 @@ int common(int B, int heads, int kv, int D, int dtype, float scale, float cap, i
     if (dtype != NA2D_F32 && dtype != NA2D_F16 && dtype != NA2D_BF16) return NA2D_ERR_DTYPE;
     if (B <= 0 || heads <= 0 || kv <= 0 || heads % kv) return NA2D_ERR_SHAPE;
     if (D != 32 && D != 64 && D != 128) return NA2D_ERR_HEAD_DIM;
-    // (a cap's scores are off by 2^-24 of it in 16 bit, see seq_common.hpp: up to 2^12 that is below what fp16 weights are rounded by)
+    // (a cap's scores are off by up to 2^-21 of it in 16 bit, see cap_form(): at 2^12 that is half of what bf16 weights are rounded by)
     if (cap != 0.f && (cap < 0x1p-20f || (dtype != NA2D_F32 && cap > 4096.f))) return NA2D_ERR_SHAPE;
     if (!std::isfinite(scale) || !std::isfinite(cap) || cap < 0.f || window < 0 || window > kFar) return NA2D_ERR_SHAPE;
     return NA2D_OK;
@@ -76,7 +76,7 @@ Args args(const seq_problem *p, const float *slopes, const int32_t *documents, b
     a.scale = p->scale;
     constexpr double log2e = 1.4426950408889634;
     if (p->softcap > 0.f) {
-        const bool sigmoid = p->dtype != NA2D_F32;
+        const bool sigmoid = cap_form(p->dtype, p->softcap) == kSigmoidCap;
         a.c = (float)(2.0 * log2e * p->scale / p->softcap);
         a.m = (float)((sigmoid ? -2.0 : 1.0) * log2e * p->softcap), a.from = sigmoid ? (float)(log2e * p->softcap) : 0.f;
         a.masked = sigmoid ? 1e18f : -1e18f;   // its square is finite, and its weight 0 for every cap from 2^-20 on
@@ -192,7 +192,7 @@ int seq_attention_fwd(const seq_problem *p, const void *q, const void *k, const 
     Args a = args(p, slopes, documents, documents != nullptr, prefix != nullptr);
     a.q = view(q, p->q, e), a.k = view(k, p->k, e), a.v = view(v, p->v, e), a.out = view(out, p->out, e), a.lse = lse, a.rest = static_cast<char *>(rest);
     if (int r = prepare(a, Space(a, p->D, documents || prefix, false), prefix, workspace, workspace_bytes, st)) return r;
-    return from_hip(launch_fwd(a, p->dtype, p->D, p->softcap > 0.f, st));
+    return from_hip(launch_fwd(a, p->dtype, p->D, cap_form(p->dtype, p->softcap), st));
 }
 
 int seq_attention_bwd(const seq_problem *p, const void *q, const void *k, const void *v, const float *slopes, const int32_t *documents, const uint8_t *prefix,
@@ -217,9 +217,10 @@ int seq_attention_bwd(const seq_problem *p, const void *q, const void *k, const 
     a.rows = reinterpret_cast<float2 *>(static_cast<char *>(workspace) + s.rows);
     a.powers = reinterpret_cast<int *>(static_cast<char *>(workspace) + s.powers);
     a.value_powers = reinterpret_cast<int *>(static_cast<char *>(workspace) + s.value_powers);
-    if (int r = from_hip(launch_rows(a, p->dtype, p->D, p->softcap > 0.f, st))) return r;
-    if (int r = from_hip(launch_bwd_q(a, p->dtype, p->D, p->softcap > 0.f, st))) return r;
-    return from_hip(launch_bwd_kv(a, p->dtype, p->D, p->softcap > 0.f, st));
+    const int cap = cap_form(p->dtype, p->softcap);
+    if (int r = from_hip(launch_rows(a, p->dtype, p->D, cap, st))) return r;
+    if (int r = from_hip(launch_bwd_q(a, p->dtype, p->D, cap, st))) return r;
+    return from_hip(launch_bwd_kv(a, p->dtype, p->D, cap, st));
 }
 
 int seq_cache_validate(const seq_cache_problem *p, int call) { return cache_validate(p, call); }
@@ -270,7 +271,7 @@ int seq_cache_attention(const seq_cache_problem *p, const void *q, const int8_t 
     a.a = view(q, p->q, e), a.b = view(out, p->out, e), a.k = const_cast<int8_t *>(k_pages), a.v = const_cast<int8_t *>(v_pages);
     a.ks = const_cast<float *>(k_scales), a.vs = const_cast<float *>(v_scales), a.table = table, a.lengths = lengths, a.slopes = slopes;
     a.part = static_cast<float *>(workspace);
-    return from_hip(launch_cache_attention(a, p->dtype, p->D, p->softcap > 0.f, static_cast<hipStream_t>(stream)));
+    return from_hip(launch_cache_attention(a, p->dtype, p->D, cap_form(NA2D_F16, p->softcap), static_cast<hipStream_t>(stream)));
 }
 
 }  // extern "C"

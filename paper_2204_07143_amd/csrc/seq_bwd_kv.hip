@@ -17,7 +17,7 @@ bool two_key_blocks(const Args &a, int D) { return D == 128 || two_blocks(a, D, 
 template <typename T, int D> constexpr bool kPair = sizeof(T) == 2 && D == 128;
 template <typename T, int D, int KB> constexpr int kKeys = 16 * KB * kWaves / (kPair<T, D> ? 2 : 1);   // of a workgroup
 
-template <typename T, int D, bool CAP, bool SLOPES, int KB>
+template <typename T, int D, int CAP, bool SLOPES, int KB>
 __global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) void bwd_kv_kernel(const Args p) {
     using L = Tile<T, D>;
     constexpr int RB = kRowBlocks<T>, NB = kTile / 16;
@@ -282,7 +282,7 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) void bwd_kv_kerne
     }
 }
 
-template <typename T, int D, bool CAP> struct BwdKV {
+template <typename T, int D, int CAP> struct BwdKV {
     template <bool SLOPES, int KB> static hipError_t launch(const Args &a, hipStream_t st) {
         constexpr int lds = 4 * Tile<T, D>::BYTES;
         static LdsAllowed allowed;
@@ -303,7 +303,7 @@ template <typename T, int D, bool CAP> struct BwdKV {
 
 }  // namespace
 
-hipError_t launch_bwd_kv(const Args &a, int dtype, int D, bool capped, hipStream_t st) { return dispatch<BwdKV>(dtype, D, capped, a, st); }
+hipError_t launch_bwd_kv(const Args &a, int dtype, int D, int cap, hipStream_t st) { return dispatch<BwdKV>(dtype, D, cap, a, st); }
 
 // A tile of 16-bit queries takes about 2.2 us.
 int k_splits(const Args &a, int dtype, int D) {

@@ -18,7 +18,7 @@ namespace seq {
 
 namespace {
 
-template <typename T, int D, bool CAP>
+template <typename T, int D, int CAP>
 __global__ __launch_bounds__(kThreads) void rows_kernel(const Args p) {
     using L = Tile<T, D>;
     constexpr int E = 16 / (int)sizeof(T);
@@ -82,7 +82,7 @@ __global__ __launch_bounds__(kThreads) void rows_kernel(const Args p) {
 
 // ---- dQ --------------------------------------------------------------------------------------------------------------------
 
-template <typename T, int D, bool CAP, bool SLOPES, int QB>
+template <typename T, int D, int CAP, bool SLOPES, int QB>
 __global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) void bwd_q_kernel(const Args p) {
     using L = Tile<T, D>;
     constexpr int RB = kRowBlocks<T>, NB = kTile / 16;
@@ -282,7 +282,7 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) void bwd_q_kernel
     }
 }
 
-template <typename T, int D, bool CAP> struct Rows {
+template <typename T, int D, int CAP> struct Rows {
     static hipError_t go(const Args &a, hipStream_t st) {
         const int64_t blocks = (int64_t)a.B * a.heads * a.query_tiles + (kScaled<T> ? (int64_t)a.B * a.kv * a.key_tiles : 0);
         if (!launch_holds(blocks, kThreads)) return hipErrorInvalidValue;
@@ -290,7 +290,7 @@ template <typename T, int D, bool CAP> struct Rows {
         return hipGetLastError();
     }
 };
-template <typename T, int D, bool CAP> struct BwdQ {
+template <typename T, int D, int CAP> struct BwdQ {
     template <bool SLOPES, int QB> static hipError_t launch(const Args &a, hipStream_t st) {
         constexpr int lds = 4 * Tile<T, D>::BYTES, rows = 16 * QB * kWaves;
         static LdsAllowed allowed;
@@ -310,7 +310,7 @@ template <typename T, int D, bool CAP> struct BwdQ {
 
 }  // namespace
 
-hipError_t launch_rows(const Args &a, int dtype, int D, bool capped, hipStream_t st) { return dispatch<Rows>(dtype, D, capped, a, st); }
-hipError_t launch_bwd_q(const Args &a, int dtype, int D, bool capped, hipStream_t st) { return dispatch<BwdQ>(dtype, D, capped, a, st); }
+hipError_t launch_rows(const Args &a, int dtype, int D, int cap, hipStream_t st) { return dispatch<Rows>(dtype, D, cap, a, st); }
+hipError_t launch_bwd_q(const Args &a, int dtype, int D, int cap, hipStream_t st) { return dispatch<BwdQ>(dtype, D, cap, a, st); }
 
 }  // namespace seq

@@ -166,7 +166,7 @@ __global__ __launch_bounds__(kThreads) void gather_kernel(const CacheArgs p, int
     }
 }
 
-template <typename T, int D, bool> struct Append {
+template <typename T, int D, int> struct Append {
     static hipError_t go(const CacheArgs &a, hipStream_t st) {
         const int page = 1 << a.page_log2, touched = (a.n + page - 2) / page + 1;   // pages that n tokens can lie in
         const int64_t blocks = (int64_t)a.B * touched * a.kv * 2;
@@ -175,7 +175,7 @@ template <typename T, int D, bool> struct Append {
         return hipGetLastError();
     }
 };
-template <typename T, int D, bool> struct Gather {
+template <typename T, int D, int> struct Gather {
     static hipError_t go(const CacheArgs &a, hipStream_t st) {
         constexpr int rows = kThreads / (D * (int)sizeof(T) / 16) * kRows;
         const int each = (a.n + rows - 1) / rows;

@@ -25,7 +25,7 @@ __device__ __forceinline__ bool page_at(const CacheArgs &p, int b, int64_t posit
 
 hipError_t launch_append(const CacheArgs &a, int dtype, int D, hipStream_t st);
 hipError_t launch_gather(const CacheArgs &a, int dtype, int D, hipStream_t st);
-hipError_t launch_cache_attention(const CacheArgs &a, int dtype, int D, bool capped, hipStream_t st);
+hipError_t launch_cache_attention(const CacheArgs &a, int dtype, int D, int cap, hipStream_t st);   // cap: the CapForm of fp16 weights, whatever the type of q
 void plan_cache_attention(CacheArgs &a, int64_t longest);   // splits, row_groups
 size_t cache_attention_bytes(const CacheArgs &a, int D);
 

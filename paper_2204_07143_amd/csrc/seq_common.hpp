@@ -299,12 +299,19 @@ __device__ __forceinline__ int block_in_order() {
 //
 // A score in base 2 is m y + from (args.m, args.from), less slope |distance|:
 //   no cap   y = <q, k>, m = scale log2(e)
-//   capped   with z = scale <q, k> / cap and y = 1 / (1 + e^2z): tanh z = 1 - 2 y, so m = -2 cap log2(e), from = cap log2(e), and the score's derivative by
-//            the product, 1 - tanh^2, is 4 y (1 - y).  That form is off by 2^-24 of the cap, below what 16-bit products carry for every cap they are given;
-//   fp32     takes the library's tanh for y, m = cap log2(e).
+//   kSigmoid with z = scale <q, k> / cap and y = 1 / (1 + e^2z): tanh z = 1 - 2 y, so m = -2 cap log2(e), from = cap log2(e), and the score's derivative by
+//            the product, 1 - tanh^2, is 4 y (1 - y).  A score of 0 is then off by up to 4 x 2^-24 of the cap, another by up to 8 x 2^-24 = 2^-21 (2^-24 of y for the sum, 2^-23
+//            each for the exponential and the reciprocal, y counting twice; the exponent and the score once each);
+//   kTanh    takes the library's tanh for y, m = cap log2(e): off by 2^-21 or so of the score itself.  More instructions, so only where the other form is not enough: fp16, 4 x 16 over
+//            4 x 2048, D 128, causal, forward 110 us with the sigmoid and 137 with the tanh, backward 371 and 440; 8 x 8192, D 64, 147 and 200, 445 and 571.
 // What is masked has a y that gives weights of 0 and, where 1 - tanh^2 is formed from it, something finite.
-template <typename T, bool CAP> struct Score {
-    static constexpr bool kSigmoid = CAP && sizeof(T) == 2;
+enum CapForm { kNoCap = 0, kSigmoidCap = 1, kTanhCap = 2 };
+// The weights are rounded by half a step of their type, 2^-11 of them in fp16 and 2^-8 in bf16.  2^-21 of the cap is no more than that up to 2^10 in fp16, and half of it
+// at 2^12, the largest that is accepted in 16 bit, in bf16.  fp32 always takes the tanh.
+inline int cap_form(int weights, float cap) { return cap == 0.f ? kNoCap : weights == NA2D_F32 || (weights == NA2D_F16 && cap > 1024.f) ? kTanhCap : kSigmoidCap; }
+
+template <typename T, int CAP> struct Score {
+    static constexpr bool kSigmoid = CAP == kSigmoidCap;
     __device__ static __forceinline__ float of(const Args &p, float s) {
         if constexpr (!CAP) return s;
         else if constexpr (kSigmoid) return __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(s * p.c));
@@ -322,10 +329,10 @@ template <typename T, bool CAP> struct Score {
 // ---- host ------------------------------------------------------------------------------------------------------------------
 
 hipError_t launch_marks(const Args &a, const uint8_t *prefix, Marks *marks, char *zeros, hipStream_t st);
-hipError_t launch_fwd(const Args &a, int dtype, int D, bool capped, hipStream_t st);
-hipError_t launch_rows(const Args &a, int dtype, int D, bool capped, hipStream_t st);
-hipError_t launch_bwd_q(const Args &a, int dtype, int D, bool capped, hipStream_t st);
-hipError_t launch_bwd_kv(const Args &a, int dtype, int D, bool capped, hipStream_t st);
+hipError_t launch_fwd(const Args &a, int dtype, int D, int cap, hipStream_t st);   // cap: a CapForm
+hipError_t launch_rows(const Args &a, int dtype, int D, int cap, hipStream_t st);
+hipError_t launch_bwd_q(const Args &a, int dtype, int D, int cap, hipStream_t st);
+hipError_t launch_bwd_kv(const Args &a, int dtype, int D, int cap, hipStream_t st);
 int q_splits(const Args &a, int dtype, int D);
 int k_splits(const Args &a, int dtype, int D);
 
@@ -364,13 +371,18 @@ struct Work {
 inline bool two_blocks(const Args &a, int D, int64_t planes, int rows) { return (D == 128 || !a.causal) && planes * ((rows + 127) / 128) >= 512; }
 inline bool two_query_blocks(const Args &a, int D) { return two_blocks(a, D, (int64_t)a.B * a.heads, a.Lq); }
 
-// L<T, D, capped>::go(...) of a type and head dim
-template <template <typename, int, bool> class L, typename... A> hipError_t dispatch(int dtype, int D, bool capped, A &&...a) {
-#define SEQ_D(T, N) (capped ? L<T, N, true>::go(a...) : L<T, N, false>::go(a...))
-#define SEQ_T(T) (D == 32 ? SEQ_D(T, 32) : D == 64 ? SEQ_D(T, 64) : SEQ_D(T, 128))
+// L<T, D, cap>::go(...) of a type, head dim and form of the cap (one that cap_form() gives for the type)
+template <typename T, int D, template <typename, int, int> class L, typename... A> hipError_t dispatch_cap(int cap, A &&...a) {
+    if (cap == kNoCap) return L<T, D, kNoCap>::go(a...);
+    if constexpr (sizeof(T) == 2)
+        if (cap == kSigmoidCap) return L<T, D, kSigmoidCap>::go(a...);
+    if constexpr (!__is_same(T, bf16_t)) return L<T, D, kTanhCap>::go(a...);
+    return hipErrorInvalidValue;
+}
+template <template <typename, int, int> class L, typename... A> hipError_t dispatch(int dtype, int D, int cap, A &&...a) {
+#define SEQ_T(T) (D == 32 ? dispatch_cap<T, 32, L>(cap, a...) : D == 64 ? dispatch_cap<T, 64, L>(cap, a...) : dispatch_cap<T, 128, L>(cap, a...))
     return dtype == NA2D_F32 ? SEQ_T(float) : dtype == NA2D_F16 ? SEQ_T(f16_t) : SEQ_T(bf16_t);
 #undef SEQ_T
-#undef SEQ_D
 }
 
 }  // namespace seq

@@ -88,7 +88,7 @@ template <int D, bool STREAM> struct Values {
     }
 };
 
-template <typename T, int D, int RT, bool CAP, bool PAGE16>
+template <typename T, int D, int RT, int CAP, bool PAGE16>
 __global__ __launch_bounds__(kThreads, RT == 1 ? 3 : 2) void decode_kernel(const CacheArgs p) {
     using S = Shape<D>;
     constexpr int ROWS = 16 * RT;
@@ -224,7 +224,8 @@ __global__ __launch_bounds__(kThreads, RT == 1 ? 3 : 2) void decode_kernel(const
 #pragma unroll
                     for (int r = 0; r < 4; ++r) {
                         float x = s[n][i][r] * by;
-                        if constexpr (CAP) x = __builtin_fmaf(-p.cap, __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(x)), 0.5f * p.cap);
+                        if constexpr (CAP == kTanhCap) x = 0.5f * p.cap * tanhf(0.5f * kLn2 * x);
+                        else if constexpr (CAP == kSigmoidCap) x = __builtin_fmaf(-p.cap, __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(x)), 0.5f * p.cap);
                         s[n][i][r] = x;
                     }
                 }
@@ -382,7 +383,7 @@ __global__ __launch_bounds__(kThreads) void join_kernel(const CacheArgs p, int r
 
 int rows_each(const CacheArgs &a) { return a.group * a.n > 16 ? 32 : 16; }
 
-template <typename T, int D, bool CAP> struct Decode {
+template <typename T, int D, int CAP> struct Decode {
     static hipError_t go(const CacheArgs &a, hipStream_t st) {
         const int64_t blocks = (int64_t)a.B * a.kv * a.row_groups * a.splits;
         if (!launch_holds(blocks, kThreads)) return hipErrorInvalidValue;
@@ -413,8 +414,8 @@ size_t cache_attention_bytes(const CacheArgs &a, int D) {
     return a.splits == 1 ? 0 : (size_t)a.B * a.kv * a.row_groups * a.splits * rows_each(a) * (D + 2) * sizeof(float);
 }
 
-hipError_t launch_cache_attention(const CacheArgs &a, int dtype, int D, bool capped, hipStream_t st) {
-#define SEQ_D(T, N) (capped ? Decode<T, N, true>::go(a, st) : Decode<T, N, false>::go(a, st))
+hipError_t launch_cache_attention(const CacheArgs &a, int dtype, int D, int cap, hipStream_t st) {
+#define SEQ_D(T, N) (cap == kNoCap ? Decode<T, N, kNoCap>::go(a, st) : cap == kSigmoidCap ? Decode<T, N, kSigmoidCap>::go(a, st) : Decode<T, N, kTanhCap>::go(a, st))
 #define SEQ_T(T) (D == 32 ? SEQ_D(T, 32) : D == 64 ? SEQ_D(T, 64) : SEQ_D(T, 128))
     return dtype == NA2D_F16 ? SEQ_T(f16_t) : SEQ_T(bf16_t);
 #undef SEQ_T

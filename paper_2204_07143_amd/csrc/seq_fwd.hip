@@ -23,7 +23,7 @@ namespace {
 // scores, makes out 1.18 and dq 1.1 times as inexact in bf16 (one key of a few that carry a row, then also in delta), for 3 % of the time.
 constexpr float kSlack = 8.f;
 
-template <typename T, int D, bool CAP, bool SLOPES, int QB>
+template <typename T, int D, int CAP, bool SLOPES, int QB>
 __global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) void fwd_kernel(const Args p) {
     using L = Tile<T, D>;
     constexpr int RB = kRowBlocks<T>, NB = kTile / 16;
@@ -251,7 +251,7 @@ __global__ __launch_bounds__(kThreads) void join_fwd_kernel(const Args p, int64_
     if (p.lse && d == 0) p.lse[row] = sum == 0.f ? -INFINITY : (most + __builtin_amdgcn_logf(sum)) * kLn2;
 }
 
-template <typename T, int D, bool CAP> struct Fwd {
+template <typename T, int D, int CAP> struct Fwd {
     template <bool SLOPES, int QB> static hipError_t launch(const Args &a, hipStream_t st) {
         constexpr int lds = 4 * Tile<T, D>::BYTES, rows = 16 * QB * kWaves;
         static LdsAllowed allowed;
@@ -302,6 +302,6 @@ int q_splits(const Args &a, int dtype, int D) {
     return parts_of((int64_t)a.B * a.heads * ((a.Lq + rows - 1) / rows), w.longest, w.tiles, 4, (int64_t)a.B * a.heads * a.Lq * (D + 2) * 4, 2.5e6);
 }
 
-hipError_t launch_fwd(const Args &a, int dtype, int D, bool capped, hipStream_t st) { return dispatch<Fwd>(dtype, D, capped, a, st); }
+hipError_t launch_fwd(const Args &a, int dtype, int D, int cap, hipStream_t st) { return dispatch<Fwd>(dtype, D, cap, a, st); }
 
 }  // namespace seq

@@ -7,7 +7,7 @@ from oracle import seq_oracle
 from paper_2204_07143_amd import binding as na
 from paper_2204_07143_amd import functional as F
 
-from seq_util import FP32, HALF, TYPES, check, expect, f64, normal
+from seq_util import FP32, HALF, TINY, TYPES, check, expect, f64, normal
 
 pytestmark = pytest.mark.gpu
 
@@ -440,3 +440,52 @@ def test_products_of_dout_and_values_beyond_fp16(D, cap):
     want, bound = expect(q, k, v, dout, "f16", **mask)
     for name, x in zip(("out", "dq", "dk", "dv"), got):
         check(name, x, want[name], bound[name])
+
+
+def _lse_of_one_key(dtype, cap, std):
+    """A query that sees one key has that score as its lse: (lse, the score in 64 bits, the size of the products that it is the sum of)."""
+    g = np.random.default_rng(25)
+    q, k = normal(g, (1, 1, 4096, 32), dtype, std), normal(g, (1, 1, 1, 32), dtype)
+    out, lse = torch.empty_like(q), torch.empty(q.shape[:3], device="cuda")
+    na.seq_attention_fwd(q, k, k, None, None, None, out, lse, scale=32 ** -0.5, softcap=cap)
+    scale = float(np.float32(32 ** -0.5))
+    size = (np.abs(f64(q)) @ np.abs(f64(k)).swapaxes(2, 3))[..., 0] * scale
+    return f64(lse), cap * np.tanh((f64(q) @ f64(k).swapaxes(2, 3))[..., 0] * scale / cap), size
+
+
+# <q, k> is a sum of 32 products in fp32, each rounding within 2^-24 of a partial sum: 2^-19 of their size.  The score from it, in base 2, and lse: factors of fp32 and their products,
+# and a tanh of a few 2^-24 or the sigmoid's form; 2^-19 of the score leaves 32 x 2^-24 for these.
+@pytest.mark.parametrize("dtype,cap", [("f16", 50.0), ("f16", 1024.0), ("bf16", 50.0), ("bf16", 1024.0), ("bf16", 4096.0)])
+@pytest.mark.parametrize("std", [0.1, 30.0, 3000.0])
+def test_capped_scores_are_off_by_little_of_the_cap(dtype, cap, std):
+    """1 - 2 / (1 + e^2z): 2^-24 of the fraction for the sum, 2^-23 each for the exponential and the reciprocal, and it counts twice at most: 6 x 2^-24, and one each for the exponent's
+    and the score's own rounding: 8 x 2^-24 = 2^-21 of the cap."""
+    lse, want, size = _lse_of_one_key(dtype, cap, std)
+    assert (np.abs(lse - want) <= 2.0 ** -21 * cap + 2.0 ** -19 * (size + np.abs(want))).all()
+
+
+@pytest.mark.parametrize("dtype,cap", [("f16", 1025.0), ("f16", 4096.0), ("f32", 50.0), ("f32", 4096.0), ("f32", 1e6)])
+@pytest.mark.parametrize("std", [0.1, 1.0, 300.0])
+def test_scores_far_below_a_large_cap_keep_their_digits(dtype, cap, std):
+    lse, want, size = _lse_of_one_key(dtype, cap, std)
+    assert (np.abs(lse - want) <= 2.0 ** -19 * (size + np.abs(want))).all()
+
+
+@TYPE
+@pytest.mark.parametrize("D", [32, 64, 128])
+@pytest.mark.parametrize("cap", [1000.0, 1500.0, 4096.0])
+def test_large_caps(dtype, D, cap):
+    """A weight is off by what its score is off by: 2^-21 of the cap where that is the sigmoid's (up to 1024 in fp16)."""
+    e = FP32 + (cap * 2.0 ** -21 if dtype == "bf16" or (dtype == "f16" and cap <= 1024) else 0.0)
+    g = np.random.default_rng(26)
+    for mask in (dict(causal=True, docs=2), dict(window=50, prefix=True)):
+        q, k, v, dout = normal(g, (2, 4, 150, D), dtype, 10.0), normal(g, (2, 2, 190, D), dtype), normal(g, (2, 2, 190, D), dtype), normal(g, (2, 4, 150, D), dtype)
+        mask["documents"], mask["prefix"] = _marks(g, 2, 190, mask.pop("docs", 0), mask.pop("prefix", False))
+        mask["softcap"] = cap
+        if not mask.get("causal"):
+            mask["slopes"] = torch.from_numpy(g.uniform(-0.1, 0.3, 4).astype(np.float32)).cuda()
+        got = _run(q, k, v, dout, **mask)
+        host = {n: (f64(x) if n == "slopes" else x.cpu().numpy()) if isinstance(x, torch.Tensor) else x for n, x in mask.items()}
+        want, bound = seq_oracle.attention(*(f64(x) for x in (q, k, v, dout)), u=HALF[dtype], e=e, tiny=TINY[dtype], **host)
+        for name, x in zip(("out", "dq", "dk", "dv"), got):
+            check(name, x, want[name], bound[name])

@@ -372,3 +372,18 @@ def test_queries_up_to_the_types_largest():
     assert (q.abs().amax(-1) >= 2.0 ** 127).all()
     got = F.seq_cache_attention(q, cache, _int(table.tolist()), _int([90, 90]), scale=2e-38)
     _check_attention(got, q, host, table, [90, 90], "bf16", scale=float(np.float32(2e-38)))
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("page,D", [(16, 32), (64, 64), (16, 128), (128, 128)])
+@pytest.mark.parametrize("cap", [1025.0, 4096.0])
+@pytest.mark.parametrize("n", [1, 6])
+def test_large_caps(dtype, page, D, cap, n):
+    """Beyond a cap of 1024 scores are off by no more than without one."""
+    g = np.random.default_rng(13)
+    lengths = [n, 33, 500, 129]
+    table, pages = _table(g, lengths, page)
+    host, cache = _cache(g, pages, 2, page, D)
+    q = normal(g, (len(lengths), 8, n, D), dtype, 3.0)
+    got = F.seq_cache_attention(q, cache, _int(table.tolist()), _int(lengths), softcap=cap)
+    _check_attention(got, q, host, table, lengths, dtype, softcap=cap)
