@@ -46,7 +46,7 @@ typedef struct {
     int32_t dtype;  /* na2d_dtype */
     int32_t causal; /* 0 or 1 */
     int32_t window; /* 0: none */
-    float scale;    /* finite */
+    float scale;    /* finite, and so in fp32 times log2(e), with a cap times 2 log2(e) / softcap */
     float softcap;  /* 0: none; else finite, from 2^-20 on, and in the 16-bit types at most 4096; up to 1024, and in bf16 to 4096, scores are off by up to 2^-21 of it */
     seq_strides q, k, v, out;      /* forward and backward */
     seq_strides dout, dq, dk, dv;  /* backward */

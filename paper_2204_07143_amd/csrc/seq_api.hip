@@ -37,6 +37,10 @@ int check_strides(const seq_strides &s, int64_t B, int64_t heads, int64_t rows, 
 }
 View view(const void *at, const seq_strides &s, int e) { return {static_cast<const char *>(at), s.batch * e, s.head * e, (int)(s.row * e)}; }
 
+constexpr double kLog2eExact = 1.4426950408889634;
+// what <q, k> is multiplied by: to a score in base 2, or to the exponent of e^2z
+float base2(float scale, float cap) { return cap > 0.f ? (float)(2.0 * kLog2eExact * scale / cap) : (float)(kLog2eExact * scale); }
+
 int common(int B, int heads, int kv, int D, int dtype, float scale, float cap, int window) {
     if (dtype != NA2D_F32 && dtype != NA2D_F16 && dtype != NA2D_BF16) return NA2D_ERR_DTYPE;
     if (B <= 0 || heads <= 0 || kv <= 0 || heads % kv) return NA2D_ERR_SHAPE;
@@ -44,6 +48,7 @@ int common(int B, int heads, int kv, int D, int dtype, float scale, float cap, i
     // (a cap's scores are off by up to 2^-21 of it in 16 bit, see cap_form(): at 2^12 that is half of what bf16 weights are rounded by)
     if (cap != 0.f && (cap < 0x1p-20f || (dtype != NA2D_F32 && cap > 4096.f))) return NA2D_ERR_SHAPE;
     if (!std::isfinite(scale) || !std::isfinite(cap) || cap < 0.f || window < 0 || window > kFar) return NA2D_ERR_SHAPE;
+    if (!std::isfinite(base2(scale, cap))) return NA2D_ERR_SHAPE;   // (infinite, it would make NaN of products that are 0)
     return NA2D_OK;
 }
 
@@ -74,14 +79,13 @@ Args args(const seq_problem *p, const float *slopes, const int32_t *documents, b
     a.causal = p->causal, a.window = p->window ? p->window : kFar;
     a.dlo = p->causal ? 0 : 1 - a.window;
     a.scale = p->scale;
-    constexpr double log2e = 1.4426950408889634;
     if (p->softcap > 0.f) {
         const bool sigmoid = cap_form(p->dtype, p->softcap) == kSigmoidCap;
-        a.c = (float)(2.0 * log2e * p->scale / p->softcap);
-        a.m = (float)((sigmoid ? -2.0 : 1.0) * log2e * p->softcap), a.from = sigmoid ? (float)(log2e * p->softcap) : 0.f;
+        a.c = base2(p->scale, p->softcap);
+        a.m = (float)((sigmoid ? -2.0 : 1.0) * kLog2eExact * p->softcap), a.from = sigmoid ? (float)(kLog2eExact * p->softcap) : 0.f;
         a.masked = sigmoid ? 1e18f : -1e18f;   // its square is finite, and its weight 0 for every cap from 2^-20 on
     } else {
-        a.m = p->scale == 0.f ? 1e-37f : (float)(log2e * p->scale);   // (0 times what is masked would be no number)
+        a.m = p->scale == 0.f ? 1e-37f : base2(p->scale, 0.f);   // (0 times what is masked would be no number)
         a.masked = a.m > 0.f ? -INFINITY : INFINITY;
     }
     a.packed = packed, a.prefix = prefix;
@@ -147,8 +151,8 @@ CacheArgs cache_args(const seq_cache_problem *p) {
     a.B = p->B, a.heads = p->heads, a.kv = p->kv_heads, a.group = p->heads / p->kv_heads, a.pages = p->pages, a.width = p->table_width, a.n = p->n;
     a.page_log2 = p->page == 16 ? 4 : p->page == 32 ? 5 : p->page == 64 ? 6 : 7;
     a.window = p->window ? p->window : kFar;
-    a.c = p->softcap > 0.f ? (float)(2.0 * 1.4426950408889634 * p->scale / p->softcap) : (float)(1.4426950408889634 * p->scale);
-    a.cap = (float)(2.0 * 1.4426950408889634 * p->softcap);
+    a.c = base2(p->scale, p->softcap);
+    a.cap = (float)(2.0 * kLog2eExact * p->softcap);
     plan_cache_attention(a, (int64_t)p->table_width * p->page);
     return a;
 }

@@ -143,3 +143,9 @@ def test_planes_whose_size_passes_64_bits():
     # the largest plane there is
     assert na.seq_validate_problem(P(B=1, heads=1, kv=1, Lq=(1 << 24) - 1, Lk=64, D=64, q=na.SeqStrides(0, 0, 64), out=na.SeqStrides(0, 0, 64))) == 0
     assert na.seq_validate_problem(P(B=1, heads=1, kv=1, Lq=1 << 24, Lk=64, D=64, q=na.SeqStrides(0, 0, 64), out=na.SeqStrides(0, 0, 64))) == -6
+
+
+@pytest.mark.parametrize("scale,cap,code", [(2.35e38, 0.0, 0), (2.4e38, 0.0, -6), (-2.4e38, 0.0, -6), (2e34, 1e-4, -6), (1e34, 1e-4, 0), (3e38, 50.0, 0), (-1e33, 2.0 ** -20, -6)])
+def test_scales_that_pass_fp32_on_the_way_to_base_2(scale, cap, code):
+    assert na.seq_validate_problem(P(scale=scale, cap=cap)) == code
+    assert tuple(na.seq_cache_validate(C(scale=scale, cap=cap), call) for call in range(3)) == (code,) * 3
