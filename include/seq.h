@@ -14,8 +14,8 @@
  *  - D in {32, 64, 128}; f32, f16, bf16.  Products, softmax statistics and sums are fp32; in the 16-bit types the weights, and
  *    in the backward pass their gradients, are rounded to the type where they enter a product.
  *  - fp16 has no step below 2^-24.  In out, a weight below 2^-14 of its row's largest loses digits, and one below 2^-25 of it counts as 0, as do a million of
- *    them.  The backward pass holds weights times 2^10, and their gradients on a scale that the largest |dout| and the largest sum |v| of a key make, whatever the size of
- *    either: rows that are flat over their keys keep the type's digits up to about 2^20 keys, and one digit less for each power of two beyond.
+ *    them.  The backward pass holds weights times 2^10, and their gradients on a scale that the largest |dout| and the largest sum |v| of the keys in reach (window and
+ *    documents, to whole tiles) make, whatever the size of either: rows that are flat over their keys keep the type's digits up to about 2^20 keys, and one digit less for each power of two beyond.
  *  - Return value: NA2D_OK or a negative na2d_status; argument errors are detected on the host before any HIP call.
  *
  * Which keys a query sees

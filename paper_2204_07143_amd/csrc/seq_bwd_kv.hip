@@ -25,7 +25,7 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) void bwd_kv_kerne
     extern __shared__ __align__(16) char lds[];
     __shared__ __align__(16) int ids[2][kTile];
     __shared__ __align__(16) float2 stats[2][kTile];
-    __shared__ int range[5][kWaves];
+    __shared__ int range[4][kWaves];
     __shared__ __align__(16) u32x4 given[PAIR ? kWaves : 1][KB][PAIR ? kWave : 1];
     const int tid = threadIdx.x, lane = tid % kWave, wave = uniform(tid / kWave), j = lane & 15, g = lane >> 4;
     const int role = PAIR ? wave & 1 : 0, group_of_keys = PAIR ? wave >> 1 : wave;
@@ -63,26 +63,32 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) void bwd_kv_kerne
             const uint64_t x = __ballot(marks[i / kTile].prefix >> (i % kTile) & 1);
             prefix_some = x != 0, prefix_all = x == ~0ull;
         }
-        int most = kNothing, values = kNothing;
-        if constexpr (kScaled<T>) {   // over the tiles of every head that shares these keys, and of all keys that their queries may see
-            const int *of = p.powers + ((int64_t)b * p.heads + kh * p.group) * p.query_tiles, *of_v = p.value_powers + (int64_t)plane * p.key_tiles;
+        int most = kNothing;
+        if constexpr (kScaled<T>) {   // over the tiles of every head that shares these keys
+            const int *of = p.powers + ((int64_t)b * p.heads + kh * p.group) * p.query_tiles;
             for (int n = tid; n < p.group * p.query_tiles; n += kThreads) most = max(most, of[n]);
-            for (int n = tid; n < p.key_tiles; n += kThreads) values = max(values, of_v[n]);
-            most = wave_max(most), values = wave_max(values);
+            most = wave_max(most);
         }
-        if (lane == 0) range[0][wave] = dw.lo, range[1][wave] = dw.hi, range[2][wave] = prefix_some, range[3][wave] = most, range[4][wave] = values;
+        if (lane == 0) range[0][wave] = dw.lo, range[1][wave] = dw.hi, range[2][wave] = prefix_some, range[3][wave] = most;
         workgroup_sync();
         dg = {range[0][0], range[1][0], false};
-        most = range[3][0], values = range[4][0];
+        most = range[3][0];
         prefix_any = range[2][0] | range[2][1] | range[2][2] | range[2][3];
 #pragma unroll
-        for (int w = 1; w < kWaves; ++w) dg.lo = min(dg.lo, range[0][w]), dg.hi = max(dg.hi, range[1][w]), most = max(most, range[3][w]), values = max(values, range[4][w]);
+        for (int w = 1; w < kWaves; ++w) dg.lo = min(dg.lo, range[0][w]), dg.hi = max(dg.hi, range[1][w]), most = max(most, range[3][w]);
         dg.lo = uniform(dg.lo), dg.hi = uniform(dg.hi);
         if (kScaled<T> && most != kNothing) power = uniform(most);
-        if (kScaled<T>) raise = raise_of(uniform(values));
     }
     const int ka = k0, kb = min(k0 + kKeys<T, D, KB>, p.Lk) - 1;
     const int wa = min(kw, p.Lk - 1), wb = min(kw + 16 * KB, p.Lk) - 1;
+    if constexpr (kScaled<T>) {   // over the keys that are seen by a query that sees these: what the window reaches from there, of their documents
+        const int qa = max(ka + p.dlo, p.off), qb = min(kb + p.window, p.Lk) - 1;
+        int e = kNothing, near = 0, far = p.key_tiles - 1;
+        if (!p.prefix) near = max(0, qa - p.window + 1) / kTile, far = min(far, max(-1, qb - p.dlo) >> 6);
+        for (int t = near + lane; t <= far; t += kWave)
+            if (!documents || Docs{marks[t].dmin, marks[t].dmax, false}.meet(dg)) e = max(e, p.value_powers[(int64_t)plane * p.key_tiles + t]);
+        raise = raise_of(uniform(wave_max(e)));
+    }
     auto of = [&](int t, Marks &m) {   // (of a tile of queries: their positions begin inside a tile of keys)
         const int qa = t * kTile + p.off, qb = min(t * kTile + kTile, p.Lq) - 1 + p.off;
         bool any = near_any(p, qa, qb, ka, kb) || prefix_any, some = near_any(p, qa, qb, wa, wb) || prefix_some, all = near_all(p, qa, qb, wa, wb) || prefix_all;

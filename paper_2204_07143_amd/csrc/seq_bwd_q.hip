@@ -159,7 +159,10 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) void bwd_q_kernel
     }
     if constexpr (kScaled<T>) {
         int e = kNothing;
-        for (int t = first + lane; t <= last; t += kWave) e = max(e, p.value_powers[((int64_t)b * p.kv + kh) * p.key_tiles + t]);
+        for (int t = first + lane; t <= last; t += kWave) {
+            Marks m;
+            if (of(t, m) & 1) e = max(e, p.value_powers[((int64_t)b * p.kv + kh) * p.key_tiles + t]);
+        }
         const int raise = raise_of(uniform(wave_max(e)));
 #pragma unroll
         for (int n = 0; n < QB; ++n) power[n] -= raise, lse[n] -= kRaise<T> + (float)power[n];

@@ -489,3 +489,27 @@ def test_large_caps(dtype, D, cap):
         want, bound = seq_oracle.attention(*(f64(x) for x in (q, k, v, dout)), u=HALF[dtype], e=e, tiny=TINY[dtype], **host)
         for name, x in zip(("out", "dq", "dk", "dv"), got):
             check(name, x, want[name], bound[name])
+
+
+@pytest.mark.parametrize("window", [None, 4096])
+def test_large_values_that_a_query_does_not_see_in_fp16(window):
+    """Values of 30000 in another document, or before the window, leave the scale of dS as it is."""
+    Lq, Lk, D, seen = 4, 5120, 64, 4096
+    g = np.random.default_rng(28)
+    q, dout = normal(g, (1, 2, Lq, D), "f16", 0.1), normal(g, (1, 2, Lq, D), "f16", 100.0)
+    k, v = normal(g, (1, 1, Lk, D), "f16"), normal(g, (1, 1, Lk, D), "f16")
+    v[:, :, :Lk - seen - Lq - 60] = 30000.0   # (960 keys: whole tiles)
+    mask = dict(causal=True, window=window)
+    if window is None:
+        mask["documents"] = (torch.arange(Lk, device="cuda") >= Lk - seen - Lq - 60).int()[None]
+    got = _run(q, k, v, dout, **mask)
+    want, bound = expect(q, k, v, dout, "f16", **mask)
+    for name, x in zip(("out", "dq"), got):
+        check(name, x, want[name], bound[name])
+    near = v[:, :, -seen - Lq - 60:]
+    step = 2.0 ** -40 * 2 * float(near.double().abs().sum(-1).max()) * 8   # half a step of dS on its scale, see above; 8: the largest |dout| of another row or head, and its power of two
+    host = {n: x.cpu().numpy() if isinstance(x, torch.Tensor) else x for n, x in mask.items()}
+    bounds = seq_oracle.attention(*(f64(x) for x in (q, k, v, dout)), u=HALF["f16"], e=FP32, tiny=step, **host)[1]
+    check("dk", got[2], want["dk"], bounds["dk"] + 2.0 ** -25)
+    bounds = seq_oracle.attention(*(f64(x) for x in (q, k, v, dout)), u=HALF["f16"], e=FP32, tiny=2.0 ** -35, **host)[1]
+    check("dv", got[3], want["dv"], bounds["dv"] + 2.0 ** -25)
