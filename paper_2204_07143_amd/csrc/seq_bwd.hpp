@@ -18,8 +18,6 @@ constexpr int kMostDout = 16, kMostValues = 23;   // fp16, and 128 of them
 __device__ __forceinline__ int raise_of(int e) { return 15 - (e == kNothing ? 0 : e); }
 __device__ __forceinline__ float two_to(int e) { return __builtin_amdgcn_ldexpf(1.f, e); }
 
-template <typename T> constexpr int kBlocks = sizeof(T) == 2 ? 2 : 1;   // blocks of 16 queries, or keys, that a wave keeps
-
 // Parts' sums [parts, (a and then b), B * heads, L, D], added in order into a and b (nullable); a thread per four channels.
 template <typename T, int D>
 __global__ __launch_bounds__(kThreads) void join_kernel(const float *sums, int parts, int heads, int L, int64_t planes, View a, View b, int64_t each) {

@@ -29,7 +29,7 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) void fwd_kernel(c
     constexpr int RB = kRowBlocks<T>, NB = kTile / 16;
     extern __shared__ __align__(16) char lds[];
     __shared__ __align__(16) int ids[2][kTile];
-    __shared__ int range[3][kWaves];
+    __shared__ int range[2][kWaves];
     const int tid = threadIdx.x, lane = tid % kWave, wave = uniform(tid / kWave), j = lane & 15, g = lane >> 4;
     const int tiles = (p.Lq + 16 * QB * kWaves - 1) / (16 * QB * kWaves);
     // key heads in turn, the last queries (in causal order the longest work) first, the query heads of one key head next to each other
