@@ -595,6 +595,7 @@ def seq_cache_problem(rows, k_pages, table, *, heads=None, window=0, softcap=0.0
 
 
 def seq_cache_validate(p: SeqCacheProblem, call: int) -> int:
+    """call: SEQ_CACHE_APPEND, SEQ_CACHE_GATHER or SEQ_CACHE_ATTENTION."""
     return int(load().seq_cache_validate(ctypes.byref(p), call))
 
 

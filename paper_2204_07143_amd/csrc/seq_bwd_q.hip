@@ -5,9 +5,9 @@
 //   keys      S = Q K^T, dP = dO V^T, dV^T += dO^T P, dK^T += Q^T dS                             a wave keeps 16 KB keys, walks the queries of
 //                                                                                               every head that shares them
 // Seven products instead of the five that a single kernel would take, and every sum in one wave's registers in a fixed order: no atomics.
-// bf16, D 128: 2 x 16 over 4 x 8192, not causal, 4.0 ms or 0.69 PFLOP/s of the five products (0.96 of the seven); 4 x 16 over 4 x 2048, causal, capped, 12 + 139 + 217 us and
-// 15 for the key side's join (vector instructions 49 and 42 % of the cycles, matrix ones 30 and 25 %).  The rows are read at the rate of memory: 100 MB in 16 us.
-// fp32, D 32, 2 x 4 x 3136, causal, slopes: 5 + 96 + 5 + 125 + 6 us, matrix instructions 52 % of the cycles.
+// bf16, D 128: 2 x 16 over 4 x 8192, not causal, 4.0 ms or 0.69 PFLOP/s of the five products (0.96 of the seven); 4 x 16 over 4 x 2048, causal, capped, 16 + 153 + 236 us and
+// 15 for the key side's join, under the profiler's lower clock (vector instructions 49 and 43 % of the cycles, matrix ones 30 and 26 %, waves wait 30 and 37 %: neither unit is full).  The
+// rows are read at the rate of memory: 100 MB in 16 us.  fp32, D 32, 2 x 4 x 3136, causal, slopes: 5 + 95 + 5 + 123 + 6 us, matrix instructions 51 to 54 % of the cycles, vector ones 25 to 28 %.
 //
 // fp16 holds 2^-24 to 65504.  The weights enter dV's product times 2^10, and dS on a scale that the largest |dout| of its query (queries) or of the heads that share
 // the key (keys) and the largest sum |v| of the keys make: as high as it can be without passing 65504 (raise_of()), so gradients far below 1, weights of 2^-20 of a

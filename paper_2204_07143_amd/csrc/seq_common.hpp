@@ -367,7 +367,8 @@ struct Work {
 // 16 bit: two blocks of 16 queries, or keys, to a wave (a fragment from LDS then serves two products) where that leaves two workgroups to each compute unit; but up
 // to 64 channels in causal order, where the work of workgroups differs, one, and the larger number of them.  Forward, us for one / two: 2 x 16 over 4 x 8192, D 128, not
 // causal 1462 / 1128; 4 x 16 over 4 x 2048, D 128, capped, causal 143 / 124; 4 x 16 x 2048, D 64, not causal 118 / 108, causal 71 / 79; D 32 76 / 71 and 58 / 70;
-// 3 x 6 x 1571, D 64, 234 workgroups of two, 39.2 / 41.5.  Key side, a backward pass: D 64, not causal 308 / 287, causal 226 / 236, capped too 290 / 318.
+// 3 x 6 x 1571, D 64, 234 workgroups of two, 39.2 / 41.5.  Key side, a backward pass: D 64, not causal 308 / 287, causal 226 / 236, capped too 290 / 318.  Long rows are even:
+// 16 x 8192, D 64, causal, forward 213 / 230, backward 627 / 606.
 inline bool two_blocks(const Args &a, int D, int64_t planes, int rows) { return (D == 128 || !a.causal) && planes * ((rows + 127) / 128) >= 512; }
 inline bool two_query_blocks(const Args &a, int D) { return two_blocks(a, D, (int64_t)a.B * a.heads, a.Lq); }
 

@@ -8,7 +8,7 @@
 //   O^T += vs V^T P  a lane holds D / 16 channels of its eight tokens; product block db takes channel db of each lane, so no value changes lanes
 // The four waves' parts are joined through LDS.  Few sequences: their ranges are split over workgroups, and a second kernel joins the splits in order.
 //
-// Bound by memory where there is much to read: 64 sequences of up to 16000 tokens, 32 heads over 8, D 128, capped, 1.2 GB in 222 us, 5.6 of the 5.7 TB/s that a
+// Bound by memory where there is much to read: 64 sequences of up to 16000 tokens, 32 heads over 8, D 128, capped, 1.25 GB in 231 us with the join, 5.4 of the 5.7 TB/s that a
 // large read reaches.  Short ranges are bound by what follows on each other: about 4 us to the first step and behind the last, 0.85 us a step of a wave (1.25 with 32 rows), two launches.
 // 16 sequences with a window of 2048 and 5 tokens each, 16 heads over 2: 15 + 4 us (reads two steps ahead 16, 48 rows to a workgroup 18, 256 tokens a split 15).
 #include "seq_cache.hpp"
@@ -401,7 +401,8 @@ template <typename T, int D, int CAP> struct Decode {
 }  // namespace
 
 // Ranges are split until there are about sixteen workgroups to each of the 256 compute units (sequences differ in length), but no split is given less than 256
-// tokens of the longest sequence that the table can hold, or 512 where a workgroup leaves 32 rows.  us, 64 sequences of 9000 tokens, 8 x 128, for 1024, 2048 and
+// tokens of the longest sequence that the table can hold (the lengths are on the GPU), or 512 where a workgroup leaves 32 rows; a table far wider than the sequences costs workgroups
+// that have nothing to do: 16 sequences of 500 tokens, 32 heads over 8, table of 32 pages of 16 9.5 us, of 8192 pages 36.  us, 64 sequences of 9000 tokens, 8 x 128, for 1024, 2048 and
 // 4096 workgroups 260, 251, 243; one of 16000 tokens in 256s and 512s 23 and 22; 4 of 8000, 32 rows, 36 and 28.
 void plan_cache_attention(CacheArgs &a, int64_t longest) {
     a.row_groups = (a.group * a.n + rows_each(a) - 1) / rows_each(a);

@@ -8,10 +8,12 @@
 // nothing are left out, tiles in which a wave sees all take no mask.
 //
 // What bounds it: the SIMDs, which issue about 35 vector instructions to every 16 products of a tile.  Two images of 64 keys each take 64 KB at 128 channels in
-// 16 bit, so two workgroups are on a compute unit, and a wave keeps 32 queries so that a fragment from LDS serves two products (no bank conflicts are left).
-// bf16, D 128: 2 x 16 over 4 x 8192, not causal, 1.08 to 1.13 ms or about 1 PFLOP/s, 88 % of a library product of 8192 x 8192; 4 x 16 over 4 x 2048, causal, capped, 124 us, where the cap's
-// exponential and reciprocal (a quarter of the rate each) make vector instructions 52 % of the cycles and matrix instructions 24 %.  fp32, D 32, 2 x 4 x 3136, causal,
-// slopes: 71 us, matrix instructions 46 % of the cycles and vector ones 30 %, which an fp32 matrix instruction does not let pass beside it.
+// 16 bit, so two workgroups are on a compute unit, and a wave keeps 32 queries so that a fragment from LDS serves two products (without bank conflicts in 16 bit; in fp32, whose
+// transposed reads take a word at a time, 40 % of the LDS's cycles are conflicts, behind the matrix instructions).
+// bf16, D 128: 2 x 16 over 4 x 8192, not causal, 1.08 to 1.13 ms or about 1 PFLOP/s, 88 % of a library product of 8192 x 8192; 4 x 16 over 4 x 2048, causal, capped, 127 us: the cap's
+// exponential and reciprocal (a quarter of the rate each) make vector instructions 52 % of the cycles, matrix instructions are 24 %, and waves wait 29 % of their time: neither unit is
+// full, and two waves to a SIMD do not cover each other.  fp32, D 32, 2 x 4 x 3136, causal, slopes: 71 us, matrix instructions 45 % of the cycles and vector ones 29 %, which an fp32
+// matrix instruction does not let pass beside it.
 #include "lds_attr.hpp"
 #include "seq_common.hpp"
 
@@ -19,8 +21,8 @@ namespace seq {
 
 namespace {
 
-// Weights reach 2^8: fp16 holds them with all digits, and their sum.  Most rows' largest weight is 1, which takes no rounding: a fixed reference instead, where a cap bounds the
-// scores, makes out 1.18 and dq 1.1 times as inexact in bf16 (one key of a few that carry a row, then also in delta), for 3 % of the time.
+// Weights reach 2^8: fp16 holds them with all digits, and their sum.  Where a row's maximum is the reference its weight is 1 and takes no rounding; elsewhere it is up to 2^8 and is
+// rounded like the others.  A fixed reference instead, where a cap bounds the scores, made out 1.18 and dq 1.1 times as inexact in bf16 (causal, cap 50, L 2048), for 3 % of the time.
 constexpr float kSlack = 8.f;
 
 template <typename T, int D, int CAP, bool SLOPES, int QB>

@@ -343,7 +343,8 @@ def seq_attention(q, k, v, *, causal: bool = False, window: int | None = None, s
     ``prefix`` (bool [B, Lk]); of all these only the keys of its own document (``documents``, int32 [B, Lk], Lq <= Lk; a
     negative one marks padding, which sees and is seen by nobody).  A score is ``softcap * tanh(scale <q, k> / softcap)`` (None: ``scale <q, k>``)
     less ``slopes[head] * |distance|`` (fp32 [heads]).  ``scale`` is D ** -0.5 unless given.  D is 32, 64 or 128; f32, f16, bf16.  The
-    tensors may be strided views ([B, L, heads, D] transposed); others than of whole 16-byte rows are copied.
+    tensors may be strided views ([B, L, heads, D] transposed); others than of whole 16-byte rows are copied.  A call that is differentiated keeps q, k, v, out and
+    its log-sum-exp for the backward pass, and in 16 bit a second tensor of out's size: what out's rounding took.
     """
     out = _native().seq_attention(q, k, v, causal, window, softcap, slopes, documents, prefix, scale)
     if out is not None:
@@ -392,7 +393,7 @@ def seq_cache_gather(cache: SeqCache, table, lengths, first, n: int, dtype=torch
 
 def seq_cache_attention(q, cache: SeqCache, table, lengths, *, window: int | None = None, softcap: float | None = None, slopes=None, scale: float | None = None):
     """Attention of each sequence's last n tokens, ``q`` [B, heads, n, D] in f16 or bf16, over its cache, which holds their keys and values already:
-    ``lengths`` counts them.  In causal order; scores as ``seq_attention`` has them.  Not differentiable."""
+    ``lengths`` counts them.  The work is laid out for sequences as long as ``table`` is wide: hand in the columns in use.  In causal order; scores as ``seq_attention`` has them.  Not differentiable."""
     out = _native().seq_cache_attention(q, *cache, table, lengths, window, softcap, slopes, scale)
     if out is not None:
         return out
