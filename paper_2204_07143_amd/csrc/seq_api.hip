@@ -67,7 +67,7 @@ int validate(const seq_problem *p, bool backward) {
     // every launch of the passes (the smallest tiles: 64 rows) holds its workgroups
     const int64_t q_tiles = ((int64_t)p->Lq + kTile - 1) / kTile, k_tiles = ((int64_t)p->Lk + kTile - 1) / kTile;
     const int64_t of_q = (int64_t)p->B * p->heads * q_tiles, of_k = (int64_t)p->B * p->kv_heads * k_tiles;
-    if (!launch_holds(of_q, kThreads) || !launch_holds(of_k, kThreads) || (backward && !launch_holds(of_q + of_k, kThreads))) return NA2D_ERR_SHAPE;
+    if (!launch_holds(of_q, kThreads) || !launch_holds(of_k, kThreads) || (backward && p->dtype == NA2D_F16 && !launch_holds(of_q + 1, kThreads))) return NA2D_ERR_SHAPE;
     return NA2D_OK;
 }
 

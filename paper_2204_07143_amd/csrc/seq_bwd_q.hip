@@ -34,8 +34,9 @@ __global__ __launch_bounds__(kThreads) void rows_kernel(const Args p) {
         return power_of(fmaxf(fmaxf(most_of[0], most_of[1]), fmaxf(most_of[2], most_of[3])), highest);
     };
     if constexpr (kScaled<T>) {
-        const int unit = (int)blockIdx.x - p.B * p.heads * p.query_tiles;
-        if (unit >= 0) {   // a tile of keys
+        const int of_queries = p.B * p.heads * p.query_tiles;
+        for (int unit = (int)blockIdx.x - of_queries; unit >= 0 && unit < p.B * p.kv * p.key_tiles; unit += gridDim.x - of_queries) {   // tiles of keys
+            most = 0.f;
             const int plane = unit / p.key_tiles, tile = unit % p.key_tiles, b = plane / p.kv;
             const char *v = p.v.at + b * p.v.b + plane % p.kv * p.v.h;
 #pragma unroll
@@ -51,8 +52,9 @@ __global__ __launch_bounds__(kThreads) void rows_kernel(const Args p) {
             }
             const int e = power(kMostValues);
             if (tid == 0) p.value_powers[unit] = e;
-            return;
+            workgroup_sync();   // (before the maxima are written again)
         }
+        if ((int)blockIdx.x >= of_queries) return;
     }
     const int plane = blockIdx.x / p.query_tiles, tile = blockIdx.x % p.query_tiles, b = plane / p.heads, h = plane % p.heads;
     const char *o = p.out.at + b * p.out.b + h * p.out.h, *d = p.dout.at + b * p.dout.b + h * p.dout.h;
@@ -287,7 +289,9 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) void bwd_q_kernel
 
 template <typename T, int D, int CAP> struct Rows {
     static hipError_t go(const Args &a, hipStream_t st) {
-        const int64_t blocks = (int64_t)a.B * a.heads * a.query_tiles + (kScaled<T> ? (int64_t)a.B * a.kv * a.key_tiles : 0);
+        const int64_t of_q = (int64_t)a.B * a.heads * a.query_tiles, of_k = (int64_t)a.B * a.kv * a.key_tiles;
+        int64_t blocks = of_q + (kScaled<T> ? (of_k < 4096 ? of_k : 4096) : 0);   // (workgroups take several tiles of keys where there are more than sixteen to a compute unit)
+        if (kScaled<T> && !launch_holds(blocks, kThreads)) blocks = of_q + 1;
         if (!launch_holds(blocks, kThreads)) return hipErrorInvalidValue;
         rows_kernel<T, D, CAP><<<(unsigned)blocks, kThreads, 0, st>>>(a);
         return hipGetLastError();

@@ -149,3 +149,13 @@ def test_planes_whose_size_passes_64_bits():
 def test_scales_that_pass_fp32_on_the_way_to_base_2(scale, cap, code):
     assert na.seq_validate_problem(P(scale=scale, cap=cap)) == code
     assert tuple(na.seq_cache_validate(C(scale=scale, cap=cap), call) for call in range(3)) == (code,) * 3
+
+
+@pytest.mark.parametrize("dtype", [0, 1, 2])
+def test_as_many_tiles_as_a_launch_holds(dtype):
+    """2^24 - 1 workgroups of 256: of queries and of keys each, in either pass; fp16's backward pass forms the keys' sizes beside the queries'."""
+    most = (1 << 24) - 1
+    for B, heads, L, code in ((most, 1, 64, 0), (1 << 12, 1 << 12, 64, -6), ((1 << 24) - 2, 1, 1, 0), (1 << 23, 1, 65, -6)):
+        p = P(B=B, heads=heads, kv=heads, Lq=L, Lk=L, D=32, dtype=dtype, **{n: na.SeqStrides(heads * L * 32, L * 32, 32) for n in ("q", "k", "v", "out", "dout", "dq", "dk", "dv")})
+        assert na.seq_validate_problem(p) == code, (B, heads, L)
+        assert na.seq_validate_problem(p, True) == (-6 if dtype == 1 and B == most else code), (B, heads, L)
