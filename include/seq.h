@@ -1,8 +1,8 @@
 /*
  * seq.h -- C ABI of the MI355X (gfx950) attention over token sequences (same library as na2d.h, whose dtype and status
  * codes are reused): softmax attention with causal order, a window, capped scores, a distance bias, a document mask and a
- * prefix mask, forward and backward; and, for serving, a cache of keys and values held in 8 bits, its append, reading it
- * back, and attention over it.
+ * prefix mask, forward and backward; the rotation of queries and keys by their positions, with the norm of each head before it, forward and
+ * backward; and, for serving, a cache of keys and values held in 8 bits, its append, reading it back, and attention over it.
  *
  * Conventions (as in na2d.h unless stated)
  * ----------------------------------------
@@ -73,6 +73,44 @@ int seq_attention_bwd(const seq_problem *p, const void *q, const void *k, const 
                       void *stream);
 
 /*
+ * Rotation of head vectors by their tokens' positions, with the norm of each vector before it:
+ *    y = x w / sqrt(mean of x^2 + eps)      (no weight: y = x)
+ *    (z_a, z_b) = (y_a cos t - y_b sin t, y_b cos t + y_a sin t),  t = position * freqs[p] of pair p
+ * Pair p is channels p and p + pairs, or if `interleaved` 2 p and 2 p + 1; channels from 2 pairs on are not rotated.  A token has a position on each axis (time, row,
+ * column); the first sections[0] pairs turn by the first axis' position, the next sections[1] by the second's, and so on.  Angles are formed and reduced in 64 bits.
+ */
+typedef struct {
+    int32_t pairs;        /* a multiple of 8, at most D / 2 */
+    int32_t axes;         /* 1 to 4 */
+    int32_t sections[4];  /* pairs of each axis, at least 1 each; their sum is pairs */
+    int32_t interleaved;  /* 0 or 1 */
+    int32_t weight_dtype; /* of the norms' weights and their gradients: the problem's dtype, or NA2D_F32 */
+    float eps;            /* above 0 and finite; sums of squares are fp32 */
+} seq_rotation;
+
+typedef struct {
+    int32_t B, heads, kv_heads, L, D; /* D in {16, 32, 64, 128}; kv_heads 0: queries only; B * L below 2^31 */
+    int32_t dtype;
+    seq_rotation rotation;
+    int32_t shared;                   /* positions: 1: int32 [axes, L], of every batch item; 0: [B, axes, L]; contiguous */
+    seq_strides q, k, q_out, k_out;   /* forward: inputs and outputs.  backward: the forward's inputs (read only where there is a weight), and the outputs' gradients */
+    seq_strides dq, dk;               /* backward */
+} seq_rotary_problem;
+
+/* Host only. */
+int seq_rotary_validate(const seq_rotary_problem *p, int backward);
+
+/* q: [B, heads, L, D], k: [B, kv_heads, L, D] to q_out, k_out (other memory).  freqs: fp32 [pairs].  q_weight, k_weight: [D], each NULL for no norm. */
+int seq_rotary_fwd(const seq_rotary_problem *p, const void *q, const void *k, const int32_t *positions, const float *freqs, const void *q_weight, const void *k_weight,
+                   void *q_out, void *k_out, void *stream);
+
+/* dq, dk and, of weights that are given, dq_weight, dk_weight [D] from the outputs' gradients dq_out, dk_out (strides p->q_out, p->k_out).  q, k may be NULL where their
+ * weight is.  Sums are added in an order that does not vary. */
+int seq_rotary_bwd(const seq_rotary_problem *p, const void *q, const void *k, const int32_t *positions, const float *freqs, const void *q_weight, const void *k_weight,
+                   const void *dq_out, const void *dk_out, void *dq, void *dk, void *dq_weight, void *dk_weight, void *workspace, size_t workspace_bytes, void *stream);
+size_t seq_rotary_bwd_workspace_bytes(const seq_rotary_problem *p);   /* for weights of both; needed only where there is one */
+
+/*
  * The cache: pages of `page` consecutive tokens of one sequence, k_pages and v_pages int8 [pages, kv_heads, page, D], contiguous, with one fp32 scale
  * for each page and head, k_scales and v_scales [pages, kv_heads]; a value is the integer times the scale.  table: int32 [B, table_width]; position t of
  * sequence b lies in page table[b, t / page] at t % page.  lengths: int32 [B], tokens of each sequence.  Entries of the table whose positions a call
@@ -100,6 +138,14 @@ int seq_cache_validate(const seq_cache_problem *p, int call);
  * one call (by two sequences, or through two entries of a table): which of the values it then holds is not defined. */
 int seq_cache_append(const seq_cache_problem *p, const void *k, const void *v, const int32_t *table, const int32_t *lengths, const int32_t *counts,
                      int8_t *k_pages, int8_t *v_pages, float *k_scales, float *v_scales, void *stream);
+
+/* The same of tokens picked out of k, v [B, kv_heads, given, D], with their keys normed and rotated on the way.  rows (nullable): int32 [B, n], the row of k and v that
+ * is new token i; a row outside [0, given) is a token of zeros; NULL: the rows as they come, n of them.  r (nullable): how keys are rotated (pairs 0: not at all), with weight
+ * (nullable) of a norm before that.  positions (nullable): int32 [axes, given] if `shared`, else [B, axes, given], of the given rows; NULL, with one axis: a token's place in its
+ * sequence.  Rotated keys are rounded once, to the cache's 8 bits. */
+int seq_cache_append_rows(const seq_cache_problem *p, const seq_rotation *r, int32_t given, const void *k, const void *v, const int32_t *rows, const int32_t *positions, int shared,
+                          const float *freqs, const void *weight, const int32_t *table, const int32_t *lengths, const int32_t *counts, int8_t *k_pages, int8_t *v_pages,
+                          float *k_scales, float *v_scales, void *stream);
 
 /* k, v [B, kv_heads, n, D] (strides p->q and p->out): the values at positions first[b] .. first[b] + n - 1, 0 where the sequence has no token. */
 int seq_cache_gather(const seq_cache_problem *p, const int8_t *k_pages, const int8_t *v_pages, const float *k_scales, const float *v_scales,

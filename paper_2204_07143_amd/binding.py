@@ -38,6 +38,7 @@ EXPORTS_1D = (
 EXPORTS_SEQ = (
     "seq_validate_problem", "seq_attention_workspace_bytes", "seq_attention_fwd", "seq_attention_bwd", "seq_cache_validate", "seq_cache_append",
     "seq_cache_gather", "seq_cache_attention", "seq_cache_attention_workspace_bytes",
+    "seq_rotary_validate", "seq_rotary_fwd", "seq_rotary_bwd", "seq_rotary_bwd_workspace_bytes", "seq_cache_append_rows",
 )
 SEQ_CACHE_APPEND, SEQ_CACHE_GATHER, SEQ_CACHE_ATTENTION = 0, 1, 2
 
@@ -69,6 +70,16 @@ class SeqProblem(ctypes.Structure):
 class SeqCacheProblem(ctypes.Structure):
     _fields_ = ([(n, ctypes.c_int32) for n in ("B", "heads", "kv_heads", "D", "page", "pages", "table_width", "dtype", "n", "window")]
                 + [(n, ctypes.c_float) for n in ("scale", "softcap")] + [(n, SeqStrides) for n in ("q", "out")])
+
+
+class SeqRotation(ctypes.Structure):
+    _fields_ = [("pairs", ctypes.c_int32), ("axes", ctypes.c_int32), ("sections", ctypes.c_int32 * 4), ("interleaved", ctypes.c_int32), ("weight_dtype", ctypes.c_int32),
+                ("eps", ctypes.c_float)]
+
+
+class SeqRotaryProblem(ctypes.Structure):
+    _fields_ = ([(n, ctypes.c_int32) for n in ("B", "heads", "kv_heads", "L", "D", "dtype")] + [("rotation", SeqRotation), ("shared", ctypes.c_int32)]
+                + [(n, SeqStrides) for n in ("q", "k", "q_out", "k_out", "dq", "dk")])
 
 
 _lib = None
@@ -129,7 +140,7 @@ def load(path: str | None = None) -> ctypes.CDLL:
             fn = getattr(lib, name)
             fn.argtypes = argtypes
             fn.restype = ctypes.c_int
-        ps, pc, size = ctypes.POINTER(SeqProblem), ctypes.POINTER(SeqCacheProblem), ctypes.c_size_t
+        ps, pc, pr, size = ctypes.POINTER(SeqProblem), ctypes.POINTER(SeqCacheProblem), ctypes.POINTER(SeqRotaryProblem), ctypes.c_size_t
         sigs_seq = {
             "seq_validate_problem": [ps, ctypes.c_int],
             "seq_attention_fwd": [ps] + [vp] * 10 + [size, vp],
@@ -138,6 +149,10 @@ def load(path: str | None = None) -> ctypes.CDLL:
             "seq_cache_append": [pc] + [vp] * 10,
             "seq_cache_gather": [pc] + [vp] * 10,
             "seq_cache_attention": [pc] + [vp] * 10 + [size, vp],
+            "seq_cache_append_rows": [pc, ctypes.POINTER(SeqRotation), ctypes.c_int32] + [vp] * 4 + [ctypes.c_int] + [vp] * 10,
+            "seq_rotary_validate": [pr, ctypes.c_int],
+            "seq_rotary_fwd": [pr] + [vp] * 9,
+            "seq_rotary_bwd": [pr] + [vp] * 13 + [size, vp],
         }
         for name, argtypes in sigs_seq.items():
             fn = getattr(lib, name)
@@ -145,6 +160,8 @@ def load(path: str | None = None) -> ctypes.CDLL:
             fn.restype = ctypes.c_int
         lib.seq_attention_workspace_bytes.argtypes = [ps, ctypes.c_int, ctypes.c_int]
         lib.seq_attention_workspace_bytes.restype = size
+        lib.seq_rotary_bwd_workspace_bytes.argtypes = [pr]
+        lib.seq_rotary_bwd_workspace_bytes.restype = size
         lib.seq_cache_attention_workspace_bytes.argtypes = [pc]
         lib.seq_cache_attention_workspace_bytes.restype = size
         lib.na1d_workspace_bytes.argtypes = [p1]
@@ -584,6 +601,69 @@ def seq_attention_bwd(q, k_, v, slopes, documents, prefix, out, lse, rest, dout,
     return dq, dk, dv
 
 
+def seq_rotation(dtype, *, sections, weights=(), eps=1e-6, interleaved=False) -> SeqRotation:
+    """sections: pairs of each axis; none for no rotation.  weights: those that are given have one type."""
+    kinds = {w.dtype for w in weights if w is not None}
+    if len(kinds) > 1:
+        raise ValueError(f"weights of one dtype are expected, got {sorted(map(str, kinds))}")
+    if len(sections) > 4:
+        raise ValueError(f"at most 4 axes, got {len(sections)}")
+    return SeqRotation(sum(sections), len(sections), (ctypes.c_int32 * 4)(*sections), int(interleaved), DTYPE_CODES.get(next(iter(kinds), dtype), -1), eps)
+
+
+def seq_rotary_problem(q, k_, positions, rotation: SeqRotation, **strided) -> SeqRotaryProblem:
+    """q: [B, heads, L, D]; k_: [B, kv_heads, L, D] or None; strided: other tensors by name (q_out, k_out, dq, dk)."""
+    if q.dim() != 4 or (k_ is not None and k_.dim() != 4):
+        raise ValueError("expected [B, heads, L, D] tensors")
+    B, heads, L, D = q.shape
+    p = SeqRotaryProblem(B, heads, 0 if k_ is None else k_.shape[1], L, D, DTYPE_CODES.get(q.dtype, -1), rotation, int(positions.dim() == 2))
+    for name, t in dict(q=q, k=k_, **strided).items():
+        if t is not None:
+            setattr(p, name, _seq_strides(t))
+    return p
+
+
+def seq_rotary_validate(p: SeqRotaryProblem, backward: bool = False) -> int:
+    return int(load().seq_rotary_validate(ctypes.byref(p), int(backward)))
+
+
+def seq_rotary_bwd_workspace_bytes(p: SeqRotaryProblem) -> int:
+    return int(load().seq_rotary_bwd_workspace_bytes(ctypes.byref(p)))
+
+
+def _axis_positions(positions, of, B, axes, L):
+    return _dense(positions, of, (axes, L) if positions.dim() == 2 else (B, axes, L), torch.int32)
+
+
+def _rotary_inputs(q, k_, positions, freqs, q_weight, k_weight, rotation):
+    B, _, L, D = q.shape
+    weight = lambda w: None if w is None else _dense(w, q, (D,), w.dtype)
+    return (_strided(q, q, q.shape), None if k_ is None else _strided(k_, q, (B, k_.shape[1], L, D)), _axis_positions(positions, q, B, rotation.axes, L),
+            _dense(freqs, q, (rotation.pairs,), torch.float32), weight(q_weight), weight(k_weight))
+
+
+def seq_rotary_fwd(q, k_, positions, freqs, q_weight, k_weight, q_out, k_out, *, sections, eps=1e-6, interleaved=False):
+    rotation = seq_rotation(q.dtype, sections=sections, weights=(q_weight, k_weight), eps=eps, interleaved=interleaved)
+    p = seq_rotary_problem(q, k_, positions, rotation, q_out=q_out, k_out=k_out)
+    inputs = _rotary_inputs(q, k_, positions, freqs, q_weight, k_weight, rotation)
+    with torch.cuda.device(q.device):
+        _check(load().seq_rotary_fwd(ctypes.byref(p), *inputs, _strided(q_out, q, q.shape), None if k_ is None else _strided(k_out, q, k_.shape), _seq_stream(q)))
+    return q_out, k_out
+
+
+def seq_rotary_bwd(q, k_, positions, freqs, q_weight, k_weight, dq_out, dk_out, dq, dk, dq_weight, dk_weight, workspace=None, *, sections, eps=1e-6, interleaved=False):
+    """q, k_: as in the forward pass (only their form counts where there is no weight)."""
+    rotation = seq_rotation(q.dtype, sections=sections, weights=(q_weight, k_weight), eps=eps, interleaved=interleaved)
+    p = seq_rotary_problem(q, k_, positions, rotation, q_out=dq_out, k_out=dk_out, dq=dq, dk=dk)
+    inputs = _rotary_inputs(q, k_, positions, freqs, q_weight, k_weight, rotation)
+    side = lambda t: None if k_ is None else _strided(t, q, k_.shape)
+    grad = lambda t, w: None if w is None else _dense(t, q, w.shape, w.dtype)
+    with torch.cuda.device(q.device):
+        _check(load().seq_rotary_bwd(ctypes.byref(p), *inputs, _strided(dq_out, q, q.shape), side(dk_out), _strided(dq, q, q.shape), side(dk), grad(dq_weight, q_weight),
+                                     grad(dk_weight, k_weight), *_bytes(workspace), _seq_stream(q)))
+    return dq, dk, dq_weight, dk_weight
+
+
 def seq_cache_problem(rows, k_pages, table, *, heads=None, window=0, softcap=0.0, scale=1.0, out=None) -> SeqCacheProblem:
     """rows: [B, heads or kv_heads, n, D]; out: the call's other tensor of that form."""
     if rows.dim() != 4 or k_pages.dim() != 4 or table.dim() != 2:
@@ -613,6 +693,26 @@ def seq_cache_append(k_, v, table, lengths, counts, k_pages, v_pages, k_scales, 
     with torch.cuda.device(k_.device):
         _check(load().seq_cache_append(ctypes.byref(p), _strided(k_, k_, shape), _strided(v, k_, shape), _dense(table, k_, (B, table.shape[1]), torch.int32),
                                        _dense(lengths, k_, (B,), torch.int32), _dense(counts, k_, (B,), torch.int32), *cache, _seq_stream(k_)))
+
+
+def seq_cache_append_rows(k_, v, table, lengths, counts, k_pages, v_pages, k_scales, v_scales, *, rows=None, positions=None, freqs=None, weight=None, sections=(), eps=1e-6,
+                          interleaved=False):
+    """k_, v: the given rows [B, kv_heads, given, D]; rows: int32 [B, n] or None."""
+    p = seq_cache_problem(k_, k_pages, table, out=v)
+    B, given, shape = k_.shape[0], k_.shape[2], (k_.shape[0], k_pages.shape[1], *k_.shape[2:])
+    if rows is not None:
+        if rows.dim() != 2:
+            raise ValueError("expected rows [B, n]")
+        p.n = rows.shape[1]
+    rotation = seq_rotation(k_.dtype, sections=sections, weights=(weight,), eps=eps, interleaved=interleaved)
+    cache = _cache_inputs(k_, k_pages, v_pages, k_scales, v_scales)
+    int32 = lambda t, s: _dense(t, k_, s, torch.int32)
+    with torch.cuda.device(k_.device):
+        _check(load().seq_cache_append_rows(
+            ctypes.byref(p), ctypes.byref(rotation), given, _strided(k_, k_, shape), _strided(v, k_, shape), int32(rows, None if rows is None else (B, rows.shape[1])),
+            None if positions is None else _axis_positions(positions, k_, B, rotation.axes, given), int(positions is not None and positions.dim() == 2),
+            _dense(freqs, k_, (rotation.pairs,), torch.float32), None if weight is None else _dense(weight, k_, (k_.shape[3],), weight.dtype),
+            int32(table, (B, table.shape[1])), int32(lengths, (B,)), int32(counts, (B,)), *cache, _seq_stream(k_)))
 
 
 def seq_cache_gather(k_pages, v_pages, k_scales, v_scales, table, lengths, first, k_, v):

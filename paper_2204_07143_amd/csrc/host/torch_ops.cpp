@@ -443,6 +443,131 @@ struct SeqAttention : torch::autograd::Function<SeqAttention> {
     }
 };
 
+// ---- rotation by position ------------------------------------------------------------------------------------------------------
+
+// Pairs of each axis: of a tuple, or all of freqs' on one axis
+struct Sections {
+    int64_t n[4] = {0, 0, 0, 0}, axes = 0;
+    bool set(const Tensor &freqs) {
+        if (!axes) axes = 1, n[0] = freqs.numel();
+        int64_t sum = 0;
+        for (int a = 0; a < axes; ++a) {
+            if (n[a] < 1 || !fits(n[a])) return false;
+            sum += n[a];
+        }
+        return freqs.dim() == 1 && sum == freqs.numel();
+    }
+};
+seq_rotation rotation_of(const Sections &x, const Tensor &of, const Tensor &weight, const Tensor &other, double eps, bool interleaved) {
+    seq_rotation r{};
+    for (int a = 0; a < 4; ++a) r.sections[a] = (int32_t)x.n[a], r.pairs += (int32_t)x.n[a];
+    r.axes = (int32_t)x.axes, r.interleaved = interleaved, r.eps = (float)eps;
+    const Tensor &w = weight.defined() ? weight : other;
+    r.weight_dtype = *dtype_code(w.defined() ? w.scalar_type() : of.scalar_type());
+    return r;
+}
+// a norm's weight, or none: [D], of the type of `of` or fp32
+bool weight_fits(const Tensor &w, const Tensor &of) {
+    return !w.defined() || (plain(w) && w.dim() == 1 && w.size(0) == of.size(3) && w.device() == of.device() && w.is_contiguous() && (w.scalar_type() == of.scalar_type() || w.scalar_type() == at::kFloat));
+}
+// positions [axes, L] or [B, axes, L]
+bool positions_fit(const Tensor &t, const Tensor &of, int64_t axes, int64_t L) {
+    if (!plain(t)) return false;
+    return t.dim() == 2 ? constant(t, of, at::kInt, {axes, L}) : constant(t, of, at::kInt, {of.size(0), axes, L});
+}
+std::optional<seq_rotary_problem> rotary_of(const Tensor &q, const Tensor &k, const Tensor &positions, const seq_rotation &r) {
+    const auto code = dtype_code(q.scalar_type());
+    if (!code || q.dim() != 4 || !small(q.sizes())) return std::nullopt;
+    seq_rotary_problem p{};
+    p.B = (int32_t)q.size(0), p.heads = (int32_t)q.size(1), p.L = (int32_t)q.size(2), p.D = (int32_t)q.size(3), p.kv_heads = k.defined() ? (int32_t)k.size(1) : 0;
+    p.dtype = *code, p.rotation = r, p.shared = positions.dim() == 2;
+    return p;
+}
+Tensor undefined_or(const std::optional<Tensor> &t) { return t.value_or(Tensor()); }
+
+struct RotaryOnceOnly : torch::autograd::Function<RotaryOnceOnly> {
+    using Maybe = const std::optional<Tensor> &;
+    static variable_list forward(AutogradContext *, Maybe a, Maybe b, Maybe c, Maybe d, Maybe, Maybe, Maybe, Maybe, Maybe, Maybe) {
+        variable_list r;
+        for (Maybe t : {std::cref(a), std::cref(b), std::cref(c), std::cref(d)})
+            if (t) r.push_back(t->view_as(*t));
+        return r;
+    }
+    static variable_list backward(AutogradContext *, variable_list) { TORCH_CHECK(false, "seq_rotary has no second derivative"); }
+};
+
+std::optional<Tensor> maybe(const Tensor &t);
+
+struct SeqRotary : torch::autograd::Function<SeqRotary> {
+    static variable_list run(const Tensor &q, const Tensor &k, const Tensor &positions, const Tensor &freqs, const Tensor &qw, const Tensor &kw, const seq_rotation &r) {
+        auto p = rotary_of(q, k, positions, r);
+        if (!p) throw Refused{};
+        variable_list out{rows_like(q)};
+        p->q = strides(q), p->q_out = strides(out[0]);
+        if (k.defined()) {
+            out.push_back(rows_like(k));
+            p->k = strides(k), p->k_out = strides(out[1]);
+        }
+        forward_check(seq_rotary_fwd(&*p, ptr(q), ptr(k), (const int32_t *)ptr(positions), (const float *)ptr(freqs), ptr(qw), ptr(kw), ptr(out[0]), k.defined() ? ptr(out[1]) : nullptr, stream()));
+        return out;
+    }
+    static variable_list forward(AutogradContext *ctx, const Tensor &q_, const std::optional<Tensor> &k_, const Tensor &positions, const Tensor &freqs, const std::optional<Tensor> &qw_,
+                                 const std::optional<Tensor> &kw_, const std::vector<int64_t> &sections, double eps, bool interleaved) {
+        const Tensor q = rows(q_), k = k_ ? rows(*k_) : Tensor(), qw = undefined_or(qw_), kw = undefined_or(kw_);
+        Sections x;
+        for (int64_t n : sections) x.n[x.axes++] = n;
+        variable_list out = run(q, k, positions, freqs, qw, kw, rotation_of(x, q, qw, kw, eps, interleaved));
+        ctx->save_for_backward({qw.defined() ? q : Tensor(), kw.defined() ? k : Tensor(), positions, freqs, qw, kw});
+        ctx->saved_data["sections"] = sections;
+        ctx->saved_data["eps"] = eps;
+        ctx->saved_data["interleaved"] = interleaved;
+        return out;
+    }
+    static variable_list backward(AutogradContext *ctx, variable_list grads) {
+        const auto saved = ctx->get_saved_variables();
+        Tensor dx[2], dw[2];
+        {
+            const at::AutoGradMode off(false);
+            const c10::DeviceGuard device(grads[0].device());
+            Tensor z[2], x[2] = {saved[0], saved[1]}, w[2] = {saved[4], saved[5]};
+            const Tensor &positions = saved[2], &freqs = saved[3];
+            const bool keys = grads.size() > 1;
+            for (int i = 0; i < (keys ? 2 : 1); ++i) {
+                z[i] = rows(grads[i].is_neg() ? grads[i].resolve_neg() : grads[i]);
+                TORCH_CHECK_VALUE(plain(z[i]) && z[i].device() == z[0].device(), "na2d takes GPU tensors only");
+                // (a saved-tensor hook may hand back tensors of another form)
+                if (w[i].defined()) {
+                    TORCH_CHECK_VALUE(weight_fits(w[i], z[i]) && plain(x[i]) && x[i].device() == z[i].device() && x[i].scalar_type() == z[i].scalar_type() && x[i].sizes() == z[i].sizes(),
+                                      "not a tensor of the forward pass");
+                    TORCH_CHECK_VALUE(whole_rows(x[i]), "the elements of a row must be contiguous");
+                    dw[i] = at::empty_like(w[i]);
+                }
+                dx[i] = rows_like(w[i].defined() ? x[i] : z[i]);
+            }
+            TORCH_CHECK_VALUE(!w[0].defined() || !w[1].defined() || w[0].scalar_type() == w[1].scalar_type(), "not a tensor of the forward pass");
+            Sections s;
+            for (int64_t n : ctx->saved_data["sections"].toIntVector()) s.n[s.axes++] = n;
+            TORCH_CHECK_VALUE(positions_fit(positions, z[0], s.axes, z[0].size(2)) && plain(freqs) && freqs.device() == z[0].device() && freqs.scalar_type() == at::kFloat && freqs.is_contiguous() && s.set(freqs),
+                              "not a tensor of the forward pass");
+            auto p = valid(rotary_of(z[0], z[1], positions, rotation_of(s, z[0], w[0], w[1], ctx->saved_data["eps"].toDouble(), ctx->saved_data["interleaved"].toBool())));
+            const seq_strides none{};
+            p.q_out = strides(z[0]), p.dq = strides(dx[0]), p.q = w[0].defined() ? strides(x[0]) : none;
+            if (keys) p.k_out = strides(z[1]), p.dk = strides(dx[1]), p.k = w[1].defined() ? strides(x[1]) : none;
+            const Tensor ws = scratch(w[0].defined() || w[1].defined() ? seq_rotary_bwd_workspace_bytes(&p) : 0, z[0]);
+            check(seq_rotary_bwd(&p, w[0].defined() ? ptr(x[0]) : nullptr, w[1].defined() ? ptr(x[1]) : nullptr, (const int32_t *)ptr(positions), (const float *)ptr(freqs), ptr(w[0]), ptr(w[1]),
+                                 ptr(z[0]), ptr(z[1]), ptr(dx[0]), ptr(dx[1]), ptr(dw[0]), ptr(dw[1]), ptr(ws), size_of(ws), stream()));
+        }
+        if (at::GradMode::is_enabled()) {
+            const variable_list r = RotaryOnceOnly::apply(maybe(dx[0]), maybe(dx[1]), maybe(dw[0]), maybe(dw[1]), maybe(saved[0]), maybe(saved[1]), maybe(saved[4]), maybe(saved[5]), maybe(grads[0]),
+                                                          grads.size() > 1 ? maybe(grads[1]) : std::nullopt);
+            size_t at = 0;
+            for (Tensor *t : {&dx[0], &dx[1], &dw[0], &dw[1]})
+                if (t->defined()) *t = r[at++];
+        }
+        return {dx[0], dx[1], Tensor(), Tensor(), dw[0], dw[1], Tensor(), Tensor(), Tensor()};
+    }
+};
+
 // The cache: k_pages, v_pages, k_scales, v_scales, then table and lengths, beside a tensor [B, heads, n, D] of the call
 struct SeqCacheArgs {
     Tensor k, v, ks, vs, table, lengths;
@@ -642,6 +767,80 @@ PyObject *py_seq_cache_append(PyObject *, PyObject *const *a, Py_ssize_t n) {
     return r;
 }
 
+// None, or a tuple of 1 to 4 whole numbers
+bool sections_arg(PyObject *o, Sections &x) {
+    if (o == Py_None) return true;
+    if (!PyTuple_CheckExact(o) || PyTuple_GET_SIZE(o) < 1 || PyTuple_GET_SIZE(o) > 4) return false;
+    for (Py_ssize_t i = 0; i < PyTuple_GET_SIZE(o); ++i) {
+        PyObject *n = PyTuple_GET_ITEM(o, i);
+        x.n[x.axes++] = PyLong_Check(n) ? PyLong_AsLongLong(n) : -1;
+        if (PyErr_Occurred()) PyErr_Clear();
+    }
+    return true;
+}
+
+// (q, k or None, positions, freqs, sections or None, q_weight or None, k_weight or None, eps, interleaved): (q,) or (q, k)
+PyObject *py_seq_rotary(PyObject *, PyObject *const *a, Py_ssize_t n) {
+    Tensor q, k, positions, freqs, qw, kw;
+    Sections x;
+    double eps;
+    if (n != 9 || !plain_modes() || !tensor_arg(a[0], q) || !tensor_arg(a[1], k, true) || !tensor_arg(a[2], positions) || !tensor_arg(a[3], freqs) || !sections_arg(a[4], x) ||
+        !tensor_arg(a[5], qw, true) || !tensor_arg(a[6], kw, true) || a[7] == Py_None || !number_arg(a[7], eps, 0) || !PyBool_Check(a[8]))
+        Py_RETURN_NONE;
+    const bool interleaved = a[8] == Py_True;
+    return guarded<variable_list>([&]() -> variable_list {
+        if (!plain(q) || q.dim() != 4 || !dtype_code(q.scalar_type()) || !small(q.sizes()) || !plain(freqs) || !x.set(freqs)) return {};
+        const auto s = q.sizes();
+        if (k.defined() && (k.dim() != 4 || !small(k.sizes()) || !matches(k, q, {s[0], k.size(1), s[2], s[3]}))) return {};
+        if (!constant(freqs, q, at::kFloat, {freqs.numel()}) || !positions_fit(positions, q, x.axes, s[2]) || !weight_fits(qw, q) || !weight_fits(kw, q) || (kw.defined() && !k.defined()) ||
+            (qw.defined() && kw.defined() && qw.scalar_type() != kw.scalar_type()) || positions.requires_grad() || freqs.requires_grad())
+            return {};
+        const c10::DeviceGuard device(q.device());
+        if (wants_grad({&q, &k, &qw, &kw}))
+            return SeqRotary::apply(q, maybe(k), positions, freqs, maybe(qw), maybe(kw), std::vector<int64_t>(x.n, x.n + x.axes), eps, interleaved);
+        const at::AutoGradMode off(false);
+        return SeqRotary::run(rows(q), k.defined() ? rows(k) : k, positions, freqs, qw, kw, rotation_of(x, q, qw, kw, eps, interleaved));
+    });
+}
+
+// (k_pages, v_pages, k_scales, v_scales, k, v, table, lengths, counts, rows, positions, freqs, sections, weight: or None, eps, interleaved): True where it was done
+PyObject *py_seq_cache_append_rows(PyObject *, PyObject *const *a, Py_ssize_t n) {
+    SeqCacheArgs c;
+    Tensor k, v, counts, picked, positions, freqs, weight;
+    Sections x;
+    double eps;
+    if (n != 16 || !plain_modes() || !cache_args(a, c, 6) || !tensor_arg(a[4], k) || !tensor_arg(a[5], v) || !tensor_arg(a[8], counts, true) || !tensor_arg(a[9], picked, true) ||
+        !tensor_arg(a[10], positions, true) || !tensor_arg(a[11], freqs, true) || !sections_arg(a[12], x) || !tensor_arg(a[13], weight, true) || a[14] == Py_None ||
+        !number_arg(a[14], eps, 0) || !PyBool_Check(a[15]))
+        Py_RETURN_NONE;
+    const bool interleaved = a[15] == Py_True;
+    bool done = false;
+    PyObject *r = guarded([&]() -> Tensor {
+        if (!plain(k) || k.dim() != 4 || !dtype_code(k.scalar_type()) || !small(k.sizes()) || !matches(v, k, k.sizes()) || !c.fit(k, k.size(1)) || !constant(counts, k, at::kInt, {k.size(0)}))
+            return Tensor();
+        if (picked.defined() && (picked.dim() != 2 || picked.size(1) < 1 || !fits(picked.size(1)) || !constant(picked, k, at::kInt, {k.size(0), picked.size(1)}))) return Tensor();
+        if (freqs.defined() ? !plain(freqs) || !x.set(freqs) || freqs.requires_grad() || !constant(freqs, k, at::kFloat, {freqs.numel()}) : x.axes || positions.defined()) return Tensor();
+        if (!weight_fits(weight, k) || (positions.defined() && !positions_fit(positions, k, x.axes, k.size(2)))) return Tensor();
+        const at::AutoGradMode off(false);
+        const c10::DeviceGuard device(k.device());
+        const Tensor kr = rows(k), vr = rows(v);
+        auto p = c.problem(kr, vr, k.size(1), 0, 0, 1);
+        if (!p) return Tensor();
+        if (picked.defined()) p->n = (int32_t)picked.size(1);
+        const seq_rotation how = rotation_of(x, k, weight, weight, eps, interleaved);
+        forward_check(seq_cache_append_rows(&*p, &how, (int32_t)k.size(2), ptr(kr), ptr(vr), (const int32_t *)ptr(picked), (const int32_t *)ptr(positions),
+                                            positions.defined() && positions.dim() == 2, (const float *)ptr(freqs), ptr(weight), (const int32_t *)ptr(c.table), (const int32_t *)ptr(c.lengths),
+                                            (const int32_t *)ptr(counts), (int8_t *)ptr(c.k), (int8_t *)ptr(c.v), (float *)ptr(c.ks), (float *)ptr(c.vs), stream()));
+        done = true;
+        return Tensor();
+    });
+    if (r && done) {
+        Py_DECREF(r);
+        Py_RETURN_TRUE;
+    }
+    return r;
+}
+
 // (k_pages, v_pages, k_scales, v_scales, table, lengths, first, n, dtype): (k, v)
 PyObject *py_seq_cache_gather(PyObject *, PyObject *const *a, Py_ssize_t count) {
     SeqCacheArgs c;
@@ -690,6 +889,8 @@ PyMethodDef methods[] = {{"na2d", (PyCFunction)(void (*)(void))py_na2d, METH_FAS
                          {"na2d_unfused", (PyCFunction)(void (*)(void))py_na2d_unfused, METH_FASTCALL, nullptr},
                          {"seq_attention", (PyCFunction)(void (*)(void))py_seq_attention, METH_FASTCALL, nullptr},
                          {"seq_cache_append", (PyCFunction)(void (*)(void))py_seq_cache_append, METH_FASTCALL, nullptr},
+                         {"seq_cache_append_rows", (PyCFunction)(void (*)(void))py_seq_cache_append_rows, METH_FASTCALL, nullptr},
+                         {"seq_rotary", (PyCFunction)(void (*)(void))py_seq_rotary, METH_FASTCALL, nullptr},
                          {"seq_cache_gather", (PyCFunction)(void (*)(void))py_seq_cache_gather, METH_FASTCALL, nullptr},
                          {"seq_cache_attention", (PyCFunction)(void (*)(void))py_seq_cache_attention, METH_FASTCALL, nullptr},
                          {nullptr, nullptr, 0, nullptr}};

@@ -162,6 +162,61 @@ bool odd4(std::initializer_list<const void *> ps) {
     return false;
 }
 
+// pairs 0: no rotation, where that is allowed
+int check_rotation(const seq_rotation &r, int D, int dtype, bool none_allowed, bool normed) {
+    if (r.pairs < 0 || r.pairs % 8 || 2 * (int64_t)r.pairs > D || (!r.pairs && !none_allowed)) return NA2D_ERR_SHAPE;
+    if (r.interleaved != 0 && r.interleaved != 1) return NA2D_ERR_SHAPE;
+    if (r.pairs) {
+        if (r.axes < 1 || r.axes > 4) return NA2D_ERR_SHAPE;
+        int64_t sum = 0;
+        for (int a = 0; a < r.axes; ++a) {
+            if (r.sections[a] < 1) return NA2D_ERR_SHAPE;
+            sum += r.sections[a];
+        }
+        if (sum != r.pairs) return NA2D_ERR_SHAPE;
+    }
+    if (normed) {
+        if (r.weight_dtype != NA2D_F32 && r.weight_dtype != dtype) return NA2D_ERR_DTYPE;
+        if (!(r.eps > 0.f) || !std::isfinite(r.eps)) return NA2D_ERR_SHAPE;
+    }
+    return NA2D_OK;
+}
+Rotation rotation(const seq_rotation &r, const int32_t *positions, int64_t batch, const float *freqs, const void *weight) {
+    Rotation x{};
+    x.positions = positions, x.batch = batch, x.freqs = freqs, x.weight = weight;
+    x.pairs = r.pairs, x.axes = r.axes, x.interleaved = r.interleaved, x.weight32 = r.weight_dtype == NA2D_F32, x.eps = r.eps;
+    for (int a = 0, at = 0; a < 3; ++a) x.ends[a] = at += a < r.axes ? r.sections[a] : 0;
+    return x;
+}
+
+int rotary_validate(const seq_rotary_problem *p, bool backward) {
+    if (!p) return NA2D_ERR_NULL;
+    if (p->dtype != NA2D_F32 && p->dtype != NA2D_F16 && p->dtype != NA2D_BF16) return NA2D_ERR_DTYPE;
+    if (p->B <= 0 || p->heads <= 0 || p->kv_heads < 0 || p->L <= 0 || (int64_t)p->B * p->L > INT32_MAX || (p->shared != 0 && p->shared != 1)) return NA2D_ERR_SHAPE;
+    if (p->D != 16 && p->D != 32 && p->D != 64 && p->D != 128) return NA2D_ERR_HEAD_DIM;
+    if (int e = check_rotation(p->rotation, p->D, p->dtype, false, false)) return e;
+    const int e = elem(p->dtype);
+    struct { const seq_strides &s; int heads; bool written, backward; } all[] = {{p->q, p->heads, false, false}, {p->q_out, p->heads, !backward, false}, {p->dq, p->heads, true, true},
+        {p->k, p->kv_heads, false, false}, {p->k_out, p->kv_heads, !backward, false}, {p->dk, p->kv_heads, true, true}};
+    for (const auto &x : all)
+        if (x.heads && (backward || !x.backward))
+            if (int r = check_strides(x.s, p->B, x.heads, p->L, p->D, e, x.written)) return r;
+    // every launch holds its workgroups: a wave has at least one token's four heads
+    for (int heads : {p->heads, p->kv_heads})
+        if (!launch_holds(((int64_t)p->B * p->L * ((heads + 3) / 4) + kWaves - 1) / kWaves + 1, kThreads)) return NA2D_ERR_SHAPE;
+    return NA2D_OK;
+}
+// of the queries (side 0) or the keys
+RotaryArgs rotary_args(const seq_rotary_problem *p, int side, const int32_t *positions, const float *freqs, const void *weight) {
+    RotaryArgs a{};
+    a.r = rotation(p->rotation, positions, p->shared ? 0 : (int64_t)p->rotation.axes * p->L, freqs, weight);
+    a.tokens = (int64_t)p->B * p->L, a.L = p->L, a.heads = side ? p->kv_heads : p->heads;
+    plan_rotary(a, p->dtype, p->D);
+    return a;
+}
+bool misaligned_weight(const void *w, const seq_rotation &r) { return reinterpret_cast<uintptr_t>(w) & (r.weight_dtype == NA2D_F32 ? 3u : 1u); }
+int64_t rotary_parts(const RotaryArgs &a, int D) { return (int64_t)sizeof(float) * rotary_bwd_blocks(a) * D; }
+
 }  // namespace
 }  // namespace seq
 
@@ -227,6 +282,71 @@ int seq_attention_bwd(const seq_problem *p, const void *q, const void *k, const 
     return from_hip(launch_bwd_kv(a, p->dtype, p->D, cap, st));
 }
 
+int seq_rotary_validate(const seq_rotary_problem *p, int backward) { return rotary_validate(p, backward != 0); }
+
+int seq_rotary_fwd(const seq_rotary_problem *p, const void *q, const void *k, const int32_t *positions, const float *freqs, const void *q_weight, const void *k_weight,
+                   void *q_out, void *k_out, void *stream) {
+    if (int e = rotary_validate(p, false)) return e;
+    if (!positions || !freqs) return NA2D_ERR_NULL;
+    if (int e = check_rotation(p->rotation, p->D, p->dtype, false, q_weight || k_weight)) return e;
+    if (odd4({positions, freqs}) || misaligned_weight(q_weight, p->rotation) || misaligned_weight(k_weight, p->rotation)) return NA2D_ERR_ALIGN;
+    SEQ_REQUIRE(q); SEQ_REQUIRE(q_out);
+    if (p->kv_heads) { SEQ_REQUIRE(k); SEQ_REQUIRE(k_out); }
+    else if (k || k_out || k_weight) return NA2D_ERR_SHAPE;
+    for (const void *o : {q_out, k_out})
+        for (const void *i : {q, k, (const void *)positions, (const void *)freqs, q_weight, k_weight})
+            if (o && o == i) return NA2D_ERR_ALIAS;
+    if (q_out == k_out) return NA2D_ERR_ALIAS;
+    const int e = elem(p->dtype);
+    for (int side = 0; side < (p->kv_heads ? 2 : 1); ++side) {
+        RotaryArgs a = rotary_args(p, side, positions, freqs, side ? k_weight : q_weight);
+        a.x = side ? view(k, p->k, e) : view(q, p->q, e), a.z = side ? view(k_out, p->k_out, e) : view(q_out, p->q_out, e);
+        if (int r = from_hip(launch_rotary(a, p->dtype, p->D, static_cast<hipStream_t>(stream)))) return r;
+    }
+    return NA2D_OK;
+}
+
+size_t seq_rotary_bwd_workspace_bytes(const seq_rotary_problem *p) {
+    if (rotary_validate(p, true) != NA2D_OK) return 0;
+    int64_t bytes = 0;
+    for (int side = 0; side < (p->kv_heads ? 2 : 1); ++side) bytes += rotary_parts(rotary_args(p, side, nullptr, nullptr, nullptr), p->D);
+    return (size_t)bytes;
+}
+
+int seq_rotary_bwd(const seq_rotary_problem *p, const void *q, const void *k, const int32_t *positions, const float *freqs, const void *q_weight, const void *k_weight,
+                   const void *dq_out, const void *dk_out, void *dq, void *dk, void *dq_weight, void *dk_weight, void *workspace, size_t workspace_bytes, void *stream) {
+    if (int e = rotary_validate(p, true)) return e;
+    if (!positions || !freqs) return NA2D_ERR_NULL;
+    if (int e = check_rotation(p->rotation, p->D, p->dtype, false, q_weight || k_weight)) return e;
+    if (odd4({positions, freqs}) || misaligned_weight(q_weight, p->rotation) || misaligned_weight(k_weight, p->rotation) || misaligned_weight(dq_weight, p->rotation) ||
+        misaligned_weight(dk_weight, p->rotation))
+        return NA2D_ERR_ALIGN;
+    if (q_weight) { SEQ_REQUIRE(q); if (!dq_weight) return NA2D_ERR_NULL; }
+    if (k_weight) { SEQ_REQUIRE(k); if (!dk_weight) return NA2D_ERR_NULL; }
+    SEQ_REQUIRE(dq_out); SEQ_REQUIRE(dq);
+    if (p->kv_heads) { SEQ_REQUIRE(dk_out); SEQ_REQUIRE(dk); }
+    else if (k || dk_out || dk || k_weight) return NA2D_ERR_SHAPE;
+    const void *outs[] = {dq, dk, dq_weight, dk_weight};
+    for (int i = 0; i < 4; ++i) {
+        for (const void *x : {q, k, (const void *)positions, (const void *)freqs, q_weight, k_weight, dq_out, dk_out})
+            if (outs[i] && outs[i] == x) return NA2D_ERR_ALIAS;
+        for (int j = 0; j < i; ++j)
+            if (outs[i] && outs[i] == outs[j]) return NA2D_ERR_ALIAS;
+    }
+    const size_t need = q_weight || k_weight ? seq_rotary_bwd_workspace_bytes(p) : 0;
+    if (need && (!workspace || misaligned(workspace) || workspace_bytes < need)) return NA2D_ERR_WORKSPACE;
+    const int e = elem(p->dtype);
+    float *parts = static_cast<float *>(workspace);
+    for (int side = 0; side < (p->kv_heads ? 2 : 1); ++side) {
+        RotaryArgs a = rotary_args(p, side, positions, freqs, side ? k_weight : q_weight);
+        a.x = side ? view(k, p->k, e) : view(q, p->q, e), a.z = side ? view(dk_out, p->k_out, e) : view(dq_out, p->q_out, e), a.dx = side ? view(dk, p->dk, e) : view(dq, p->dq, e);
+        a.parts = parts;
+        if (need) parts += rotary_parts(a, p->D) / sizeof(float);
+        if (int r = from_hip(launch_rotary_bwd(a, p->dtype, p->D, side ? dk_weight : dq_weight, static_cast<hipStream_t>(stream)))) return r;
+    }
+    return NA2D_OK;
+}
+
 int seq_cache_validate(const seq_cache_problem *p, int call) { return cache_validate(p, call); }
 
 int seq_cache_append(const seq_cache_problem *p, const void *k, const void *v, const int32_t *table, const int32_t *lengths, const int32_t *counts,
@@ -241,6 +361,37 @@ int seq_cache_append(const seq_cache_problem *p, const void *k, const void *v, c
     a.a = view(k, p->q, e), a.b = view(v, p->out, e), a.k = k_pages, a.v = v_pages, a.ks = k_scales, a.vs = v_scales;
     a.table = table, a.lengths = lengths, a.extra = counts;
     return from_hip(launch_append(a, p->dtype, p->D, static_cast<hipStream_t>(stream)));
+}
+
+int seq_cache_append_rows(const seq_cache_problem *p, const seq_rotation *r, int32_t given, const void *k, const void *v, const int32_t *rows, const int32_t *positions, int shared,
+                          const float *freqs, const void *weight, const int32_t *table, const int32_t *lengths, const int32_t *counts, int8_t *k_pages, int8_t *v_pages,
+                          float *k_scales, float *v_scales, void *stream) {
+    if (!p) return NA2D_ERR_NULL;
+    if (given <= 0 || given > 1 << 24 || p->n > 1 << 24 || (!rows && p->n > given) || (shared != 0 && shared != 1)) return NA2D_ERR_SHAPE;
+    seq_cache_problem of_given = *p;
+    of_given.n = given;
+    if (p->n <= 0) return NA2D_ERR_SHAPE;
+    if (int e = cache_validate(&of_given, SEQ_CACHE_APPEND)) return e;
+    if (r) {
+        if (int e = check_rotation(*r, p->D, p->dtype, true, weight != nullptr)) return e;
+        if (r->pairs && !freqs) return NA2D_ERR_NULL;
+        if (r->pairs && !positions && r->axes != 1) return NA2D_ERR_SHAPE;
+        if (misaligned_weight(weight, *r)) return NA2D_ERR_ALIGN;
+    } else if (weight || positions || freqs) {
+        return NA2D_ERR_NULL;
+    }
+    SEQ_REQUIRE(k); SEQ_REQUIRE(v); SEQ_REQUIRE(k_pages); SEQ_REQUIRE(v_pages);
+    if (!table || !lengths || !k_scales || !v_scales) return NA2D_ERR_NULL;
+    if (odd4({table, lengths, counts, rows, positions, freqs, k_scales, v_scales})) return NA2D_ERR_ALIGN;
+    if (k_pages == v_pages || k_scales == v_scales) return NA2D_ERR_ALIAS;
+    RowsArgs a{};
+    a.c = cache_args(p);
+    const int e = elem(p->dtype);
+    a.c.a = view(k, p->q, e), a.c.b = view(v, p->out, e), a.c.k = k_pages, a.c.v = v_pages, a.c.ks = k_scales, a.c.vs = v_scales;
+    a.c.table = table, a.c.lengths = lengths, a.c.extra = counts;
+    a.rows = rows, a.given = given;
+    if (r) a.r = rotation(*r, positions, shared ? 0 : (int64_t)r->axes * given, freqs, weight);
+    return from_hip(launch_append_rows(a, p->dtype, p->D, static_cast<hipStream_t>(stream)));
 }
 
 int seq_cache_gather(const seq_cache_problem *p, const int8_t *k_pages, const int8_t *v_pages, const float *k_scales, const float *v_scales, const int32_t *table,

@@ -40,6 +40,18 @@ __device__ __forceinline__ int whole(float x, float by, float over) {
     return max(-127, min(127, (int)__builtin_rintf(r)));
 }
 
+// What a page held, in words of four bytes, on its new scale.
+__device__ __forceinline__ void round_again(int8_t *cells, int count, float ratio, int tid) {
+    uint32_t *words = reinterpret_cast<uint32_t *>(cells);
+    for (int i = tid; i < count; i += kThreads) {
+        const uint32_t w = words[i];
+        uint32_t r = 0;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) r |= (uint32_t)(uint8_t)(int8_t)__builtin_rintf((float)(int8_t)(w >> 8 * e) * ratio) << 8 * e;
+        words[i] = r;
+    }
+}
+
 template <typename T, int D>
 __global__ __launch_bounds__(kThreads) void append_kernel(const CacheArgs p, int touched) {
     constexpr int E = 16 / (int)sizeof(T), CH = D / E;   // elements of a chunk, chunks of a row
@@ -93,17 +105,7 @@ __global__ __launch_bounds__(kThreads) void append_kernel(const CacheArgs p, int
     }
     const float scale = fmaxf(before, most / 127.f), by = scale > 0.f ? scale : 1.f;
     if (tid == 0) scales[unit] = scale;
-    if (old && scale != before) {
-        const float ratio = before / by;
-        uint32_t *words = reinterpret_cast<uint32_t *>(cells);
-        for (int i = tid; i < old * D / 4; i += kThreads) {
-            const uint32_t w = words[i];
-            uint32_t r = 0;
-#pragma unroll
-            for (int e = 0; e < 4; ++e) r |= (uint32_t)(uint8_t)(int8_t)__builtin_rintf((float)(int8_t)(w >> 8 * e) * ratio) << 8 * e;
-            words[i] = r;
-        }
-    }
+    if (old && scale != before) round_again(cells, old * D / 4, before / by, tid);
     // every element is divided where 1 / by may be no ordinary number either
     const bool divide = !ordinary || !(by > 0x1p-100f && by < 0x1p100f);
     const float over = 1.f / by;
@@ -119,6 +121,114 @@ __global__ __launch_bounds__(kThreads) void append_kernel(const CacheArgs p, int
             for (int e = 0; e < E; ++e) r[e] = (int8_t)whole((float)y[e], by, over);
         }
         *reinterpret_cast<bytes *>(cells + (int64_t)(old + i / CH) * D + i % CH * E) = r;
+    }
+}
+
+// The same with rows picked out of those given, and keys normed and rotated on the way: a page's fresh tokens stay in registers, in fp32, from their one read to the
+// bytes that are stored, lanes and chunks as seq_rotary.hpp has them.  What is stored is rounded once, from the rotated value.
+template <typename T, int D>
+__global__ __launch_bounds__(kThreads) void append_rows_kernel(const RowsArgs a, int touched) {
+    using S = HeadShape<T, D>;
+    constexpr int E = S::E, ROWS = kThreads / S::LANES, STEPS = 128 / ROWS;   // rows of the workgroup at a time, and how many times there may be
+    typedef typename S::vec vec;
+    typedef int8_t bytes __attribute__((ext_vector_type(E)));
+    __shared__ float mosts[kWaves];
+    const CacheArgs &p = a.c;
+    const int tid = threadIdx.x;
+    int id = blockIdx.x;
+    const bool values = id & 1;
+    id >>= 1;
+    const int kh = id % p.kv;
+    id /= p.kv;
+    const int b = id / touched, page = 1 << p.page_log2;
+    const int64_t length = p.lengths[b];
+    const int count = p.extra ? min(p.extra[b], p.n) : p.n;
+    if (length < 0 || count <= 0) return;
+    const int64_t at = (length >> p.page_log2) + id % touched, start = at << p.page_log2;
+    const int64_t lo = length > start ? length : start, hi = length + count < start + page ? length + count : start + page;
+    int to;
+    if (lo >= hi || !page_at(p, b, start, to)) return;
+    const int64_t unit = (int64_t)to * p.kv + kh;
+    int8_t *cells = (values ? p.v : p.k) + unit * page * D;
+    float *scales = values ? p.vs : p.ks;
+    const View &x = values ? p.b : p.a;
+    const int old = (int)(lo - start), fresh = (int)(hi - lo), first = (int)(lo - length);
+    const char *plane = x.at + b * x.b + kh * x.h;
+    const float before = old ? scales[unit] : 0.f;
+
+    const int i = tid % S::LANES, row0 = tid / S::LANES;
+    const bool turned = !values && a.r.pairs, normed = !values && a.r.weight;
+    int c0, c1;
+    chunks_of<E>(a.r, i, c0, c1);
+    float l[STEPS][E], h[STEPS][E], most = 0.f;
+    int src[STEPS];
+#pragma unroll
+    for (int s = 0; s < STEPS; ++s) {
+        const int row = s * ROWS + row0;
+        src[s] = -1;
+        if (row < fresh) {
+            src[s] = a.rows ? a.rows[(int64_t)b * p.n + first + row] : first + row;
+            if ((unsigned)src[s] >= (unsigned)a.given) src[s] = -1;
+        }
+    }
+#pragma unroll
+    for (int s = 0; s < STEPS; ++s) {
+        vec y{}, z{};
+        if (src[s] >= 0) {
+            const char *row = plane + (int64_t)src[s] * x.row;
+            y = *reinterpret_cast<const vec *>(row + c0 * sizeof(T)), z = *reinterpret_cast<const vec *>(row + c1 * sizeof(T));
+        }
+#pragma unroll
+        for (int e = 0; e < E; ++e) l[s][e] = (float)y[e], h[s][e] = (float)z[e];
+    }
+    if (normed) {
+        float wl[E], wh[E];
+        load_weight<T, E>(a.r, c0, c1, wl, wh);
+#pragma unroll
+        for (int s = 0; s < STEPS; ++s) {
+            const float r = over_rms<D, S::LANES>(l[s], h[s], a.r.eps);
+#pragma unroll
+            for (int e = 0; e < E; ++e) l[s][e] *= r * wl[e], h[s][e] *= r * wh[e];
+        }
+    }
+    if (turned) {
+#pragma unroll
+        for (int s = 0; s < STEPS; ++s) {
+            if (src[s] < 0) continue;
+            Angles<E> angles;
+            angles.set(a.r, i, a.r.positions ? a.r.positions + b * a.r.batch + src[s] : nullptr, a.given, (int)(lo + s * ROWS + row0));
+            angles.template turn<false>(a.r.interleaved, l[s], h[s]);
+        }
+    }
+#pragma unroll
+    for (int s = 0; s < STEPS; ++s)
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+            l[s][e] = finite(l[s][e]), h[s][e] = finite(h[s][e]);
+            most = fmaxf(most, fmaxf(fabsf(l[s][e]), fabsf(h[s][e])));
+        }
+#pragma unroll
+    for (int d = 1; d < kWave; d *= 2) most = fmaxf(most, __shfl_xor(most, d));
+    if (tid % kWave == 0) mosts[tid / kWave] = most;
+    workgroup_sync();
+    most = fmaxf(fmaxf(mosts[0], mosts[1]), fmaxf(mosts[2], mosts[3]));
+    const float scale = fmaxf(before, most / 127.f), by = scale > 0.f ? scale : 1.f;
+    if (tid == 0) scales[unit] = scale;
+    if (old && scale != before) round_again(cells, old * D / 4, before / by, tid);
+    const bool divide = !(by > 0x1p-100f && by < 0x1p100f);
+    const float over = 1.f / by;
+#pragma unroll
+    for (int s = 0; s < STEPS; ++s) {
+        const int row = s * ROWS + row0;
+        if (row >= fresh) break;
+        bytes u, w;
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+            u[e] = (int8_t)(divide ? max(-127, min(127, (int)__builtin_rintf(l[s][e] / by))) : whole(l[s][e], by, over));
+            w[e] = (int8_t)(divide ? max(-127, min(127, (int)__builtin_rintf(h[s][e] / by))) : whole(h[s][e], by, over));
+        }
+        int8_t *cell = cells + (int64_t)(old + row) * D;
+        *reinterpret_cast<bytes *>(cell + c0) = u, *reinterpret_cast<bytes *>(cell + c1) = w;
     }
 }
 
@@ -166,12 +276,25 @@ __global__ __launch_bounds__(kThreads) void gather_kernel(const CacheArgs p, int
     }
 }
 
+int pages_touched(const CacheArgs &a) {   // that n tokens can lie in
+    const int page = 1 << a.page_log2;
+    return (a.n + page - 2) / page + 1;
+}
 template <typename T, int D, int> struct Append {
     static hipError_t go(const CacheArgs &a, hipStream_t st) {
-        const int page = 1 << a.page_log2, touched = (a.n + page - 2) / page + 1;   // pages that n tokens can lie in
+        const int touched = pages_touched(a);
         const int64_t blocks = (int64_t)a.B * touched * a.kv * 2;
         if (!launch_holds(blocks, kThreads)) return hipErrorInvalidValue;
         append_kernel<T, D><<<(unsigned)blocks, kThreads, 0, st>>>(a, touched);
+        return hipGetLastError();
+    }
+};
+template <typename T, int D, int> struct AppendRows {
+    static hipError_t go(const RowsArgs &a, hipStream_t st) {
+        const int touched = pages_touched(a.c);
+        const int64_t blocks = (int64_t)a.c.B * touched * a.c.kv * 2;
+        if (!launch_holds(blocks, kThreads)) return hipErrorInvalidValue;
+        append_rows_kernel<T, D><<<(unsigned)blocks, kThreads, 0, st>>>(a, touched);
         return hipGetLastError();
     }
 };
@@ -189,6 +312,7 @@ template <typename T, int D, int> struct Gather {
 }  // namespace
 
 hipError_t launch_append(const CacheArgs &a, int dtype, int D, hipStream_t st) { return dispatch<Append>(dtype, D, false, a, st); }
+hipError_t launch_append_rows(const RowsArgs &a, int dtype, int D, hipStream_t st) { return dispatch<AppendRows>(dtype, D, false, a, st); }
 hipError_t launch_gather(const CacheArgs &a, int dtype, int D, hipStream_t st) { return dispatch<Gather>(dtype, D, false, a, st); }
 
 }  // namespace seq

@@ -1,7 +1,7 @@
 // The cache in 8 bits: what its kernels take.
 #pragma once
 
-#include "seq_common.hpp"
+#include "seq_rotary.hpp"
 
 namespace seq {
 
@@ -24,6 +24,14 @@ __device__ __forceinline__ bool page_at(const CacheArgs &p, int b, int64_t posit
 }
 
 hipError_t launch_append(const CacheArgs &a, int dtype, int D, hipStream_t st);
+// Of `given` rows of each sequence the n that `rows` names (null: the first n), keys normed and rotated where `r` says so.
+struct RowsArgs {
+    CacheArgs c;
+    Rotation r;            // positions of the given rows; null: a token's place in its sequence
+    const int *rows;       // [B, n]
+    int given;
+};
+hipError_t launch_append_rows(const RowsArgs &a, int dtype, int D, hipStream_t st);
 hipError_t launch_gather(const CacheArgs &a, int dtype, int D, hipStream_t st);
 hipError_t launch_cache_attention(const CacheArgs &a, int dtype, int D, int cap, hipStream_t st);   // cap: the CapForm of fp16 weights, whatever the type of q
 void plan_cache_attention(CacheArgs &a, int64_t longest);   // splits, row_groups

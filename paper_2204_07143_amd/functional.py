@@ -6,7 +6,7 @@ between them left to the framework (arXiv 2204.07143, Appendix A, "Implementatio
 through the fused forward and the fused backward, which keep the attention tensor out of memory.
 
 Only argument marshalling and buffer allocation happen here: every gradient comes from the
-library's kernels.  ``na2d``, ``na1d``, ``na2d_unfused`` and the attention over sequences (``seq_*``) do it in native code (``na2d_torch.so``, from
+library's kernels.  ``na2d``, ``na1d``, ``na2d_unfused`` and the operators on sequences (``seq_*``) do it in native code (``na2d_torch.so``, from
 ``csrc/host/torch_ops.cpp``): a call on small tensors takes longer in the interpreter than on the GPU.  The functions below
 serve ``na2d_qk_rpb``, ``na2d_av`` and ``na2d_softmax``, and whatever the native code hands back: invalid arguments (the
 binding's errors), functorch transforms, forward-mode differentiation, tracing, tensors that are not plain ones.  Tensors are ``[B, heads, H, W, D]`` (q, k, v, out), ``[B, heads, H, W, k*k]``
@@ -264,12 +264,13 @@ class _OnceOnly(torch.autograd.Function):
     """Gradients as they are, tied to what they depend on by a node that raises: no second derivative, and none that is silently zero."""
 
     @staticmethod
-    def forward(ctx, count, *tensors):
+    def forward(ctx, name, count, *tensors):
+        ctx.name = name
         return tuple(t.view_as(t) for t in tensors[:count])
 
     @staticmethod
     def backward(ctx, *_):
-        raise RuntimeError("seq_attention has no second derivative")
+        raise RuntimeError(f"{ctx.name} has no second derivative")
 
 
 class _SeqAttention(torch.autograd.Function):
@@ -299,7 +300,7 @@ class _SeqAttention(torch.autograd.Function):
         with torch.no_grad():
             grads = _SeqAttention.gradients(ctx, dout)
         if torch.is_grad_enabled():
-            grads = _OnceOnly.apply(3, *grads, q, k, v, dout)
+            grads = _OnceOnly.apply("seq_attention", 3, *grads, q, k, v, dout)
         return (*grads, None, None, None, None)
 
     @staticmethod
@@ -354,6 +355,89 @@ def seq_attention(q, k, v, *, causal: bool = False, window: int | None = None, s
     return _SeqAttention.apply(q, k, v, slopes, documents, prefix, settings)
 
 
+class _SeqRotary(torch.autograd.Function):
+    """Norm of head vectors and their rotation by position (include/seq.h)."""
+
+    @staticmethod
+    def forward(ctx, q, k, positions, freqs, q_weight, k_weight, settings):
+        q, k = _rows(q), None if k is None else _rows(k)
+        q_out, k_out = _like(q), None if k is None else _like(k)
+        if q.numel() or (k is not None and k.numel()):
+            na.seq_rotary_fwd(q, k, positions, freqs, q_weight, k_weight, q_out, k_out, **settings)
+        if any(ctx.needs_input_grad):
+            ctx.settings = settings
+            ctx.save_for_backward(None if q_weight is None else q, None if k_weight is None else k, positions, freqs, q_weight, k_weight)
+        return q_out if k is None else (q_out, k_out)
+
+    @staticmethod
+    def backward(ctx, *dz):
+        q, k, positions, freqs, q_weight, k_weight = ctx.saved_tensors
+        with torch.no_grad():
+            upstream = [_rows(z) for z in dz]
+            x = [z if t is None else t for z, t in zip(upstream, (q, k))]
+            dx = [_like(t) for t in x]
+            dw = [None if w is None else torch.empty_like(w) for w in (q_weight, k_weight)]
+            args = lambda pair: (*pair, None)[:2]
+            if any(z.numel() for z in upstream):
+                settings = ctx.settings
+                rotation = na.seq_rotation(x[0].dtype, weights=(q_weight, k_weight), **settings)
+                p = na.seq_rotary_problem(*args(x), positions, rotation, **dict(zip(("q_out", "k_out"), upstream)), **dict(zip(("dq", "dk"), dx)))
+                ws = _scratch(na.seq_rotary_bwd_workspace_bytes(p) if dw != [None, None] else 0, x[0])
+                na.seq_rotary_bwd(*args(x), positions, freqs, q_weight, k_weight, *args(upstream), *args(dx), *dw, ws, **settings)
+            else:
+                dw = [None if w is None else w.zero_() for w in dw]
+        made = [t for t in (*dx, *dw) if t is not None]
+        if torch.is_grad_enabled():
+            made = list(_OnceOnly.apply("seq_rotary", len(made), *made, *(t for t in (q, k, q_weight, k_weight, *dz) if t is not None)))
+        dx = made[:len(dx)]
+        left = iter(made[len(dx):])
+        dw = [None if w is None else next(left) for w in dw]
+        return (*(*dx, None)[:2], None, None, *dw, None)
+
+
+def _sections(freqs, sections) -> tuple:
+    sections = (freqs.numel(),) if sections is None else tuple(int(x) for x in sections)
+    if sum(sections) != freqs.numel() or not 1 <= len(sections) <= 4 or min(sections) < 1:
+        raise ValueError(f"sections are the pairs of 1 to 4 axes, {freqs.numel()} in all, got {sections}")
+    return sections
+
+
+def _rotary_constants(positions, freqs):
+    for name, t in (("positions", positions), ("freqs", freqs)):
+        if t is not None and t.requires_grad:
+            raise ValueError(f"{name} are constants: they have no gradient")
+
+
+def seq_rotary(q, k, positions, freqs, *, sections=None, q_weight=None, k_weight=None, eps: float = 1e-6, interleaved: bool = False):
+    """Queries [B, heads, L, D] and keys [B, kv_heads, L, D] (or None) rotated by their positions, each head's vector normed before that where its weight ([D], of q's
+    type or fp32) is given; differentiable in q, k and the weights.  Returns (q, k).
+
+    Pair p of a vector, channels p and p + P (``interleaved``: 2 p and 2 p + 1) of P pairs, turns by ``positions[axis of p] * freqs[p]``; channels from 2 P on are
+    not rotated.  ``freqs``: fp32 [P], P a multiple of 8.  ``positions``: int32 [axes, L], or [B, axes, L]; ``sections`` says how many of the pairs each axis has, in order (None: one
+    axis).  The norm is ``x * weight / sqrt(mean(x ** 2) + eps)``.  Angles are formed in 64 bits: positions may be as far as int32 goes.  Maps [B, heads, H, W, D],
+    with positions [axes, H, W], are taken as well, before the neighbourhood operators.  D is 16, 32, 64 or 128; f32, f16, bf16; strided as in ``seq_attention``.
+    """
+    if q.dim() == 5:
+        if k is not None and k.dim() != 5:
+            raise ValueError("expected queries and keys of one form")
+        shape = q.shape[2:4]
+        turned = seq_rotary(q.flatten(2, 3), None if k is None else k.flatten(2, 3), positions.flatten(-2), freqs, sections=sections, q_weight=q_weight, k_weight=k_weight, eps=eps,
+                            interleaved=interleaved)
+        return tuple(None if t is None else t.unflatten(2, shape) for t in turned)
+    out = _native().seq_rotary(q, k, positions, freqs, sections, q_weight, k_weight, eps, interleaved)
+    if out is not None:
+        return out if k is not None else (*out, None)
+    if q.dim() != 4 or (k is not None and (k.dim() != 4 or k.shape[0] != q.shape[0] or k.shape[2:] != q.shape[2:])):
+        raise ValueError("expected [B, heads, L, D] tensors of one B, L and D")
+    if positions.dim() not in (2, 3):
+        raise ValueError("expected positions [axes, L] or [B, axes, L]")
+    if k is None and k_weight is not None:
+        raise ValueError("a weight of keys that are not given")
+    _rotary_constants(positions, freqs)
+    out = _SeqRotary.apply(q, k, positions, freqs, q_weight, k_weight, dict(sections=_sections(freqs, sections), eps=float(eps), interleaved=bool(interleaved)))
+    return out if k is not None else (out, None)
+
+
 class SeqCache(NamedTuple):
     """Keys and values in 8 bits: pages int8 [pages, kv_heads, page, D] and a scale for each page and head, fp32 [pages, kv_heads]; a value is
     the integer times the scale.  Which page holds what is the caller's: a table, int32 [B, width], gives each sequence's pages in order."""
@@ -368,17 +452,31 @@ class SeqCache(NamedTuple):
         return cls(*cells, *(torch.zeros((pages, kv_heads), dtype=torch.float32, device=device) for _ in range(2)))
 
 
-def seq_cache_append(cache: SeqCache, k, v, table, lengths, counts=None) -> None:
+def seq_cache_append(cache: SeqCache, k, v, table, lengths, counts=None, *, rows=None, freqs=None, positions=None, sections=None, weight=None, eps: float = 1e-6,
+                     interleaved: bool = False) -> None:
     """Puts ``k``, ``v`` [B, kv_heads, n, D] behind the ``lengths`` (int32 [B]) tokens of each sequence, the first ``counts[b]`` of the n where ``counts``
     (int32 [B]) is given.  A page's scale grows with its largest value; what it held is then rounded again.  ``lengths`` stays as it is.  No page may be
-    appended to twice in one call; a page number that is none is passed over."""
-    if _native().seq_cache_append(*cache, k, v, table, lengths, counts):
+    appended to twice in one call; a page number that is none is passed over.
+
+    ``rows`` (int32 [B, m]): the m tokens appended are these rows of k and v, as a path that ``seq_verify`` accepted; a row that is none is a token of zeros.
+    ``freqs`` and ``weight``: keys are rotated, and normed before that, on the way, as ``seq_rotary`` has it; a token's position is its place in its
+    sequence, or ``positions`` (int32 [axes, n] or [B, axes, n], with ``sections``) of the rows given."""
+    more = rows is not None or freqs is not None or weight is not None
+    if not more and positions is None and sections is None:
+        if _native().seq_cache_append(*cache, k, v, table, lengths, counts):
+            return
+    elif _native().seq_cache_append_rows(*cache, k, v, table, lengths, counts, rows, positions, freqs, sections, weight, eps, interleaved):
         return
     if k.dim() != 4 or v.dim() != 4:
         raise ValueError("expected [B, heads, L, D] tensors")
-    if 0 not in k.shape:
+    if freqs is None and (positions is not None or sections is not None):
+        raise ValueError("positions and sections are for keys that are rotated: freqs are missing")
+    _rotary_constants(positions, freqs)
+    how = dict(rows=rows, positions=positions, freqs=freqs, weight=weight, sections=() if freqs is None else _sections(freqs, sections), eps=float(eps), interleaved=bool(interleaved))
+    if 0 not in k.shape and not (rows is not None and 0 in rows.shape):
         with torch.no_grad():
-            na.seq_cache_append(_rows(k), _rows(v), table, lengths, counts, *cache)
+            args = (_rows(k), _rows(v), table, lengths, counts, *cache)
+            na.seq_cache_append_rows(*args, **how) if more else na.seq_cache_append(*args)
 
 
 def seq_cache_gather(cache: SeqCache, table, lengths, first, n: int, dtype=torch.bfloat16):
