@@ -159,6 +159,40 @@ int seq_cache_attention(const seq_cache_problem *p, const void *q, const int8_t 
                         size_t workspace_bytes, void *stream);
 size_t seq_cache_attention_workspace_bytes(const seq_cache_problem *p);
 
+/* Attention of a tree of n <= 64 drafted tokens, its nodes, over each sequence's cache, which does not hold them: q [B, heads, n, D]; k, v [B, kv_heads, n, D], the nodes'
+ * own, in the problem dtype, with strides k_strides and v_strides.  parents: int32 [B, n]; a node's parent is a node before it, or -1: it follows the cache's last token.  Any
+ * other value: no node (as padding), and neither is what descends from it; its q, k and v may be anything, and its row of out is 0.  A node stands at position lengths[b] +
+ * its depth, and sees the cache, its ancestors and itself, all within `window` before it.  Scores as above.  Over the cache weights are rounded as in seq_cache_attention; over
+ * the nodes to fp16, or in bf16 to a sum of two of them.  The workspace is always needed. */
+int seq_cache_tree_attention(const seq_cache_problem *p, const seq_strides *k_strides, const seq_strides *v_strides, const void *q, const void *k, const void *v, const int32_t *parents,
+                             const int8_t *k_pages, const int8_t *v_pages, const float *k_scales, const float *v_scales, const int32_t *table, const int32_t *lengths, const float *slopes,
+                             void *out, void *workspace, size_t workspace_bytes, void *stream);
+size_t seq_cache_tree_attention_workspace_bytes(const seq_cache_problem *p);
+
+/* Which drafted tokens a target accepts, and the token behind them.  tokens: int32 [B, n]; node 0 of a sequence is the token that its draft follows, the others are drafted.
+ * logits: [B, n, V], the target's behind each node; rows' elements contiguous.  Of a row, p = softmax(logits / T), T = temperatures[b] (fp32 [B]; NULL: 1); T not above 0: all on the
+ * largest logit, at its lowest index.  A logit of -infinity, or a NaN, is a token that is not chosen; an infinite one counts as the largest finite fp32 value.
+ * A token is drawn from weights w by a number u: the lowest t with w_0 + .. + w_t > u (w_0 + .. + w_V-1), w_t > 0.  Everything from the logits on is in 64 bits.
+ *
+ * drafted 0: parents, int32 [B, n], makes the nodes a tree as seq_cache_tree_attention has it (NULL: a line).  At a node i a token is drawn from p_i by
+ * uniforms[b, i] (fp32 [B, n]); if a child of it (the lowest) has this token the walk goes on there, else the token is the next one.
+ * drafted 1: draft [B, n - 1, V], in the type of logits: the logits that tokens 1 .. n - 1 of a line were drawn from (parents NULL), q = softmax(draft / T).  Token x of node i + 1 is
+ * accepted if uniforms[b, i] q_i(x) < p_i(x) (uniforms fp32 [B, n + 1]; T not above 0: if it is the largest logit's).  The first that is not, or whose number is no token (outside [0, V):
+ * the end of a draft), ends the line; the next token is then drawn by uniforms[b, n], from max(p - q, 0) (from p where that is 0 throughout), at the end of the draft from p.
+ * Numbers outside [0, 1) count as the nearest inside, a NaN as 0.
+ *
+ * path: int32 [B, n], the accepted nodes from node 0 on, then -1.  counts: int32 [B], how many there are (at least 1).  next: int32 [B], the next token; -1 from a row that gives none. */
+typedef struct {
+    int32_t B, n, V; /* n <= 64; V <= 2^24 */
+    int32_t dtype;   /* of logits and draft */
+    int32_t drafted; /* 1: with the draft's logits (draft is not read where n is 1) */
+    int64_t batch, row, draft_batch, draft_row; /* strides in elements, 0 or more */
+} seq_verify_problem;
+int seq_verify_validate(const seq_verify_problem *p);
+size_t seq_verify_workspace_bytes(const seq_verify_problem *p);
+int seq_verify(const seq_verify_problem *p, const void *logits, const void *draft, const int32_t *tokens, const int32_t *parents, const float *uniforms, const float *temperatures,
+               int32_t *path, int32_t *counts, int32_t *next, void *workspace, size_t workspace_bytes, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -34,15 +34,15 @@ def visible(Lq, Lk, causal=False, window=None, documents=None, prefix=None):
     return see
 
 
-def head(q, k, v, dout, see, *, scale, softcap=None, slope=0.0, u=0.0, e=0.0, tiny=0.0):
-    """One head: q [Lq, D], k and v [Lk, D], dout [Lq, D] or None, see [Lq, Lk] -> dict of results and dict of bounds."""
+def head(q, k, v, dout, see, *, scale, softcap=None, slope=0.0, u=0.0, e=0.0, tiny=0.0, far=None):
+    """One head: q [Lq, D], k and v [Lk, D], dout [Lq, D] or None, see [Lq, Lk], far [Lq, Lk] (None: of tokens in a row) -> dict of results and dict of bounds."""
     Lq, Lk = see.shape
     live_q, live_k = see.any(1), see.any(0)
     q, k, v = (np.where(alive[:, None], x, 0.0) for x, alive in ((q, live_q), (k, live_k), (v, live_k)))   # the rest may be anything
     raw = scale * (q @ k.T)
     t = np.tanh(raw / softcap) if softcap else None
     s = softcap * t if softcap else raw
-    far = np.abs(np.arange(Lq)[:, None] + Lk - Lq - np.arange(Lk)[None])
+    far = np.abs(np.arange(Lq)[:, None] + Lk - Lq - np.arange(Lk)[None]) if far is None else far
     s = np.where(see, s - slope * far, -INF)
     m = np.where(live_q, s.max(1, initial=-INF), 0.0)
     p = np.exp(s - m[:, None])
@@ -182,3 +182,81 @@ def rotary(x, positions, freqs, sections, weight=None, eps=1e-6, interleaved=Fal
             bound["dw"] = u * np.abs(res["dw"]) + (2 * e + 400 * 2.0 ** -24) * (size / np.abs(w) * np.abs(xr)).sum((0, 1, 2)) + tiny / 2
         bound["dx"] = u * np.abs(res["dx"]) + off + tiny / 2
     return res, bound
+
+
+# ---- a tree of drafted tokens ------------------------------------------------------------------------------------------
+
+def depths(parents):
+    """Nodes above each node; -1: no node."""
+    out = []
+    for i, p in enumerate(parents):
+        out.append(0 if p == -1 else out[p] + 1 if 0 <= p < i and out[p] >= 0 else -1)
+    return out
+
+
+def tree(q, k, v, parents, there, L, window=None):
+    """What the nodes of one sequence see of its L tokens and of themselves: see [n, L + n] and far.  there: bool [L], tokens whose page is one."""
+    n, depth = len(parents), depths(parents)
+    see = np.zeros((n, L + n), dtype=bool)
+    for i in range(n):
+        if depth[i] >= 0:
+            see[i, :L] = there
+            at = i
+            while at >= 0:
+                see[i, L + at] = True
+                at = parents[at]
+    stands = L + np.array(depth)
+    far = stands[:, None] - np.concatenate([np.arange(L), stands])[None]
+    return see & (far < (window or L + n + 1)), np.maximum(far, 0)
+
+
+def _probabilities(logits, temperature):
+    x = np.where(np.isnan(logits), -INF, np.minimum(logits, np.finfo(np.float32).max))
+    if x.max() == -INF:
+        return np.zeros_like(x)
+    if not temperature > 0:
+        p = np.zeros_like(x)
+        p[x.argmax()] = 1
+        return p
+    p = np.zeros_like(x)
+    some = x > -INF
+    p[some] = np.exp((x[some] - x.max()) / temperature)
+    return p / p.sum()
+
+
+def _drawn(p, u):
+    """-1: p gives none."""
+    sums = np.cumsum(p)
+    some = np.flatnonzero(p > 0)
+    if len(some) == 0:
+        return -1
+    u = min(max(u, 0.0), 1 - 2.0 ** -24) if u == u else 0.0
+    passed = some[sums[some] > u * sums[-1]]
+    return int(passed[0] if len(passed) else some[-1])
+
+
+def verify(logits, tokens, uniforms, parents=None, draft=None, temperature=1.0):
+    """One sequence: logits [n, V], tokens [n], uniforms [n] (with draft [n - 1, V]: [n + 1]) -> (path, next)."""
+    n, V = logits.shape
+    number = lambda u: min(max(u, 0.0), 1 - 2.0 ** -24) if u == u else 0.0
+    if draft is None:
+        node, path = 0, [0]
+        while True:
+            token = _drawn(_probabilities(logits[node], temperature), uniforms[node])
+            child = [c for c in range(node + 1, n) if (c - 1 if parents is None else parents[c]) == node and tokens[c] == token and token >= 0]
+            if not child:
+                return path, token
+            node = child[0]
+            path.append(node)
+    for i in range(n):
+        p, path = _probabilities(logits[i], temperature), list(range(i + 1))
+        if i == n - 1 or not 0 <= tokens[i + 1] < V:
+            return path, _drawn(p, uniforms[n])
+        if not temperature > 0:
+            if p[tokens[i + 1]] != 1:
+                return path, _drawn(p, 0.0)
+            continue
+        q = _probabilities(draft[i], temperature)
+        if not number(uniforms[i]) * q[tokens[i + 1]] < p[tokens[i + 1]]:
+            rest = np.maximum(p - q, 0)
+            return path, _drawn(rest if rest.sum() > 0 else p, uniforms[n])

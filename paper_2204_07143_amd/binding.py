@@ -39,6 +39,7 @@ EXPORTS_SEQ = (
     "seq_validate_problem", "seq_attention_workspace_bytes", "seq_attention_fwd", "seq_attention_bwd", "seq_cache_validate", "seq_cache_append",
     "seq_cache_gather", "seq_cache_attention", "seq_cache_attention_workspace_bytes",
     "seq_rotary_validate", "seq_rotary_fwd", "seq_rotary_bwd", "seq_rotary_bwd_workspace_bytes", "seq_cache_append_rows",
+    "seq_cache_tree_attention", "seq_cache_tree_attention_workspace_bytes", "seq_verify_validate", "seq_verify", "seq_verify_workspace_bytes",
 )
 SEQ_CACHE_APPEND, SEQ_CACHE_GATHER, SEQ_CACHE_ATTENTION = 0, 1, 2
 
@@ -80,6 +81,10 @@ class SeqRotation(ctypes.Structure):
 class SeqRotaryProblem(ctypes.Structure):
     _fields_ = ([(n, ctypes.c_int32) for n in ("B", "heads", "kv_heads", "L", "D", "dtype")] + [("rotation", SeqRotation), ("shared", ctypes.c_int32)]
                 + [(n, SeqStrides) for n in ("q", "k", "q_out", "k_out", "dq", "dk")])
+
+
+class SeqVerifyProblem(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("B", "n", "V", "dtype", "drafted")] + [(n, ctypes.c_int64) for n in ("batch", "row", "draft_batch", "draft_row")]
 
 
 _lib = None
@@ -140,7 +145,7 @@ def load(path: str | None = None) -> ctypes.CDLL:
             fn = getattr(lib, name)
             fn.argtypes = argtypes
             fn.restype = ctypes.c_int
-        ps, pc, pr, size = ctypes.POINTER(SeqProblem), ctypes.POINTER(SeqCacheProblem), ctypes.POINTER(SeqRotaryProblem), ctypes.c_size_t
+        ps, pc, pr, pv, size = (*(ctypes.POINTER(t) for t in (SeqProblem, SeqCacheProblem, SeqRotaryProblem, SeqVerifyProblem)), ctypes.c_size_t)
         sigs_seq = {
             "seq_validate_problem": [ps, ctypes.c_int],
             "seq_attention_fwd": [ps] + [vp] * 10 + [size, vp],
@@ -150,6 +155,9 @@ def load(path: str | None = None) -> ctypes.CDLL:
             "seq_cache_gather": [pc] + [vp] * 10,
             "seq_cache_attention": [pc] + [vp] * 10 + [size, vp],
             "seq_cache_append_rows": [pc, ctypes.POINTER(SeqRotation), ctypes.c_int32] + [vp] * 4 + [ctypes.c_int] + [vp] * 10,
+            "seq_cache_tree_attention": [pc, ctypes.POINTER(SeqStrides), ctypes.POINTER(SeqStrides)] + [vp] * 13 + [size, vp],
+            "seq_verify_validate": [pv],
+            "seq_verify": [pv] + [vp] * 10 + [size, vp],
             "seq_rotary_validate": [pr, ctypes.c_int],
             "seq_rotary_fwd": [pr] + [vp] * 9,
             "seq_rotary_bwd": [pr] + [vp] * 13 + [size, vp],
@@ -160,8 +168,9 @@ def load(path: str | None = None) -> ctypes.CDLL:
             fn.restype = ctypes.c_int
         lib.seq_attention_workspace_bytes.argtypes = [ps, ctypes.c_int, ctypes.c_int]
         lib.seq_attention_workspace_bytes.restype = size
-        lib.seq_rotary_bwd_workspace_bytes.argtypes = [pr]
-        lib.seq_rotary_bwd_workspace_bytes.restype = size
+        for name, problem in (("seq_rotary_bwd", pr), ("seq_cache_tree_attention", pc), ("seq_verify", pv)):
+            fn = getattr(lib, name + "_workspace_bytes")
+            fn.argtypes, fn.restype = [problem], size
         lib.seq_cache_attention_workspace_bytes.argtypes = [pc]
         lib.seq_cache_attention_workspace_bytes.restype = size
         lib.na1d_workspace_bytes.argtypes = [p1]
@@ -738,3 +747,54 @@ def seq_cache_attention(q, k_pages, v_pages, k_scales, v_scales, table, lengths,
                                           _dense(lengths, q, (B,), torch.int32), _dense(slopes, q, (q.shape[1],), torch.float32), _strided(out, q, q.shape),
                                           *_bytes(workspace), _seq_stream(q)))
     return out
+
+
+def seq_cache_tree_attention_workspace_bytes(p: SeqCacheProblem) -> int:
+    return int(load().seq_cache_tree_attention_workspace_bytes(ctypes.byref(p)))
+
+
+def seq_cache_tree_attention(q, k_, v, parents, k_pages, v_pages, k_scales, v_scales, table, lengths, slopes, out, workspace, *, window=0, softcap=0.0, scale=1.0):
+    p = seq_cache_problem(q, k_pages, table, heads=q.shape[1], window=window, softcap=softcap, scale=scale, out=out)
+    B, _, n, D = q.shape
+    shape, cache = (B, k_pages.shape[1], n, D), _cache_inputs(q, k_pages, v_pages, k_scales, v_scales)
+    inputs = (_strided(q, q, q.shape), _strided(k_, q, shape), _strided(v, q, shape), _dense(parents, q, (B, n), torch.int32))
+    ks, vs = _seq_strides(k_), _seq_strides(v)
+    with torch.cuda.device(q.device):
+        _check(load().seq_cache_tree_attention(ctypes.byref(p), ctypes.byref(ks), ctypes.byref(vs), *inputs, *cache, _dense(table, q, (B, table.shape[1]), torch.int32),
+                                               _dense(lengths, q, (B,), torch.int32), _dense(slopes, q, (q.shape[1],), torch.float32), _strided(out, q, q.shape), *_bytes(workspace),
+                                               _seq_stream(q)))
+    return out
+
+
+def seq_verify_problem(logits, draft=None) -> SeqVerifyProblem:
+    if logits.dim() != 3 or (draft is not None and draft.dim() != 3):
+        raise ValueError("expected [B, n, V] logits and [B, n - 1, V] logits of a draft")
+    B, n, V = logits.shape
+    p = SeqVerifyProblem(B, n, V, DTYPE_CODES.get(logits.dtype, -1), int(draft is not None), *_row_strides(logits))
+    if draft is not None:
+        p.draft_batch, p.draft_row = _row_strides(draft)
+    return p
+
+
+def _row_strides(t):
+    return tuple(0 if n <= 1 else s for n, s in zip(t.shape[:2], t.stride()[:2]))
+
+
+def seq_verify_validate(p: SeqVerifyProblem) -> int:
+    return int(load().seq_verify_validate(ctypes.byref(p)))
+
+
+def seq_verify_workspace_bytes(p: SeqVerifyProblem) -> int:
+    return int(load().seq_verify_workspace_bytes(ctypes.byref(p)))
+
+
+def seq_verify(logits, draft, tokens, parents, uniforms, temperatures, path, counts, next_, workspace):
+    p = seq_verify_problem(logits, draft)
+    B, n, V = logits.shape
+    int32 = lambda t, shape: _dense(t, logits, shape, torch.int32)
+    f32 = lambda t, shape: _dense(t, logits, shape, torch.float32)
+    inputs = (_strided(logits, logits, logits.shape), None if draft is None else _strided(draft, logits, (B, n - 1, V)), int32(tokens, (B, n)), int32(parents, (B, n)),
+              f32(uniforms, (B, n if draft is None else n + 1)), f32(temperatures, (B,)))
+    with torch.cuda.device(logits.device):
+        _check(load().seq_verify(ctypes.byref(p), *inputs, int32(path, (B, n)), int32(counts, (B,)), int32(next_, (B,)), *_bytes(workspace), _seq_stream(logits)))
+    return path, counts, next_

@@ -884,6 +884,64 @@ PyObject *py_seq_cache_attention(PyObject *, PyObject *const *a, Py_ssize_t n) {
     });
 }
 
+// (q, k_pages, v_pages, k_scales, v_scales, table, lengths, k, v, parents, window or None, softcap or None, slopes or None, scale or None)
+PyObject *py_seq_cache_tree_attention(PyObject *, PyObject *const *a, Py_ssize_t n) {
+    SeqCacheArgs c;
+    Tensor q, k, v, parents, slopes;
+    SeqSettings x{};
+    if (n != 14 || !plain_modes() || !tensor_arg(a[0], q) || !cache_args(a + 1, c, 4) || !tensor_arg(a[7], k) || !tensor_arg(a[8], v) || !tensor_arg(a[9], parents) || !tensor_arg(a[12], slopes, true) ||
+        !settings_args(a[10], a[11], a[13], q, x))
+        Py_RETURN_NONE;
+    return guarded([&]() -> Tensor {
+        if (!plain(q) || q.dim() != 4 || !small(q.sizes()) || c.k.dim() != 4 || !c.fit(q, c.k.size(1)) || !constant(slopes, q, at::kFloat, {q.size(1)}) || (slopes.defined() && slopes.requires_grad()))
+            return Tensor();
+        const std::vector<int64_t> own{q.size(0), c.k.size(1), q.size(2), q.size(3)};
+        if (!matches(k, q, own) || !matches(v, q, own) || !constant(parents, q, at::kInt, {q.size(0), q.size(2)})) return Tensor();
+        const at::AutoGradMode off(false);
+        const c10::DeviceGuard device(q.device());
+        const Tensor r = rows(q), out = rows_like(r), kr = rows(k), vr = rows(v);
+        const auto p = c.problem(r, out, q.size(1), x.window, x.softcap, x.scale);
+        if (!p) return Tensor();
+        const seq_strides ks = strides(kr), vs = strides(vr);
+        const Tensor ws = scratch(seq_cache_tree_attention_workspace_bytes(&*p), q);
+        forward_check(seq_cache_tree_attention(&*p, &ks, &vs, ptr(r), ptr(kr), ptr(vr), (const int32_t *)ptr(parents), (const int8_t *)ptr(c.k), (const int8_t *)ptr(c.v), (const float *)ptr(c.ks),
+                                               (const float *)ptr(c.vs), (const int32_t *)ptr(c.table), (const int32_t *)ptr(c.lengths), (const float *)ptr(slopes), ptr(out), ptr(ws), size_of(ws), stream()));
+        return out;
+    });
+}
+
+// (logits, tokens, uniforms, parents or None, draft or None, temperatures or None): (path, counts, next)
+PyObject *py_seq_verify(PyObject *, PyObject *const *a, Py_ssize_t count) {
+    Tensor logits, tokens, uniforms, parents, draft, temperatures;
+    if (count != 6 || !plain_modes() || !tensor_arg(a[0], logits) || !tensor_arg(a[1], tokens) || !tensor_arg(a[2], uniforms) || !tensor_arg(a[3], parents, true) || !tensor_arg(a[4], draft, true) ||
+        !tensor_arg(a[5], temperatures, true))
+        Py_RETURN_NONE;
+    return guarded<variable_list>([&]() -> variable_list {
+        if (!plain(logits) || logits.dim() != 3 || !small(logits.sizes())) return {};
+        const int64_t B = logits.size(0), n = logits.size(1), V = logits.size(2);
+        const auto code = dtype_code(logits.scalar_type());
+        const bool drafted = draft.defined();
+        if (!code || !constant(tokens, logits, at::kInt, {B, n}) || !constant(parents, logits, at::kInt, {B, n}) || !constant(uniforms, logits, at::kFloat, {B, drafted ? n + 1 : n}) ||
+            !constant(temperatures, logits, at::kFloat, {B}) || (drafted && (parents.defined() || !matches(draft, logits, {B, n - 1, V}))))
+            return {};
+        const at::AutoGradMode off(false);
+        const c10::DeviceGuard device(logits.device());
+        const auto dense = [](const Tensor &t) { return t.size(2) == 1 || t.stride(2) == 1 ? t : t.contiguous(); };
+        const Tensor l = dense(logits), d = drafted ? dense(draft) : draft;
+        seq_verify_problem p{};
+        p.B = (int32_t)B, p.n = (int32_t)n, p.V = (int32_t)V, p.dtype = *code, p.drafted = drafted;
+        const auto stride = [](const Tensor &t, int i) { return t.size(i) <= 1 ? 0 : t.stride(i); };
+        p.batch = stride(l, 0), p.row = stride(l, 1);
+        if (drafted) p.draft_batch = stride(d, 0), p.draft_row = stride(d, 1);
+        const auto options = logits.options().dtype(at::kInt);
+        const variable_list out{at::empty({B, n}, options), at::empty({B}, options), at::empty({B}, options)};
+        const Tensor ws = scratch(seq_verify_workspace_bytes(&p), logits);
+        forward_check(seq_verify(&p, ptr(l), drafted && n > 1 ? ptr(d) : nullptr, (const int32_t *)ptr(tokens), (const int32_t *)ptr(parents), (const float *)ptr(uniforms), (const float *)ptr(temperatures),
+                                 (int32_t *)ptr(out[0]), (int32_t *)ptr(out[1]), (int32_t *)ptr(out[2]), ptr(ws), size_of(ws), stream()));
+        return out;
+    });
+}
+
 PyMethodDef methods[] = {{"na2d", (PyCFunction)(void (*)(void))py_na2d, METH_FASTCALL, nullptr},
                          {"na1d", (PyCFunction)(void (*)(void))py_na1d, METH_FASTCALL, nullptr},
                          {"na2d_unfused", (PyCFunction)(void (*)(void))py_na2d_unfused, METH_FASTCALL, nullptr},
@@ -893,6 +951,8 @@ PyMethodDef methods[] = {{"na2d", (PyCFunction)(void (*)(void))py_na2d, METH_FAS
                          {"seq_rotary", (PyCFunction)(void (*)(void))py_seq_rotary, METH_FASTCALL, nullptr},
                          {"seq_cache_gather", (PyCFunction)(void (*)(void))py_seq_cache_gather, METH_FASTCALL, nullptr},
                          {"seq_cache_attention", (PyCFunction)(void (*)(void))py_seq_cache_attention, METH_FASTCALL, nullptr},
+                         {"seq_cache_tree_attention", (PyCFunction)(void (*)(void))py_seq_cache_tree_attention, METH_FASTCALL, nullptr},
+                         {"seq_verify", (PyCFunction)(void (*)(void))py_seq_verify, METH_FASTCALL, nullptr},
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "na2d_torch", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

@@ -4,6 +4,7 @@
 #include <initializer_list>
 
 #include "seq_cache.hpp"
+#include "seq_verify.hpp"
 
 namespace seq {
 namespace {
@@ -156,6 +157,46 @@ CacheArgs cache_args(const seq_cache_problem *p) {
     plan_cache_attention(a, (int64_t)p->table_width * p->page);
     return a;
 }
+// attention of a tree: the nodes' own keys and values beside the call's
+int tree_validate(const seq_cache_problem *p, const seq_strides *k, const seq_strides *v) {
+    if (int e = cache_validate(p, SEQ_CACHE_ATTENTION)) return e;
+    if (p->n > 64) return NA2D_ERR_SHAPE;
+    if (!k != !v) return NA2D_ERR_NULL;
+    for (const seq_strides *s : {k, v})
+        if (s)
+            if (int r = check_strides(*s, p->B, p->kv_heads, p->n, p->D, elem(p->dtype), false)) return r;
+    return NA2D_OK;
+}
+CacheArgs tree_args(const seq_cache_problem *p) {
+    CacheArgs a = cache_args(p);
+    if (!p->window) a.window = INT32_MAX;   // (nodes stand as far as a length says, whatever the table holds)
+    plan_cache_tree(a, (int64_t)p->table_width * p->page);
+    return a;
+}
+
+int verify_validate(const seq_verify_problem *p) {
+    if (!p) return NA2D_ERR_NULL;
+    if (p->dtype != NA2D_F32 && p->dtype != NA2D_F16 && p->dtype != NA2D_BF16) return NA2D_ERR_DTYPE;
+    if (p->B <= 0 || p->B > 1 << 24 || p->n <= 0 || p->n > 64 || p->V <= 0 || p->V > 1 << 24 || (p->drafted != 0 && p->drafted != 1)) return NA2D_ERR_SHAPE;
+    for (int64_t s : {p->batch, p->row, p->draft_batch, p->draft_row})
+        if (s < 0 || s > (int64_t)1 << 45) return NA2D_ERR_SHAPE;
+    if ((double)(p->B - 1) * p->batch > 0x1p58 || (double)(p->B - 1) * p->draft_batch > 0x1p58) return NA2D_ERR_SHAPE;
+    VerifyArgs a{};
+    a.B = p->B, a.n = p->n, a.V = p->V, a.drafted = p->drafted;
+    plan_verify(a, p->dtype);
+    return launch_holds((int64_t)p->B * (2 * p->n) * a.parts, kThreads) ? NA2D_OK : NA2D_ERR_SHAPE;
+}
+VerifyArgs verify_args(const seq_verify_problem *p) {
+    VerifyArgs a{};
+    const int e = elem(p->dtype);
+    a.B = p->B, a.n = p->n, a.V = p->V, a.drafted = p->drafted;
+    a.batch = p->batch * e, a.row = p->row * e, a.draft_batch = p->draft_batch * e, a.draft_row = p->draft_row * e;
+    plan_verify(a, p->dtype);
+    return a;
+}
+// stats, then the tokens drawn or the parts' rests
+int64_t verify_stats_bytes(const VerifyArgs &a) { return (int64_t)sizeof(PartStats) * a.B * (a.drafted ? 2 * a.n - 1 : a.n) * a.parts; }
+
 bool odd4(std::initializer_list<const void *> ps) {
     for (const void *p : ps)
         if (reinterpret_cast<uintptr_t>(p) & 3u) return true;
@@ -427,6 +468,60 @@ int seq_cache_attention(const seq_cache_problem *p, const void *q, const int8_t 
     a.ks = const_cast<float *>(k_scales), a.vs = const_cast<float *>(v_scales), a.table = table, a.lengths = lengths, a.slopes = slopes;
     a.part = static_cast<float *>(workspace);
     return from_hip(launch_cache_attention(a, p->dtype, p->D, cap_form(NA2D_F16, p->softcap), static_cast<hipStream_t>(stream)));
+}
+
+size_t seq_cache_tree_attention_workspace_bytes(const seq_cache_problem *p) {
+    return tree_validate(p, nullptr, nullptr) == NA2D_OK ? cache_tree_bytes(tree_args(p), p->D) : 0;
+}
+
+int seq_cache_tree_attention(const seq_cache_problem *p, const seq_strides *k_strides, const seq_strides *v_strides, const void *q, const void *k, const void *v, const int32_t *parents,
+                             const int8_t *k_pages, const int8_t *v_pages, const float *k_scales, const float *v_scales, const int32_t *table, const int32_t *lengths, const float *slopes,
+                             void *out, void *workspace, size_t workspace_bytes, void *stream) {
+    if (int e = tree_validate(p, k_strides, v_strides)) return e;
+    SEQ_REQUIRE(q); SEQ_REQUIRE(k); SEQ_REQUIRE(v); SEQ_REQUIRE(out); SEQ_REQUIRE(k_pages); SEQ_REQUIRE(v_pages);
+    if (!k_strides || !parents || !table || !lengths || !k_scales || !v_scales) return NA2D_ERR_NULL;
+    if (odd4({parents, table, lengths, slopes, k_scales, v_scales})) return NA2D_ERR_ALIGN;
+    if (out == q || out == k || out == v) return NA2D_ERR_ALIAS;
+    CacheArgs a = tree_args(p);
+    if (!workspace || misaligned(workspace) || workspace_bytes < cache_tree_bytes(a, p->D)) return NA2D_ERR_WORKSPACE;
+    const int e = elem(p->dtype);
+    a.a = view(q, p->q, e), a.b = view(out, p->out, e), a.tk = view(k, *k_strides, e), a.tv = view(v, *v_strides, e), a.parents = parents;
+    a.k = const_cast<int8_t *>(k_pages), a.v = const_cast<int8_t *>(v_pages), a.ks = const_cast<float *>(k_scales), a.vs = const_cast<float *>(v_scales);
+    a.table = table, a.lengths = lengths, a.slopes = slopes;
+    a.part = static_cast<float *>(workspace);
+    return from_hip(launch_cache_tree(a, p->dtype, p->D, cap_form(NA2D_F16, p->softcap), static_cast<hipStream_t>(stream)));
+}
+
+int seq_verify_validate(const seq_verify_problem *p) { return verify_validate(p); }
+
+size_t seq_verify_workspace_bytes(const seq_verify_problem *p) {
+    if (verify_validate(p) != NA2D_OK) return 0;
+    const VerifyArgs a = verify_args(p);
+    return (size_t)(verify_stats_bytes(a) + (p->drafted ? (int64_t)sizeof(double) * a.B * a.parts : (int64_t)sizeof(int) * a.B * a.n));
+}
+
+int seq_verify(const seq_verify_problem *p, const void *logits, const void *draft, const int32_t *tokens, const int32_t *parents, const float *uniforms, const float *temperatures,
+               int32_t *path, int32_t *counts, int32_t *next, void *workspace, size_t workspace_bytes, void *stream) {
+    if (int e = verify_validate(p)) return e;
+    if (!logits || !tokens || !uniforms || !path || !counts || !next || (p->drafted && p->n > 1 && !draft)) return NA2D_ERR_NULL;
+    if (p->drafted ? parents != nullptr : draft != nullptr) return NA2D_ERR_SHAPE;
+    const uintptr_t element = (uintptr_t)elem(p->dtype) - 1;
+    if (((uintptr_t)logits | (uintptr_t)draft) & element || odd4({tokens, parents, uniforms, temperatures, path, counts, next})) return NA2D_ERR_ALIGN;
+    const int32_t *outs[] = {path, counts, next};
+    for (int i = 0; i < 3; ++i) {
+        for (const void *x : {logits, draft, (const void *)tokens, (const void *)parents, (const void *)uniforms, (const void *)temperatures})
+            if ((const void *)outs[i] == x) return NA2D_ERR_ALIAS;
+        for (int j = 0; j < i; ++j)
+            if (outs[i] == outs[j]) return NA2D_ERR_ALIAS;
+    }
+    if (!workspace || misaligned(workspace) || workspace_bytes < seq_verify_workspace_bytes(p)) return NA2D_ERR_WORKSPACE;
+    VerifyArgs a = verify_args(p);
+    a.logits = static_cast<const char *>(logits), a.draft = static_cast<const char *>(draft), a.tokens = tokens, a.parents = parents, a.uniforms = uniforms, a.temperatures = temperatures;
+    a.path = path, a.counts = counts, a.next = next;
+    a.stats = static_cast<PartStats *>(workspace);
+    char *behind = static_cast<char *>(workspace) + verify_stats_bytes(a);
+    a.drawn = reinterpret_cast<int *>(behind), a.rest = reinterpret_cast<double *>(behind);
+    return from_hip(launch_verify(a, p->dtype, static_cast<hipStream_t>(stream)));
 }
 
 }  // extern "C"

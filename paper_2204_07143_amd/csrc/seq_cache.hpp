@@ -6,6 +6,8 @@
 namespace seq {
 
 struct CacheArgs {
+    View tk, tv;           // a tree of nodes: their own keys and values,
+    const int *parents;    // [B, n]
     View a, b;             // append: new keys and values; gather: keys and values read; attention: q and out
     int8_t *k, *v;
     float *ks, *vs;
@@ -34,6 +36,9 @@ struct RowsArgs {
 hipError_t launch_append_rows(const RowsArgs &a, int dtype, int D, hipStream_t st);
 hipError_t launch_gather(const CacheArgs &a, int dtype, int D, hipStream_t st);
 hipError_t launch_cache_attention(const CacheArgs &a, int dtype, int D, int cap, hipStream_t st);   // cap: the CapForm of fp16 weights, whatever the type of q
+hipError_t launch_cache_tree(const CacheArgs &a, int dtype, int D, int cap, hipStream_t st);
+void plan_cache_tree(CacheArgs &a, int64_t longest);
+size_t cache_tree_bytes(const CacheArgs &a, int D);
 void plan_cache_attention(CacheArgs &a, int64_t longest);   // splits, row_groups
 size_t cache_attention_bytes(const CacheArgs &a, int D);
 

@@ -1,0 +1,40 @@
+// Attention of a tree of drafted tokens over a cache in 8 bits: rows as in seq_decode.hpp, their last part being the nodes' own keys and values.
+#include "seq_decode.hpp"
+
+namespace seq {
+
+namespace {
+
+template <typename T, int D, int CAP> struct TreeAttention {
+    static hipError_t go(const CacheArgs &a, hipStream_t st) {
+        const int64_t blocks = (int64_t)a.B * a.kv * a.row_groups * a.splits;
+        if (!launch_holds(blocks, kThreads)) return hipErrorInvalidValue;
+        const bool wide = rows_each(a) > 16, page16 = a.page_log2 == 4;
+        auto *kernel = wide ? page16 ? decode_kernel<T, D, 2, CAP, true, true> : decode_kernel<T, D, 2, CAP, false, true>
+                            : page16 ? decode_kernel<T, D, 1, CAP, true, true> : decode_kernel<T, D, 1, CAP, false, true>;
+        kernel<<<(unsigned)blocks, kThreads, 0, st>>>(a);
+        if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
+        const int64_t rows = (int64_t)a.B * a.heads * a.n;
+        if (!launch_holds(rows, kThreads)) return hipErrorInvalidValue;
+        join_kernel<T, D><<<(unsigned)rows, kThreads, 0, st>>>(a, rows_each(a));
+        return hipGetLastError();
+    }
+};
+
+}  // namespace
+
+void plan_cache_tree(CacheArgs &a, int64_t longest) {
+    plan_cache_attention(a, longest);
+    a.splits += 1;   // the nodes' own part
+}
+size_t cache_tree_bytes(const CacheArgs &a, int D) { return (size_t)a.B * a.kv * a.row_groups * a.splits * rows_each(a) * (D + 2) * sizeof(float); }
+
+hipError_t launch_cache_tree(const CacheArgs &a, int dtype, int D, int cap, hipStream_t st) {
+#define SEQ_D(T, N) (cap == kNoCap ? TreeAttention<T, N, kNoCap>::go(a, st) : cap == kSigmoidCap ? TreeAttention<T, N, kSigmoidCap>::go(a, st) : TreeAttention<T, N, kTanhCap>::go(a, st))
+#define SEQ_T(T) (D == 32 ? SEQ_D(T, 32) : D == 64 ? SEQ_D(T, 64) : SEQ_D(T, 128))
+    return dtype == NA2D_F16 ? SEQ_T(f16_t) : SEQ_T(bf16_t);
+#undef SEQ_T
+#undef SEQ_D
+}
+
+}  // namespace seq

@@ -1,0 +1,29 @@
+// Verification of drafted tokens: what its kernels take.
+#pragma once
+
+#include "seq_common.hpp"
+
+namespace seq {
+
+struct PartStats {   // of a part of a row: its largest logit (-inf: none), where that is first (rows taken at their largest), the sum of its weights beside that one's
+    double sum;
+    float most;
+    int at;
+};
+
+struct VerifyArgs {
+    const char *logits, *draft;
+    int64_t batch, row, draft_batch, draft_row;   // bytes
+    const int *tokens, *parents;
+    const float *uniforms, *temperatures;
+    int *path, *counts, *next;
+    PartStats *stats;      // [B * n, parts], then of the draft [B * (n - 1), parts]
+    int *drawn;            // the token drawn at every node, [B, n]
+    double *rest;          // of the row that a line ends at: each part's sum of max(p - q, 0), [B, parts]
+    int B, n, V, drafted, parts, unroll;
+};
+
+void plan_verify(VerifyArgs &a, int dtype);   // parts, unroll
+hipError_t launch_verify(const VerifyArgs &a, int dtype, hipStream_t st);
+
+}  // namespace seq

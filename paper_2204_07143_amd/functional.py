@@ -505,3 +505,55 @@ def seq_cache_attention(q, cache: SeqCache, table, lengths, *, window: int | Non
             return out
         p = na.seq_cache_problem(q, cache.k_pages, table, heads=q.shape[1], out=out, **settings)
         return na.seq_cache_attention(q, *cache, table, lengths, slopes, out, _scratch(na.seq_cache_attention_workspace_bytes(p), q), **settings)
+
+
+def seq_cache_tree_attention(q, k, v, parents, cache: SeqCache, table, lengths, *, window: int | None = None, softcap: float | None = None, slopes=None, scale: float | None = None):
+    """Attention of a tree of drafted tokens, its nodes (64 at most), over each sequence's cache, which does not hold them: ``q`` [B, heads, n, D] in f16 or bf16, ``k`` and
+    ``v`` [B, kv_heads, n, D] the nodes' own.
+
+    ``parents`` (int32 [B, n]): a node before it, or -1 for what follows the cache's last token; any other number is no node (padding), nor is what descends from it: its
+    values may be anything, and its row of the result is 0.  A node stands at position ``lengths[b]`` plus its depth, and sees the cache, its ancestors and itself, within
+    the window.  Otherwise as ``seq_cache_attention``.  Not differentiable."""
+    out = _native().seq_cache_tree_attention(q, *cache, table, lengths, k, v, parents, window, softcap, slopes, scale)
+    if out is not None:
+        return out
+    _heads_of(q, k, v)
+    settings = _settings(q, window, softcap, scale, slopes)
+    with torch.no_grad():
+        q, k, v = _rows(q), _rows(k), _rows(v)
+        out = _like(q)
+        if q.numel() == 0:
+            return out
+        p = na.seq_cache_problem(q, cache.k_pages, table, heads=q.shape[1], out=out, **settings)
+        return na.seq_cache_tree_attention(q, k, v, parents, *cache, table, lengths, slopes, out, _scratch(na.seq_cache_tree_attention_workspace_bytes(p), q), **settings)
+
+
+def _logits(t: torch.Tensor) -> torch.Tensor:
+    t = t.resolve_neg()
+    return t if t.shape[-1] == 1 or t.stride(-1) == 1 else t.contiguous()
+
+
+def seq_verify(logits, tokens, uniforms, *, parents=None, draft=None, temperatures=None):
+    """Which drafted tokens the target's probabilities accept, and the token behind them: ``(path, counts, next)``, int32 [B, n], [B] and [B].
+
+    ``tokens`` (int32 [B, n]): node 0 is the token that a sequence's draft follows, the others (63 at most) are drafted.  ``logits`` [B, n, V]: the target's behind each node, f32, f16 or
+    bf16; p is their softmax over ``temperatures`` (fp32 [B]; None: 1; 0: the largest logit, at its lowest index).  ``path`` holds the accepted nodes from node 0 on, then
+    -1; ``counts`` how many; with both, ``seq_cache_append`` (``rows``, ``counts``) keeps their keys and values.
+
+    Without ``draft``: at a node a token is drawn from p by its number in ``uniforms`` (fp32 [B, n], each in [0, 1)); the walk goes on at the child that has it, and ends with this
+    token where none does.  ``parents`` (int32 [B, n]) as in ``seq_cache_tree_attention``; None: a line.
+    With ``draft`` [B, n - 1, V], the logits that tokens 1 .. n - 1 of a line were drawn from: node i + 1 is accepted while ``uniforms[b, i] * q(x) < p(x)``; the first that is not is
+    replaced by a draw from max(p - q, 0), and behind the last (or before a token outside [0, V)) one is drawn from p, by ``uniforms[b, n]`` (fp32 [B, n + 1]).
+    Either way the tokens are distributed as the target alone would have them.  All of it is in 64 bits."""
+    out = _native().seq_verify(logits, tokens, uniforms, parents, draft, temperatures)
+    if out is not None:
+        return out
+    if draft is not None and parents is not None:
+        raise ValueError("a draft's logits belong to a line of tokens: no parents are expected")
+    with torch.no_grad():
+        logits, draft = _logits(logits), None if draft is None else _logits(draft)
+        p = na.seq_verify_problem(logits, draft)
+        outs = (torch.empty(logits.shape[:2], dtype=torch.int32, device=logits.device), *(torch.empty(logits.shape[:1], dtype=torch.int32, device=logits.device) for _ in range(2)))
+        if logits.shape[0] == 0:
+            return outs
+        return na.seq_verify(logits, draft, tokens, parents, uniforms, temperatures, *outs, _scratch(na.seq_verify_workspace_bytes(p), logits))
