@@ -171,7 +171,7 @@ size_t seq_cache_tree_attention_workspace_bytes(const seq_cache_problem *p);
 
 /* Which drafted tokens a target accepts, and the token behind them.  tokens: int32 [B, n]; node 0 of a sequence is the token that its draft follows, the others are drafted.
  * logits: [B, n, V], the target's behind each node; rows' elements contiguous.  Of a row, p = softmax(logits / T), T = temperatures[b] (fp32 [B]; NULL: 1); T not above 0: all on the
- * largest logit, at its lowest index.  A logit of -infinity, or a NaN, is a token that is not chosen; an infinite one counts as the largest finite fp32 value.
+ * largest logit, at its lowest index.  A logit of -infinity, or a NaN, is a token that is not chosen; an infinite one counts as the type's largest finite value.
  * A token is drawn from weights w by a number u: the lowest t with w_0 + .. + w_t > u (w_0 + .. + w_V-1), w_t > 0.  Everything from the logits on is in 64 bits.
  *
  * drafted 0: parents, int32 [B, n], makes the nodes a tree as seq_cache_tree_attention has it (NULL: a line).  At a node i a token is drawn from p_i by

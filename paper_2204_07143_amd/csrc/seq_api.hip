@@ -194,8 +194,15 @@ VerifyArgs verify_args(const seq_verify_problem *p) {
     plan_verify(a, p->dtype);
     return a;
 }
-// stats, then the tokens drawn or the parts' rests
-int64_t verify_stats_bytes(const VerifyArgs &a) { return (int64_t)sizeof(PartStats) * a.B * (a.drafted ? 2 * a.n - 1 : a.n) * a.parts; }
+// The workspace: the parts' statistics, then the parts' rests or the tokens drawn, then tickets.
+struct VerifySpace {
+    int64_t behind, tickets, bytes;
+    VerifySpace(const VerifyArgs &a) {
+        behind = (int64_t)sizeof(PartStats) * a.B * (a.drafted ? 2 * a.n - 1 : a.n) * a.parts;
+        tickets = behind + (a.drafted ? (int64_t)sizeof(double) * a.B * a.parts : (int64_t)sizeof(int) * a.B * a.n);
+        bytes = tickets + (int64_t)sizeof(int) * a.B * (a.drafted ? 1 : a.n + 1);
+    }
+};
 
 bool odd4(std::initializer_list<const void *> ps) {
     for (const void *p : ps)
@@ -496,8 +503,7 @@ int seq_verify_validate(const seq_verify_problem *p) { return verify_validate(p)
 
 size_t seq_verify_workspace_bytes(const seq_verify_problem *p) {
     if (verify_validate(p) != NA2D_OK) return 0;
-    const VerifyArgs a = verify_args(p);
-    return (size_t)(verify_stats_bytes(a) + (p->drafted ? (int64_t)sizeof(double) * a.B * a.parts : (int64_t)sizeof(int) * a.B * a.n));
+    return (size_t)VerifySpace(verify_args(p)).bytes;
 }
 
 int seq_verify(const seq_verify_problem *p, const void *logits, const void *draft, const int32_t *tokens, const int32_t *parents, const float *uniforms, const float *temperatures,
@@ -519,8 +525,9 @@ int seq_verify(const seq_verify_problem *p, const void *logits, const void *draf
     a.logits = static_cast<const char *>(logits), a.draft = static_cast<const char *>(draft), a.tokens = tokens, a.parents = parents, a.uniforms = uniforms, a.temperatures = temperatures;
     a.path = path, a.counts = counts, a.next = next;
     a.stats = static_cast<PartStats *>(workspace);
-    char *behind = static_cast<char *>(workspace) + verify_stats_bytes(a);
-    a.drawn = reinterpret_cast<int *>(behind), a.rest = reinterpret_cast<double *>(behind);
+    const VerifySpace space(a);
+    char *ws = static_cast<char *>(workspace);
+    a.drawn = reinterpret_cast<int *>(ws + space.behind), a.rest = reinterpret_cast<double *>(ws + space.behind), a.tickets = reinterpret_cast<int *>(ws + space.tickets);
     return from_hip(launch_verify(a, p->dtype, static_cast<hipStream_t>(stream)));
 }
 

@@ -18,12 +18,13 @@ struct VerifyArgs {
     const float *uniforms, *temperatures;
     int *path, *counts, *next;
     PartStats *stats;      // [B * n, parts], then of the draft [B * (n - 1), parts]
-    int *drawn;            // the token drawn at every node, [B, n]
-    double *rest;          // of the row that a line ends at: each part's sum of max(p - q, 0), [B, parts]
-    int B, n, V, drafted, parts, unroll;
+    double *rest;          // line: each part's sum of what the next token is drawn from, [B, parts]
+    int *drawn;            // tree: the token drawn at every node, [B, n]
+    int *tickets;          // workgroups that are done: tree [B, n] of rows, [B] of sequences; line [B]
+    int B, n, V, drafted, parts, blocks;   // blocks: of a part
 };
 
-void plan_verify(VerifyArgs &a, int dtype);   // parts, unroll
+void plan_verify(VerifyArgs &a, int dtype);   // parts, blocks
 hipError_t launch_verify(const VerifyArgs &a, int dtype, hipStream_t st);
 
 }  // namespace seq
