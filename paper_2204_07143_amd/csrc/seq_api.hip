@@ -170,7 +170,8 @@ int tree_validate(const seq_cache_problem *p, const seq_strides *k, const seq_st
 CacheArgs tree_args(const seq_cache_problem *p) {
     CacheArgs a = cache_args(p);
     if (!p->window) a.window = INT32_MAX;   // (nodes stand as far as a length says, whatever the table holds)
-    plan_cache_tree(a, (int64_t)p->table_width * p->page);
+    a.tanh = cap_form(NA2D_F16, p->softcap) == kTanhCap;
+    plan_cache_tree(a, (int64_t)p->table_width * p->page, p->D);
     return a;
 }
 

@@ -8,6 +8,7 @@ namespace seq {
 struct CacheArgs {
     View tk, tv;           // a tree of nodes: their own keys and values,
     const int *parents;    // [B, n]
+    bool tanh;             // scores are capped by the library's tanh
     View a, b;             // append: new keys and values; gather: keys and values read; attention: q and out
     int8_t *k, *v;
     float *ks, *vs;
@@ -37,8 +38,13 @@ hipError_t launch_append_rows(const RowsArgs &a, int dtype, int D, hipStream_t s
 hipError_t launch_gather(const CacheArgs &a, int dtype, int D, hipStream_t st);
 hipError_t launch_cache_attention(const CacheArgs &a, int dtype, int D, int cap, hipStream_t st);   // cap: the CapForm of fp16 weights, whatever the type of q
 hipError_t launch_cache_tree(const CacheArgs &a, int dtype, int D, int cap, hipStream_t st);
-void plan_cache_tree(CacheArgs &a, int64_t longest);
+void plan_cache_tree(CacheArgs &a, int64_t longest, int D);
 size_t cache_tree_bytes(const CacheArgs &a, int D);
+// the same where a key head has many rows (seq_tree_tile.hip)
+int tree_row_blocks(const CacheArgs &a, int D);
+void plan_tree_tiles(CacheArgs &a, int64_t longest, int D);
+size_t tree_tile_bytes(const CacheArgs &a, int D);
+hipError_t launch_tree_tiles(const CacheArgs &a, int dtype, int D, int cap, hipStream_t st);
 void plan_cache_attention(CacheArgs &a, int64_t longest);   // splits, row_groups
 size_t cache_attention_bytes(const CacheArgs &a, int D);
 

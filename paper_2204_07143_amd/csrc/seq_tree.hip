@@ -21,15 +21,23 @@ template <typename T, int D, int CAP> struct TreeAttention {
     }
 };
 
+// Up to 32 rows to a key head here, more in tiles of 64 tokens (seq_tree_tile.hip).
+bool tiled(const CacheArgs &a) { return a.group * a.n > 32; }
+
 }  // namespace
 
-void plan_cache_tree(CacheArgs &a, int64_t longest) {
+void plan_cache_tree(CacheArgs &a, int64_t longest, int D) {
+    if (tiled(a)) return plan_tree_tiles(a, longest, D);
     plan_cache_attention(a, longest);
     a.splits += 1;   // the nodes' own part
 }
-size_t cache_tree_bytes(const CacheArgs &a, int D) { return (size_t)a.B * a.kv * a.row_groups * a.splits * rows_each(a) * (D + 2) * sizeof(float); }
+size_t cache_tree_bytes(const CacheArgs &a, int D) {
+    if (tiled(a)) return tree_tile_bytes(a, D);
+    return (size_t)a.B * a.kv * a.row_groups * a.splits * rows_each(a) * (D + 2) * sizeof(float);
+}
 
 hipError_t launch_cache_tree(const CacheArgs &a, int dtype, int D, int cap, hipStream_t st) {
+    if (tiled(a)) return launch_tree_tiles(a, dtype, D, cap, st);
 #define SEQ_D(T, N) (cap == kNoCap ? TreeAttention<T, N, kNoCap>::go(a, st) : cap == kSigmoidCap ? TreeAttention<T, N, kSigmoidCap>::go(a, st) : TreeAttention<T, N, kTanhCap>::go(a, st))
 #define SEQ_T(T) (D == 32 ? SEQ_D(T, 32) : D == 64 ? SEQ_D(T, 64) : SEQ_D(T, 128))
     return dtype == NA2D_F16 ? SEQ_T(f16_t) : SEQ_T(bf16_t);

@@ -407,11 +407,11 @@ template <typename T> struct Rest {
     }
 };
 
-// Line: a workgroup to a part of what the next token is drawn from.  Each finds for itself where the line ends, 16 lanes to a row; then the parts' sums; a sequence's last
+// Line: a workgroup to a part of what the next token is drawn from.  Each finds for itself where the line ends, LANES lanes to a row; then the parts' sums; a sequence's last
 // workgroup draws.
-template <typename T, int U>
+template <typename T, int U, int LANES>
 __global__ __launch_bounds__(kThreads) void line_kernel(const VerifyArgs p) {
-    constexpr int E = Row<T>::E, LANES = 16;
+    constexpr int E = Row<T>::E;
     __shared__ uint64_t roots[32];
     __shared__ double sums[kWaves], drawn[3], over[64], over_d[64];
     __shared__ float most[64], most_d[64];
@@ -426,13 +426,14 @@ __global__ __launch_bounds__(kThreads) void line_kernel(const VerifyArgs p) {
         const bool last_row = i == p.n - 1;
         const int x = last_row ? -1 : p.tokens[(int64_t)b * p.n + i + 1];
         const bool token = (unsigned)x < (unsigned)p.V;
+        const double u = number(p.uniforms[(int64_t)b * (p.n + 1) + i]);
         const float xp = token ? Row<T>(p.logits + b * p.batch + i * p.row, p.V).at(x) : -INFINITY, xq = token ? Row<T>(p.draft + b * p.draft_batch + j * p.draft_row, p.V).at(x) : -INFINITY;
         const RowStats<LANES, false> s(target + (int64_t)i * p.parts, p.parts, t, tid % LANES), q(draft + (int64_t)j * p.parts, last_row ? 0 : p.parts, t, tid % LANES);
         if (tid % LANES == 0) {
             const double os = s.sum > 0.0 ? 1.0 / s.sum : 0.0, oq = q.sum > 0.0 ? 1.0 / q.sum : 0.0;
             most[i] = s.most, most_d[i] = q.most, over[i] = os, over_d[i] = oq, at[i] = s.at;
             const double px = s.sum > 0.0 ? t.weight(xp, s.most) * os : 0.0, qx = q.sum > 0.0 ? t.weight(xq, q.most) * oq : 0.0;
-            taken[i] = !token ? -1 : t.greedy ? x == s.at : number(p.uniforms[(int64_t)b * (p.n + 1) + i]) * qx < px;
+            taken[i] = !token ? -1 : t.greedy ? x == s.at : u * qx < px;
         }
     }
     workgroup_sync();
@@ -465,13 +466,14 @@ __global__ __launch_bounds__(kThreads) void line_kernel(const VerifyArgs p) {
     if (tid == 0) leave(parts + part, (sums[0] + sums[1]) + (sums[2] + sums[3]));
     if (!last_of(p.tickets + b, p.parts)) return;
     if (tid < kWave) {
-        double all = 0.0, before;
-        for (int k = lane; k < p.parts; k += kWave) all += take(parts + k);
+        const double mine = lane < p.parts ? take(parts + lane) : 0.0;
+        double all = mine, before;
+        for (int k = lane + kWave; k < p.parts; k += kWave) all += take(parts + k);
         all = wave_sum(all);
         const bool left = all > 0.0;   // else p and q are one
         const PartStats *stats = target + (int64_t)last * p.parts;
         const double to = number(p.uniforms[(int64_t)b * (p.n + 1) + p.n]) * (left ? all : rest.over > 0.0 ? 1.0 : 0.0);
-        const int k = find_part([&](int k) { return left ? take(parts + k) : rest.over > 0.0 ? stats[k].sum * t.weight(stats[k].most, rest.most) * rest.over : 0.0; }, p.parts, to, lane, before);
+        const int k = find_part([&](int k) { return left ? k == lane ? mine : take(parts + k) : rest.over > 0.0 ? stats[k].sum * t.weight(stats[k].most, rest.most) * rest.over : 0.0; }, p.parts, to, lane, before);
         if (lane == 0) found = k, drawn[0] = before, drawn[1] = to, drawn[2] = left ? rest.over_d : 0.0;
     }
     workgroup_sync();
@@ -485,7 +487,8 @@ template <typename T, int U> hipError_t verify(const VerifyArgs &a, hipStream_t 
     if (a.drafted) {
         stats_kernel<T, U><<<(unsigned)((int64_t)a.B * (2 * a.n - 1) * groups), kThreads, 0, st>>>(a);
         if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
-        line_kernel<T, U><<<(unsigned)(a.B * a.parts), kThreads, 0, st>>>(a);
+        auto *kernel = a.n <= 4 ? line_kernel<T, U, 64> : a.n <= 8 ? line_kernel<T, U, 32> : line_kernel<T, U, 16>;   // all rows at once, up to 16
+        kernel<<<(unsigned)(a.B * a.parts), kThreads, 0, st>>>(a);
     } else {
         const int tickets = a.B * (a.n + 1);
         tickets_kernel<<<(tickets + kThreads - 1) / kThreads, kThreads, 0, st>>>(a.tickets, tickets);

@@ -88,6 +88,35 @@ def test_windows_and_long_ranges(window, page, n, heads):
 
 
 @pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("D,page", [(32, 64), (64, 16), (128, 32), (128, 128)])
+@pytest.mark.parametrize("n,heads", [(31, 6), (12, 8), (33, 1), (64, 3), (64, 9)])   # 186, 96, 33, 192 and 576 rows
+@pytest.mark.parametrize("cap,window", [(None, None), (5.0, None), (1500.0, None), (None, 70), (5.0, 300)])
+def test_many_rows_to_a_key_head(dtype, D, page, n, heads, cap, window):
+    g = np.random.default_rng(n + heads + D)
+    lengths = [700, 64, 0, 129]
+    table, pages = _table(g, lengths, page)
+    host, cache = _cache(g, pages, 1, page, D)
+    q, k, v = _inputs(g, 4, heads, 1, n, D, dtype)
+    parents = _parents(g, 4, n)
+    slopes = torch.from_numpy(g.uniform(0, 0.1, heads).astype(np.float32)).cuda() if window == 300 else None
+    scale = -0.1 if window == 70 else None   # a scale may be negative
+    got = F.seq_cache_tree_attention(q, k, v, _int(parents.tolist()), cache, _int(table.tolist()), _int(lengths), softcap=cap, window=window, slopes=slopes, scale=scale)
+    _check(got, q, k, v, parents, host, table, lengths, dtype, softcap=cap, window=window, slopes=None if slopes is None else f64(slopes), scale=scale)
+
+
+def test_many_short_sequences():
+    """More sequences than a wave has lanes, some of nothing: runs that hold several rows' work, and rows that several runs hold."""
+    g = np.random.default_rng(13)
+    lengths = [int(x) for x in g.integers(0, 300, 150)]
+    table, pages = _table(g, lengths, 16)
+    host, cache = _cache(g, pages, 2, 16, 32)
+    q, k, v = _inputs(g, 150, 6, 2, 20, 32, "f16")
+    parents = _parents(g, 150, 20)
+    got = F.seq_cache_tree_attention(q, k, v, _int(parents.tolist()), cache, _int(table.tolist()), _int(lengths))
+    _check(got, q, k, v, parents, host, table, lengths, "f16")
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
 @pytest.mark.parametrize("n", [5, 40])
 def test_what_is_no_node_may_be_anything(dtype, n):
     g = np.random.default_rng(1)
