@@ -250,21 +250,17 @@ int rotary_validate(const seq_rotary_problem *p, bool backward) {
     for (const auto &x : all)
         if (x.heads && (backward || !x.backward))
             if (int r = check_strides(x.s, p->B, x.heads, p->L, p->D, e, x.written)) return r;
-    // every launch holds its workgroups: a wave has at least one token's four heads
-    for (int heads : {p->heads, p->kv_heads})
-        if (!launch_holds(((int64_t)p->B * p->L * ((heads + 3) / 4) + kWaves - 1) / kWaves + 1, kThreads)) return NA2D_ERR_SHAPE;
     return NA2D_OK;
 }
-// of the queries (side 0) or the keys
-RotaryArgs rotary_args(const seq_rotary_problem *p, int side, const int32_t *positions, const float *freqs, const void *weight) {
+RotaryArgs rotary_args(const seq_rotary_problem *p, const int32_t *positions, const float *freqs, bool backward) {
     RotaryArgs a{};
-    a.r = rotation(p->rotation, positions, p->shared ? 0 : (int64_t)p->rotation.axes * p->L, freqs, weight);
-    a.tokens = (int64_t)p->B * p->L, a.L = p->L, a.heads = side ? p->kv_heads : p->heads;
-    plan_rotary(a, p->dtype, p->D);
+    a.r = rotation(p->rotation, positions, p->shared ? 0 : (int64_t)p->rotation.axes * p->L, freqs, nullptr);
+    a.tokens = (int64_t)p->B * p->L, a.L = p->L, a.sides = p->kv_heads ? 2 : 1;
+    a.side[0].heads = p->heads, a.side[1].heads = p->kv_heads;
+    plan_rotary(a, p->dtype, p->D, backward);
     return a;
 }
 bool misaligned_weight(const void *w, const seq_rotation &r) { return reinterpret_cast<uintptr_t>(w) & (r.weight_dtype == NA2D_F32 ? 3u : 1u); }
-int64_t rotary_parts(const RotaryArgs &a, int D) { return (int64_t)sizeof(float) * rotary_bwd_blocks(a) * D; }
 
 }  // namespace
 }  // namespace seq
@@ -347,19 +343,16 @@ int seq_rotary_fwd(const seq_rotary_problem *p, const void *q, const void *k, co
             if (o && o == i) return NA2D_ERR_ALIAS;
     if (q_out == k_out) return NA2D_ERR_ALIAS;
     const int e = elem(p->dtype);
-    for (int side = 0; side < (p->kv_heads ? 2 : 1); ++side) {
-        RotaryArgs a = rotary_args(p, side, positions, freqs, side ? k_weight : q_weight);
-        a.x = side ? view(k, p->k, e) : view(q, p->q, e), a.z = side ? view(k_out, p->k_out, e) : view(q_out, p->q_out, e);
-        if (int r = from_hip(launch_rotary(a, p->dtype, p->D, static_cast<hipStream_t>(stream)))) return r;
-    }
-    return NA2D_OK;
+    RotaryArgs a = rotary_args(p, positions, freqs, false);
+    a.side[0].x = view(q, p->q, e), a.side[0].z = view(q_out, p->q_out, e), a.side[0].weight = q_weight;
+    a.side[1].x = view(k, p->k, e), a.side[1].z = view(k_out, p->k_out, e), a.side[1].weight = k_weight;
+    return from_hip(launch_rotary(a, p->dtype, p->D, static_cast<hipStream_t>(stream)));
 }
 
 size_t seq_rotary_bwd_workspace_bytes(const seq_rotary_problem *p) {
     if (rotary_validate(p, true) != NA2D_OK) return 0;
-    int64_t bytes = 0;
-    for (int side = 0; side < (p->kv_heads ? 2 : 1); ++side) bytes += rotary_parts(rotary_args(p, side, nullptr, nullptr, nullptr), p->D);
-    return (size_t)bytes;
+    const RotaryArgs a = rotary_args(p, nullptr, nullptr, true);
+    return sizeof(float) * (size_t)(a.side[0].blocks + a.side[1].blocks) * p->D;
 }
 
 int seq_rotary_bwd(const seq_rotary_problem *p, const void *q, const void *k, const int32_t *positions, const float *freqs, const void *q_weight, const void *k_weight,
@@ -385,15 +378,12 @@ int seq_rotary_bwd(const seq_rotary_problem *p, const void *q, const void *k, co
     const size_t need = q_weight || k_weight ? seq_rotary_bwd_workspace_bytes(p) : 0;
     if (need && (!workspace || misaligned(workspace) || workspace_bytes < need)) return NA2D_ERR_WORKSPACE;
     const int e = elem(p->dtype);
-    float *parts = static_cast<float *>(workspace);
-    for (int side = 0; side < (p->kv_heads ? 2 : 1); ++side) {
-        RotaryArgs a = rotary_args(p, side, positions, freqs, side ? k_weight : q_weight);
-        a.x = side ? view(k, p->k, e) : view(q, p->q, e), a.z = side ? view(dk_out, p->k_out, e) : view(dq_out, p->q_out, e), a.dx = side ? view(dk, p->dk, e) : view(dq, p->dq, e);
-        a.parts = parts;
-        if (need) parts += rotary_parts(a, p->D) / sizeof(float);
-        if (int r = from_hip(launch_rotary_bwd(a, p->dtype, p->D, side ? dk_weight : dq_weight, static_cast<hipStream_t>(stream)))) return r;
-    }
-    return NA2D_OK;
+    RotaryArgs a = rotary_args(p, positions, freqs, true);
+    a.side[0].x = view(q, p->q, e), a.side[0].z = view(dq_out, p->q_out, e), a.side[0].dx = view(dq, p->dq, e);
+    a.side[1].x = view(k, p->k, e), a.side[1].z = view(dk_out, p->k_out, e), a.side[1].dx = view(dk, p->dk, e);
+    a.side[0].weight = q_weight, a.side[0].weight_grad = dq_weight, a.side[1].weight = k_weight, a.side[1].weight_grad = dk_weight;
+    a.side[0].parts = static_cast<float *>(workspace), a.side[1].parts = a.side[0].parts + (need ? (int64_t)a.side[0].blocks * p->D : 0);
+    return from_hip(launch_rotary_bwd(a, p->dtype, p->D, static_cast<hipStream_t>(stream)));
 }
 
 int seq_cache_validate(const seq_cache_problem *p, int call) { return cache_validate(p, call); }

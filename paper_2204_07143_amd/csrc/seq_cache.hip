@@ -126,10 +126,10 @@ __global__ __launch_bounds__(kThreads) void append_kernel(const CacheArgs p, int
 
 // The same with rows picked out of those given, and keys normed and rotated on the way: a page's fresh tokens stay in registers, in fp32, from their one read to the
 // bytes that are stored, lanes and chunks as seq_rotary.hpp has them.  What is stored is rounded once, from the rotated value.
-template <typename T, int D>
+template <typename T, int D, int STEPS>   // STEPS: how often the workgroup's rows go into a page
 __global__ __launch_bounds__(kThreads) void append_rows_kernel(const RowsArgs a, int touched) {
     using S = HeadShape<T, D>;
-    constexpr int E = S::E, ROWS = kThreads / S::LANES, STEPS = 128 / ROWS;   // rows of the workgroup at a time, and how many times there may be
+    constexpr int E = S::E, ROWS = kThreads / S::LANES;   // rows of the workgroup at a time
     typedef typename S::vec vec;
     typedef int8_t bytes __attribute__((ext_vector_type(E)));
     __shared__ float mosts[kWaves];
@@ -143,6 +143,19 @@ __global__ __launch_bounds__(kThreads) void append_rows_kernel(const RowsArgs a,
     const int b = id / touched, page = 1 << p.page_log2;
     const int64_t length = p.lengths[b];
     const int count = p.extra ? min(p.extra[b], p.n) : p.n;
+    const int i = tid % S::LANES, row0 = tid / S::LANES;
+    const bool turned = !values && a.r.pairs, normed = !values && a.r.weight;
+    int c0, c1;
+    chunks_of<E>(a.r, i, c0, c1);
+    // what does not depend on lengths and table is on its way while those are waited for
+    float freqs[E], wl[E], wh[E];
+#pragma unroll
+    for (int e = 0; e < E; ++e) freqs[e] = 0.f, wl[e] = wh[e] = 1.f;
+    if (turned && E * i < a.r.pairs) {
+#pragma unroll
+        for (int e = 0; e < E; ++e) freqs[e] = a.r.freqs[E * i + e];
+    }
+    if (normed) load_weight<T, E>(a.r, a.r.weight, c0, c1, wl, wh);
     if (length < 0 || count <= 0) return;
     const int64_t at = (length >> p.page_log2) + id % touched, start = at << p.page_log2;
     const int64_t lo = length > start ? length : start, hi = length + count < start + page ? length + count : start + page;
@@ -156,10 +169,6 @@ __global__ __launch_bounds__(kThreads) void append_rows_kernel(const RowsArgs a,
     const char *plane = x.at + b * x.b + kh * x.h;
     const float before = old ? scales[unit] : 0.f;
 
-    const int i = tid % S::LANES, row0 = tid / S::LANES;
-    const bool turned = !values && a.r.pairs, normed = !values && a.r.weight;
-    int c0, c1;
-    chunks_of<E>(a.r, i, c0, c1);
     float l[STEPS][E], h[STEPS][E], most = 0.f;
     int src[STEPS];
 #pragma unroll
@@ -181,32 +190,27 @@ __global__ __launch_bounds__(kThreads) void append_rows_kernel(const RowsArgs a,
 #pragma unroll
         for (int e = 0; e < E; ++e) l[s][e] = (float)y[e], h[s][e] = (float)z[e];
     }
-    if (normed) {
-        float wl[E], wh[E];
-        load_weight<T, E>(a.r, c0, c1, wl, wh);
 #pragma unroll
-        for (int s = 0; s < STEPS; ++s) {
+    for (int s = 0; s < STEPS; ++s) {
+        if (s * ROWS >= fresh) break;
+        if (normed) {
             const float r = over_rms<D, S::LANES>(l[s], h[s], a.r.eps);
 #pragma unroll
             for (int e = 0; e < E; ++e) l[s][e] *= r * wl[e], h[s][e] *= r * wh[e];
         }
-    }
-    if (turned) {
-#pragma unroll
-        for (int s = 0; s < STEPS; ++s) {
-            if (src[s] < 0) continue;
-            Angles<E> angles;
-            angles.set(a.r, i, a.r.positions ? a.r.positions + b * a.r.batch + src[s] : nullptr, a.given, (int)(lo + s * ROWS + row0));
+        if (turned && src[s] >= 0) {
+            Angles<E, false> angles;
+            int position[4] = {(int)(lo + s * ROWS + row0), 0, 0, 0};
+            if (a.r.positions) a.r.load(position, a.r.positions + b * a.r.batch + src[s], a.given);
+            angles.set(a.r, i, freqs, position);
             angles.template turn<false>(a.r.interleaved, l[s], h[s]);
         }
-    }
-#pragma unroll
-    for (int s = 0; s < STEPS; ++s)
 #pragma unroll
         for (int e = 0; e < E; ++e) {
             l[s][e] = finite(l[s][e]), h[s][e] = finite(h[s][e]);
             most = fmaxf(most, fmaxf(fabsf(l[s][e]), fabsf(h[s][e])));
         }
+    }
 #pragma unroll
     for (int d = 1; d < kWave; d *= 2) most = fmaxf(most, __shfl_xor(most, d));
     if (tid % kWave == 0) mosts[tid / kWave] = most;
@@ -294,7 +298,10 @@ template <typename T, int D, int> struct AppendRows {
         const int touched = pages_touched(a.c);
         const int64_t blocks = (int64_t)a.c.B * touched * a.c.kv * 2;
         if (!launch_holds(blocks, kThreads)) return hipErrorInvalidValue;
-        append_rows_kernel<T, D><<<(unsigned)blocks, kThreads, 0, st>>>(a, touched);
+        constexpr int rows = kThreads / HeadShape<T, D>::LANES;
+        const int steps = (1 << a.c.page_log2) / rows;
+        auto *kernel = steps <= 1 ? append_rows_kernel<T, D, 1> : steps == 2 ? append_rows_kernel<T, D, 2> : append_rows_kernel<T, D, 128 / rows>;
+        kernel<<<(unsigned)blocks, kThreads, 0, st>>>(a, touched);
         return hipGetLastError();
     }
 };

@@ -12,20 +12,33 @@ namespace seq {
 struct Rotation {
     const int *positions;      // [axes, tokens] of batch item b at positions + b * batch; null: given by the kernel, on one axis
     const float *freqs;        // radians a position, [pairs]
-    const void *weight;        // of the norm, [D]; null: no norm
+    const void *weight;        // of the append's norm, [D]; null: no norm
     int64_t batch;
     int pairs, axes, ends[3];  // axis a has the pairs below ends[a] that the axes before it do not have
     int interleaved, weight32;
     float eps;
+    // a token's positions: at the first axis', `step` from axis to axis
+    __device__ __forceinline__ void load(int (&p)[4], const int *at, int64_t step) const {
+        p[0] = at[0];
+#pragma unroll
+        for (int a = 1; a < 4; ++a) p[a] = a < axes ? at[a * step] : 0;
+    }
 };
 
+// Queries, or keys.
+struct RotarySide {
+    View x, z, dx;             // forward: x to z.  backward: x (where there is a norm) and z's gradient to dx
+    const void *weight;
+    void *weight_grad;
+    float *parts;              // backward with a norm: every workgroup's sums of the weight's gradient, [blocks, D]
+    int64_t steps;             // groups of tokens times heads
+    int heads, blocks;         // blocks: workgroups that share them
+};
 struct RotaryArgs {
     Rotation r;
-    View x, z, dx;             // forward: x to z.  backward: x (where there is a norm) and z's gradient to dx
-    float *parts;              // backward with a norm: every workgroup's sums of the weight's gradient, [blocks, D]
+    RotarySide side[2];
     int64_t tokens;            // B * L
-    int L, heads, head_parts;  // head_parts: waves that share a token's heads
-    int64_t units;             // groups of tokens times head_parts
+    int L, sides;
 };
 
 template <typename T, int D> struct HeadShape {
@@ -39,30 +52,26 @@ template <int E> __device__ __forceinline__ void chunks_of(const Rotation &r, in
     lo = split ? E * i : 2 * E * i, hi = split ? r.pairs + E * i : 2 * E * i + E;
 }
 
-// cos and sin of position * freq.  The angle is formed in turns in 64 bits (2^-53 of them: 2^31 turns leave 22 bits of the last), reduced there, and rounded to fp32.
-__device__ __forceinline__ void cos_sin(int position, float freq, float &c, float &s) {
+// cos and sin of position * freq.  The angle is formed in turns in 64 bits (2^-53 of them: 2^31 turns leave 22 bits of the last), reduced there, and rounded to fp32.  What
+// becomes 16 or 8 bits takes the processor's own functions of turns, off by 2^-22.9 at most (measured over 2^22 angles), fp32 the library's, off by 2^-24.2.
+template <bool EXACT> __device__ __forceinline__ void cos_sin(int position, float freq, float &c, float &s) {
     double turns = (double)position * ((double)freq * 0.15915494309189534561);
     turns -= __builtin_rint(turns);
-    sincospif(2.f * (float)turns, &s, &c);
+    if constexpr (EXACT) sincospif(2.f * (float)turns, &s, &c);
+    else s = __builtin_amdgcn_sinf((float)turns), c = __builtin_amdgcn_cosf((float)turns);
 }
 
-// Of lane i's pairs; cos 1 and sin 0 where a pair is not rotated.  at: the token's index among the positions, step: from axis to axis.
-template <int E> struct Angles {
+// Of lane i's pairs, freqs theirs, at a token's positions; cos 1 and sin 0 where a pair is not rotated.
+template <int E, bool EXACT> struct Angles {
     float c[E], s[E];
-    __device__ __forceinline__ void set(const Rotation &r, int i, const int *at, int64_t step, int own) {
-        int p[4] = {own, 0, 0, 0};
-        if (at && E * i < r.pairs) {
-#pragma unroll
-            for (int a = 0; a < 4; ++a)
-                if (a < r.axes) p[a] = at[a * step];
-        }
+    __device__ __forceinline__ void set(const Rotation &r, int i, const float (&freqs)[E], const int (&p)[4]) {
 #pragma unroll
         for (int e = 0; e < E; ++e) {
             const int pair = E * i + e;
             c[e] = 1.f, s[e] = 0.f;
             if (pair < r.pairs) {   // (all of a lane's pairs or none: pairs is a multiple of 8)
                 const int position = pair < r.ends[0] ? p[0] : pair < r.ends[1] ? p[1] : pair < r.ends[2] ? p[2] : p[3];
-                cos_sin(position, r.freqs[pair], c[e], s[e]);
+                cos_sin<EXACT>(position, freqs[e], c[e], s[e]);
             }
         }
     }
@@ -90,11 +99,11 @@ template <int LANES> __device__ __forceinline__ float lanes_sum(float x) {
     return x;
 }
 
-template <typename T, int E> __device__ __forceinline__ void load_weight(const Rotation &r, int lo, int hi, float (&wl)[E], float (&wh)[E]) {
+template <typename T, int E> __device__ __forceinline__ void load_weight(const Rotation &r, const void *weight, int lo, int hi, float (&wl)[E], float (&wh)[E]) {
 #pragma unroll
     for (int e = 0; e < E; ++e) {
-        wl[e] = !r.weight ? 1.f : r.weight32 ? static_cast<const float *>(r.weight)[lo + e] : (float)static_cast<const T *>(r.weight)[lo + e];
-        wh[e] = !r.weight ? 1.f : r.weight32 ? static_cast<const float *>(r.weight)[hi + e] : (float)static_cast<const T *>(r.weight)[hi + e];
+        wl[e] = !weight ? 1.f : r.weight32 ? static_cast<const float *>(weight)[lo + e] : (float)static_cast<const T *>(weight)[lo + e];
+        wh[e] = !weight ? 1.f : r.weight32 ? static_cast<const float *>(weight)[hi + e] : (float)static_cast<const T *>(weight)[hi + e];
     }
 }
 
@@ -107,8 +116,7 @@ template <int D, int LANES, int E> __device__ __forceinline__ float over_rms(con
 }
 
 hipError_t launch_rotary(const RotaryArgs &a, int dtype, int D, hipStream_t st);
-hipError_t launch_rotary_bwd(const RotaryArgs &a, int dtype, int D, void *weight_grad, hipStream_t st);
-int rotary_bwd_blocks(const RotaryArgs &a);
-void plan_rotary(RotaryArgs &a, int dtype, int D);   // head_parts, units
+hipError_t launch_rotary_bwd(const RotaryArgs &a, int dtype, int D, hipStream_t st);
+void plan_rotary(RotaryArgs &a, int dtype, int D, bool backward);   // steps, blocks
 
 }  // namespace seq
