@@ -124,15 +124,36 @@ __global__ __launch_bounds__(kThreads) void append_kernel(const CacheArgs p, int
     }
 }
 
+// x / by to whole numbers, nearest even, as bytes, where |x / by| is at most 127 and a little: x over (1 / by) is off by less than 2^-17 there, and behind 1.5 2^23 it is rounded in
+// place, the byte at the bottom.  Where an element of the wave lies next to a middle all are divided (one chunk of a wave in ten or so).
+template <int E> __device__ __forceinline__ void whole_bytes(const float (&x)[E], float by, float over, uint32_t (&r)[E / 4]) {
+    constexpr float kMagic = 0x1.8p23f;
+    float y[E], near = 0.f;
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+        y[e] = __builtin_fmaf(x[e], over, kMagic);
+        near = fmaxf(near, fabsf(__builtin_fmaf(x[e], over, -(y[e] - kMagic))));
+    }
+    if (__any(near > 0.5f - 0x1p-14f)) {
+#pragma unroll
+        for (int e = 0; e < E; ++e) y[e] = __builtin_rintf(x[e] / by) + kMagic;
+    }
+#pragma unroll
+    for (int i = 0; i < E / 4; ++i) {
+        const uint32_t a = __builtin_amdgcn_perm(__float_as_uint(y[4 * i + 1]), __float_as_uint(y[4 * i]), 0x0c0c0400u), b = __builtin_amdgcn_perm(__float_as_uint(y[4 * i + 3]), __float_as_uint(y[4 * i + 2]), 0x04000c0cu);
+        r[i] = a | b;
+    }
+}
+
 // The same with rows picked out of those given, and keys normed and rotated on the way: a page's fresh tokens stay in registers, in fp32, from their one read to the
 // bytes that are stored, lanes and chunks as seq_rotary.hpp has them.  What is stored is rounded once, from the rotated value.
 template <typename T, int D, int STEPS>   // STEPS: how often the workgroup's rows go into a page
-__global__ __launch_bounds__(kThreads) void append_rows_kernel(const RowsArgs a, int touched) {
+__global__ __launch_bounds__(kThreads, STEPS <= 2 ? 5 : 3) void append_rows_kernel(const RowsArgs a, int touched) {
     using S = HeadShape<T, D>;
     constexpr int E = S::E, ROWS = kThreads / S::LANES;   // rows of the workgroup at a time
     typedef typename S::vec vec;
     typedef int8_t bytes __attribute__((ext_vector_type(E)));
-    __shared__ float mosts[kWaves];
+    __shared__ uint32_t mosts[kWaves];
     const CacheArgs &p = a.c;
     const int tid = threadIdx.x;
     int id = blockIdx.x;
@@ -169,7 +190,8 @@ __global__ __launch_bounds__(kThreads) void append_rows_kernel(const RowsArgs a,
     const char *plane = x.at + b * x.b + kh * x.h;
     const float before = old ? scales[unit] : 0.f;
 
-    float l[STEPS][E], h[STEPS][E], most = 0.f;
+    float l[STEPS][E], h[STEPS][E];
+    uint32_t bits = 0;   // of the largest magnitude; at or above those of infinity if one is not finite
     int src[STEPS];
 #pragma unroll
     for (int s = 0; s < STEPS; ++s) {
@@ -206,16 +228,29 @@ __global__ __launch_bounds__(kThreads) void append_rows_kernel(const RowsArgs a,
             angles.template turn<false>(a.r.interleaved, l[s], h[s]);
         }
 #pragma unroll
-        for (int e = 0; e < E; ++e) {
-            l[s][e] = finite(l[s][e]), h[s][e] = finite(h[s][e]);
-            most = fmaxf(most, fmaxf(fabsf(l[s][e]), fabsf(h[s][e])));
-        }
+        for (int e = 0; e < E; ++e) bits = max(bits, max(__float_as_uint(l[s][e]) & 0x7fffffffu, __float_as_uint(h[s][e]) & 0x7fffffffu));
     }
 #pragma unroll
-    for (int d = 1; d < kWave; d *= 2) most = fmaxf(most, __shfl_xor(most, d));
-    if (tid % kWave == 0) mosts[tid / kWave] = most;
+    for (int d = 1; d < kWave; d *= 2) bits = max(bits, (uint32_t)__shfl_xor((int)bits, d));
+    if (tid % kWave == 0) mosts[tid / kWave] = bits;
     workgroup_sync();
-    most = fmaxf(fmaxf(mosts[0], mosts[1]), fmaxf(mosts[2], mosts[3]));
+    float most = __uint_as_float(max(max(mosts[0], mosts[1]), max(mosts[2], mosts[3])));
+    if (!(most < INFINITY)) {   // once more, without what is no number
+        most = 0.f;
+#pragma unroll
+        for (int s = 0; s < STEPS; ++s)
+#pragma unroll
+            for (int e = 0; e < E; ++e) {
+                l[s][e] = finite(l[s][e]), h[s][e] = finite(h[s][e]);
+                most = fmaxf(most, fmaxf(fabsf(l[s][e]), fabsf(h[s][e])));
+            }
+#pragma unroll
+        for (int d = 1; d < kWave; d *= 2) most = fmaxf(most, __shfl_xor(most, d));
+        workgroup_sync();
+        if (tid % kWave == 0) mosts[tid / kWave] = __float_as_uint(most);
+        workgroup_sync();
+        most = __uint_as_float(max(max(mosts[0], mosts[1]), max(mosts[2], mosts[3])));
+    }
     const float scale = fmaxf(before, most / 127.f), by = scale > 0.f ? scale : 1.f;
     if (tid == 0) scales[unit] = scale;
     if (old && scale != before) round_again(cells, old * D / 4, before / by, tid);
@@ -226,10 +261,16 @@ __global__ __launch_bounds__(kThreads) void append_rows_kernel(const RowsArgs a,
         const int row = s * ROWS + row0;
         if (row >= fresh) break;
         bytes u, w;
+        if (divide) {
 #pragma unroll
-        for (int e = 0; e < E; ++e) {
-            u[e] = (int8_t)(divide ? max(-127, min(127, (int)__builtin_rintf(l[s][e] / by))) : whole(l[s][e], by, over));
-            w[e] = (int8_t)(divide ? max(-127, min(127, (int)__builtin_rintf(h[s][e] / by))) : whole(h[s][e], by, over));
+            for (int e = 0; e < E; ++e) {
+                u[e] = (int8_t)max(-127, min(127, (int)__builtin_rintf(l[s][e] / by)));
+                w[e] = (int8_t)max(-127, min(127, (int)__builtin_rintf(h[s][e] / by)));
+            }
+        } else {
+            uint32_t a[E / 4], b[E / 4];
+            whole_bytes<E>(l[s], by, over, a), whole_bytes<E>(h[s], by, over, b);
+            u = __builtin_bit_cast(bytes, a), w = __builtin_bit_cast(bytes, b);
         }
         int8_t *cell = cells + (int64_t)(old + row) * D;
         *reinterpret_cast<bytes *>(cell + c0) = u, *reinterpret_cast<bytes *>(cell + c1) = w;

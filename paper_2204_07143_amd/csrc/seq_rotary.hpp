@@ -70,7 +70,7 @@ template <int E, bool EXACT> struct Angles {
             const int pair = E * i + e;
             c[e] = 1.f, s[e] = 0.f;
             if (pair < r.pairs) {   // (all of a lane's pairs or none: pairs is a multiple of 8)
-                const int position = pair < r.ends[0] ? p[0] : pair < r.ends[1] ? p[1] : pair < r.ends[2] ? p[2] : p[3];
+                const int position = r.axes == 1 || pair < r.ends[0] ? p[0] : pair < r.ends[1] ? p[1] : pair < r.ends[2] ? p[2] : p[3];
                 cos_sin<EXACT>(position, freqs[e], c[e], s[e]);
             }
         }
