@@ -468,19 +468,41 @@ seq_rotation rotation_of(const Sections &x, const Tensor &of, const Tensor &weig
 }
 // a norm's weight, or none: [D], of the type of `of` or fp32
 bool weight_fits(const Tensor &w, const Tensor &of) {
-    return !w.defined() || (plain(w) && w.dim() == 1 && w.size(0) == of.size(3) && w.device() == of.device() && w.is_contiguous() && (w.scalar_type() == of.scalar_type() || w.scalar_type() == at::kFloat));
+    return !w.defined() || (plain(w) && w.dim() == 1 && w.size(0) == of.size(-1) && w.device() == of.device() && w.is_contiguous() && (w.scalar_type() == of.scalar_type() || w.scalar_type() == at::kFloat));
 }
-// positions [axes, L] or [B, axes, L]
-bool positions_fit(const Tensor &t, const Tensor &of, int64_t axes, int64_t L) {
+// Tensors [B, heads, L, D], or maps [B, heads, H, W, D] whose rows and columns are one axis of tokens, without a view in between
+int64_t tokens_of(const Tensor &t) { return t.dim() == 5 ? t.size(2) * t.size(3) : t.size(2); }
+bool whole_tokens(const Tensor &t) {
+    if (t.dim() == 4) return whole_rows(t);
+    const auto n = t.sizes(), s = t.strides();
+    const int64_t step = 16 / t.element_size();
+    for (int i = 0; i < 4; ++i)
+        if (n[i] != 1 && s[i] % step) return false;
+    const bool one_axis = n[2] == 1 || n[3] == 1 || s[2] == n[3] * s[3];
+    return one_axis && (n[4] == 1 || s[4] == 1) && (uintptr_t)t.data_ptr() % 16 == 0 && (n[2] * n[3] - 1) * s[n[3] == 1 ? 2 : 3] + n[4] < ((int64_t)1 << 31) / t.element_size();
+}
+Tensor token_rows(const Tensor &t) { return whole_tokens(t) ? t : t.clone(at::MemoryFormat::Contiguous); }
+Tensor tokens_like(const Tensor &t) {
+    Tensor r = at::empty_like(t);
+    return r.stride(-1) == 1 && whole_tokens(r) ? r : at::empty(t.sizes(), t.options());
+}
+seq_strides token_strides(const Tensor &t) {
+    if (t.dim() == 4) return strides(t);
+    const auto n = t.sizes(), s = t.strides();
+    return {n[0] == 1 ? 0 : s[0], n[1] == 1 ? 0 : s[1], n[3] != 1 ? s[3] : n[2] != 1 ? s[2] : 0};
+}
+// positions [axes, L] or [B, axes, L], of maps [axes, H, W] or [B, axes, H, W]
+bool positions_fit(const Tensor &t, const Tensor &of, int64_t axes) {
     if (!plain(t)) return false;
-    return t.dim() == 2 ? constant(t, of, at::kInt, {axes, L}) : constant(t, of, at::kInt, {of.size(0), axes, L});
+    if (of.dim() == 5) return t.dim() == 3 ? constant(t, of, at::kInt, {axes, of.size(2), of.size(3)}) : constant(t, of, at::kInt, {of.size(0), axes, of.size(2), of.size(3)});
+    return t.dim() == 2 ? constant(t, of, at::kInt, {axes, of.size(2)}) : constant(t, of, at::kInt, {of.size(0), axes, of.size(2)});
 }
 std::optional<seq_rotary_problem> rotary_of(const Tensor &q, const Tensor &k, const Tensor &positions, const seq_rotation &r) {
     const auto code = dtype_code(q.scalar_type());
-    if (!code || q.dim() != 4 || !small(q.sizes())) return std::nullopt;
+    if (!code || (q.dim() != 4 && q.dim() != 5) || !small(q.sizes()) || !fits(tokens_of(q))) return std::nullopt;
     seq_rotary_problem p{};
-    p.B = (int32_t)q.size(0), p.heads = (int32_t)q.size(1), p.L = (int32_t)q.size(2), p.D = (int32_t)q.size(3), p.kv_heads = k.defined() ? (int32_t)k.size(1) : 0;
-    p.dtype = *code, p.rotation = r, p.shared = positions.dim() == 2;
+    p.B = (int32_t)q.size(0), p.heads = (int32_t)q.size(1), p.L = (int32_t)tokens_of(q), p.D = (int32_t)q.size(-1), p.kv_heads = k.defined() ? (int32_t)k.size(1) : 0;
+    p.dtype = *code, p.rotation = r, p.shared = positions.dim() == (q.dim() == 5 ? 3 : 2);
     return p;
 }
 Tensor undefined_or(const std::optional<Tensor> &t) { return t.value_or(Tensor()); }
@@ -502,18 +524,18 @@ struct SeqRotary : torch::autograd::Function<SeqRotary> {
     static variable_list run(const Tensor &q, const Tensor &k, const Tensor &positions, const Tensor &freqs, const Tensor &qw, const Tensor &kw, const seq_rotation &r) {
         auto p = rotary_of(q, k, positions, r);
         if (!p) throw Refused{};
-        variable_list out{rows_like(q)};
-        p->q = strides(q), p->q_out = strides(out[0]);
+        variable_list out{tokens_like(q)};
+        p->q = token_strides(q), p->q_out = token_strides(out[0]);
         if (k.defined()) {
-            out.push_back(rows_like(k));
-            p->k = strides(k), p->k_out = strides(out[1]);
+            out.push_back(tokens_like(k));
+            p->k = token_strides(k), p->k_out = token_strides(out[1]);
         }
         forward_check(seq_rotary_fwd(&*p, ptr(q), ptr(k), (const int32_t *)ptr(positions), (const float *)ptr(freqs), ptr(qw), ptr(kw), ptr(out[0]), k.defined() ? ptr(out[1]) : nullptr, stream()));
         return out;
     }
     static variable_list forward(AutogradContext *ctx, const Tensor &q_, const std::optional<Tensor> &k_, const Tensor &positions, const Tensor &freqs, const std::optional<Tensor> &qw_,
                                  const std::optional<Tensor> &kw_, const std::vector<int64_t> &sections, double eps, bool interleaved) {
-        const Tensor q = rows(q_), k = k_ ? rows(*k_) : Tensor(), qw = undefined_or(qw_), kw = undefined_or(kw_);
+        const Tensor q = token_rows(q_), k = k_ ? token_rows(*k_) : Tensor(), qw = undefined_or(qw_), kw = undefined_or(kw_);
         Sections x;
         for (int64_t n : sections) x.n[x.axes++] = n;
         variable_list out = run(q, k, positions, freqs, qw, kw, rotation_of(x, q, qw, kw, eps, interleaved));
@@ -533,26 +555,26 @@ struct SeqRotary : torch::autograd::Function<SeqRotary> {
             const Tensor &positions = saved[2], &freqs = saved[3];
             const bool keys = grads.size() > 1;
             for (int i = 0; i < (keys ? 2 : 1); ++i) {
-                z[i] = rows(grads[i].is_neg() ? grads[i].resolve_neg() : grads[i]);
+                z[i] = token_rows(grads[i].is_neg() ? grads[i].resolve_neg() : grads[i]);
                 TORCH_CHECK_VALUE(plain(z[i]) && z[i].device() == z[0].device(), "na2d takes GPU tensors only");
                 // (a saved-tensor hook may hand back tensors of another form)
                 if (w[i].defined()) {
                     TORCH_CHECK_VALUE(weight_fits(w[i], z[i]) && plain(x[i]) && x[i].device() == z[i].device() && x[i].scalar_type() == z[i].scalar_type() && x[i].sizes() == z[i].sizes(),
                                       "not a tensor of the forward pass");
-                    TORCH_CHECK_VALUE(whole_rows(x[i]), "the elements of a row must be contiguous");
+                    TORCH_CHECK_VALUE(whole_tokens(x[i]), "the elements of a row must be contiguous");
                     dw[i] = at::empty_like(w[i]);
                 }
-                dx[i] = rows_like(w[i].defined() ? x[i] : z[i]);
+                dx[i] = tokens_like(w[i].defined() ? x[i] : z[i]);
             }
             TORCH_CHECK_VALUE(!w[0].defined() || !w[1].defined() || w[0].scalar_type() == w[1].scalar_type(), "not a tensor of the forward pass");
             Sections s;
             for (int64_t n : ctx->saved_data["sections"].toIntVector()) s.n[s.axes++] = n;
-            TORCH_CHECK_VALUE(positions_fit(positions, z[0], s.axes, z[0].size(2)) && plain(freqs) && freqs.device() == z[0].device() && freqs.scalar_type() == at::kFloat && freqs.is_contiguous() && s.set(freqs),
+            TORCH_CHECK_VALUE(positions_fit(positions, z[0], s.axes) && plain(freqs) && freqs.device() == z[0].device() && freqs.scalar_type() == at::kFloat && freqs.is_contiguous() && s.set(freqs),
                               "not a tensor of the forward pass");
             auto p = valid(rotary_of(z[0], z[1], positions, rotation_of(s, z[0], w[0], w[1], ctx->saved_data["eps"].toDouble(), ctx->saved_data["interleaved"].toBool())));
             const seq_strides none{};
-            p.q_out = strides(z[0]), p.dq = strides(dx[0]), p.q = w[0].defined() ? strides(x[0]) : none;
-            if (keys) p.k_out = strides(z[1]), p.dk = strides(dx[1]), p.k = w[1].defined() ? strides(x[1]) : none;
+            p.q_out = token_strides(z[0]), p.dq = token_strides(dx[0]), p.q = w[0].defined() ? token_strides(x[0]) : none;
+            if (keys) p.k_out = token_strides(z[1]), p.dk = token_strides(dx[1]), p.k = w[1].defined() ? token_strides(x[1]) : none;
             const Tensor ws = scratch(w[0].defined() || w[1].defined() ? seq_rotary_bwd_workspace_bytes(&p) : 0, z[0]);
             check(seq_rotary_bwd(&p, w[0].defined() ? ptr(x[0]) : nullptr, w[1].defined() ? ptr(x[1]) : nullptr, (const int32_t *)ptr(positions), (const float *)ptr(freqs), ptr(w[0]), ptr(w[1]),
                                  ptr(z[0]), ptr(z[1]), ptr(dx[0]), ptr(dx[1]), ptr(dw[0]), ptr(dw[1]), ptr(ws), size_of(ws), stream()));
@@ -789,17 +811,21 @@ PyObject *py_seq_rotary(PyObject *, PyObject *const *a, Py_ssize_t n) {
         Py_RETURN_NONE;
     const bool interleaved = a[8] == Py_True;
     return guarded<variable_list>([&]() -> variable_list {
-        if (!plain(q) || q.dim() != 4 || !dtype_code(q.scalar_type()) || !small(q.sizes()) || !plain(freqs) || !x.set(freqs)) return {};
-        const auto s = q.sizes();
-        if (k.defined() && (k.dim() != 4 || !small(k.sizes()) || !matches(k, q, {s[0], k.size(1), s[2], s[3]}))) return {};
-        if (!constant(freqs, q, at::kFloat, {freqs.numel()}) || !positions_fit(positions, q, x.axes, s[2]) || !weight_fits(qw, q) || !weight_fits(kw, q) || (kw.defined() && !k.defined()) ||
+        if (!plain(q) || (q.dim() != 4 && q.dim() != 5) || !dtype_code(q.scalar_type()) || !small(q.sizes()) || !plain(freqs) || !x.set(freqs)) return {};
+        if (k.defined()) {
+            if (k.dim() != q.dim() || !small(k.sizes())) return {};
+            std::vector<int64_t> sizes = q.sizes().vec();
+            sizes[1] = k.size(1);
+            if (!matches(k, q, sizes)) return {};
+        }
+        if (!constant(freqs, q, at::kFloat, {freqs.numel()}) || !positions_fit(positions, q, x.axes) || !weight_fits(qw, q) || !weight_fits(kw, q) || (kw.defined() && !k.defined()) ||
             (qw.defined() && kw.defined() && qw.scalar_type() != kw.scalar_type()) || positions.requires_grad() || freqs.requires_grad())
             return {};
         const c10::DeviceGuard device(q.device());
         if (wants_grad({&q, &k, &qw, &kw}))
             return SeqRotary::apply(q, maybe(k), positions, freqs, maybe(qw), maybe(kw), std::vector<int64_t>(x.n, x.n + x.axes), eps, interleaved);
         const at::AutoGradMode off(false);
-        return SeqRotary::run(rows(q), k.defined() ? rows(k) : k, positions, freqs, qw, kw, rotation_of(x, q, qw, kw, eps, interleaved));
+        return SeqRotary::run(token_rows(q), k.defined() ? token_rows(k) : k, positions, freqs, qw, kw, rotation_of(x, q, qw, kw, eps, interleaved));
     });
 }
 
@@ -820,7 +846,7 @@ PyObject *py_seq_cache_append_rows(PyObject *, PyObject *const *a, Py_ssize_t n)
             return Tensor();
         if (picked.defined() && (picked.dim() != 2 || picked.size(1) < 1 || !fits(picked.size(1)) || !constant(picked, k, at::kInt, {k.size(0), picked.size(1)}))) return Tensor();
         if (freqs.defined() ? !plain(freqs) || !x.set(freqs) || freqs.requires_grad() || !constant(freqs, k, at::kFloat, {freqs.numel()}) : x.axes || positions.defined()) return Tensor();
-        if (!weight_fits(weight, k) || (positions.defined() && !positions_fit(positions, k, x.axes, k.size(2)))) return Tensor();
+        if (!weight_fits(weight, k) || (positions.defined() && !positions_fit(positions, k, x.axes))) return Tensor();
         const at::AutoGradMode off(false);
         const c10::DeviceGuard device(k.device());
         const Tensor kr = rows(k), vr = rows(v);

@@ -8,7 +8,7 @@ namespace seq {
 struct CacheArgs {
     View tk, tv;           // a tree of nodes: their own keys and values,
     const int *parents;    // [B, n]
-    bool tanh;             // scores are capped by the library's tanh
+    bool tanh, tiled;      // scores are capped by the library's tanh; in tiles (seq_tree_tile.hip)
     View a, b;             // append: new keys and values; gather: keys and values read; attention: q and out
     int8_t *k, *v;
     float *ks, *vs;

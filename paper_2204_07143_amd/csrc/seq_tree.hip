@@ -21,23 +21,28 @@ template <typename T, int D, int CAP> struct TreeAttention {
     }
 };
 
-// Up to 32 rows to a key head here, more in tiles of 64 tokens (seq_tree_tile.hip).
-bool tiled(const CacheArgs &a) { return a.group * a.n > 32; }
-
 }  // namespace
 
 void plan_cache_tree(CacheArgs &a, int64_t longest, int D) {
-    if (tiled(a)) return plan_tree_tiles(a, longest, D);
+    // More than 32 rows to a key head go in tiles of 64 tokens (seq_tree_tile.hip), which look at the cache once for up to 192 rows but take 20 us before the first tile, where these
+    // take 12, if there is enough work: 81 rows, bf16, D 128, us here / in tiles: 20 sequences and key heads with a window of 2048 (640 tiles) 21 / 33; 192 rows, 128
+    // sequences and key heads to 8000 tokens (9000 tiles) 225 / 127.
+    const int64_t rows = (int64_t)a.group * a.n, reach = longest < (int64_t)a.window ? longest : (int64_t)a.window, tiles = (int64_t)a.B * a.kv * ((reach + kTile - 1) / kTile);
+    a.tiled = rows > 32 && (double)tiles * rows >= 65536;
+    if (a.tiled) return plan_tree_tiles(a, longest, D);
+    // There is a join in any case: parts of 128 tokens, where workgroups are few.
     plan_cache_attention(a, longest);
-    a.splits += 1;   // the nodes' own part
+    const int64_t units = (int64_t)a.B * a.kv * a.row_groups, wanted = (512 + units - 1) / units, most = reach / 128;
+    const int64_t s = wanted < most ? wanted : most;
+    a.splits = (int)(s > 128 ? 128 : s > a.splits ? s : a.splits) + 1;   // and the nodes' own part
 }
 size_t cache_tree_bytes(const CacheArgs &a, int D) {
-    if (tiled(a)) return tree_tile_bytes(a, D);
+    if (a.tiled) return tree_tile_bytes(a, D);
     return (size_t)a.B * a.kv * a.row_groups * a.splits * rows_each(a) * (D + 2) * sizeof(float);
 }
 
 hipError_t launch_cache_tree(const CacheArgs &a, int dtype, int D, int cap, hipStream_t st) {
-    if (tiled(a)) return launch_tree_tiles(a, dtype, D, cap, st);
+    if (a.tiled) return launch_tree_tiles(a, dtype, D, cap, st);
 #define SEQ_D(T, N) (cap == kNoCap ? TreeAttention<T, N, kNoCap>::go(a, st) : cap == kSigmoidCap ? TreeAttention<T, N, kSigmoidCap>::go(a, st) : TreeAttention<T, N, kTanhCap>::go(a, st))
 #define SEQ_T(T) (D == 32 ? SEQ_D(T, 32) : D == 64 ? SEQ_D(T, 64) : SEQ_D(T, 128))
     return dtype == NA2D_F16 ? SEQ_T(f16_t) : SEQ_T(bf16_t);

@@ -14,7 +14,7 @@ namespace seq {
 
 namespace {
 
-constexpr int kLeastRun = 4;   // tiles of a workgroup, where there are so many
+constexpr int kLeastRun = 2;   // tiles of a workgroup, where there are so many
 
 __device__ __forceinline__ int64_t uniform(int64_t x) {
     return (int64_t)((uint64_t)(uint32_t)seq::uniform((int)(uint32_t)x) | (uint64_t)(uint32_t)seq::uniform((int)(uint32_t)((uint64_t)x >> 32)) << 32);
@@ -28,8 +28,8 @@ __device__ __forceinline__ int afresh(int x) {
 // What of a sequence its rows see of the cache.
 struct Span {
     int tokens, length, least, begin, tiles;   // tiles: of the cache from `begin` on, and the nodes' own
-    __device__ __forceinline__ Span(const CacheArgs &p, int b) {
-        tokens = min(max(p.lengths[b], 0), INT32_MAX - kNodes);
+    __device__ __forceinline__ Span(const CacheArgs &p, int held) {   // held: the sequence's length as it is given
+        tokens = min(max(held, 0), INT32_MAX - kNodes);
         length = (int)min((int64_t)tokens, (int64_t)p.width << p.page_log2);
         least = max(0, tokens - p.window + 1);
         begin = least / kTile;
@@ -40,15 +40,18 @@ struct Span {
 // The runs of the workgroups: the tiles of a sequence's units (key heads, and groups of their rows), unit after unit, sequence after sequence.
 struct Schedule {
     int64_t total;
-    int units, runs;
+    int units, runs, held;   // held: the length of sequence `lane`
     __device__ __forceinline__ Schedule(const CacheArgs &p, int lane) : total(0), units(p.kv * p.row_groups) {
-        for (int b = lane; b < p.B; b += kWave) total += Span(p, b).tiles;
+        held = lane < p.B ? p.lengths[lane] : 0;
+        if (lane < p.B) total = Span(p, held).tiles;
+        for (int b = lane + kWave; b < p.B; b += kWave) total += Span(p, p.lengths[b]).tiles;
 #pragma unroll
         for (int d = 1; d < kWave; d *= 2) total += __shfl_xor(total, d);
         total = uniform(total * units);
         const int64_t wanted = total / kLeastRun;
         runs = wanted < 1 ? 1 : wanted < p.splits ? (int)wanted : p.splits;
     }
+    __device__ __forceinline__ Span span(const CacheArgs &p, int b) const { return Span(p, b < kWave ? __builtin_amdgcn_readlane(held, b) : p.lengths[b]); }   // b: the same in all lanes
     __device__ __forceinline__ int64_t start(int run) const { return total * run / runs; }
     __device__ __forceinline__ int run_of(int64_t tile) const {
         int w = (int)(tile * runs / total);
@@ -59,7 +62,7 @@ struct Schedule {
     __device__ __forceinline__ int find(const CacheArgs &p, int64_t tile, int lane, int64_t &before) const {
         before = 0;
         for (int base = 0;; base += kWave) {
-            const int64_t mine = base + lane < p.B ? (int64_t)Span(p, base + lane).tiles * units : 0;
+            const int64_t mine = base + lane < p.B ? (int64_t)Span(p, base ? p.lengths[base + lane] : held).tiles * units : 0;
             int64_t upto = mine;
 #pragma unroll
             for (int d = 1; d < kWave; d *= 2) {
@@ -77,7 +80,7 @@ struct Schedule {
     }
     __device__ __forceinline__ int64_t tiles_before(const CacheArgs &p, int b, int lane) const {
         int64_t n = 0;
-        for (int i = lane; i < b; i += kWave) n += Span(p, i).tiles;
+        for (int i = lane; i < b; i += kWave) n += Span(p, i < kWave ? held : p.lengths[i]).tiles;
 #pragma unroll
         for (int d = 1; d < kWave; d *= 2) n += __shfl_xor(n, d);
         return uniform(n * units);
@@ -127,14 +130,46 @@ __global__ __launch_bounds__(kThreads, 2) void tree_tile_kernel(const CacheArgs 
 
 #pragma unroll 1
     for (int64_t at = from; at < to;) {
-        Span span(p, b);
+        auto span_of = [&](int b) { return RB == 3 ? Span(p, p.lengths[b]) : schedule.span(p, b); };   // (three blocks: the registers)
+        Span span = span_of(b);
         while (at >= before + (int64_t)span.tiles * schedule.units) {
             before += (int64_t)span.tiles * schedule.units;
-            span = Span(p, ++b);
+            span = span_of(++b);
         }
         const int unit_id = (int)((at - before) / span.tiles), first = (int)((at - before) - (int64_t)unit_id * span.tiles);
         const int count = (int)min(to - at, (int64_t)(span.tiles - first)), kh = unit_id / p.row_groups, row0 = unit_id % p.row_groups * ROWS + wave * 16 * RB;
         const bool whole = count == span.tiles;
+        // where the cache's tiles lie, and the first one's bytes, on their way from here on
+        const int cached = min(count, span.tiles - 1 - first);   // of this run
+        const int pieces = page >= kTile ? 1 : kTile / page, shift = page >= kTile ? 2 : p.page_log2 - 4, chunk = kWave / pieces;   // of a tile: pages, and 16-token blocks to one
+        int unit = -1;                // of one of the next 64 pieces: its page, and of that
+        float ks = 0.f, lv = 0.f, over = 0.f;   // the keys' scale, the values' in base 2, and one over it
+        auto look_up = [&](int tile) {
+            const int size = kTile / pieces;
+            const int64_t token = (int64_t)tile * kTile + (int64_t)size * lane;
+            const bool seen = token < span.length && token + size > span.least;
+            const int id = p.table[(int64_t)b * p.width + (seen ? token >> p.page_log2 : 0)];
+            unit = seen && (unsigned)id < (unsigned)p.pages ? id : -1;
+            const int64_t u = (int64_t)max(unit, 0) * p.kv + kh;
+            const float k = p.ks[u], v = fmaxf(p.vs[u], 0x1p-100f);   // (values of a scale of 0 are 0: their weights count)
+            ks = unit < 0 ? 0.f : k, lv = unit < 0 ? 0.f : __builtin_amdgcn_logf(v), over = unit < 0 ? 0.f : 1.f / v;
+        };
+        auto lane_of = [](float x, int l) { return __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(x), l)); };
+        B keys, values;
+        auto load = [&](int t) {   // the run's tile t; its blocks have been looked up
+            const int t0 = (span.begin + first + t) * kTile, tid = RB == 3 ? afresh(threadIdx.x) : (int)threadIdx.x;
+#pragma unroll
+            for (int i = 0; i < B::LOADS; ++i) {
+                const int u = __builtin_amdgcn_readlane(unit, (t & (chunk - 1)) * pieces + (B::block(i, wave) >> shift));
+                const int64_t cell = (((int64_t)max(u, 0) * p.kv + kh) * page + ((t0 + B::row(i, tid)) & (page - 1))) * D + (tid + i * kThreads) % B::C * (4 * B::W);
+                keys.x[i] = *reinterpret_cast<const typename B::words *>(p.k + cell);
+                values.x[i] = *reinterpret_cast<const typename B::words *>(p.v + cell);
+            }
+        };
+        if (cached > 0) {
+            look_up(span.begin + first);
+            load(0);
+        }
         workgroup_sync();   // (what the run before reads of LDS)
         if (b != built) {
             tree.build(p.parents + (int64_t)b * p.n, p.n, tid);
@@ -207,36 +242,6 @@ __global__ __launch_bounds__(kThreads, 2) void tree_tile_kernel(const CacheArgs 
         };
 
         // ---- the cache's tiles
-        const int cached = min(count, span.tiles - 1 - first);   // of this run
-        const int pieces = page >= kTile ? 1 : kTile / page, shift = page >= kTile ? 2 : p.page_log2 - 4, chunk = kWave / pieces;   // of a tile: pages, and 16-token blocks to one
-        int unit = -1;                // of one of the next 64 pieces: its page, and of that
-        float ks = 0.f, lv = 0.f, over = 0.f;   // the keys' scale, the values' in base 2, and one over it
-        auto look_up = [&](int tile) {
-            const int size = kTile / pieces;
-            const int64_t token = (int64_t)tile * kTile + (int64_t)size * lane;
-            const bool seen = token < span.length && token + size > span.least;
-            const int id = p.table[(int64_t)b * p.width + (seen ? token >> p.page_log2 : 0)];
-            unit = seen && (unsigned)id < (unsigned)p.pages ? id : -1;
-            const int64_t u = (int64_t)max(unit, 0) * p.kv + kh;
-            const float k = p.ks[u], v = fmaxf(p.vs[u], 0x1p-100f);   // (values of a scale of 0 are 0: their weights count)
-            ks = unit < 0 ? 0.f : k, lv = unit < 0 ? 0.f : __builtin_amdgcn_logf(v), over = unit < 0 ? 0.f : 1.f / v;
-        };
-        auto lane_of = [](float x, int l) { return __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(x), l)); };
-        B keys, values;
-        auto load = [&](int t) {   // the run's tile t; its blocks have been looked up
-            const int t0 = (span.begin + first + t) * kTile, tid = RB == 3 ? afresh(threadIdx.x) : (int)threadIdx.x;
-#pragma unroll
-            for (int i = 0; i < B::LOADS; ++i) {
-                const int u = __builtin_amdgcn_readlane(unit, (t & (chunk - 1)) * pieces + (B::block(i, wave) >> shift));
-                const int64_t cell = (((int64_t)max(u, 0) * p.kv + kh) * page + ((t0 + B::row(i, tid)) & (page - 1))) * D + (tid + i * kThreads) % B::C * (4 * B::W);
-                keys.x[i] = *reinterpret_cast<const typename B::words *>(p.k + cell);
-                values.x[i] = *reinterpret_cast<const typename B::words *>(p.v + cell);
-            }
-        };
-        if (cached > 0) {
-            look_up(span.begin + first);
-            load(0);
-        }
 #pragma unroll 1
         for (int t = 0; t < cached; ++t) {
             const int ki = img + (t & 1) * 2 * L::BYTES, vi = ki + L::BYTES, t0 = (span.begin + first + t) * kTile, slot = (t & (chunk - 1)) * pieces;
@@ -434,7 +439,7 @@ __global__ __launch_bounds__(kThreads) void tree_join_kernel(const CacheArgs p) 
     const int unit = (int)(blockIdx.x / blocks) % (p.kv * p.row_groups), b = (int)(blockIdx.x / blocks) / (p.kv * p.row_groups);
     const int row = unit % p.row_groups * ROWS + in_unit, kh = unit / p.row_groups;
     const Schedule schedule(p, lane);
-    const int tiles = Span(p, b).tiles;
+    const int tiles = schedule.span(p, b).tiles;
     const int64_t first = schedule.tiles_before(p, b, lane) + (int64_t)unit * tiles;
     const int from = schedule.run_of(first), to = schedule.run_of(first + tiles - 1);
     if (from == to || row >= p.group * p.n) return;

@@ -417,6 +417,9 @@ def seq_rotary(q, k, positions, freqs, *, sections=None, q_weight=None, k_weight
     axis).  The norm is ``x * weight / sqrt(mean(x ** 2) + eps)``.  Angles are formed in 64 bits: positions may be as far as int32 goes.  Maps [B, heads, H, W, D],
     with positions [axes, H, W], are taken as well, before the neighbourhood operators.  D is 16, 32, 64 or 128; f32, f16, bf16; strided as in ``seq_attention``.
     """
+    out = _native().seq_rotary(q, k, positions, freqs, sections, q_weight, k_weight, eps, interleaved)
+    if out is not None:
+        return out if k is not None else (*out, None)
     if q.dim() == 5:
         if k is not None and k.dim() != 5:
             raise ValueError("expected queries and keys of one form")
@@ -424,9 +427,6 @@ def seq_rotary(q, k, positions, freqs, *, sections=None, q_weight=None, k_weight
         turned = seq_rotary(q.flatten(2, 3), None if k is None else k.flatten(2, 3), positions.flatten(-2), freqs, sections=sections, q_weight=q_weight, k_weight=k_weight, eps=eps,
                             interleaved=interleaved)
         return tuple(None if t is None else t.unflatten(2, shape) for t in turned)
-    out = _native().seq_rotary(q, k, positions, freqs, sections, q_weight, k_weight, eps, interleaved)
-    if out is not None:
-        return out if k is not None else (*out, None)
     if q.dim() != 4 or (k is not None and (k.dim() != 4 or k.shape[0] != q.shape[0] or k.shape[2:] != q.shape[2:])):
         raise ValueError("expected [B, heads, L, D] tensors of one B, L and D")
     if positions.dim() not in (2, 3):

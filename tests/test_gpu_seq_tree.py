@@ -91,13 +91,14 @@ def test_windows_and_long_ranges(window, page, n, heads):
 @pytest.mark.parametrize("D,page", [(32, 64), (64, 16), (128, 32), (128, 128)])
 @pytest.mark.parametrize("n,heads", [(31, 6), (12, 8), (33, 1), (64, 3), (64, 9)])   # 186, 96, 33, 192 and 576 rows
 @pytest.mark.parametrize("cap,window", [(None, None), (5.0, None), (1500.0, None), (None, 70), (5.0, 300)])
-def test_many_rows_to_a_key_head(dtype, D, page, n, heads, cap, window):
+@pytest.mark.parametrize("wide", [False, True])   # a table that may hold long sequences makes it a large call: tiles
+def test_many_rows_to_a_key_head(dtype, D, page, n, heads, cap, window, wide):
     g = np.random.default_rng(n + heads + D)
-    lengths = [700, 64, 0, 129]
-    table, pages = _table(g, lengths, page)
+    lengths = [700, 64, 0, 129] + [5] * (0 if window is None or not wide else 65536 // (window // 64 + 1) // (n * heads) - 3)
+    table, pages = _table(g, lengths, page, width=max(-(-700 // page), 65536 * 64 // (4 * n * heads * page) + 1) if wide else None)
     host, cache = _cache(g, pages, 1, page, D)
-    q, k, v = _inputs(g, 4, heads, 1, n, D, dtype)
-    parents = _parents(g, 4, n)
+    q, k, v = _inputs(g, len(lengths), heads, 1, n, D, dtype)
+    parents = _parents(g, len(lengths), n)
     slopes = torch.from_numpy(g.uniform(0, 0.1, heads).astype(np.float32)).cuda() if window == 300 else None
     scale = -0.1 if window == 70 else None   # a scale may be negative
     got = F.seq_cache_tree_attention(q, k, v, _int(parents.tolist()), cache, _int(table.tolist()), _int(lengths), softcap=cap, window=window, slopes=slopes, scale=scale)
@@ -108,7 +109,7 @@ def test_many_short_sequences():
     """More sequences than a wave has lanes, some of nothing: runs that hold several rows' work, and rows that several runs hold."""
     g = np.random.default_rng(13)
     lengths = [int(x) for x in g.integers(0, 300, 150)]
-    table, pages = _table(g, lengths, 16)
+    table, pages = _table(g, lengths, 16, width=40)
     host, cache = _cache(g, pages, 2, 16, 32)
     q, k, v = _inputs(g, 150, 6, 2, 20, 32, "f16")
     parents = _parents(g, 150, 20)
@@ -117,11 +118,11 @@ def test_many_short_sequences():
 
 
 @pytest.mark.parametrize("dtype", ["f16", "bf16"])
-@pytest.mark.parametrize("n", [5, 40])
-def test_what_is_no_node_may_be_anything(dtype, n):
+@pytest.mark.parametrize("n,width", [(5, None), (40, None), (40, 200)])   # few rows, many, and many of a large call
+def test_what_is_no_node_may_be_anything(dtype, n, width):
     g = np.random.default_rng(1)
     lengths = [100, 33, 0]
-    table, pages = _table(g, lengths, 32)
+    table, pages = _table(g, lengths, 32, width=width)
     host, cache = _cache(g, pages, 2, 32, 64)
     q, k, v = _inputs(g, 3, 8, 2, n, 64, dtype)
     parents = np.stack([[-1] + [0] * (n - 1), [-1, 0] + [-2] * (n - 2), [-2] + [0] * (n - 1)]).astype(np.int32)
@@ -145,7 +146,7 @@ def test_scales_far_apart_pages_that_are_none_and_never_written(page, n):
     q, k, v = _inputs(g, 3, 4, 2, n, 64, "bf16")
     results = []
     for behind in (-1, 5):   # behind the sequences
-        wide = np.concatenate([table, np.full((3, 2), behind, np.int32)], 1)
+        wide = np.concatenate([table, np.full((3, 2 if n == 3 else 8192 // page), behind, np.int32)], 1)
         cache = F.SeqCache(*(torch.from_numpy(x).cuda() for x in host))
         parents = np.tile(np.arange(-1, n - 1, dtype=np.int32), (3, 1))
         results.append(F.seq_cache_tree_attention(q, k, v, _int(parents.tolist()), cache, _int(wide.tolist()), _int(lengths)))
@@ -212,8 +213,8 @@ def test_same_bits_again_replayed_on_another_stream_and_interpreted():
         def __torch_function__(self, f, types, args=(), kwargs=None):
             return f(*args, **(kwargs or {}))
     g = np.random.default_rng(7)
-    for n in (5, 48):
-        table, pages = _table(g, [3000, 17], 16)
+    for n, width in ((5, None), (48, None), (48, 700)):   # few rows, many, and many of a large call
+        table, pages = _table(g, [3000, 17], 16, width=width)
         _, cache = _cache(g, pages, 2, 16, 128)
         q, k, v = _inputs(g, 2, 8, 2, n, 128, "bf16")
         args = (q, k, v, _int(_parents(g, 2, n).tolist()), cache, _int(table.tolist()), _int([2990, 10]))
@@ -238,10 +239,11 @@ def test_same_bits_again_replayed_on_another_stream_and_interpreted():
             assert torch.equal(out, eager)
 
 
-def test_pages_behind_32_bits():
+@pytest.mark.parametrize("n,width", [(5, 7), (20, 7), (20, 200)])   # few rows, many, and many of a large call
+def test_pages_behind_32_bits(n, width):
     g = np.random.default_rng(8)
-    kv, page, D, n = 8, 64, 128, 20
-    small_table, pages = _table(g, [400, 150], page, spare=0)
+    kv, page, D = 8, 64, 128
+    small_table, pages = _table(g, [400, 150], page, spare=0, width=width)
     _, small = _cache(g, pages, kv, page, D)
     far = 70000 - 1 - 3 * np.arange(pages)
     assert far.min() * kv * page * D > 1 << 32
