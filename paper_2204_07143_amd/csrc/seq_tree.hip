@@ -32,7 +32,7 @@ void plan_cache_tree(CacheArgs &a, int64_t longest, int D) {
     if (a.tiled) return plan_tree_tiles(a, longest, D);
     // There is a join in any case: parts of 128 tokens, where workgroups are few.
     plan_cache_attention(a, longest);
-    const int64_t units = (int64_t)a.B * a.kv * a.row_groups, wanted = (512 + units - 1) / units, most = reach / 128;
+    const int64_t units = (int64_t)a.B * a.kv * a.row_groups, wanted = (256 + units - 1) / units, most = reach / 128;
     const int64_t s = wanted < most ? wanted : most;
     a.splits = (int)(s > 128 ? 128 : s > a.splits ? s : a.splits) + 1;   // and the nodes' own part
 }

@@ -52,10 +52,12 @@ struct Schedule {
         runs = wanted < 1 ? 1 : wanted < p.splits ? (int)wanted : p.splits;
     }
     __device__ __forceinline__ Span span(const CacheArgs &p, int b) const { return Span(p, b < kWave ? __builtin_amdgcn_readlane(held, b) : p.lengths[b]); }   // b: the same in all lanes
-    __device__ __forceinline__ int64_t start(int run) const { return total * run / runs; }
+    // (in 64-bit floating point, a division of few instructions: products stay below 2^53, the quotient of the last is exact, and all that matters is that everybody cuts alike)
+    __device__ __forceinline__ int64_t start(int run) const { return (int64_t)((double)total * run / runs); }
     __device__ __forceinline__ int run_of(int64_t tile) const {
-        int w = (int)(tile * runs / total);
+        int w = (int)((double)tile * runs / (double)total);
         while (start(w + 1) <= tile) ++w;
+        while (start(w) > tile) --w;
         return w;
     }
     // The sequence that has `tile`, or (tile beyond what lies before it) the tiles before sequence b.
@@ -120,7 +122,7 @@ __global__ __launch_bounds__(kThreads, 2) void tree_tile_kernel(const CacheArgs 
     const Schedule schedule(p, lane);
     const int run = blockIdx.x;
     if (run >= schedule.runs) return;
-    const int64_t from = schedule.start(run), to = schedule.start(run + 1);
+    const int64_t from = uniform(schedule.start(run)), to = uniform(schedule.start(run + 1));
     int64_t before;
     int b = seq::uniform(schedule.find(p, from, lane, before));
     const int page = 1 << p.page_log2, all_rows = p.group * p.n;
@@ -136,7 +138,7 @@ __global__ __launch_bounds__(kThreads, 2) void tree_tile_kernel(const CacheArgs 
             before += (int64_t)span.tiles * schedule.units;
             span = span_of(++b);
         }
-        const int unit_id = (int)((at - before) / span.tiles), first = (int)((at - before) - (int64_t)unit_id * span.tiles);
+        const int unit_id = seq::uniform((int)((double)(at - before) / span.tiles)), first = (int)((at - before) - (int64_t)unit_id * span.tiles);
         const int count = (int)min(to - at, (int64_t)(span.tiles - first)), kh = unit_id / p.row_groups, row0 = unit_id % p.row_groups * ROWS + wave * 16 * RB;
         const bool whole = count == span.tiles;
         // where the cache's tiles lie, and the first one's bytes, on their way from here on
@@ -280,6 +282,7 @@ __global__ __launch_bounds__(kThreads, 2) void tree_tile_kernel(const CacheArgs 
                 f32x4 s[RB][2];
 #pragma unroll
                 for (int n = 0; n < RB; ++n) s[n][0] = s[n][1] = f32x4{0.f, 0.f, 0.f, 0.f};
+                __builtin_amdgcn_s_setprio(1);
 #pragma unroll
                 for (int st = 0; st < STEPS; ++st) {
                     if (st + AHEAD < STEPS) read_keys(st + AHEAD);
@@ -289,6 +292,7 @@ __global__ __launch_bounds__(kThreads, 2) void tree_tile_kernel(const CacheArgs 
                         for (int n = 0; n < RB; ++n) s[n][i] = mma<f16_t>(a[st % (AHEAD + 1)][i], q[n][st], s[n][i]);
                     if constexpr (RB == 3) __builtin_amdgcn_sched_barrier(0);
                 }
+                __builtin_amdgcn_s_setprio(0);
 #pragma unroll
                 for (int db = 0; db < VAHEAD; ++db) read_values(db);
                 __builtin_amdgcn_sched_barrier(0);
@@ -323,6 +327,7 @@ __global__ __launch_bounds__(kThreads, 2) void tree_tile_kernel(const CacheArgs 
                     weigh(n, s[n], by, plus, o2);
                     w[n] = pack<f16_t>(s[n]);
                 }
+                __builtin_amdgcn_s_setprio(1);
 #pragma unroll
                 for (int db = 0; db < DB; ++db) {
 #pragma unroll
@@ -330,6 +335,7 @@ __global__ __launch_bounds__(kThreads, 2) void tree_tile_kernel(const CacheArgs 
                     if (db + VAHEAD < DB) read_values(db + VAHEAD);
                     if constexpr (RB == 3) __builtin_amdgcn_sched_barrier(0);
                 }
+                __builtin_amdgcn_s_setprio(0);
             }
             if (t + 1 < cached && !known) {
                 look_up(span.begin + first + t + 1);
