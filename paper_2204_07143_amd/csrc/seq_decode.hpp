@@ -116,12 +116,58 @@ struct Tree {
         above[tid] = bad ? 0 : mine;
         depth[tid] = __builtin_popcountll(mine) - 1;
     }
+    // the nodes that node i sees
+    __device__ __forceinline__ uint64_t seen(int i, int window) const {
+        uint64_t all = above[i];
+        if (depth[i] >= window)
+            for (uint64_t left = all; left; left &= left - 1) {
+                const int k = __builtin_ctzll(left);
+                if (depth[i] - depth[k] >= window) all &= ~(1ull << k);
+            }
+        return all;
+    }
+};
+
+// Values of nodes that are infinite or no numbers, which would reach the rows that do not see them as 0 times them.  Products have 0 in their place; for each channel the nodes
+// with such a value are bits, and rows that see one get what it is.
+template <int D> struct Wild {
+    uint64_t up[D], down[D];   // infinite; no numbers: both
+    int any;
+    __device__ __forceinline__ void clear(int tid) {
+        for (int d = tid; d < D; d += kThreads) up[d] = down[d] = 0;
+        if (tid == 0) any = 0;
+    }
+    // w: the node's values from `channel` on, two to a word; true where it is changed
+    template <typename T, class Words> __device__ __forceinline__ bool take(Words &w, int count, int node, int channel) {
+        constexpr uint32_t kStep = __is_same(T, f16_t) ? 0x04000400u : 0x00800080u;   // of the exponent
+        uint32_t bad = 0;
+#pragma unroll
+        for (int i = 0; i < count; ++i) bad |= ((w[i] & 0x7fff7fffu) + kStep) & 0x80008000u;
+        if (!bad) return false;
+        any = 1;
+#pragma unroll
+        for (int i = 0; i < count; ++i)
+#pragma unroll
+            for (int half = 0; half < 2; ++half) {
+                const uint32_t x = w[i] >> 16 * half;
+                if (!(((x & 0x7fffu) + (kStep & 0xffffu)) & 0x8000u)) continue;
+                const bool number = !(x & 0x7fffu & ~(0x8000u - (kStep & 0xffffu))), minus = x & 0x8000u;
+                if (!number || !minus) atomicOr((unsigned long long *)&up[channel + 2 * i + half], 1ull << node);
+                if (!number || minus) atomicOr((unsigned long long *)&down[channel + 2 * i + half], 1ull << node);
+                w[i] &= 0xffffu << 16 * (1 - half);
+            }
+        return true;
+    }
+    __device__ __forceinline__ float of(float x, int channel, uint64_t seen) const {
+        const bool plus = up[channel] & seen, minus = down[channel] & seen;
+        return plus && minus ? NAN : plus ? INFINITY : minus ? -INFINITY : x;
+    }
 };
 
 // The nodes' own part of a row's attention, 16 keys to a wave, products in the type of q.  In bfloat16 weights are the sum of two of them, 2^-17 off at most: no less exact than
 // the cache's, in fp16.
 template <typename T, int D, int RT, int CAP>
-__device__ __forceinline__ void attend_nodes(const CacheArgs &p, const Tree &tree, int b, int kh, int row0, int wave, int lane, const float (&slope)[RT], f32x4 (&out)[RT][D / 16], float (&ref)[RT],
+__device__ __forceinline__ void attend_nodes(const CacheArgs &p, const Tree &tree, Wild<D> &wild, int b, int kh, int row0, int wave, int lane, const float (&slope)[RT], f32x4 (&out)[RT][D / 16], float (&ref)[RT],
                                              float (&sum)[RT]) {
     constexpr int STEPS = D / 32, DB = D / 16;
     const int j = lane & 15, g = lane >> 4, all_rows = p.group * p.n, key = min(16 * wave + j, p.n - 1);
@@ -137,14 +183,16 @@ __device__ __forceinline__ void attend_nodes(const CacheArgs &p, const Tree &tre
         const uint32_t *from = reinterpret_cast<const uint32_t *>(p.tv.at + b * p.tv.b + kh * p.tv.h + (int64_t)min(at, p.n - 1) * p.tv.row + DB * j * 2);
 #pragma unroll
         for (int i = 0; i < DB / 2; ++i) v[e][i] = there ? from[i] : 0u;
+        wild.template take<T>(v[e], DB / 2, at, DB * j);
     }
 #pragma unroll
     for (int n = 0; n < RT; ++n) {
         const int row = min(row0 + 16 * n + j, all_rows - 1), h = kh * p.group + row / p.n, i = row % p.n;
         const char *at = p.a.at + b * p.a.b + h * p.a.h + (int64_t)i * p.a.row;
-        f32x4 s{0.f, 0.f, 0.f, 0.f};
+        f32x4 products[1] = {{0.f, 0.f, 0.f, 0.f}}, &s = products[0];
 #pragma unroll
         for (int st = 0; st < STEPS; ++st) s = mma<T>(k[st], *reinterpret_cast<const u32x4 *>(at + (32 * st + 8 * g) * 2), s);
+        settle_products(products);
         const uint64_t seen = tree.above[i] >> (16 * wave + 4 * g);
         float most = -INFINITY;
 #pragma unroll
@@ -190,7 +238,9 @@ __global__ __launch_bounds__(kThreads, RT == 1 ? 3 : 2) void decode_kernel(const
     __shared__ __align__(16) float parts[kWaves][16][D + 4];
     __shared__ float refs[kWaves][ROWS], sums[kWaves][ROWS];
     __shared__ __align__(16) char tree_at[TREE ? sizeof(Tree) : 16];
+    __shared__ __align__(16) char wild_at[TREE ? sizeof(Wild<D>) : 16];
     Tree &tree = *reinterpret_cast<Tree *>(tree_at);
+    Wild<D> &wild = *reinterpret_cast<Wild<D> *>(wild_at);
     const int tid = threadIdx.x, lane = tid % kWave, wave = uniform(tid / kWave), j = lane & 15, g = lane >> 4;
     int id = blockIdx.x;
     const int split = id % p.splits;
@@ -204,6 +254,7 @@ __global__ __launch_bounds__(kThreads, RT == 1 ? 3 : 2) void decode_kernel(const
     const int first_query = TREE ? tokens : tokens - p.n, ranges = TREE ? p.splits - 1 : p.splits;
     if constexpr (TREE) {
         tree.build(p.parents + (int64_t)b * p.n, p.n, tid);
+        wild.clear(tid);
         workgroup_sync();
     }
 
@@ -255,7 +306,7 @@ __global__ __launch_bounds__(kThreads, RT == 1 ? 3 : 2) void decode_kernel(const
     // entry, or the first page's scales, and takes nothing from them: without branches the reads are on their way together.  Of a step's two pages one may hold
     // no token that is seen: its entry and its scale may be anything (a weight of 0 times a scale that is NaN would be NaN), and it is none.
     if constexpr (TREE)
-        if (split == ranges) attend_nodes<T, D, RT, CAP>(p, tree, b, kh, row0, wave, lane, slope, out, ref, sum);
+        if (split == ranges) attend_nodes<T, D, RT, CAP>(p, tree, wild, b, kh, row0, wave, lane, slope, out, ref, sum);
     constexpr int PAGES = PAGE16 ? 2 : 1;
     int unit[PAGES];
     float ks[PAGES], vs[PAGES];
@@ -445,6 +496,12 @@ __global__ __launch_bounds__(kThreads, RT == 1 ? 3 : 2) void decode_kernel(const
             float x[8];
 #pragma unroll
             for (int e = 0; e < 8; ++e) x[e] = parts[0][r][d + e] + parts[1][r][d + e] + parts[2][r][d + e] + parts[3][r][d + e];
+            if constexpr (TREE)
+                if (wild.any) {
+                    const uint64_t seen = tree.seen(row % p.n, p.window);
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) x[e] = wild.of(x[e], d + e, seen);
+                }
             if (p.splits == 1) {
                 const float by_sum = total == 0.f ? 0.f : 1.f / total;
 #pragma unroll

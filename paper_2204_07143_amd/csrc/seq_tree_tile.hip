@@ -117,35 +117,37 @@ __global__ __launch_bounds__(kThreads, 2) void tree_tile_kernel(const CacheArgs 
     constexpr int ROWS = 16 * RB * kWaves, STEPS = L::STEPS, DB = L::DB;
     extern __shared__ __align__(16) char lds[];
     __shared__ Tree tree;
+    __shared__ Wild<D> wild;
     __shared__ int2 row_info[ROWS];   // position, and slope as bits
     const int tid = threadIdx.x, lane = tid % kWave, wave = seq::uniform(tid / kWave), g = lane >> 4, img = lds_addr(lds);
     const Schedule schedule(p, lane);
     const int run = blockIdx.x;
     if (run >= schedule.runs) return;
-    const int64_t from = uniform(schedule.start(run)), to = uniform(schedule.start(run + 1));
-    int64_t before;
-    int b = seq::uniform(schedule.find(p, from, lane, before));
+    int64_t at = uniform(schedule.start(run)), left = uniform(schedule.start(run + 1)) - at, before;   // at: from here on, of the sequence's tiles
+    int b = seq::uniform(schedule.find(p, at, lane, before));
+    at -= before;
     const int page = 1 << p.page_log2, all_rows = p.group * p.n;
     const typename L::RowReader rows(lane);
     const typename L::ColumnReader columns(lane);
     int built = -1;
+    wild.clear(tid);
 
 #pragma unroll 1
-    for (int64_t at = from; at < to;) {
+    for (bool begun = false; left > 0; begun = true) {
         auto span_of = [&](int b) { return RB == 3 ? Span(p, p.lengths[b]) : schedule.span(p, b); };   // (three blocks: the registers)
         Span span = span_of(b);
-        while (at >= before + (int64_t)span.tiles * schedule.units) {
-            before += (int64_t)span.tiles * schedule.units;
+        while (at >= (int64_t)span.tiles * schedule.units) {
+            at -= (int64_t)span.tiles * schedule.units;
             span = span_of(++b);
         }
-        const int unit_id = seq::uniform((int)((double)(at - before) / span.tiles)), first = (int)((at - before) - (int64_t)unit_id * span.tiles);
-        const int count = (int)min(to - at, (int64_t)(span.tiles - first)), kh = unit_id / p.row_groups, row0 = unit_id % p.row_groups * ROWS + wave * 16 * RB;
+        const int unit_id = seq::uniform((int)((double)at / span.tiles)), first = (int)(at - (int64_t)unit_id * span.tiles);
+        const int count = (int)min(left, (int64_t)(span.tiles - first)), kh = unit_id / p.row_groups, row0 = unit_id % p.row_groups * ROWS + wave * 16 * RB;
         const bool whole = count == span.tiles;
         // where the cache's tiles lie, and the first one's bytes, on their way from here on
         const int cached = min(count, span.tiles - 1 - first);   // of this run
         const int pieces = page >= kTile ? 1 : kTile / page, shift = page >= kTile ? 2 : p.page_log2 - 4, chunk = kWave / pieces;   // of a tile: pages, and 16-token blocks to one
         int unit = -1;                // of one of the next 64 pieces: its page, and of that
-        float ks = 0.f, lv = 0.f, over = 0.f;   // the keys' scale, the values' in base 2, and one over it
+        float ks = 0.f, lv = 0.f;   // the keys' scale, the values' in base 2
         auto look_up = [&](int tile) {
             const int size = kTile / pieces;
             const int64_t token = (int64_t)tile * kTile + (int64_t)size * lane;
@@ -154,7 +156,7 @@ __global__ __launch_bounds__(kThreads, 2) void tree_tile_kernel(const CacheArgs 
             unit = seen && (unsigned)id < (unsigned)p.pages ? id : -1;
             const int64_t u = (int64_t)max(unit, 0) * p.kv + kh;
             const float k = p.ks[u], v = fmaxf(p.vs[u], 0x1p-100f);   // (values of a scale of 0 are 0: their weights count)
-            ks = unit < 0 ? 0.f : k, lv = unit < 0 ? 0.f : __builtin_amdgcn_logf(v), over = unit < 0 ? 0.f : 1.f / v;
+            ks = unit < 0 ? 0.f : k, lv = unit < 0 ? 0.f : __builtin_amdgcn_logf(v);
         };
         auto lane_of = [](float x, int l) { return __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(x), l)); };
         B keys, values;
@@ -266,10 +268,10 @@ __global__ __launch_bounds__(kThreads, 2) void tree_tile_kernel(const CacheArgs 
 #pragma unroll
                 for (int i = 0; i < 2; ++i) {
                     const int from = slot + ((2 * half + i) >> shift);
-                    k2[i] = lane_of(ks, from), l2[i] = lane_of(lv, from), o2[i] = lane_of(over, from);
+                    k2[i] = lane_of(ks, from), l2[i] = lane_of(lv, from), o2[i] = __builtin_amdgcn_exp2f(-l2[i]);
                 }
-                // reads of LDS on their way ahead of the products that take them: all of a half's, or where the registers are full the next
-                constexpr int AHEAD = RB < 3 ? STEPS : 1, VAHEAD = RB < 3 ? DB : 2;
+                // reads of LDS on their way ahead of the products that take them: all of a half's, or where the registers are full the next, or with a cap none of the keys
+                constexpr int AHEAD = RB < 3 ? STEPS : CAP ? 0 : 1, VAHEAD = RB < 3 ? DB : 2;
                 u32x4 a[AHEAD + 1][2], v[VAHEAD];
                 auto read_keys = [&](int st) {
 #pragma unroll
@@ -359,6 +361,12 @@ __global__ __launch_bounds__(kThreads, 2) void tree_tile_kernel(const CacheArgs 
                 *lds_ptr<u32x4>(ki + place) = x;
                 *lds_ptr<u32x4>(vi + place) = y;
             }
+#pragma unroll 1
+            for (int id = tid; id < kNodes * N::CH; id += kThreads) {   // (this thread's own, once more: the registers)
+                const int r = id / N::CH, ch = id % N::CH, place = vi + r * N::ROWB + (ch ^ N::swizzle(r)) * 16;
+                u32x4 y = *lds_ptr<u32x4>(place);
+                if (wild.template take<T>(y, 4, r, 8 * ch)) *lds_ptr<u32x4>(place) = y;
+            }
             workgroup_sync();
 #pragma unroll
             for (int n = 0; n < RB; ++n) {
@@ -405,7 +413,7 @@ __global__ __launch_bounds__(kThreads, 2) void tree_tile_kernel(const CacheArgs 
 
         // ---- this run's rows
         const int lane = afresh(threadIdx.x) % kWave, j = lane & 15, g = lane >> 4;
-        const int place = at == from ? 2 * run : 2 * run + 1;
+        const int place = 2 * run + begun;
         float *parts = p.part + (int64_t)place * ROWS * D, *stats = p.part + (int64_t)p.splits * 2 * ROWS * D + (int64_t)place * ROWS * 2;
 #pragma unroll
         for (int n = 0; n < RB; ++n) {
@@ -414,6 +422,15 @@ __global__ __launch_bounds__(kThreads, 2) void tree_tile_kernel(const CacheArgs 
             float total = column_sum(sum[n]);
             if (row >= all_rows) continue;
             const bool node = tree.above[row % p.n] != 0;
+            if (wild.any) {
+                const uint64_t seen = tree.seen(row % p.n, p.window);
+#pragma unroll
+                for (int db = 0; db < DB; ++db) {
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) out[n][db][r] = wild.of(out[n][db][r], 16 * db + 4 * g + r, seen);
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+            }
             if (!node) total = 0.f;   // whatever its query is
             if (whole) {
                 const int h = kh * p.group + row / p.n;
@@ -432,7 +449,11 @@ __global__ __launch_bounds__(kThreads, 2) void tree_tile_kernel(const CacheArgs 
                 if (g == 0) reinterpret_cast<float2 *>(stats)[in_unit] = float2{node ? ref[n] : kLowest, total};
             }
         }
-        at += count;
+        if (wild.any) {
+            workgroup_sync();
+            wild.clear(afresh(threadIdx.x));
+        }
+        at += count, left -= count;
     }
 }
 

@@ -134,6 +134,39 @@ def test_what_is_no_node_may_be_anything(dtype, n, width):
     assert (got[2] == 0).all() and (got[1, :, 2:] == 0).all() and torch.isfinite(got).all()
 
 
+@pytest.mark.parametrize("dtype,D", [("f16", 128), ("bf16", 64), ("bf16", 128), ("f16", 32)])
+@pytest.mark.parametrize("n,width,window", [(5, None, None), (40, None, 3), (40, 400, None), (40, 400, 3)])
+def test_values_that_are_no_numbers_reach_the_rows_that_see_them_alone(dtype, D, n, width, window):
+    """Products have 0 where a value is infinite or none: the other rows keep their bits."""
+    g = np.random.default_rng(21)
+    lengths = [100, 0, 33]
+    table, pages = _table(g, lengths, 32, width=width)
+    host, cache = _cache(g, pages, 2, 32, D)
+    q, k, v = _inputs(g, 3, 8, 2, n, D, dtype)
+    parents = np.stack([[-1] + [(i - 1) // 2 for i in range(1, n)], np.arange(-1, n - 1), [-1] + [max(i - 2, 0) for i in range(1, n)]]).astype(np.int32)
+    wild = {(1, 0): "inf", (2, 7): "-inf", (3, 7): "nan", (4, D - 1): "inf", (n - 2, 9): "-inf"}
+    for (node, channel) in wild:
+        v[:, :, node, channel] = 0
+    call = lambda k, v: F.seq_cache_tree_attention(q, k, v, _int(parents.tolist()), cache, _int(table.tolist()), _int(lengths), window=window)
+    clean = call(k, v)
+    _check(clean, q, k, v, parents, host, table, lengths, dtype, window=window)
+    expected, bad, all_of = clean.clone(), v.clone(), clean.clone()
+    for b in range(3):
+        see = seq_oracle.tree(None, None, None, parents[b].tolist(), np.zeros(0, bool), 0, window)[0]
+        for (node, channel), x in wild.items():
+            rows = torch.from_numpy(see[:, node].astype(bool)).cuda()
+            expected[b, :, rows, channel] += float(x)
+            all_of[b, :, rows] = float("nan") if node == 2 else all_of[b, :, rows]
+    for (node, channel), x in wild.items():
+        bad[:, :, node, channel] = float(x)
+    got = call(k, bad)
+    assert torch.equal(got.isnan(), expected.isnan()) and torch.equal(got.nan_to_num(nan=0.0, posinf=1e4, neginf=-1e4), expected.nan_to_num(nan=0.0, posinf=1e4, neginf=-1e4))
+    bad = k.clone()
+    bad[:, :, 2, 3] = float("nan")
+    got = call(bad, v)
+    assert torch.equal(got.isnan(), all_of.isnan()) and torch.equal(got.nan_to_num(nan=0.0), all_of.nan_to_num(nan=0.0))
+
+
 @pytest.mark.parametrize("page", [16, 64])
 @pytest.mark.parametrize("n", [3, 40])
 def test_scales_far_apart_pages_that_are_none_and_never_written(page, n):
