@@ -30,7 +30,8 @@ void plan_cache_tree(CacheArgs &a, int64_t longest, int D) {
     const int64_t rows = (int64_t)a.group * a.n, reach = longest < (int64_t)a.window ? longest : (int64_t)a.window, tiles = (int64_t)a.B * a.kv * ((reach + kTile - 1) / kTile);
     a.tiled = rows > 32 && (double)tiles * rows >= 65536;
     if (a.tiled) return plan_tree_tiles(a, longest, D);
-    // There is a join in any case: parts of 128 tokens, where workgroups are few.
+    // There is a join in any case: parts of 128 tokens, where workgroups are few (fewer than the 256 compute units: 5 sequences, 12 heads over 4, 27 nodes, window 2048, capped, 17 + 4 us, up to 512
+    // workgroups 21 + 4).
     plan_cache_attention(a, longest);
     const int64_t units = (int64_t)a.B * a.kv * a.row_groups, wanted = (256 + units - 1) / units, most = reach / 128;
     const int64_t s = wanted < most ? wanted : most;
