@@ -6,7 +6,7 @@
 // again.  The nodes' own keys and values are the last tile of a row's work.
 //
 // Bound by the vector instructions (half of the cycles) and the products (a quarter), which two waves to a SIMD lay over each other in part; waves wait 26 % of their time.  192 rows of 128
-// channels fill the registers.  16 sequences to 8000 tokens, 48 nodes, 32 heads over 8, D 128, bf16: 124 us, 0.49 PFLOP/s of products, and the join 16 (up to 100 MB of sums); 225 in workgroups
+// channels fill the registers.  16 sequences to 8000 tokens, 48 nodes, 32 heads over 8, D 128, bf16: 124 us, 0.49 PFLOP/s of products, and the join 14 (64 MB of sums; 16 with a workgroup for each 8 rows); 225 in workgroups
 // of 32 rows that each make fp16 of all bytes (seq_decode.hpp); 64 and 128 rows to a workgroup 168 and 163; 126 without the products' priority over another wave's softmax.
 //
 // The tiles of all sequences and key heads, in a row, are shared evenly by the workgroups, wherever the cuts fall: a run that has all of a row's tiles stores its result, others
@@ -461,42 +461,52 @@ __global__ __launch_bounds__(kThreads, 2) void tree_tile_kernel(const CacheArgs 
     }
 }
 
-// The runs of a row that several have, in order: a thread per four channels.
+// The runs of a row that several have, in order: a thread per four channels, of several rows (finding a unit's runs takes longer than a row's sums).
+template <int D, int RB> struct Joined {
+    static constexpr int ROWS = 16 * RB * kWaves, COLS = D / 4, EACH = kThreads / COLS, TIMES = RB, BLOCKS = ROWS / EACH / TIMES;   // of a unit
+    static_assert(BLOCKS * EACH * TIMES == ROWS, "rows of a unit");
+};
 template <typename T, int D, int RB>
 __global__ __launch_bounds__(kThreads) void tree_join_kernel(const CacheArgs p) {
-    constexpr int ROWS = 16 * RB * kWaves, COLS = D / 4, EACH = kThreads / COLS;
-    const int lane = threadIdx.x % kWave, col = threadIdx.x % COLS, blocks = ROWS / EACH;
-    const int in_unit = (int)(blockIdx.x % blocks) * EACH + threadIdx.x / COLS;
-    const int unit = (int)(blockIdx.x / blocks) % (p.kv * p.row_groups), b = (int)(blockIdx.x / blocks) / (p.kv * p.row_groups);
-    const int row = unit % p.row_groups * ROWS + in_unit, kh = unit / p.row_groups;
+    using J = Joined<D, RB>;
+    constexpr int ROWS = J::ROWS;
+    const int lane = threadIdx.x % kWave, col = threadIdx.x % J::COLS;
+    const int unit = (int)(blockIdx.x / J::BLOCKS) % (p.kv * p.row_groups), b = (int)(blockIdx.x / J::BLOCKS) / (p.kv * p.row_groups);
     const Schedule schedule(p, lane);
     const int tiles = schedule.span(p, b).tiles;
     const int64_t first = schedule.tiles_before(p, b, lane) + (int64_t)unit * tiles;
-    const int from = schedule.run_of(first), to = schedule.run_of(first + tiles - 1);
-    if (from == to || row >= p.group * p.n) return;
-    const float2 *stats = reinterpret_cast<const float2 *>(p.part + (int64_t)p.splits * 2 * ROWS * D) + in_unit;
-    float m = kLowest, sum = 0.f;
-    f32x4 x{0.f, 0.f, 0.f, 0.f};
+    const int from = seq::uniform(schedule.run_of(first)), to = seq::uniform(schedule.run_of(first + tiles - 1));
+    if (from == to) return;
+    const int begun = seq::uniform((int)(schedule.start(from) < first));   // the first run had another row's work before
+    const int kh = unit / p.row_groups;
+#pragma unroll 1
+    for (int i = 0; i < J::TIMES; ++i) {
+        const int in_unit = ((int)(blockIdx.x % J::BLOCKS) * J::TIMES + i) * J::EACH + threadIdx.x / J::COLS, row = unit % p.row_groups * ROWS + in_unit;
+        if (row >= p.group * p.n) return;
+        const float2 *stats = reinterpret_cast<const float2 *>(p.part + (int64_t)p.splits * 2 * ROWS * D) + in_unit;
+        float m = kLowest, sum = 0.f;
+        f32x4 x{0.f, 0.f, 0.f, 0.f};
 #pragma unroll 4
-    for (int run = from; run <= to; ++run) {
-        const int64_t place = schedule.start(run) >= first ? 2 * run : 2 * run + 1;
-        const float2 st = stats[place * ROWS];
-        const f32x4 y = *reinterpret_cast<const f32x4 *>(p.part + (place * ROWS + in_unit) * D + col * 4);
-        const float now = fmaxf(m, st.x), old = __builtin_amdgcn_exp2f(m - now), by = __builtin_amdgcn_exp2f(st.x - now);
-        m = now, sum = sum * old + st.y * by, x = x * old + y * by;
+        for (int run = from; run <= to; ++run) {
+            const int64_t place = 2 * run + (run == from ? begun : 0);
+            const float2 st = stats[place * ROWS];
+            const f32x4 y = *reinterpret_cast<const f32x4 *>(p.part + (place * ROWS + in_unit) * D + col * 4);
+            const float now = fmaxf(m, st.x), old = __builtin_amdgcn_exp2f(m - now), by = __builtin_amdgcn_exp2f(st.x - now);
+            m = now, sum = sum * old + st.y * by, x = x * old + y * by;
+        }
+        const int h = kh * p.group + row / p.n;
+        Tile<T, D>::store4(const_cast<char *>(p.b.at) + b * p.b.b + h * p.b.h + (int64_t)(row % p.n) * p.b.row + col * 4 * (int)sizeof(T), x * (sum == 0.f ? 0.f : 1.f / sum));
     }
-    const int h = kh * p.group + row / p.n;
-    Tile<T, D>::store4(const_cast<char *>(p.b.at) + b * p.b.b + h * p.b.h + (int64_t)(row % p.n) * p.b.row + col * 4 * (int)sizeof(T), x * (sum == 0.f ? 0.f : 1.f / sum));
 }
 
 template <typename T, int D, int CAP> struct TreeTile {
     template <int RB> static hipError_t launch(const CacheArgs &a, hipStream_t st) {
-        constexpr int lds = 4 * Tile<f16_t, D>::BYTES, each = kThreads / (D / 4);
+        constexpr int lds = 4 * Tile<f16_t, D>::BYTES;
         static LdsAllowed allowed;
         if (hipError_t e = allow_lds(tree_tile_kernel<T, D, RB, CAP>, lds, allowed); e != hipSuccess) return e;
         tree_tile_kernel<T, D, RB, CAP><<<(unsigned)a.splits, kThreads, lds, st>>>(a);
         if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
-        const int64_t joins = (int64_t)a.B * a.kv * a.row_groups * (16 * RB * kWaves / each);
+        const int64_t joins = (int64_t)a.B * a.kv * a.row_groups * Joined<D, RB>::BLOCKS;
         if (!launch_holds(joins, kThreads)) return hipErrorInvalidValue;
         tree_join_kernel<T, D, RB><<<(unsigned)joins, kThreads, 0, st>>>(a);
         return hipGetLastError();
