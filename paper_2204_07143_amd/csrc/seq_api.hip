@@ -201,7 +201,7 @@ struct VerifySpace {
     VerifySpace(const VerifyArgs &a) {
         behind = (int64_t)sizeof(PartStats) * a.B * (a.drafted ? 2 * a.n - 1 : a.n) * a.parts;
         tickets = behind + (a.drafted ? (int64_t)sizeof(double) * a.B * a.parts : (int64_t)sizeof(int) * a.B * a.n);
-        bytes = tickets + (int64_t)sizeof(int) * a.B * (a.drafted ? 1 : a.n + 1);
+        bytes = tickets + (int64_t)sizeof(int) * kTicket * a.B * (a.drafted ? 1 : a.n + 1);
     }
 };
 

@@ -10,7 +10,7 @@
 // max(p - q, 0) there, and its last workgroup draws from them.
 //
 // The floor is reading the logits once; an element's 14 instructions in 64 bits and about as many others are 60 % of the cycles, and at the end of a row comes the latency of the last workgroup.  16 x 48 rows of 131072,
-// bf16: 90 us (2.2 TB/s) and 4.6 for the tickets' zeros; 130 with the library's exponential and rows' draws in launches of their own.  24 lines of 8 in fp32, 50021: 22 + 21; one of 6 in fp16,
+// bf16: 90 us (2.2 TB/s) and 4.6 for the tickets' zeros; 130 with the library's exponential and rows' draws in launches of their own.  24 lines of 8 in fp32, 50021: 22 + 16; one of 6 in fp16,
 // 32000: 5 + 11, dependent reads.
 #include "seq_verify.hpp"
 
@@ -303,7 +303,7 @@ template <typename T> struct Plain {
 // Zeros: the tickets of a tree's rows and sequences.
 __global__ __launch_bounds__(kThreads) void tickets_kernel(int *tickets, int count) {
     const int at = blockIdx.x * kThreads + threadIdx.x;
-    if (at < count) tickets[at] = 0;
+    if (at < count) tickets[(int64_t)at * kTicket] = 0;
 }
 
 // Tree: from node 0 on, by a wave, a node to a lane.
@@ -342,7 +342,7 @@ __global__ __launch_bounds__(kThreads) void tree_kernel(const VerifyArgs p) {
         const PartStats s = part_stats<T, U>(r, part, t, lane);
         if (lane == 0) leave(stats + part, s);
     }
-    if (!last_of(p.tickets + row, groups)) return;
+    if (!last_of(p.tickets + (int64_t)row * kTicket, groups)) return;
     if (tid < kWave) {
         const RowStats<kWave, true> s(stats, p.parts, t, lane);
         double before = 0.0, target = 0.0;
@@ -360,7 +360,7 @@ __global__ __launch_bounds__(kThreads) void tree_kernel(const VerifyArgs p) {
         token = find_token<T, U>(r, token, shared[0], shared[1], Plain<T>{r, most, t.weight});
     }
     if (tid == 0) leave(p.drawn + row, token);
-    if (last_of(p.tickets + (int64_t)p.B * p.n + b, p.n) && tid < kWave) walk(p, b, lane);
+    if (last_of(p.tickets + ((int64_t)p.B * p.n + b) * kTicket, p.n) && tid < kWave) walk(p, b, lane);
 }
 
 // Line: a part of a row of the target, or of the draft.
@@ -381,7 +381,7 @@ __global__ __launch_bounds__(kThreads) void stats_kernel(const VerifyArgs p) {
     const PartStats s = part_stats<T, U>(r, part, t, lane);
     if (lane == 0) {
         *to = s;
-        if (!of_draft && i == 0 && part == 0) p.tickets[b] = 0;
+        if (!of_draft && i == 0 && part == 0) p.tickets[(int64_t)b * kTicket] = 0;
     }
 }
 
@@ -468,7 +468,7 @@ __global__ __launch_bounds__(kThreads) void line_kernel(const VerifyArgs p) {
     if (lane == 0) sums[wave] = sum;
     workgroup_sync();
     if (tid == 0) leave(parts + part, (sums[0] + sums[1]) + (sums[2] + sums[3]));
-    if (!last_of(p.tickets + b, p.parts)) return;
+    if (!last_of(p.tickets + (int64_t)b * kTicket, p.parts)) return;
     if (tid < kWave) {
         const double mine = lane < p.parts ? take(parts + lane) : 0.0;
         double all = mine, before;
@@ -505,7 +505,7 @@ template <typename T> hipError_t verify(const VerifyArgs &a, hipStream_t st) { r
 
 }  // namespace
 
-// Parts of four blocks (two: 98 us for 90 at 16 x 48 rows of 131072, bf16; eight: 106), or of one where that leaves compute units without work (24 lines of 8 in fp32, 50021: 44 us for 48).  A
+// Parts of four blocks (two: 98 us for 90 at 16 x 48 rows of 131072, bf16; eight: 106), or of one where that leaves compute units without work (24 lines of 8 in fp32, 50021: 4 us less).  A
 // part is kThreads chunks for each of its blocks.
 void plan_verify(VerifyArgs &a, int dtype) {
     static_assert(kThreads == kWave * kChunks, "a workgroup that looks for a token in a part gives each thread `blocks` chunks");
