@@ -104,6 +104,25 @@ def test_rows_alone_are_the_plain_append_of_those_rows(dtype, page, D):
     _same(cache, host)
 
 
+def test_pages_behind_32_bits():
+    g = np.random.default_rng(12)
+    kv, page, D, lengths = 8, 64, 128, [60, 0]
+    small_table, pages = _table(g, [x + 70 for x in lengths], page, spare=0)
+    _, small = _cache(g, pages, kv, page, D)
+    far = 70000 - 1 - 3 * np.arange(pages)
+    assert far.min() * kv * page * D > 1 << 32
+    where = torch.from_numpy(far).cuda()
+    large = F.SeqCache(*(torch.empty((70000, *x.shape[1:]), dtype=x.dtype, device="cuda") for x in small))
+    for a, b in zip(large, small):
+        a[where] = b
+    k, v = (normal(g, (2, kv, 70, D), "bf16") for _ in range(2))
+    freqs = torch.tensor([0.9 ** i for i in range(32)], device="cuda")
+    for cache, table in ((small, small_table), (large, np.where(small_table >= 0, far[np.maximum(small_table, 0)], -1))):
+        F.seq_cache_append(cache, k, v, _int(table.tolist()), _int(lengths), freqs=freqs)
+    for a, b in zip(large, small):
+        assert torch.equal(a[where], b)
+
+
 def test_more_rows_than_given():
     g = np.random.default_rng(3)
     host, cache = _cache(g, 4, 1, 16, 64)

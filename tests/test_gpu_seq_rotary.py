@@ -129,6 +129,22 @@ def test_strides_and_broadcast_gradients():
     _compare("f16", odd, normal(g, (2, 5, 13, 130), "f16")[..., ::2][..., 1:], positions, _freqs(32), None, *w)
 
 
+def test_tensors_behind_32_bits():
+    g = np.random.default_rng(11)
+    near = [normal(g, (2, 3, 7, 64), "f16") for _ in range(2)]
+    far = [torch.empty((1 << 31) + 3 * 7 * 64, dtype=torch.float16, device="cuda").as_strided((2, 3, 7, 64), (1 << 31, 7 * 64, 64, 1)) for _ in near]
+    for a, b in zip(far, near):
+        a.copy_(b)
+    positions, w = torch.arange(7, dtype=torch.int32, device="cuda")[None], _weights(g, 64, "f16")[0].requires_grad_()
+    results = []
+    for q, dz in (near, far):
+        q = q.detach().requires_grad_()
+        z = F.seq_rotary(q, None, positions, _freqs(32), q_weight=w)[0]
+        results.append((z, *torch.autograd.grad(z, (q, w), dz)))
+    for a, b in zip(*results):
+        assert torch.equal(a, b)
+
+
 def test_nothing_to_do():
     w = torch.ones(64, device="cuda", requires_grad=True)
     q = torch.zeros((0, 4, 5, 64), device="cuda", requires_grad=True)

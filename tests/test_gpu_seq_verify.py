@@ -213,6 +213,20 @@ def test_same_answers_again_replayed_on_another_stream_and_interpreted(drafted):
             assert torch.equal(a, b)
 
 
+@pytest.mark.parametrize("drafted", [False, True])
+def test_logits_behind_32_bits(drafted):
+    g = np.random.default_rng(31)
+    n, V = 5, 1000
+    near = [_logits(g, 2, m, V, "f16") for m in (n, n - 1)]
+    far = [torch.empty((1 << 31) + 5 + x[0].numel(), dtype=torch.float16, device="cuda").as_strided(x.shape, ((1 << 31) + 5, V, 1)) for x in near]
+    for a, b in zip(far, near):
+        a.copy_(b)
+    tokens, uniforms = _int(g.integers(0, V, (2, n))), _f32(g.uniform(0, 1, (2, n + drafted)))
+    results = [F.seq_verify(x, tokens, uniforms, draft=d if drafted else None) for x, d in (near, far)]
+    for a, b in zip(*results):
+        assert torch.equal(a, b)
+
+
 def test_nothing_to_do():
     path, counts, following = F.seq_verify(torch.zeros((0, 3, 10), device="cuda"), _int(np.zeros((0, 3))), _f32(np.zeros((0, 3))))
     assert path.shape == (0, 3) and counts.shape == following.shape == (0,)
