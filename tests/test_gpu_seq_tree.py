@@ -272,6 +272,36 @@ def test_same_bits_again_replayed_on_another_stream_and_interpreted():
             assert torch.equal(out, eager)
 
 
+@pytest.mark.parametrize("n,width", [(5, None), (48, 700)])
+def test_lengths_and_tables_that_change_between_replays(n, width):
+    """Two graphs of one stream, each replayed after the sequences have grown and their pages have moved."""
+    g = np.random.default_rng(17)
+    table, pages = _table(g, [3000, 900], 16, width=width)
+    _, cache = _cache(g, pages, 2, 16, 64)
+    calls = []
+    for _ in range(2):
+        q, k, v = _inputs(g, 2, 8, 2, n, 64, "f16")
+        calls.append((q, k, v, _int(_parents(g, 2, n).tolist()), cache, _int(table.tolist()), _int([1, 0])))
+    F.seq_cache_tree_attention(*calls[0])
+    torch.cuda.synchronize()
+    graphs, outs = [], []
+    for args in calls:
+        graphs.append(torch.cuda.CUDAGraph())
+        with torch.cuda.graph(graphs[-1]):
+            outs.append(F.seq_cache_tree_attention(*args))
+    for lengths in ([3000, 900], [0, 17], [64, 2000], [1500, 1]):
+        moved = np.roll(table, 1, axis=0)
+        for args in calls:
+            args[5].copy_(torch.from_numpy(moved).cuda()), args[6].copy_(_int(lengths))
+        table = moved
+        for graph in graphs:
+            graph.replay()
+        eager = [F.seq_cache_tree_attention(*args) for args in calls]
+        torch.cuda.synchronize()
+        for a, b in zip(outs, eager):
+            assert torch.equal(a, b)
+
+
 @pytest.mark.parametrize("n,width", [(5, 7), (20, 7), (20, 200)])   # few rows, many, and many of a large call
 def test_pages_behind_32_bits(n, width):
     g = np.random.default_rng(8)
