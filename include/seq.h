@@ -112,7 +112,8 @@ size_t seq_rotary_bwd_workspace_bytes(const seq_rotary_problem *p);   /* for wei
 
 /*
  * The cache: pages of `page` consecutive tokens of one sequence, k_pages and v_pages int8 [pages, kv_heads, page, D], contiguous, with one fp32 scale
- * for each page and head, k_scales and v_scales [pages, kv_heads]; a value is the integer times the scale.  table: int32 [B, table_width]; position t of
+ * for each page and head, k_scales and v_scales [pages, kv_heads]; a value is the integer times the scale, of either
+ * sign.  table: int32 [B, table_width]; position t of
  * sequence b lies in page table[b, t / page] at t % page.  lengths: int32 [B], tokens of each sequence.  Entries of the table whose positions a call
  * does not reach (behind the sequence, or before every query's window) may be anything, pages that nothing was ever written to included.  A page number outside [0, pages) is no page: nothing is written there, and nothing there is seen or
  * read; positions beyond table_width pages likewise.
@@ -132,8 +133,8 @@ typedef enum { SEQ_CACHE_APPEND = 0, SEQ_CACHE_GATHER = 1, SEQ_CACHE_ATTENTION =
 int seq_cache_validate(const seq_cache_problem *p, int call);
 
 /* Writes k, v [B, kv_heads, n, D] (strides p->q and p->out) at positions lengths[b] .. of every sequence; counts (nullable): int32 [B], how many of the n are
- * taken (at most n; 0 leaves the sequence alone).  A page's scale becomes the larger of the old one and its new tokens' largest magnitude / 127; where it grows, the
- * tokens that the page held are rounded again, to nearest even, on the new scale.  The first token of a page starts it afresh.  A NaN is
+ * taken (at most n; 0 leaves the sequence alone).  A page's scale becomes the larger of the old one's magnitude and its new tokens' largest / 127; where that is another, the
+ * tokens that the page held are rounded again, to nearest even, on the new scale (to 127 at most).  The first token of a page starts it afresh.  A NaN is
  * stored as 0, an infinity as the largest finite fp32 value.  lengths is not changed.  A page must not be appended to twice in
  * one call (by two sequences, or through two entries of a table): which of the values it then holds is not defined. */
 int seq_cache_append(const seq_cache_problem *p, const void *k, const void *v, const int32_t *table, const int32_t *lengths, const int32_t *counts,

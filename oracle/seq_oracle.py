@@ -105,10 +105,10 @@ def append(cells, scales, x, table, lengths, counts=None):
             new = np.nan_to_num(x[b, :, lo - L:hi - L].astype(f32), nan=0.0, posinf=np.finfo(f32).max, neginf=np.finfo(f32).min)
             for h in range(cells.shape[1]):
                 before = scales[i, h] if old else f32(0)
-                scale = max(before, np.abs(new[h]).max() / f32(127))
+                scale = max(abs(before), np.abs(new[h]).max() / f32(127))
                 by = scale if scale > 0 else f32(1)
                 if old and scale != before:
-                    cells[i, h, :old] = np.rint(cells[i, h, :old].astype(f32) * (before / by))
+                    cells[i, h, :old] = np.rint(np.minimum(cells[i, h, :old].astype(f32) * (before / by), f32(127)))
                 cells[i, h, old:old + hi - lo] = np.clip(np.rint(new[h] / by), -127, 127)
                 scales[i, h] = scale
     return cells, scales

@@ -40,14 +40,14 @@ __device__ __forceinline__ int whole(float x, float by, float over) {
     return max(-127, min(127, (int)__builtin_rintf(r)));
 }
 
-// What a page held, in words of four bytes, on its new scale.
+// What a page held, in words of four bytes, on its new scale; of one below zero with the other sign (and -128 as 127).
 __device__ __forceinline__ void round_again(int8_t *cells, int count, float ratio, int tid) {
     uint32_t *words = reinterpret_cast<uint32_t *>(cells);
     for (int i = tid; i < count; i += kThreads) {
         const uint32_t w = words[i];
         uint32_t r = 0;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) r |= (uint32_t)(uint8_t)(int8_t)__builtin_rintf((float)(int8_t)(w >> 8 * e) * ratio) << 8 * e;
+        for (int e = 0; e < 4; ++e) r |= (uint32_t)(uint8_t)(int8_t)__builtin_rintf(fminf((float)(int8_t)(w >> 8 * e) * ratio, 127.f)) << 8 * e;
         words[i] = r;
     }
 }
@@ -103,7 +103,7 @@ __global__ __launch_bounds__(kThreads) void append_kernel(const CacheArgs p, int
         workgroup_sync();
         most = __uint_as_float(max(max(mosts[0], mosts[1]), max(mosts[2], mosts[3])));
     }
-    const float scale = fmaxf(before, most / 127.f), by = scale > 0.f ? scale : 1.f;
+    const float scale = fmaxf(fabsf(before), most / 127.f), by = scale > 0.f ? scale : 1.f;
     if (tid == 0) scales[unit] = scale;
     if (old && scale != before) round_again(cells, old * D / 4, before / by, tid);
     // every element is divided where 1 / by may be no ordinary number either
@@ -254,7 +254,7 @@ __global__ __launch_bounds__(kThreads, STEPS <= 2 ? 5 : 3) void append_rows_kern
         workgroup_sync();
         most = __uint_as_float(max(max(mosts[0], mosts[1]), max(mosts[2], mosts[3])));
     }
-    const float scale = fmaxf(before, most / 127.f), by = scale > 0.f ? scale : 1.f;
+    const float scale = fmaxf(fabsf(before), most / 127.f), by = scale > 0.f ? scale : 1.f;
     if (tid == 0) scales[unit] = scale;
     if (old && scale != before) round_again(cells, old * D / 4, before / by, tid);
     const bool divide = !(by > 0x1p-100f && by < 0x1p100f);
