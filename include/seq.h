@@ -165,7 +165,7 @@ size_t seq_cache_attention_workspace_bytes(const seq_cache_problem *p);
  * other value: no node (as padding), and neither is what descends from it; its q, k and v may be anything, and its row of out is 0.  A node stands at position lengths[b] +
  * its depth, and sees the cache, its ancestors and itself, all within `window` before it.  Scores as above.  Over the cache q and the
  * weights are rounded as in seq_cache_attention, but where a key head has more than 32 rows it is the weight times its page's value scale that is held as fp16, on the power of two of the
- * largest of those; a value scale below 2^-100, 0 too, counts as 2^-100 there, and those that a row sees
+ * largest of those; a value scale smaller in size than 2^-100, 0 too, counts as 2^-100 there, and those that a row sees
  * must lie within a factor of 2^126.  Over the nodes weights are rounded to fp16, or in bf16 to a sum of two of them.  A node's k or v that is
  * infinite or no number reaches the rows that see the node, and no others.  The workspace is always needed. */
 int seq_cache_tree_attention(const seq_cache_problem *p, const seq_strides *k_strides, const seq_strides *v_strides, const void *q, const void *k, const void *v, const int32_t *parents,

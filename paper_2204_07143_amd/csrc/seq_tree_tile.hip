@@ -2,8 +2,8 @@
 //
 // A workgroup keeps 64 RB rows, 16 RB to a wave, and walks tiles of 64 tokens: the cache's bytes are read into registers a tile ahead, become fp16 (exactly: 0x64 in front of a
 // byte, minus 1152) once for all rows on their way to LDS, and are read from there as seq_fwd.hip reads keys and values, S^T = K Q^T, O^T += V^T P.  A page's key scale multiplies
-// its scores; its value scale goes into the weights' exponent, 2^(s + log2 vs - ref), so that the products need no scale of their own; a row's sum takes a page's weights over vs
-// again.  The nodes' own keys and values are the last tile of a row's work.
+// its scores (one below zero goes the way of the masks: it turns the order of the scores); the size of its value scale goes into the weights' exponent, 2^(s + log2 |vs| - ref), so that the
+// products need no scale of their own, and the sign of one below zero into the values; a row's sum takes a page's weights over |vs| again.  The nodes' own keys and values are the last tile of a row's work.
 //
 // Bound by the vector instructions (half of the cycles) and the products (a quarter), which two waves to a SIMD lay over each other in part; waves wait 26 % of their time.  192 rows of 128
 // channels fill the registers.  16 sequences to 8000 tokens, 48 nodes, 32 heads over 8, D 128, bf16: 124 us, 0.49 PFLOP/s of products, and the join 14 (64 MB of sums; 16 with a workgroup for each 8 rows); 225 in workgroups
@@ -112,6 +112,16 @@ template <int D> struct TileBytes {
             }
         }
     }
+    // What this thread left there, of the pieces in `minus` (2^shift blocks of 16 rows each), with the other sign.
+    __device__ __forceinline__ static void negate(int img, int tid, int wave, uint64_t minus, int shift) {
+        using L = Tile<f16_t, D>;
+#pragma unroll 1
+        for (int i = 0; i < LOADS; ++i) {
+            if (!(minus >> (block(i, wave) >> shift) & 1)) continue;
+            const int r = row(i, tid), c = (tid + i * kThreads) % C;
+            for (int k = 0; k < W / 2; ++k) *lds_ptr<u32x4>(img + r * L::ROWB + (((W / 2) * c + k) ^ L::swizzle(r)) * 16) ^= 0x80008000u;
+        }
+    }
 };
 
 template <typename T, int D, int RB, int CAP>
@@ -151,7 +161,8 @@ __global__ __launch_bounds__(kThreads, 2) void tree_tile_kernel(const CacheArgs 
         const int cached = min(count, span.tiles - 1 - first);   // of this run
         const int pieces = page >= kTile ? 1 : kTile / page, shift = page >= kTile ? 2 : p.page_log2 - 4, chunk = kWave / pieces;   // of a tile: pages, and 16-token blocks to one
         int unit = -1;                // of one of the next 64 pieces: its page, and of that
-        float ks = 0.f, lv = 0.f;   // the keys' scale, the values' in base 2
+        float ks = 0.f, lv = 0.f;   // the keys' scale, the size of the values' in base 2
+        uint64_t minus = 0;         // those whose values' scale is below zero
         auto look_up = [&](int tile) {
             const int size = kTile / pieces;
             const int64_t token = (int64_t)tile * kTile + (int64_t)size * lane;
@@ -159,8 +170,9 @@ __global__ __launch_bounds__(kThreads, 2) void tree_tile_kernel(const CacheArgs 
             const int id = p.table[(int64_t)b * p.width + (seen ? token >> p.page_log2 : 0)];
             unit = seen && (unsigned)id < (unsigned)p.pages ? id : -1;
             const int64_t u = (int64_t)max(unit, 0) * p.kv + kh;
-            const float k = p.ks[u], v = fmaxf(p.vs[u], 0x1p-100f);   // (values of a scale of 0 are 0: their weights count)
+            const float k = p.ks[u], scale = p.vs[u], v = fmaxf(fabsf(scale), 0x1p-100f);   // (values of a scale of 0 are 0: their weights count)
             ks = unit < 0 ? 0.f : k, lv = unit < 0 ? 0.f : __builtin_amdgcn_logf(v);
+            minus = __ballot(unit >= 0 && scale < 0.f);
         };
         auto lane_of = [](float x, int l) { return __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(x), l)); };
         B keys, values;
@@ -256,6 +268,8 @@ __global__ __launch_bounds__(kThreads, 2) void tree_tile_kernel(const CacheArgs 
             const int mine = RB == 3 ? afresh(threadIdx.x) : tid;   // (the registers)
             keys.to_lds(ki, mine);
             values.to_lds(vi, mine);
+            const uint64_t here = ((1ull << pieces) - 1) << slot;   // the tile's pieces
+            if (minus & here) values.negate(vi, mine, wave, minus >> slot, shift);
             uint64_t there = 0;
 #pragma unroll
             for (int rb = 0; rb < 4; ++rb)
@@ -263,8 +277,8 @@ __global__ __launch_bounds__(kThreads, 2) void tree_tile_kernel(const CacheArgs 
             const bool known = ((t + 1) & (chunk - 1)) != 0;   // where the next tile lies: else that is looked up when this one's scales are not needed any more
             if (t + 1 < cached && known) load(t + 1);
             workgroup_sync();
-            // every row sees all of it
-            const bool all = there == ~0ull && t0 + kTile <= span.length && span.tokens + p.n - 1 - t0 < p.window;
+            // every row sees all of it, and no scale turns the order of its scores
+            const bool all = there == ~0ull && t0 + kTile <= span.length && span.tokens + p.n - 1 - t0 < p.window && !(__ballot(ks < 0.f) & here);
 #pragma unroll 1
             for (int half = 0; half < 2; ++half) {
                 const int kh_at = ki + half * 32 * L::ROWB;

@@ -440,7 +440,7 @@ def seq_rotary(q, k, positions, freqs, *, sections=None, q_weight=None, k_weight
 
 class SeqCache(NamedTuple):
     """Keys and values in 8 bits: pages int8 [pages, kv_heads, page, D] and a scale for each page and head, fp32 [pages, kv_heads]; a value is
-    the integer times the scale.  Which page holds what is the caller's: a table, int32 [B, width], gives each sequence's pages in order."""
+    the integer times the scale, of either sign.  Which page holds what is the caller's: a table, int32 [B, width], gives each sequence's pages in order."""
     k_pages: torch.Tensor
     v_pages: torch.Tensor
     k_scales: torch.Tensor

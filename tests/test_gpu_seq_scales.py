@@ -8,8 +8,39 @@ from paper_2204_07143_amd import functional as F
 
 from seq_util import f64, normal
 from test_gpu_seq_cache import _cache, _check_attention, _int, _table
+from test_gpu_seq_tree import _check, _inputs, _parents
+from test_gpu_seq_tree_tiles import _wide, in_tiles
 
 pytestmark = pytest.mark.gpu
+
+
+def _trees(g, host, table, lengths, n, dtype, tiled, cap=None, slope=0.0, scale=None, std=1.0):
+    """Trees over a cache, in tiles or not, against the oracle."""
+    kv, page, D = host[0].shape[1:]
+    heads = 4 * kv
+    cache = F.SeqCache(*(torch.from_numpy(x).cuda() for x in host))
+    q, k, v = _inputs(g, len(lengths), heads, kv, n, D, dtype, std)
+    parents = _parents(g, len(lengths), n)
+    slopes = torch.full((heads,), slope, device="cuda") if slope else None
+    wide = _int(_wide(table, page, 32768).tolist() if tiled else table.tolist())
+    assert in_tiles(q, cache, wide, softcap=cap) == tiled
+    got = F.seq_cache_tree_attention(q, k, v, _int(parents.tolist()), cache, wide, _int(lengths), softcap=cap, slopes=slopes, scale=scale)
+    assert torch.isfinite(got).all()
+    _check(got, q, k, v, parents, host, table, lengths, dtype, softcap=cap, slopes=None if slopes is None else f64(slopes), scale=scale)
+
+
+@pytest.mark.parametrize("dtype,D", [("f16", 64), ("bf16", 128), ("f16", 32)])
+@pytest.mark.parametrize("page", [16, 32, 64, 128])
+@pytest.mark.parametrize("cap,slope,scale", [(None, 0.0, None), (5.0, 0.0, None), (1500.0, 0.0, None), (None, 0.02, None), (None, 0.0, -0.2)])
+@pytest.mark.parametrize("tiled", [False, True])
+def test_trees_with_scales_of_either_sign(dtype, D, page, cap, slope, scale, tiled):
+    g = np.random.default_rng(page + D)
+    lengths, n = [700, 0, 257], 40
+    table, pages = _table(g, lengths, page)
+    host, _ = _cache(g, pages, 2, page, D)
+    for scales in host[2:]:
+        scales *= g.choice([-1, 1], scales.shape).astype(np.float32)
+    _trees(g, host, table, lengths, n, dtype, tiled, cap, slope, scale)
 
 
 @pytest.mark.parametrize("page", [16, 64])
