@@ -164,9 +164,10 @@ size_t seq_cache_attention_workspace_bytes(const seq_cache_problem *p);
  * own, in the problem dtype, with strides k_strides and v_strides.  parents: int32 [B, n]; a node's parent is a node before it, or -1: it follows the cache's last token.  Any
  * other value: no node (as padding), and neither is what descends from it; its q, k and v may be anything, and its row of out is 0.  A node stands at position lengths[b] +
  * its depth, and sees the cache, its ancestors and itself, all within `window` before it.  Scores as above.  Over the cache q and the
- * weights are rounded as in seq_cache_attention, but where a key head has more than 32 rows it is the weight times its page's value scale that is held as fp16, on the power of two of the
- * largest of those; a value scale smaller in size than 2^-100, 0 too, counts as 2^-100 there, and those that a row sees
- * must lie within a factor of 2^126.  Over the nodes weights are rounded to fp16, or in bf16 to a sum of two of them.  A node's k or v that is
+ * weights are rounded as in seq_cache_attention, but where a key head has more than 32 rows and the table holds work enough (rows times
+ * tiles of 64 tokens of all sequences and key heads from 2^16 on) it is the weight times the size of its page's value scale that is held as fp16, on the power of two of the largest of those.  A value
+ * scale of 2^-100 in size, or less, counts as 0 there; and of the tokens that a row sees one whose weight times scale (the nodes' own: 1) is not 0, but below 2^-126 of the largest such, is
+ * left out of the row's sum.  Over the nodes weights are rounded to fp16, or in bf16 to a sum of two of them.  A node's k or v that is
  * infinite or no number reaches the rows that see the node, and no others.  The workspace is always needed. */
 int seq_cache_tree_attention(const seq_cache_problem *p, const seq_strides *k_strides, const seq_strides *v_strides, const void *q, const void *k, const void *v, const int32_t *parents,
                              const int8_t *k_pages, const int8_t *v_pages, const float *k_scales, const float *v_scales, const int32_t *table, const int32_t *lengths, const float *slopes,

@@ -3,7 +3,8 @@
 // A workgroup keeps 64 RB rows, 16 RB to a wave, and walks tiles of 64 tokens: the cache's bytes are read into registers a tile ahead, become fp16 (exactly: 0x64 in front of a
 // byte, minus 1152) once for all rows on their way to LDS, and are read from there as seq_fwd.hip reads keys and values, S^T = K Q^T, O^T += V^T P.  A page's key scale multiplies
 // its scores (one below zero goes the way of the masks: it turns the order of the scores); the size of its value scale goes into the weights' exponent, 2^(s + log2 |vs| - ref), so that the
-// products need no scale of their own, and the sign of one below zero into the values; a row's sum takes a page's weights over |vs| again.  The nodes' own keys and values are the last tile of a row's work.
+// products need no scale of their own, and the sign of one below zero into the values; a row's sum takes a page's weights over |vs| again.
+// Pages whose value scale is 0 have no such exponent: their tokens go into a sum of their own.  The nodes' own keys and values are the last tile of a row's work.
 //
 // Bound by the vector instructions (half of the cycles) and the products (a quarter), which two waves to a SIMD lay over each other in part; waves wait 26 % of their time.  192 rows of 128
 // channels fill the registers.  16 sequences to 8000 tokens, 48 nodes, 32 heads over 8, D 128, bf16: 124 us, 0.49 PFLOP/s of products, and the join 14 (64 MB of sums; 16 with a workgroup for each 8 rows); 225 in workgroups
@@ -19,6 +20,7 @@ namespace seq {
 namespace {
 
 constexpr int kLeastRun = 2;   // tiles of a workgroup, where there are so many
+constexpr float kNothing = -100.f;   // a value scale of this power of two, or below, counts as 0
 
 __device__ __forceinline__ int64_t uniform(int64_t x) {
     return (int64_t)((uint64_t)(uint32_t)seq::uniform((int)(uint32_t)x) | (uint64_t)(uint32_t)seq::uniform((int)(uint32_t)((uint64_t)x >> 32)) << 32);
@@ -28,6 +30,9 @@ __device__ __forceinline__ int afresh(int x) {
     asm volatile("" : "+v"(x));
     return x;
 }
+
+// x 2^by, by not above 0: also where 2^by alone would be below 2^-126, and 0
+__device__ __forceinline__ float lowered(float x, float by) { return x * __builtin_amdgcn_exp2f(fmaxf(by, -126.f)) * __builtin_amdgcn_exp2f(fminf(by + 126.f, 0.f)); }
 
 // What of a sequence its rows see of the cache.
 struct Span {
@@ -133,6 +138,7 @@ __global__ __launch_bounds__(kThreads, 2) void tree_tile_kernel(const CacheArgs 
     __shared__ Tree tree;
     __shared__ Wild<D> wild;
     __shared__ int2 row_info[ROWS];   // position, and slope as bits
+    __shared__ float2 aside[RB][kThreads];   // a thread's tokens whose values' scale is 0: largest score, and sum of weights beside it
     const int tid = threadIdx.x, lane = tid % kWave, wave = seq::uniform(tid / kWave), g = lane >> 4, img = lds_addr(lds);
     const Schedule schedule(p, lane);
     const int run = blockIdx.x;
@@ -145,6 +151,8 @@ __global__ __launch_bounds__(kThreads, 2) void tree_tile_kernel(const CacheArgs 
     const typename L::ColumnReader columns(lane);
     int built = -1;
     wild.clear(tid);
+#pragma unroll
+    for (int n = 0; n < RB; ++n) aside[n][tid] = float2{kLowest, 0.f};
 
 #pragma unroll 1
     for (bool begun = false; left > 0; begun = true) {
@@ -161,7 +169,7 @@ __global__ __launch_bounds__(kThreads, 2) void tree_tile_kernel(const CacheArgs 
         const int cached = min(count, span.tiles - 1 - first);   // of this run
         const int pieces = page >= kTile ? 1 : kTile / page, shift = page >= kTile ? 2 : p.page_log2 - 4, chunk = kWave / pieces;   // of a tile: pages, and 16-token blocks to one
         int unit = -1;                // of one of the next 64 pieces: its page, and of that
-        float ks = 0.f, lv = 0.f;   // the keys' scale, the size of the values' in base 2
+        float ks = 0.f, lv = 0.f;   // the keys' scale, the size of the values' in base 2, kNothing for 0
         uint64_t minus = 0;         // those whose values' scale is below zero
         auto look_up = [&](int tile) {
             const int size = kTile / pieces;
@@ -170,8 +178,8 @@ __global__ __launch_bounds__(kThreads, 2) void tree_tile_kernel(const CacheArgs 
             const int id = p.table[(int64_t)b * p.width + (seen ? token >> p.page_log2 : 0)];
             unit = seen && (unsigned)id < (unsigned)p.pages ? id : -1;
             const int64_t u = (int64_t)max(unit, 0) * p.kv + kh;
-            const float k = p.ks[u], scale = p.vs[u], v = fmaxf(fabsf(scale), 0x1p-100f);   // (values of a scale of 0 are 0: their weights count)
-            ks = unit < 0 ? 0.f : k, lv = unit < 0 ? 0.f : __builtin_amdgcn_logf(v);
+            const float k = p.ks[u], scale = p.vs[u];
+            ks = unit < 0 ? 0.f : k, lv = unit < 0 ? 0.f : fmaxf(__builtin_amdgcn_logf(fabsf(scale)), kNothing);
             minus = __ballot(unit >= 0 && scale < 0.f);
         };
         auto lane_of = [](float x, int l) { return __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(x), l)); };
@@ -192,7 +200,7 @@ __global__ __launch_bounds__(kThreads, 2) void tree_tile_kernel(const CacheArgs 
         }
         workgroup_sync();   // (what the run before reads of LDS)
         if (b != built) {
-            tree.build(p.parents + (int64_t)b * p.n, p.n, tid);
+            tree.build(p.parents + (int64_t)b * p.n, p.n, RB == 3 ? afresh(threadIdx.x) : tid);   // (afresh: the registers)
             built = b;
             workgroup_sync();
         }
@@ -274,6 +282,50 @@ __global__ __launch_bounds__(kThreads, 2) void tree_tile_kernel(const CacheArgs 
 #pragma unroll
             for (int rb = 0; rb < 4; ++rb)
                 if (__builtin_amdgcn_readlane(unit, slot + (rb >> shift)) >= 0) there |= 0xffffull << 16 * rb;
+            // Values that are 0 add to a row's sum alone, and have no scale whose exponent their weights could take: into the thread's own sum, by scores formed once more.
+            if (const uint64_t zero = __ballot(lv == kNothing) & here) {
+                uint64_t apart = 0;
+#pragma unroll
+                for (int rb = 0; rb < 4; ++rb)
+                    if (zero >> (slot + (rb >> shift)) & 1) apart |= 0xffffull << 16 * rb;
+                there &= ~apart;
+                workgroup_sync();
+#pragma unroll 1
+                for (int half = 0; half < 2; ++half) {
+#pragma unroll
+                    for (int n = 0; n < RB; ++n) {
+                        f32x4 s[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
+#pragma unroll
+                        for (int st = 0; st < STEPS; ++st)
+#pragma unroll
+                            for (int i = 0; i < 2; ++i) s[i] = mma<f16_t>(rows.read(ki + half * 32 * L::ROWB, i, st), q[n][st], s[i]);
+                        settle_products(s);
+                        const int lane = afresh(threadIdx.x) % kWave, g = lane >> 4;
+                        const int2 info = row_info[wave * 16 * RB + 16 * n + (lane & 15)];
+                        const float near = (float)(info.x - t0 - 32 * half - 4 * g), slope = __uint_as_float((uint32_t)info.y);
+                        const uint64_t seen = (bits_between(info.x - p.window + 1 - t0, span.length - t0) & apart) >> (32 * half + 4 * g);
+                        float2 &mine = aside[n][wave * kWave + lane];
+                        const float2 old = mine;
+                        float now = old.x;
+#pragma unroll
+                        for (int i = 0; i < 2; ++i) {
+                            const float by = c[n] * lane_of(ks, slot + ((2 * half + i) >> shift));
+#pragma unroll
+                            for (int r = 0; r < 4; ++r) {
+                                s[i][r] = keep(__builtin_fmaf(near - (float)(16 * i + r), -slope, capped(s[i][r] * by)), seen, 16 * i + r, -INFINITY);
+                                now = fmaxf(now, s[i][r]);
+                            }
+                        }
+                        float all_of = old.y * __builtin_amdgcn_exp2f(old.x - now);
+#pragma unroll
+                        for (int i = 0; i < 2; ++i)
+#pragma unroll
+                            for (int r = 0; r < 4; ++r) all_of += __builtin_amdgcn_exp2f(s[i][r] - now);
+                        mine = float2{now, all_of};
+                        __builtin_amdgcn_sched_barrier(0);
+                    }
+                }
+            }
             const bool known = ((t + 1) & (chunk - 1)) != 0;   // where the next tile lies: else that is looked up when this one's scales are not needed any more
             if (t + 1 < cached && known) load(t + 1);
             workgroup_sync();
@@ -437,6 +489,14 @@ __global__ __launch_bounds__(kThreads, 2) void tree_tile_kernel(const CacheArgs 
         for (int n = 0; n < RB; ++n) {
             settle_products(out[n]);
             const int row = row0 + 16 * n + j, in_unit = wave * 16 * RB + 16 * n + j;
+            const float2 rest = aside[n][wave * kWave + lane];
+            if (__any(rest.y != 0.f)) {   // both under the larger reference
+                const float now = fmaxf(ref[n], column_max(rest.x)), down = __builtin_amdgcn_exp2f(ref[n] - now);
+                sum[n] = __builtin_fmaf(sum[n], down, lowered(rest.y, rest.x - now));
+#pragma unroll
+                for (int db = 0; db < DB; ++db) out[n][db] *= down;
+                ref[n] = now, aside[n][wave * kWave + lane] = float2{kLowest, 0.f};
+            }
             float total = column_sum(sum[n]);
             if (row >= all_rows) continue;
             const bool node = tree.above[row % p.n] != 0;
@@ -506,7 +566,7 @@ __global__ __launch_bounds__(kThreads) void tree_join_kernel(const CacheArgs p) 
             const float2 st = stats[place * ROWS];
             const f32x4 y = *reinterpret_cast<const f32x4 *>(p.part + (place * ROWS + in_unit) * D + col * 4);
             const float now = fmaxf(m, st.x), old = __builtin_amdgcn_exp2f(m - now), by = __builtin_amdgcn_exp2f(st.x - now);
-            m = now, sum = sum * old + st.y * by, x = x * old + y * by;
+            sum = lowered(sum, m - now) + lowered(st.y, st.x - now), x = x * old + y * by, m = now;
         }
         const int h = kh * p.group + row / p.n;
         Tile<T, D>::store4(const_cast<char *>(p.b.at) + b * p.b.b + h * p.b.h + (int64_t)(row % p.n) * p.b.row + col * 4 * (int)sizeof(T), x * (sum == 0.f ? 0.f : 1.f / sum));

@@ -80,3 +80,43 @@ def test_appends_to_pages_of_a_scale_below_zero(picked, std):
         assert (np.abs(f64(got) - want) <= (0.5 + 127 * 2.0 ** -22) * step[None, :, None, None]).all()   # half a step; the scale's own and the ratio's rounding, 127 times at most
         cells, scales = seq_oracle.append(host[i], host[i + 2], new.cpu().numpy(), table, [L])
         assert np.array_equal(cache[i].cpu().numpy(), cells) and np.array_equal(cache[i + 2].cpu().numpy(), scales)
+
+
+@pytest.mark.parametrize("page", [16, 64])
+@pytest.mark.parametrize("cap,slope", [(None, 0.0), (5.0, 0.0), (None, 0.02)])
+@pytest.mark.parametrize("large,small", [(2.0 ** 20, 0.0), (2.0 ** 110, 0.0), (1e-2, 0.0), (1e-25, 0.0), (0.0, 0.0), (2.0 ** 40, 2.0 ** -60), (-1.0, -0.0)])
+@pytest.mark.parametrize("tiled", [False, True])
+def test_pages_of_no_values_count_in_the_sums(page, cap, slope, large, small, tiled):
+    """Values that are 0, or as good as that, beside large ones: their tokens' weights are part of a row's sum all the same."""
+    g = np.random.default_rng(page)
+    lengths, n = [500, 64, 1, 130], 40
+    table, pages = _table(g, lengths, page)
+    host, _ = _cache(g, pages, 2, page, 64)
+    host[3][:] = np.where(g.random(host[3].shape) < 0.3, large, small)
+    host[3][table[1]] = small   # a sequence of nothing else
+    _trees(g, host, table, lengths, n, "bf16", tiled, cap, slope, std=1.5)
+
+
+@pytest.mark.parametrize("page", [16, 128])
+@pytest.mark.parametrize("score,power", [(-4, -99), (20, -99), (-6, -97), (0, -60)])
+@pytest.mark.parametrize("tiled", [False, True])
+def test_weights_next_to_the_least_that_count(page, score, power, tiled):
+    """Scores in base 2 that are whole numbers: weight times value scale of most tokens is 2^-124 of the first page's in the first and the third case, and they are most of a row's sum."""
+    g = np.random.default_rng(page)
+    L, n, D, heads = 40 * page + 5, 40, 64, 4
+    table, pages = _table(g, [L], page)
+    host, _ = _cache(g, pages, 1, page, D)
+    host[0][:] = 0
+    host[0][..., 0] = score
+    host[0][table[0, 0], ..., 0] = 0
+    host[2][:], host[3][:], host[3][table[0, 0]] = 1.0, 2.0 ** power, 2.0 ** 21
+    cache = F.SeqCache(*(torch.from_numpy(x).cuda() for x in host))
+    q, k, v = (normal(g, (1, h, n, D), "bf16") for h in (heads, 1, 1))
+    q[..., 0], k[..., 0] = 1, 0
+    q[..., 1:], k[..., 1:] = 0, 0
+    parents = np.tile(np.arange(-1, n - 1, dtype=np.int32), (1, 1))
+    wide = _int(_wide(table, page, 65536).tolist() if tiled else table.tolist())
+    assert in_tiles(q, cache, wide) == tiled
+    scale = float(np.float32(np.log(2.0)))
+    got = F.seq_cache_tree_attention(q, k, v, _int(parents.tolist()), cache, wide, _int([L]), scale=scale)
+    _check(got, q, k, v, parents, host, table, [L], "bf16", scale=scale)
