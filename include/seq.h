@@ -135,7 +135,7 @@ int seq_cache_validate(const seq_cache_problem *p, int call);
 /* Writes k, v [B, kv_heads, n, D] (strides p->q and p->out) at positions lengths[b] .. of every sequence; counts (nullable): int32 [B], how many of the n are
  * taken (at most n; 0 leaves the sequence alone).  A page's scale becomes the larger of the old one's magnitude and its new tokens' largest / 127; where that is another, the
  * tokens that the page held are rounded again, to nearest even, on the new scale (to 127 at most).  The first token of a page starts it afresh.  A NaN is
- * stored as 0, an infinity as the largest finite fp32 value.  lengths is not changed.  A page must not be appended to twice in
+ * stored as 0, an infinity as the largest finite fp32 value (127 times the scale, which that rounding may make infinite again in fp32).  lengths is not changed.  A page must not be appended to twice in
  * one call (by two sequences, or through two entries of a table): which of the values it then holds is not defined. */
 int seq_cache_append(const seq_cache_problem *p, const void *k, const void *v, const int32_t *table, const int32_t *lengths, const int32_t *counts,
                      int8_t *k_pages, int8_t *v_pages, float *k_scales, float *v_scales, void *stream);

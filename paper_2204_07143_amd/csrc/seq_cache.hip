@@ -148,7 +148,7 @@ template <int E> __device__ __forceinline__ void whole_bytes(const float (&x)[E]
 // The same with rows picked out of those given, and keys normed and rotated on the way: a page's fresh tokens stay in registers, in fp32, from their one read to the
 // bytes that are stored, lanes and chunks as seq_rotary.hpp has them.  What is stored is rounded once, from the rotated value.  A workgroup to a page of a head, of keys or of values:
 // the page's scale needs all of its tokens, and a page's length decides the registers (STEPS; in 16 bit and 128 channels a round is 32 rows: up to 64 tokens leave room for 5 workgroups a unit, 128 for 3).
-// Bound by memory and by the reads that wait for each other (length, table, row, values).  8 x 8 x 1000 tokens after 700, D 128, pages of 64, bf16: 24 us (49 MB, 2.0 TB/s; 38 with a division and a clamp for each
+// Bound by memory and by the reads that wait for each other (length and count, frequencies, the norm's weights one by one, table, row, values).  8 x 8 x 1000 tokens after 700, D 128, pages of 64, bf16: 24 us (49 MB, 2.0 TB/s; 38 with a division and a clamp for each
 // byte and one size of registers), vector instructions 40 % of the cycles, waves wait 50 % of theirs; one token of 64 sequences 7.6 us, latency.
 template <typename T, int D, int STEPS>   // STEPS: how often the workgroup's rows go into a page
 __global__ __launch_bounds__(kThreads, STEPS <= 2 ? 5 : 3) void append_rows_kernel(const RowsArgs a, int touched) {
@@ -171,7 +171,7 @@ __global__ __launch_bounds__(kThreads, STEPS <= 2 ? 5 : 3) void append_rows_kern
     const bool turned = !values && a.r.pairs, normed = !values && a.r.weight;
     int c0, c1;
     chunks_of<E>(a.r, i, c0, c1);
-    // what does not depend on lengths and table is on its way while those are waited for
+    // what depends on neither length nor table; a read at a time, waited for, in front of the table's
     float freqs[E], wl[E], wh[E];
 #pragma unroll
     for (int e = 0; e < E; ++e) freqs[e] = 0.f, wl[e] = wh[e] = 1.f;

@@ -6,7 +6,8 @@
 // Bound by memory: about seven operations an element, and each element read and written once.  A wave takes the tokens of a group, LANES lanes to each, and walks their heads, so
 // that angles (in 64 bits) are formed once for all of them.  All (group, head) steps are shared evenly by as many waves as there are at once; a wave reads the next step's vectors
 // while it works on one.  2 x (16 + 4) x 8192 tokens, D 128, bf16, three axes, norms: forward 34 us (168 MB, 4.9 TB/s, where a copy of 1 GiB reaches 5.2), backward 50 and 4 (252 MB, 5.0);
-// as a launch for each of queries and keys, a wave to a token, 40 and 65.  Vector instructions take 45 % of the cycles; with the library's sine and cosine 40 and 52.  64 x (2 + 2) x 3136, D 32, fp16: 23.5 (103 MB) and 34 + 4.  One token of 40 heads: 6.5, a launch and four reads after one another.
+// as a launch for each of queries and keys, a wave to a token, 40 and 65.  Vector instructions take 45 % of the cycles; with the library's sine and cosine 40 and 52.  64 x (2 + 2) x 3136, D 32, fp16: 23.5 (103 MB) and 34 + 4.  Eight tokens, one each of 8 sequences, of 40 heads: 6.5, a launch,
+// and reads that wait for each other: a lane's frequencies in pairs, the positions, the first row, and the norm's weights one by one (their type is looked up for each).
 #include "seq_rotary.hpp"
 
 namespace seq {

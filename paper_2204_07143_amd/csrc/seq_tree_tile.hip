@@ -1,4 +1,4 @@
-// Attention of a tree of drafted tokens over a cache in 8 bits, where a key head has more than 32 rows (its query heads times the nodes).
+// Attention of a tree of drafted tokens over a cache in 8 bits, where a key head has more than 32 rows (its query heads times the nodes) and there is enough work (plan_cache_tree()).
 //
 // A workgroup keeps 64 RB rows, 16 RB to a wave, and walks tiles of 64 tokens: the cache's bytes are read into registers a tile ahead, become fp16 (exactly: 0x64 in front of a
 // byte, minus 1152) once for all rows on their way to LDS, and are read from there as seq_fwd.hip reads keys and values, S^T = K Q^T, O^T += V^T P.  A page's key scale multiplies
@@ -6,8 +6,9 @@
 // products need no scale of their own, and the sign of one below zero into the values; a row's sum takes a page's weights over |vs| again.
 // Pages whose value scale is 0 have no such exponent: their tokens go into a sum of their own.  The nodes' own keys and values are the last tile of a row's work.
 //
-// Bound by the vector instructions (half of the cycles) and the products (a quarter), which two waves to a SIMD lay over each other in part; waves wait 26 % of their time.  192 rows of 128
-// channels fill the registers.  16 sequences to 8000 tokens, 48 nodes, 32 heads over 8, D 128, bf16: 124 us, 0.49 PFLOP/s of products, and the join 14 (64 MB of sums; 16 with a workgroup for each 8 rows); 225 in workgroups
+// Bound by the vector instructions (half of the cycles) and the products (a quarter), which two waves to a SIMD lay over each other in part; waves wait 27 % of their time; a quarter of the LDS's cycles
+// are conflicts of the bytes' way in.  192 rows of 128
+// channels fill the registers.  16 sequences to 8000 tokens, 48 nodes, 32 heads over 8, D 128, bf16: 126 us (124 with scales above 0 alone), 0.48 PFLOP/s of products, and the join 14 (64 MB of sums; 16 with a workgroup for each 8 rows); 225 in workgroups
 // of 32 rows that each make fp16 of all bytes (seq_decode.hpp); 64 and 128 rows to a workgroup 168 and 163; 126 without the products' priority over another wave's softmax.
 //
 // The tiles of all sequences and key heads, in a row, are shared evenly by the workgroups, wherever the cuts fall: a run that has all of a row's tiles stores its result, others

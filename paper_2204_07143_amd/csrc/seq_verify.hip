@@ -56,7 +56,8 @@ __device__ const uint64_t kRoots[32] = {
     0x3feee89f995ad3ad, 0x3feeff76f2fb5e47, 0x3fef199bdd85529c, 0x3fef3720dcef9069, 0x3fef5818dcfba487, 0x3fef7c97337b9b5f,
     0x3fefa4afa2a490da, 0x3fefd0765b6e4540};
 
-// e^((x - most) / T) in 64 bits, 0 where x is -inf or no number.  With y = 32 (x - most) log2(e) / T, n the whole number next to it and f = y - n:
+// e^((x - most) / T) in 64 bits, 0 where x is -inf or no number: a table of roots and a short polynomial, as P. T. P. Tang has it (Table-driven implementation of the exponential function in
+// IEEE floating-point arithmetic, ACM Transactions on Mathematical Software 15, 1989); the number added to round is 1.5 2^52, whose last place is 1.  With y = 32 (x - most) log2(e) / T, n the whole number next to it and f = y - n:
 // 2^(n / 32) from a table and the exponent, 2^(f / 32) as its Taylor polynomial of degree 5, off by (ln 2 / 64)^6 / 720 < 2^-48; y's own rounding is 2^-53 of it.  y is held at
 // 32 times -1023, where the exponent's bits, and with them the weight, are 0 (down from 2^-1022 weights are no longer exact).  14 instructions in 64 bits an
 // element; the table's entries lie in different banks of the LDS.

@@ -513,7 +513,7 @@ def seq_cache_tree_attention(q, k, v, parents, cache: SeqCache, table, lengths, 
 
     ``parents`` (int32 [B, n]): a node before it, or -1 for what follows the cache's last token; any other number is no node (padding), nor is what descends from it: its
     values may be anything, and its row of the result is 0.  What is no number in a node's k or v reaches the rows that see it alone.  A node stands at position ``lengths[b]`` plus its depth, and sees the cache, its ancestors and itself, within
-    the window.  Otherwise as ``seq_cache_attention``.  Not differentiable."""
+    the window.  Otherwise as ``seq_cache_attention``; in large calls (include/seq.h) a value scale of 2^-100 in size, or less, counts as 0.  Not differentiable."""
     out = _native().seq_cache_tree_attention(q, *cache, table, lengths, k, v, parents, window, softcap, slopes, scale)
     if out is not None:
         return out
